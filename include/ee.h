@@ -33,7 +33,8 @@
  * Conventions
  *   - All pointers in the signatures are HOST pointers.  Device memory is owned
  *     by the library.  Input arrays belong to the caller and are copied before
- *     the call returns.
+ *     the call returns.  (The operators on device memory at the end take DEVICE
+ *     pointers and a stream of the caller's and say so.)
  *   - Every function returns an int status: EE_OK (0) or a negative EE_E* code;
  *     ee_last_error() gives a thread-local message for the last failure.
  *     Nothing throws, nothing aborts.
@@ -378,6 +379,108 @@ int ee_debug_mfma_layout(int device);
    (the range the model loader admits) for which that differs from x / d, for each of the n
    divisors (host array, each >= 1, n <= 65536); *mismatches must come back 0. */
 int ee_debug_div_small(int device, const int32_t *divisors, int n, long long *mismatches);
+
+/* ------------------------------------------------------------------ operators on device memory
+   Steps of a decoder layer's attention and of a round's verification, for callers that run layers of their own around a
+   paged cache.  They take DEVICE pointers (of GPU `device`, which need not be the current one) and enqueue kernels on
+   `stream` (a hipStream_t of that GPU, NULL: its default stream); nothing is allocated, copied or waited for, so that calls can
+   be captured into a graph, and what a call is given has to stay until its kernels are done.  Lengths, tables and tokens are read
+   by the kernels: the host checks sizes, types, strides and alignment (EE_EINVAL before anything is enqueued), the kernels bounds.
+   Calls that share an output or a workspace must not overlap in time; calls on one stream do not.
+
+   A batch is n_seqs sequences whose new rows follow each other in arrays of n_rows rows: sequence s has the rows
+   row_start[s] .. row_start[s+1] - 1 (row_start: int32 [n_seqs + 1], not decreasing, within [0, n_rows]; a sequence may have none), and rows from
+   row_start[n_seqs] on are padding: never written, and what they hold does not matter.  kv_len[s] (int32) counts a sequence's positions, the
+   new rows' included: the last row is position kv_len[s] - 1. */
+
+/* element types */
+#define EE_BF16 0
+#define EE_FP16 1
+#define EE_FP32 2
+
+/* A paged cache of one attention layer, in the layout of a session's: a page holds 16 positions, an element is the sum of `terms`
+   bf16 values (1: bf16 precision; 2: hi + lo, what sessions use).
+     k_pool [n_pages][n_kv_heads][16][terms][head_dim],   v_pool [n_pages][n_kv_heads][terms][head_dim][16]   (16-byte aligned)
+   page_table: int32 [n_seqs][table_stride], the page of positions 16 i .. 16 i + 15 of sequence s at [s][i]; sequences may have pages in
+   common.  head_dim is 64 or 128.  Positions on entries outside [0, n_pages), and beyond the table, are neither
+   written nor attended to. */
+typedef struct {
+    int32_t device, n_kv_heads, head_dim, terms, n_pages, n_seqs, table_stride, reserved;
+    void *k_pool, *v_pool;
+    const int32_t *page_table;
+} ee_paged_cache;
+
+/* ee_kv_append: the new rows' queries, keys and values on their way into the attention, one pass over each.
+     queries and keys:  x <- x / sqrt(mean(x^2) + eps) * gain  for every head (q_gain, k_gain: fp32 [head_dim]; NULL: not normed),
+                        then (a, b) <- (a c - b s, b c + a s) with (c, s) = rope[position][j] (fp32 [rope_len][head_dim/2][2]; NULL: not
+                        rotated) for the pairs (a, b) = (x_j, x_{j + head_dim/2}), or (x_2j, x_2j+1) with rope_pairs = 1;
+     queries  -> q_out (may be q where type and strides agree);  keys and values -> their positions' places in the cache.
+   fp32 arithmetic, one rounding to the type stored.  q, k, v are of type `dtype`, q_out of q_out_dtype; strides count elements from row to
+   row and from head to head, a head's elements are contiguous; every row and head starts at a multiple of 16 bytes.  n_heads may be
+   0 (keys and values only).  Rows whose position is negative, or beyond the page table or the rope table, get zeros in q_out and no
+   place in the cache.  The places of two sequences' new rows must differ. */
+typedef struct {
+    int32_t dtype, q_out_dtype, n_heads, n_rows, rope_len, rope_pairs;
+    float eps;
+    int32_t reserved;
+    const int32_t *row_start, *kv_len;
+    const void *q, *k, *v;
+    void *q_out;
+    int64_t q_stride, q_head_stride, k_stride, k_head_stride, v_stride, v_head_stride, q_out_stride, q_out_head_stride;
+    const float *q_gain, *k_gain, *rope;
+} ee_append_args;
+int ee_kv_append(const ee_paged_cache *cache, const ee_append_args *args, void *stream);
+
+/* ee_attend: causal attention of the new rows over the cache (which holds their own keys and values already):
+     out_i = sum_j softmax_j(scale q_i . k_j) v_j   over the positions j <= kv_len - (rows of the sequence) + i;
+   a row that sees no position gets zeros, and what stands in places that a row does not see (infinities and NaN too) does not touch it.
+   An infinity among the keys and values that a row does see may make its result NaN (0 times an infinity in a product of terms).
+   Query head h reads key head h / (n_heads / n_kv_heads).  fp32 softmax and sums; queries of fp16 and fp32 are split into two bf16 terms,
+   as are the softmax's weights.
+   Pages that sequences have in common can be read once for all of them: group g is the sequences group_start[g] .. group_start[g+1] - 1
+   (int32 [n_groups + 1]; sequences outside all groups stand alone) whose first group_pages[g] page-table entries are the
+   same pages (the caller's word: only one member's are read).  n_groups = 0: nothing is shared.
+   max_kv, max_shared: positions of the longest sequence and of the longest common part, as well as the caller knows them (0: the
+   table's); they only choose how the work is split.
+   workspace: ee_attend_workspace bytes (may be 0), 256-byte aligned, for the same arguments (it reads no pointer); contents do not matter. */
+typedef struct {
+    int32_t dtype, out_dtype, n_heads, n_rows, n_groups, max_kv, max_shared;
+    float scale;
+    const int32_t *row_start, *kv_len, *group_start, *group_pages;
+    const void *q;
+    void *out;
+    int64_t q_stride, q_head_stride, out_stride, out_head_stride;
+} ee_attend_args;
+int ee_attend_workspace(const ee_paged_cache *cache, const ee_attend_args *args, size_t *bytes);
+int ee_attend(const ee_paged_cache *cache, const ee_attend_args *args, void *workspace, size_t workspace_bytes, void *stream);
+
+/* ee_accept_drafts: the rule of ee_verify_sampled (and, at temperature 0, of ee_verify) for logits in device memory, decided in 64-bit
+   arithmetic.  Row r of a sequence holds the logits after its token r, drafts[r] the token drafted to follow (of a sequence's last
+   row: nothing; the same for u and draft_probs):
+     q_r = softmax(logits_r / temperature);   draft x is kept iff u[r] * p_r(x) < q_r(x);   the first row whose draft is not kept emits
+     the first token k with sum_{j<=k} w_j > v[r] * sum_j w_j,  w = max(q_r - p_r, 0)  (w = q_r if that is zero everywhere, and in
+     the last row if all drafts are kept).
+   temperature 0: draft x is kept iff it is the row's largest logit, which is what the row emits (ties: the lowest token).
+   logits: [n_rows][vocab] of type `dtype`, logits_stride elements from row to row;  draft_probs: fp32 [n_rows][vocab] with probs_stride,
+   or NULL: every draft was certain (p = 1 for it, 0 for the others);  drafts int32 [n_rows];  u, v fp32 [n_rows] in [0, 1) (NULL where
+   every temperature is 0);  temperature fp32 [n_seqs].
+   Results, int32 [n_seqs]: accept_len (drafts kept), next_token; 0 and -1 for a sequence without rows.  A draft outside
+   [0, vocab) is not kept.  A row without a softmax (NaN, +infinity or nothing but -infinity among its logits), and every row at a temperature
+   that is negative or not finite, keeps nothing and emits token 0; at temperature 0 NaN is never the largest.
+   workspace: ee_accept_workspace bytes, 256-byte aligned; contents do not matter. */
+typedef struct {
+    int32_t device, dtype, n_seqs, n_rows, vocab, reserved;
+    const int32_t *row_start;
+    const void *logits;
+    int64_t logits_stride;
+    const int32_t *drafts;
+    const float *draft_probs;
+    int64_t probs_stride;
+    const float *u, *v, *temperature;
+    int32_t *accept_len, *next_token;
+} ee_accept_args;
+int ee_accept_workspace(const ee_accept_args *args, size_t *bytes);
+int ee_accept_drafts(const ee_accept_args *args, void *workspace, size_t workspace_bytes, void *stream);
 
 #ifdef __cplusplus
 }

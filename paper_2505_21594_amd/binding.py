@@ -30,6 +30,7 @@ SAMPLING = 4
 TIME_LAUNCHES = 16
 FORM_AUTO, FORM_PLAIN, FORM_PACKED = 0, 1, 2
 OPT_ATT_SPLITS, OPT_SCATTER_PAGES, OPT_HEAD_BATCH, OPT_PREFILL_GEMM, OPT_PREFILL_ATT_ROWS = 1, 2, 3, 4, 5
+BF16, FP16, FP32 = 0, 1, 2
 LAUNCH_NAMES = ("qkv", "o", "gu", "dn", "head", "adapter_down", "adapter_up", "embed", "att", "sample")
 
 EXPORTS = [
@@ -39,6 +40,7 @@ EXPORTS = [
     "ee_pass_time_ms", "ee_kv_truncate", "ee_set_pending", "ee_kv_len", "ee_pending",
     "ee_verify_sampled_batch", "ee_debug_logits", "ee_debug_mfma_layout", "ee_debug_div_small", "ee_tune_k_split", "ee_device_synchronize", "ee_session_option",
     "ee_launch_times", "ee_debug_copy", "ee_exit_pop", "ee_exit_order", "ee_latency_model",
+    "ee_kv_append", "ee_attend", "ee_attend_workspace", "ee_accept_drafts", "ee_accept_workspace",
 ]
 
 
@@ -80,6 +82,30 @@ class LatencyParamsC(ctypes.Structure):
 class LatencyC(ctypes.Structure):
     _fields_ = [(k, ctypes.c_double) for k in ("ar_ms", "sd_ms", "fsd_ms", "ar_ms_per_token", "sd_ms_per_token", "fsd_ms_per_token",
                                                 "speedup_ar_to_sd", "speedup_sd_to_fsd", "c", "projected_sd_to_fsd")]
+
+
+class PagedCacheC(ctypes.Structure):
+    _fields_ = [(k, ctypes.c_int32) for k in ("device", "n_kv_heads", "head_dim", "terms", "n_pages", "n_seqs", "table_stride", "reserved")] + [
+        (k, ctypes.c_void_p) for k in ("k_pool", "v_pool", "page_table")]
+
+
+class AppendArgsC(ctypes.Structure):
+    _fields_ = [(k, ctypes.c_int32) for k in ("dtype", "q_out_dtype", "n_heads", "n_rows", "rope_len", "rope_pairs")] + [
+        ("eps", ctypes.c_float), ("reserved", ctypes.c_int32)] + [(k, ctypes.c_void_p) for k in ("row_start", "kv_len", "q", "k", "v", "q_out")] + [
+        (k, ctypes.c_int64) for k in ("q_stride", "q_head_stride", "k_stride", "k_head_stride", "v_stride", "v_head_stride", "q_out_stride", "q_out_head_stride")] + [
+        (k, ctypes.c_void_p) for k in ("q_gain", "k_gain", "rope")]
+
+
+class AttendArgsC(ctypes.Structure):
+    _fields_ = [(k, ctypes.c_int32) for k in ("dtype", "out_dtype", "n_heads", "n_rows", "n_groups", "max_kv", "max_shared")] + [("scale", ctypes.c_float)] + [
+        (k, ctypes.c_void_p) for k in ("row_start", "kv_len", "group_start", "group_pages", "q", "out")] + [
+        (k, ctypes.c_int64) for k in ("q_stride", "q_head_stride", "out_stride", "out_head_stride")]
+
+
+class AcceptArgsC(ctypes.Structure):
+    _fields_ = [(k, ctypes.c_int32) for k in ("device", "dtype", "n_seqs", "n_rows", "vocab", "reserved")] + [
+        ("row_start", ctypes.c_void_p), ("logits", ctypes.c_void_p), ("logits_stride", ctypes.c_int64), ("drafts", ctypes.c_void_p), ("draft_probs", ctypes.c_void_p),
+        ("probs_stride", ctypes.c_int64)] + [(k, ctypes.c_void_p) for k in ("u", "v", "temperature", "accept_len", "next_token")]
 
 
 _lib = None
@@ -137,6 +163,12 @@ def load_library():
     lib.ee_latency_model.argtypes = [P(LatencyParamsC), P(LatencyC)]
     lib.ee_debug_copy.argtypes = [ci, ctypes.c_size_t, ci]
     lib.ee_launch_times.argtypes = [vp, i32p, P(ctypes.c_float), ci, P(ci)]
+    sz = ctypes.c_size_t
+    lib.ee_kv_append.argtypes = [P(PagedCacheC), P(AppendArgsC), vp]
+    lib.ee_attend_workspace.argtypes = [P(PagedCacheC), P(AttendArgsC), P(sz)]
+    lib.ee_attend.argtypes = [P(PagedCacheC), P(AttendArgsC), vp, sz, vp]
+    lib.ee_accept_workspace.argtypes = [P(AcceptArgsC), P(sz)]
+    lib.ee_accept_drafts.argtypes = [P(AcceptArgsC), vp, sz, vp]
     for name in EXPORTS:
         if name != "ee_last_error":
             getattr(lib, name).restype = ci
@@ -418,3 +450,185 @@ def ee_verify_batch(sessions: List[Session], drafts: List[Sequence[int]], exit_l
     _check(lib.ee_verify_batch(hs, n, dp, gamma, _p(ex), ex.size, outs))
     for i, s in enumerate(sessions):
         s._res, s._n_exits, s._gamma = outs[i], ex.size, gamma
+
+
+# ---------------------------------------------------------------- operators on device memory
+#
+# Arrays are objects in device memory with `data_ptr()`, `shape`, `stride()` (in elements), `dtype` and `device`, as a torch tensor has
+# them (this module does not import torch; a program that uses both imports torch first, so that one HIP runtime is loaded).  `stream` is a
+# hipStream_t as an integer (torch.cuda.current_stream().cuda_stream), 0 the device's default stream.
+
+_TYPE_OF = {}
+
+
+def _type(t) -> str:
+    """Name of an array's element type: "float32", "bfloat16", "int32", ..."""
+    name = _TYPE_OF.get(t.dtype)
+    if name is None:
+        name = _TYPE_OF[t.dtype] = str(t.dtype).rpartition(".")[2]
+    return name
+
+
+_FLOATS = {"bfloat16": BF16, "float16": FP16, "float32": FP32}
+
+
+def _on(t, what: str) -> int:
+    """Index of the GPU that holds the array."""
+    d = t.device
+    if d.type != "cuda":
+        raise ValueError(f"{what} is not in device memory")
+    return d.index or 0
+
+
+def _array(t, what: str, types, ndim: int, device: int, n=None) -> int:
+    """Address of a contiguous array of one of the types (None: 0), its length checked."""
+    if t is None:
+        return 0
+    if _type(t) not in types or len(t.shape) != ndim or (n is not None and t.shape[0] < n) or _on(t, what) != device:
+        raise ValueError(f"{what}: {ndim} dimension(s) of {'/'.join(types)} on device {device}" + (f", at least {n} long," if n is not None else "") + " expected")
+    if t.stride()[-1] != 1 and t.shape[-1] > 1:
+        raise ValueError(f"{what} must be contiguous")
+    return t.data_ptr()
+
+
+def _heads(t, what: str, rows, heads, dim: int, device: int):
+    """(address, type, row stride, head stride) of [rows][heads][dim] with contiguous heads."""
+    s = t.stride()
+    if len(t.shape) != 3 or t.shape[2] != dim or (rows is not None and t.shape[0] != rows) or (heads is not None and t.shape[1] != heads) or s[2] != 1:
+        raise ValueError(f"{what}: [{rows if rows is not None else 'rows'}][{heads if heads is not None else 'heads'}][{dim}] with contiguous heads expected")
+    kind = _FLOATS.get(_type(t))
+    if kind is None or _on(t, what) != device:
+        raise ValueError(f"{what}: bf16, fp16 or fp32 on device {device} expected")
+    return t.data_ptr(), kind, s[0], s[1]
+
+
+class PagedCache:
+    """ee_paged_cache over a caller's arrays, which it keeps: k_pool bf16 [n_pages][n_kv_heads][16][terms][head_dim], v_pool bf16
+    [n_pages][n_kv_heads][terms][head_dim][16], page_table int32 [n_seqs][pages of a sequence]."""
+
+    def __init__(self, k_pool, v_pool, page_table):
+        if len(k_pool.shape) != 5 or k_pool.shape[2] != 16 or len(v_pool.shape) != 5:
+            raise ValueError("k_pool [n_pages][n_kv_heads][16][terms][head_dim] and v_pool [n_pages][n_kv_heads][terms][head_dim][16] expected")
+        n, heads, _, terms, dim = k_pool.shape
+        if tuple(v_pool.shape) != (n, heads, terms, dim, 16):
+            raise ValueError("v_pool: the same pages, heads and terms as k_pool expected")
+        self.device = _on(k_pool, "k_pool")
+        for t, what in ((k_pool, "k_pool"), (v_pool, "v_pool")):
+            want, at = [], 1
+            for size in reversed(t.shape):
+                want.append(at)
+                at *= size
+            if _type(t) != "bfloat16" or tuple(t.stride()) != tuple(reversed(want)) or _on(t, what) != self.device:
+                raise ValueError(f"{what}: contiguous bf16 on device {self.device} expected")
+        if len(page_table.shape) != 2 or _type(page_table) != "int32" or page_table.stride()[1] != 1 or _on(page_table, "page_table") != self.device:
+            raise ValueError("page_table: int32 [n_seqs][entries] expected")
+        self.k_pool, self.v_pool, self.page_table = k_pool, v_pool, page_table
+        self.n_kv_heads, self.head_dim, self.n_seqs = heads, dim, page_table.shape[0]
+        stride = page_table.stride()[0] if self.n_seqs > 1 else page_table.shape[1]
+        if stride != page_table.shape[1]:
+            raise ValueError("page_table: contiguous expected")
+        self.c = PagedCacheC(self.device, heads, dim, terms, n, self.n_seqs, stride, 0, k_pool.data_ptr(), v_pool.data_ptr(), page_table.data_ptr())
+
+
+def ee_kv_append(cache: PagedCache, row_start, kv_len, q, k, v, q_out, q_gain=None, k_gain=None, eps: float = 1e-5, rope=None, rope_pairs: bool = False,
+                 stream: int = 0) -> None:
+    """q, q_out [rows][heads][head_dim] (q may be None: keys and values only), k, v [rows][n_kv_heads][head_dim], gains fp32 [head_dim],
+    rope fp32 [positions][head_dim / 2][2]."""
+    dev, dim, n = cache.device, cache.head_dim, cache.n_seqs
+    rows = k.shape[0]
+    kp, kind, ks, kh = _heads(k, "k", rows, cache.n_kv_heads, dim, dev)
+    vp_, kind_v, vs, vh = _heads(v, "v", rows, cache.n_kv_heads, dim, dev)
+    if kind_v != kind:
+        raise ValueError("q, k and v must be of one type")
+    qp = qs = qh = op = os_ = oh = heads = 0
+    kind_o = kind
+    if q is not None:
+        heads = q.shape[1]
+        qp, kind_q, qs, qh = _heads(q, "q", rows, None, dim, dev)
+        op, kind_o, os_, oh = _heads(q_out, "q_out", rows, heads, dim, dev)
+        if kind_q != kind:
+            raise ValueError("q, k and v must be of one type")
+    f32 = ("float32",)
+    gq, gk = _array(q_gain, "q_gain", f32, 1, dev, dim), _array(k_gain, "k_gain", f32, 1, dev, dim)
+    rp = _array(rope, "rope", f32, 3, dev)
+    if rope is not None and (tuple(rope.shape[1:]) != (dim // 2, 2) or rope.stride()[:2] != (dim, 2)):
+        raise ValueError("rope: contiguous [positions][head_dim / 2][2] expected")
+    a = AppendArgsC(kind, kind_o, heads, rows, rope.shape[0] if rope is not None else 0, 1 if rope_pairs else 0, eps, 0,
+                    _array(row_start, "row_start", ("int32",), 1, dev, n + 1), _array(kv_len, "kv_len", ("int32",), 1, dev, n),
+                    qp, kp, vp_, op, qs, qh, ks, kh, vs, vh, os_, oh, gq, gk, rp)
+    _check(load_library().ee_kv_append(ctypes.byref(cache.c), ctypes.byref(a), stream))
+
+
+def _attend_args(cache: PagedCache, row_start, kv_len, q, out, scale, max_kv, group_start, group_pages, max_shared) -> AttendArgsC:
+    dev, dim, n = cache.device, cache.head_dim, cache.n_seqs
+    qp, kind, qs, qh = _heads(q, "q", None, None, dim, dev)
+    op, kind_o, os_, oh = _heads(out, "out", q.shape[0], q.shape[1], dim, dev) if out is not None else (0, kind, qs, qh)
+    groups = 0
+    if group_start is not None:
+        groups = group_start.shape[0] - 1
+        if group_pages is None or groups < 0:
+            raise ValueError("group_start [groups + 1] comes with group_pages [groups]")
+    i32 = ("int32",)
+    return AttendArgsC(kind, kind_o, q.shape[1], q.shape[0], groups, max_kv, max_shared, scale, _array(row_start, "row_start", i32, 1, dev, n + 1),
+                       _array(kv_len, "kv_len", i32, 1, dev, n), _array(group_start, "group_start", i32, 1, dev),
+                       _array(group_pages, "group_pages", i32, 1, dev, groups) if groups else 0, qp, op, qs, qh, os_, oh)
+
+
+def ee_attend_workspace(cache: PagedCache, row_start, q, max_kv: int = 0, group_start=None, group_pages=None, max_shared: int = 0) -> int:
+    """Bytes of workspace for calls of ee_attend with these sizes."""
+    a = _attend_args(cache, row_start, None, q, None, 1.0, max_kv, group_start, group_pages, max_shared)
+    n = ctypes.c_size_t()
+    _check(load_library().ee_attend_workspace(ctypes.byref(cache.c), ctypes.byref(a), ctypes.byref(n)))
+    return int(n.value)
+
+
+def _space(t, device: int):
+    if t is None:
+        return 0, 0
+    size = 1
+    for x in t.shape:
+        size *= x
+    if _type(t) != "uint8" or len(t.shape) != 1 or _on(t, "workspace") != device:
+        raise ValueError(f"workspace: uint8 array on device {device} expected")
+    return t.data_ptr(), size
+
+
+def ee_attend(cache: PagedCache, row_start, kv_len, q, out, scale: float, max_kv: int = 0, group_start=None, group_pages=None, max_shared: int = 0,
+              workspace=None, stream: int = 0) -> None:
+    """q, out [rows][heads][head_dim]; group_start int32 [groups + 1] and group_pages int32 [groups] where sequences have pages in common."""
+    a = _attend_args(cache, row_start, kv_len, q, out, scale, max_kv, group_start, group_pages, max_shared)
+    wp, size = _space(workspace, cache.device)
+    _check(load_library().ee_attend(ctypes.byref(cache.c), ctypes.byref(a), wp, size, stream))
+
+
+def _accept_args(logits, row_start, drafts=None, draft_probs=None, u=None, v=None, temperature=None, accept_len=None, next_token=None) -> AcceptArgsC:
+    dev = _on(logits, "logits")
+    kind = _FLOATS.get(_type(logits))
+    if len(logits.shape) != 2 or kind is None or logits.stride()[1] != 1:
+        raise ValueError("logits: [rows][vocab] of bf16, fp16 or fp32 with contiguous rows expected")
+    rows, V = logits.shape
+    n = row_start.shape[0] - 1
+    f32, i32 = ("float32",), ("int32",)
+    if draft_probs is not None and (tuple(draft_probs.shape) != (rows, V)):
+        raise ValueError("draft_probs: [rows][vocab] expected")
+    # (a single row's stride says nothing)
+    return AcceptArgsC(dev, kind, n, rows, V, 0, _array(row_start, "row_start", i32, 1, dev, 1), logits.data_ptr(), max(logits.stride()[0], V) if rows < 2 else logits.stride()[0],
+                       _array(drafts, "drafts", i32, 1, dev, rows), _array(draft_probs, "draft_probs", f32, 2, dev),
+                       0 if draft_probs is None else max(draft_probs.stride()[0], V) if rows < 2 else draft_probs.stride()[0],
+                       _array(u, "u", f32, 1, dev, rows), _array(v, "v", f32, 1, dev, rows), _array(temperature, "temperature", f32, 1, dev, n),
+                       _array(accept_len, "accept_len", i32, 1, dev, n), _array(next_token, "next_token", i32, 1, dev, n))
+
+
+def ee_accept_workspace(logits, row_start) -> int:
+    """Bytes of workspace for calls of ee_accept_drafts with these sizes."""
+    n = ctypes.c_size_t()
+    _check(load_library().ee_accept_workspace(ctypes.byref(_accept_args(logits, row_start)), ctypes.byref(n)))
+    return int(n.value)
+
+
+def ee_accept_drafts(logits, row_start, drafts, draft_probs, u, v, temperature, accept_len, next_token, workspace, stream: int = 0) -> None:
+    """logits [rows][vocab], drafts int32 [rows], draft_probs fp32 [rows][vocab] or None, u and v fp32 [rows], temperature fp32 [sequences];
+    results accept_len, next_token int32 [sequences]."""
+    a = _accept_args(logits, row_start, drafts, draft_probs, u, v, temperature, accept_len, next_token)
+    wp, size = _space(workspace, a.device)
+    _check(load_library().ee_accept_drafts(ctypes.byref(a), wp, size, stream))

@@ -1,0 +1,135 @@
+// What the operators on device memory (ee_kv_append, ee_attend, ee_accept_drafts) share: the sequences of a batch as the
+// kernels read them, element types, and the host's checks.
+#pragma once
+
+#include <math.h>
+
+#include <algorithm>
+
+#include "ee_host.hpp"
+#include "ee_kernels.hpp"
+
+namespace ee {
+
+constexpr int OPS_MAX_GRID_Y = 65535;
+
+// A cache and the new rows of its sequences, as a caller of the operators holds them.  Everything that is read from
+// device memory is clamped to what the host knows, so that no value of it leads outside an array.
+struct BatchDev {
+    uint16_t *kpool, *vpool;
+    const int *table, *row_start, *kv_len;
+    int n_pages, n_seqs, n_rows, table_stride, n_kv_heads;
+
+    // first row of sequence s (s <= n_seqs)
+    __device__ __forceinline__ int start(int s) const { return min(max(as_global(row_start)[s], 0), n_rows); }
+    // positions of sequence s that the cache has room for
+    __device__ __forceinline__ int length(int s) const { return max(as_global(kv_len)[s], 0); }
+    __device__ __forceinline__ int capacity() const { return min(table_stride, 0x7FFFFFF0 / KV_PAGE) * KV_PAGE; }
+};
+
+// inclusive sum over the lanes of a wave
+__device__ __forceinline__ int wave_scan(int x, int lane)
+{
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+        const int y = __shfl_up(x, d, 64);
+        x += lane >= d ? y : 0;
+    }
+    return x;
+}
+
+// Which of n things item `item` belongs to when thing i has count(i) items, and its place there; false past the last.  All
+// lanes of a wave call it and get the same answer; 64 things a round.
+template <typename F>
+__device__ __forceinline__ bool find_item(int n, int item, int lane, F count, int &index, int &place)
+{
+    for (int base = 0; base < n; base += 64) {
+        const int c = base + lane < n ? count(base + lane) : 0;
+        const int incl = wave_scan(c, lane), total = __shfl(incl, 63, 64);
+        if (item < total) {
+            const int l = __builtin_ctzll(__ballot(incl > item));
+            index = __builtin_amdgcn_readfirstlane(base + l);
+            place = __builtin_amdgcn_readfirstlane(item - __shfl(incl - c, l, 64));
+            return true;
+        }
+        item -= total;
+    }
+    return false;
+}
+
+// eight neighbouring elements as floats; 16-byte aligned
+template <int TYPE>
+__device__ __forceinline__ void load8(const void *base, size_t at, float (&x)[8])
+{
+    if constexpr (TYPE == EE_FP32) {
+        const f32x4_t *p = reinterpret_cast<const f32x4_t *>(static_cast<const float *>(base) + at);
+        const f32x4_t a = as_global(p)[0], b = as_global(p)[1];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            x[i] = a[i];
+            x[4 + i] = b[i];
+        }
+    } else {
+        const uint4 v = load_global16(static_cast<const uint16_t *>(base) + at);
+        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if constexpr (TYPE == EE_BF16) {
+                x[2 * i] = __uint_as_float(w[i] << 16);
+                x[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
+            } else {
+                typedef __attribute__((ext_vector_type(2))) _Float16 f16x2_t;
+                const f16x2_t h = __builtin_bit_cast(f16x2_t, w[i]);
+                x[2 * i] = (float)h[0];
+                x[2 * i + 1] = (float)h[1];
+            }
+        }
+    }
+}
+
+__device__ __forceinline__ uint32_t pack_fp16(float a, float b)
+{
+    return (uint32_t)__builtin_bit_cast(uint16_t, (_Float16)a) | (uint32_t)__builtin_bit_cast(uint16_t, (_Float16)b) << 16;
+}
+
+// four neighbouring elements of the type, rounded once
+__device__ __forceinline__ void store4(int type, void *base, size_t at, float a, float b, float c, float d)
+{
+    if (type == EE_FP32) {
+        *as_global_mut(reinterpret_cast<f32x4_t *>(static_cast<float *>(base) + at)) = (f32x4_t){a, b, c, d};
+    } else {
+        const u32x2_t v = type == EE_BF16 ? (u32x2_t){pack_bf16(a, b), pack_bf16(c, d)} : (u32x2_t){pack_fp16(a, b), pack_fp16(c, d)};
+        *as_global_mut(reinterpret_cast<u32x2_t *>(static_cast<uint16_t *>(base) + at)) = v;
+    }
+}
+
+// ------------------------------------------------------------------ host
+
+inline size_t size_of_type(int type) { return type == EE_FP32 ? 4 : 2; }
+inline bool aligned(const void *p, size_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) == 0; }
+// a row or head stride: its multiples keep 16-byte alignment
+inline bool stride_ok(int64_t stride, int type) { return stride >= 0 && stride < (int64_t)1 << 40 && stride * (int64_t)size_of_type(type) % 16 == 0; }
+
+// The GPU that a call works on is current inside it, the caller's again after it.
+struct DeviceScope {
+    int before = -1;
+    hipError_t status;
+    explicit DeviceScope(int device)
+    {
+        status = hipGetDevice(&before);
+        if (status == hipSuccess && before != device)
+            status = hipSetDevice(device);
+        else
+            before = -1;
+    }
+    ~DeviceScope()
+    {
+        if (before >= 0) hipSetDevice(before);
+    }
+};
+
+// What ee_kv_append and ee_attend demand of a cache and of the batch's rows.
+int check_cache(const char *call, const ee_paged_cache *c, int n_rows, int n_heads, const void *row_start, const void *kv_len);
+BatchDev batch_of(const ee_paged_cache &c, int n_rows, const int32_t *row_start, const int32_t *kv_len);
+
+}  // namespace ee

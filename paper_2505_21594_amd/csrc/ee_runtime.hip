@@ -16,6 +16,7 @@
 #include <utility>
 #include <vector>
 
+#include "ee_host.hpp"
 #include "ee_once.hpp"
 
 using namespace ee;
@@ -24,7 +25,7 @@ using namespace ee;
 
 static thread_local char g_err[512] = "";
 
-static int fail(int code, const char *fmt, ...)
+int ee::fail(int code, const char *fmt, ...)
 {
     va_list ap;
     va_start(ap, fmt);
@@ -32,13 +33,6 @@ static int fail(int code, const char *fmt, ...)
     va_end(ap);
     return code;
 }
-
-#define HIP_TRY(expr)                                                                          \
-    do {                                                                                       \
-        hipError_t e_ = (expr);                                                                \
-        if (e_ != hipSuccess)                                                                  \
-            return fail(EE_EDEVICE, "%s failed: %s (%s:%d)", #expr, hipGetErrorString(e_), __FILE__, __LINE__); \
-    } while (0)
 
 extern "C" const char *ee_last_error(void) { return g_err; }
 
