@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 from dataclasses import dataclass
 from typing import List, Optional, Sequence
 
@@ -164,11 +165,11 @@ def load_library():
     lib.ee_debug_copy.argtypes = [ci, ctypes.c_size_t, ci]
     lib.ee_launch_times.argtypes = [vp, i32p, P(ctypes.c_float), ci, P(ci)]
     sz = ctypes.c_size_t
-    lib.ee_kv_append.argtypes = [P(PagedCacheC), P(AppendArgsC), vp]
-    lib.ee_attend_workspace.argtypes = [P(PagedCacheC), P(AttendArgsC), P(sz)]
-    lib.ee_attend.argtypes = [P(PagedCacheC), P(AttendArgsC), vp, sz, vp]
-    lib.ee_accept_workspace.argtypes = [P(AcceptArgsC), P(sz)]
-    lib.ee_accept_drafts.argtypes = [P(AcceptArgsC), vp, sz, vp]
+    lib.ee_kv_append.argtypes = [vp, vp, vp]              # (structures by address, or packed as bytes)
+    lib.ee_attend_workspace.argtypes = [vp, vp, P(sz)]
+    lib.ee_attend.argtypes = [vp, vp, vp, sz, vp]
+    lib.ee_accept_workspace.argtypes = [vp, P(sz)]
+    lib.ee_accept_drafts.argtypes = [vp, vp, sz, vp]
     for name in EXPORTS:
         if name != "ee_last_error":
             getattr(lib, name).restype = ci
@@ -457,8 +458,16 @@ def ee_verify_batch(sessions: List[Session], drafts: List[Sequence[int]], exit_l
 # Arrays are objects in device memory with `data_ptr()`, `shape`, `stride()` (in elements), `dtype` and `device`, as a torch tensor has
 # them (this module does not import torch; a program that uses both imports torch first, so that one HIP runtime is loaded).  `stream` is a
 # hipStream_t as an integer (torch.cuda.current_stream().cuda_stream), 0 the device's default stream.
+#
+# A call of a few microseconds is bound by what happens here, so the checks read each attribute once and the arguments are packed
+# in one go (a ctypes structure of 25 fields takes 4 us to fill, struct.pack 1).
+
+_APPEND_PACK = struct.Struct("@6ifi6P8q3P").pack
+_ATTEND_PACK = struct.Struct("@7if6P4q").pack
+_ACCEPT_PACK = struct.Struct("@6i2Pq2Pq5P").pack
 
 _TYPE_OF = {}
+_FLOATS = {"bfloat16": BF16, "float16": FP16, "float32": FP32}
 
 
 def _type(t) -> str:
@@ -469,9 +478,6 @@ def _type(t) -> str:
     return name
 
 
-_FLOATS = {"bfloat16": BF16, "float16": FP16, "float32": FP32}
-
-
 def _on(t, what: str) -> int:
     """Index of the GPU that holds the array."""
     d = t.device
@@ -480,26 +486,25 @@ def _on(t, what: str) -> int:
     return d.index or 0
 
 
-def _array(t, what: str, types, ndim: int, device: int, n=None) -> int:
-    """Address of a contiguous array of one of the types (None: 0), its length checked."""
+def _vector(t, what: str, kind: str, device, n: int) -> int:
+    """Address of a contiguous one-dimensional array of at least n elements (None: 0)."""
     if t is None:
         return 0
-    if _type(t) not in types or len(t.shape) != ndim or (n is not None and t.shape[0] < n) or _on(t, what) != device:
-        raise ValueError(f"{what}: {ndim} dimension(s) of {'/'.join(types)} on device {device}" + (f", at least {n} long," if n is not None else "") + " expected")
-    if t.stride()[-1] != 1 and t.shape[-1] > 1:
-        raise ValueError(f"{what} must be contiguous")
+    shape = t.shape
+    if len(shape) != 1 or shape[0] < n or _type(t) != kind or t.device != device or (shape[0] > 1 and t.stride()[0] != 1):
+        raise ValueError(f"{what}: contiguous {kind} array of at least {n} elements on {device} expected")
     return t.data_ptr()
 
 
-def _heads(t, what: str, rows, heads, dim: int, device: int):
-    """(address, type, row stride, head stride) of [rows][heads][dim] with contiguous heads."""
-    s = t.stride()
-    if len(t.shape) != 3 or t.shape[2] != dim or (rows is not None and t.shape[0] != rows) or (heads is not None and t.shape[1] != heads) or s[2] != 1:
-        raise ValueError(f"{what}: [{rows if rows is not None else 'rows'}][{heads if heads is not None else 'heads'}][{dim}] with contiguous heads expected")
+def _heads(t, what: str, rows, heads, dim: int, device):
+    """(address, type, row stride, head stride, rows, heads) of [rows][heads][dim] with contiguous heads."""
+    shape, s = t.shape, t.stride()
     kind = _FLOATS.get(_type(t))
-    if kind is None or _on(t, what) != device:
-        raise ValueError(f"{what}: bf16, fp16 or fp32 on device {device} expected")
-    return t.data_ptr(), kind, s[0], s[1]
+    if len(shape) != 3 or shape[2] != dim or (rows is not None and shape[0] != rows) or (heads is not None and shape[1] != heads) or s[2] != 1:
+        raise ValueError(f"{what}: [{rows if rows is not None else 'rows'}][{heads if heads is not None else 'heads'}][{dim}] with contiguous heads expected")
+    if kind is None or t.device != device:
+        raise ValueError(f"{what}: bf16, fp16 or fp32 on {device} expected")
+    return t.data_ptr(), kind, s[0], s[1], shape[0], shape[1]
 
 
 class PagedCache:
@@ -512,117 +517,104 @@ class PagedCache:
         n, heads, _, terms, dim = k_pool.shape
         if tuple(v_pool.shape) != (n, heads, terms, dim, 16):
             raise ValueError("v_pool: the same pages, heads and terms as k_pool expected")
-        self.device = _on(k_pool, "k_pool")
+        device = _on(k_pool, "k_pool")
+        self.device = k_pool.device
         for t, what in ((k_pool, "k_pool"), (v_pool, "v_pool")):
             want, at = [], 1
             for size in reversed(t.shape):
                 want.append(at)
                 at *= size
-            if _type(t) != "bfloat16" or tuple(t.stride()) != tuple(reversed(want)) or _on(t, what) != self.device:
-                raise ValueError(f"{what}: contiguous bf16 on device {self.device} expected")
-        if len(page_table.shape) != 2 or _type(page_table) != "int32" or page_table.stride()[1] != 1 or _on(page_table, "page_table") != self.device:
+            if _type(t) != "bfloat16" or tuple(t.stride()) != tuple(reversed(want)) or t.device != self.device:
+                raise ValueError(f"{what}: contiguous bf16 on {self.device} expected")
+        if len(page_table.shape) != 2 or _type(page_table) != "int32" or page_table.device != self.device or page_table.stride()[1] != 1:
             raise ValueError("page_table: int32 [n_seqs][entries] expected")
-        self.k_pool, self.v_pool, self.page_table = k_pool, v_pool, page_table
         self.n_kv_heads, self.head_dim, self.n_seqs = heads, dim, page_table.shape[0]
-        stride = page_table.stride()[0] if self.n_seqs > 1 else page_table.shape[1]
-        if stride != page_table.shape[1]:
+        if self.n_seqs > 1 and page_table.stride()[0] != page_table.shape[1]:
             raise ValueError("page_table: contiguous expected")
-        self.c = PagedCacheC(self.device, heads, dim, terms, n, self.n_seqs, stride, 0, k_pool.data_ptr(), v_pool.data_ptr(), page_table.data_ptr())
+        self.k_pool, self.v_pool, self.page_table = k_pool, v_pool, page_table
+        self.c = PagedCacheC(device, heads, dim, terms, n, self.n_seqs, page_table.shape[1], 0, k_pool.data_ptr(), v_pool.data_ptr(), page_table.data_ptr())
+        self._at = ctypes.addressof(self.c)
 
 
 def ee_kv_append(cache: PagedCache, row_start, kv_len, q, k, v, q_out, q_gain=None, k_gain=None, eps: float = 1e-5, rope=None, rope_pairs: bool = False,
                  stream: int = 0) -> None:
     """q, q_out [rows][heads][head_dim] (q may be None: keys and values only), k, v [rows][n_kv_heads][head_dim], gains fp32 [head_dim],
     rope fp32 [positions][head_dim / 2][2]."""
-    dev, dim, n = cache.device, cache.head_dim, cache.n_seqs
-    rows = k.shape[0]
-    kp, kind, ks, kh = _heads(k, "k", rows, cache.n_kv_heads, dim, dev)
-    vp_, kind_v, vs, vh = _heads(v, "v", rows, cache.n_kv_heads, dim, dev)
-    if kind_v != kind:
-        raise ValueError("q, k and v must be of one type")
+    dev, dim, n, kv_heads = cache.device, cache.head_dim, cache.n_seqs, cache.n_kv_heads
+    kp, kind, ks, kh, rows, _ = _heads(k, "k", None, kv_heads, dim, dev)
+    vp, kind_v, vs, vh, _, _ = _heads(v, "v", rows, kv_heads, dim, dev)
     qp = qs = qh = op = os_ = oh = heads = 0
-    kind_o = kind
+    kind_q = kind_o = kind
     if q is not None:
-        heads = q.shape[1]
-        qp, kind_q, qs, qh = _heads(q, "q", rows, None, dim, dev)
-        op, kind_o, os_, oh = _heads(q_out, "q_out", rows, heads, dim, dev)
-        if kind_q != kind:
-            raise ValueError("q, k and v must be of one type")
-    f32 = ("float32",)
-    gq, gk = _array(q_gain, "q_gain", f32, 1, dev, dim), _array(k_gain, "k_gain", f32, 1, dev, dim)
-    rp = _array(rope, "rope", f32, 3, dev)
-    if rope is not None and (tuple(rope.shape[1:]) != (dim // 2, 2) or rope.stride()[:2] != (dim, 2)):
-        raise ValueError("rope: contiguous [positions][head_dim / 2][2] expected")
-    a = AppendArgsC(kind, kind_o, heads, rows, rope.shape[0] if rope is not None else 0, 1 if rope_pairs else 0, eps, 0,
-                    _array(row_start, "row_start", ("int32",), 1, dev, n + 1), _array(kv_len, "kv_len", ("int32",), 1, dev, n),
-                    qp, kp, vp_, op, qs, qh, ks, kh, vs, vh, os_, oh, gq, gk, rp)
-    _check(load_library().ee_kv_append(ctypes.byref(cache.c), ctypes.byref(a), stream))
+        qp, kind_q, qs, qh, _, heads = _heads(q, "q", rows, None, dim, dev)
+        op, kind_o, os_, oh, _, _ = _heads(q_out, "q_out", rows, heads, dim, dev)
+    if kind_v != kind or kind_q != kind:
+        raise ValueError("q, k and v must be of one type")
+    rp = positions = 0
+    if rope is not None:
+        shape = rope.shape
+        if len(shape) != 3 or shape[1] != dim // 2 or shape[2] != 2 or _type(rope) != "float32" or rope.device != dev or tuple(rope.stride()) != (dim, 2, 1):
+            raise ValueError(f"rope: contiguous fp32 [positions][{dim // 2}][2] on {dev} expected")
+        rp, positions = rope.data_ptr(), shape[0]
+    a = _APPEND_PACK(kind, kind_o, heads, rows, positions, 1 if rope_pairs else 0, eps, 0, _vector(row_start, "row_start", "int32", dev, n + 1),
+                     _vector(kv_len, "kv_len", "int32", dev, n), qp, kp, vp, op, qs, qh, ks, kh, vs, vh, os_, oh, _vector(q_gain, "q_gain", "float32", dev, dim),
+                     _vector(k_gain, "k_gain", "float32", dev, dim), rp)
+    _check((_lib or load_library()).ee_kv_append(cache._at, a, stream))
 
 
-def _attend_args(cache: PagedCache, row_start, kv_len, q, out, scale, max_kv, group_start, group_pages, max_shared) -> AttendArgsC:
+def _attend_args(cache: PagedCache, row_start, kv_len, q, out, scale, max_kv, group_start, group_pages, max_shared) -> bytes:
     dev, dim, n = cache.device, cache.head_dim, cache.n_seqs
-    qp, kind, qs, qh = _heads(q, "q", None, None, dim, dev)
-    op, kind_o, os_, oh = _heads(out, "out", q.shape[0], q.shape[1], dim, dev) if out is not None else (0, kind, qs, qh)
+    qp, kind, qs, qh, rows, heads = _heads(q, "q", None, None, dim, dev)
+    op, kind_o, os_, oh = (0, kind, qs, qh) if out is None else _heads(out, "out", rows, heads, dim, dev)[:4]
     groups = 0
     if group_start is not None:
         groups = group_start.shape[0] - 1
         if group_pages is None or groups < 0:
             raise ValueError("group_start [groups + 1] comes with group_pages [groups]")
-    i32 = ("int32",)
-    return AttendArgsC(kind, kind_o, q.shape[1], q.shape[0], groups, max_kv, max_shared, scale, _array(row_start, "row_start", i32, 1, dev, n + 1),
-                       _array(kv_len, "kv_len", i32, 1, dev, n), _array(group_start, "group_start", i32, 1, dev),
-                       _array(group_pages, "group_pages", i32, 1, dev, groups) if groups else 0, qp, op, qs, qh, os_, oh)
+    return _ATTEND_PACK(kind, kind_o, heads, rows, groups, max_kv, max_shared, scale, _vector(row_start, "row_start", "int32", dev, n + 1),
+                        _vector(kv_len, "kv_len", "int32", dev, n), _vector(group_start, "group_start", "int32", dev, 0),
+                        _vector(group_pages, "group_pages", "int32", dev, groups), qp, op, qs, qh, os_, oh)
 
 
 def ee_attend_workspace(cache: PagedCache, row_start, q, max_kv: int = 0, group_start=None, group_pages=None, max_shared: int = 0) -> int:
     """Bytes of workspace for calls of ee_attend with these sizes."""
     a = _attend_args(cache, row_start, None, q, None, 1.0, max_kv, group_start, group_pages, max_shared)
     n = ctypes.c_size_t()
-    _check(load_library().ee_attend_workspace(ctypes.byref(cache.c), ctypes.byref(a), ctypes.byref(n)))
+    _check(load_library().ee_attend_workspace(cache._at, a, ctypes.byref(n)))
     return int(n.value)
-
-
-def _space(t, device: int):
-    if t is None:
-        return 0, 0
-    size = 1
-    for x in t.shape:
-        size *= x
-    if _type(t) != "uint8" or len(t.shape) != 1 or _on(t, "workspace") != device:
-        raise ValueError(f"workspace: uint8 array on device {device} expected")
-    return t.data_ptr(), size
 
 
 def ee_attend(cache: PagedCache, row_start, kv_len, q, out, scale: float, max_kv: int = 0, group_start=None, group_pages=None, max_shared: int = 0,
               workspace=None, stream: int = 0) -> None:
     """q, out [rows][heads][head_dim]; group_start int32 [groups + 1] and group_pages int32 [groups] where sequences have pages in common."""
     a = _attend_args(cache, row_start, kv_len, q, out, scale, max_kv, group_start, group_pages, max_shared)
-    wp, size = _space(workspace, cache.device)
-    _check(load_library().ee_attend(ctypes.byref(cache.c), ctypes.byref(a), wp, size, stream))
+    _check((_lib or load_library()).ee_attend(cache._at, a, _vector(workspace, "workspace", "uint8", cache.device, 0), 0 if workspace is None else workspace.shape[0], stream))
 
 
-def _accept_args(logits, row_start, drafts=None, draft_probs=None, u=None, v=None, temperature=None, accept_len=None, next_token=None) -> AcceptArgsC:
-    dev = _on(logits, "logits")
+def _accept_args(logits, row_start, drafts=None, draft_probs=None, u=None, v=None, temperature=None, accept_len=None, next_token=None) -> bytes:
+    dev, shape, s = logits.device, logits.shape, logits.stride()
     kind = _FLOATS.get(_type(logits))
-    if len(logits.shape) != 2 or kind is None or logits.stride()[1] != 1:
+    if len(shape) != 2 or kind is None or s[1] != 1:
         raise ValueError("logits: [rows][vocab] of bf16, fp16 or fp32 with contiguous rows expected")
-    rows, V = logits.shape
+    rows, V = shape
     n = row_start.shape[0] - 1
-    f32, i32 = ("float32",), ("int32",)
-    if draft_probs is not None and (tuple(draft_probs.shape) != (rows, V)):
-        raise ValueError("draft_probs: [rows][vocab] expected")
+    pp = ps = 0
+    if draft_probs is not None:
+        t = draft_probs.stride()
+        if tuple(draft_probs.shape) != (rows, V) or _type(draft_probs) != "float32" or draft_probs.device != dev or t[1] != 1:
+            raise ValueError(f"draft_probs: fp32 [{rows}][{V}] with contiguous rows on {dev} expected")
+        pp, ps = draft_probs.data_ptr(), t[0] if rows > 1 else V
     # (a single row's stride says nothing)
-    return AcceptArgsC(dev, kind, n, rows, V, 0, _array(row_start, "row_start", i32, 1, dev, 1), logits.data_ptr(), max(logits.stride()[0], V) if rows < 2 else logits.stride()[0],
-                       _array(drafts, "drafts", i32, 1, dev, rows), _array(draft_probs, "draft_probs", f32, 2, dev),
-                       0 if draft_probs is None else max(draft_probs.stride()[0], V) if rows < 2 else draft_probs.stride()[0],
-                       _array(u, "u", f32, 1, dev, rows), _array(v, "v", f32, 1, dev, rows), _array(temperature, "temperature", f32, 1, dev, n),
-                       _array(accept_len, "accept_len", i32, 1, dev, n), _array(next_token, "next_token", i32, 1, dev, n))
+    return _ACCEPT_PACK(_on(logits, "logits"), kind, n, rows, V, 0, _vector(row_start, "row_start", "int32", dev, 1), logits.data_ptr(), s[0] if rows > 1 else V,
+                        _vector(drafts, "drafts", "int32", dev, rows), pp, ps, _vector(u, "u", "float32", dev, rows), _vector(v, "v", "float32", dev, rows),
+                        _vector(temperature, "temperature", "float32", dev, n), _vector(accept_len, "accept_len", "int32", dev, n),
+                        _vector(next_token, "next_token", "int32", dev, n))
 
 
 def ee_accept_workspace(logits, row_start) -> int:
     """Bytes of workspace for calls of ee_accept_drafts with these sizes."""
     n = ctypes.c_size_t()
-    _check(load_library().ee_accept_workspace(ctypes.byref(_accept_args(logits, row_start)), ctypes.byref(n)))
+    _check(load_library().ee_accept_workspace(_accept_args(logits, row_start), ctypes.byref(n)))
     return int(n.value)
 
 
@@ -630,5 +622,4 @@ def ee_accept_drafts(logits, row_start, drafts, draft_probs, u, v, temperature, 
     """logits [rows][vocab], drafts int32 [rows], draft_probs fp32 [rows][vocab] or None, u and v fp32 [rows], temperature fp32 [sequences];
     results accept_len, next_token int32 [sequences]."""
     a = _accept_args(logits, row_start, drafts, draft_probs, u, v, temperature, accept_len, next_token)
-    wp, size = _space(workspace, a.device)
-    _check(load_library().ee_accept_drafts(ctypes.byref(a), wp, size, stream))
+    _check((_lib or load_library()).ee_accept_drafts(a, _vector(workspace, "workspace", "uint8", logits.device, 0), workspace.shape[0], stream))

@@ -5,6 +5,7 @@ import numpy as np
 import pytest
 
 import paper_2505_21594_amd as ee
+from paper_2505_21594_amd import binding
 from paper_2505_21594_amd.binding import AcceptArgsC, AppendArgsC, AttendArgsC, PagedCacheC
 from tests import operators_ref as ref
 
@@ -114,6 +115,11 @@ def test_struct_layouts_match_header():
     assert ctypes.sizeof(AppendArgsC) == 8 * 4 + 6 * 8 + 8 * 8 + 3 * 8
     assert ctypes.sizeof(AttendArgsC) == 8 * 4 + 6 * 8 + 4 * 8
     assert ctypes.sizeof(AcceptArgsC) == 6 * 4 + 11 * 8
+    for fmt, c in ((binding._APPEND_PACK, AppendArgsC), (binding._ATTEND_PACK, AttendArgsC), (binding._ACCEPT_PACK, AcceptArgsC)):
+        kinds = [f[1] for f in c._fields_]
+        values = [0.5 + i if k is ctypes.c_float else i + 1 for i, k in enumerate(kinds)]
+        got = c.from_buffer_copy(fmt(*values))
+        assert [getattr(got, f[0]) for f in c._fields_] == values
 
 
 def test_reference_forms_agree_with_themselves():
