@@ -2,273 +2,80 @@
 
 namespace ee {
 
-// Pages that the members [s0, s1) of a group read together: the entries they have in common, as far as every new row of every
-// member sees all of their positions.
-__device__ __forceinline__ int common_pages(const AttendDev &a, int group, int s0, int s1, int lane, int &first_member)
-{
-    int pages = min(max(as_global(a.group_pages)[group], 0), a.b.table_stride);
-    first_member = s1;
-    for (int base = s0; base < s1; base += 64) {
-        const int s = base + lane;
-        int mine = 0x7FFFFFFF, has = 0;
-        if (s < s1) {
-            const int n = a.b.start(s + 1) - a.b.start(s);
-            has = n > 0;
-            if (has) mine = max(a.b.length(s) - n + 1, 0) >> 4;
-        }
-        if (const unsigned long long who = __ballot(has); who && first_member == s1) first_member = base + __builtin_ctzll(who);
-#pragma unroll
-        for (int d = 1; d < 64; d <<= 1) mine = min(mine, __shfl_xor(mine, d, 64));
-        pages = min(pages, mine);
-    }
-    pages = __builtin_amdgcn_readfirstlane(pages);
-    return pages;
-}
-
-__device__ __forceinline__ int group_bound(const AttendDev &a, int g) { return min(max(as_global(a.group_start)[g], 0), a.b.n_seqs); }
-
-// Group of sequence `seq`, or -1.
-__device__ __forceinline__ int group_of(const AttendDev &a, int seq, int lane)
-{
-    for (int base = 0; base < a.n_groups; base += 64) {
-        const int g = base + lane;
-        const bool in = g < a.n_groups && group_bound(a, g) <= seq && seq < group_bound(a, g + 1);
-        if (const unsigned long long who = __ballot(in)) return base + __builtin_ctzll(who);
-    }
-    return -1;
-}
-
-template <int HD, int TERMS, int QT, int RT>
-__global__ void __launch_bounds__(ATT_W * 64) ee_attend_kernel(AttendDev a)
-{
-    extern __shared__ __align__(16) char lds_raw[];
-    constexpr int KT = HD / 32, NT = HD / 16, LINES = RT * 16;
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int lm = lane & 15, quad = lane >> 4;
-    const int G = a.per_key, kvh = blockIdx.y;
-    const int shared_items = a.chunks_shared * a.parts_shared;
-    int item = blockIdx.x;
-    const bool shared = item < shared_items;
-    const int parts = shared ? a.parts_shared : a.parts_own;
-    if (!shared) item -= shared_items;
-    const int chunk = item / parts, part = item - chunk * parts;
-
-    AttendItem it;
-    int row0, n_rows, seq, group = -1, place, slot, first_pos = 0;
-    bool clear_shared = false;
-    if (shared) {
-        if (!find_item(a.n_groups, chunk, lane, [&](int g) {
-                const int s0 = group_bound(a, g), s1 = max(group_bound(a, g + 1), s0);
-                return (max(a.b.start(s1) - a.b.start(s0), 0) * G + LINES - 1) / LINES;
-            }, group, place))
-            return;
-        const int s0 = group_bound(a, group), s1 = max(group_bound(a, group + 1), s0);
-        row0 = a.b.start(s0);
-        n_rows = a.b.start(s1) - row0;
-        const int pages = common_pages(a, group, s0, s1, lane, seq);
-        if (seq >= s1) return;                                              // (row_start decreases somewhere)
-        it.pg_lo = (int)((long long)pages * part / parts);
-        it.pg_hi = (int)((long long)pages * (part + 1) / parts);
-        slot = part;
-    } else {
-        if (!find_item(a.b.n_seqs, chunk, lane, [&](int s) { return (max(a.b.start(s + 1) - a.b.start(s), 0) * G + LINES - 1) / LINES; }, seq, place)) return;
-        row0 = a.b.start(seq);
-        n_rows = a.b.start(seq + 1) - row0;
-        first_pos = a.b.length(seq) - n_rows;                               // position of the first row
-        int from = 0;
-        if (a.n_groups) {
-            group = group_of(a, seq, lane);
-            int member;
-            if (group >= 0)
-                from = common_pages(a, group, group_bound(a, group), group_bound(a, group + 1), lane, member);
-            else
-                clear_shared = part == 0;
-        }
-        const int last_line = min(place * LINES + LINES, n_rows * G) - 1;
-        const int visible = min(first_pos + last_line / G + 1, a.b.capacity());
-        const int pages = max(((max(visible, 0) + KV_PAGE - 1) >> 4) - from, 0);
-        it.pg_lo = from + (int)((long long)pages * part / parts);
-        it.pg_hi = from + (int)((long long)pages * (part + 1) / parts);
-        slot = a.parts_shared + part;
-    }
-    it.line0 = place * LINES;
-    it.lines = min(LINES, n_rows * G - it.line0);
-    it.n_pages = a.b.n_pages;
-    it.table = a.b.table + (size_t)seq * a.b.table_stride;
-    it.page_step = (size_t)a.b.n_kv_heads * KV_PAGE * TERMS * HD;
-    it.k = a.b.kpool + (size_t)kvh * KV_PAGE * TERMS * HD;
-    it.v = a.b.vpool + (size_t)kvh * KV_PAGE * TERMS * HD;
-
-    // this lane's lines: row, head, last position seen
-    int row[RT], head[RT], last[RT], max_last = 0x7FFFFFF0;
-    bf16x8_t q[RT][KT][QT];
-    const bool any = it.pg_hi > it.pg_lo;
-#pragma unroll
-    for (int t = 0; t < RT; ++t) {
-        const int line = it.line0 + min(t * 16 + lm, it.lines - 1), i = line / G;
-        row[t] = row0 + i;
-        head[t] = kvh * G + line - i * G;
-        last[t] = shared ? 0x7FFFFFF0 : first_pos + i;
-    }
-    it.first_last = shared ? 0x7FFFFFF0 : first_pos + it.line0 / G;
-    if (!shared) max_last = min(first_pos + (it.line0 + it.lines - 1) / G, a.b.capacity() - 1);
-    AttendState<RT, NT> st;
-#pragma unroll
-    for (int t = 0; t < RT; ++t) {
-        st.mx[t] = -INFINITY;
-        st.sum[t] = 0.f;
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt) st.o[t][nt] = (f32x4_t){0.f, 0.f, 0.f, 0.f};
-    }
-    if (any) {
-#pragma unroll
-        for (int t = 0; t < RT; ++t) {
-            if (t * 16 >= it.lines) continue;
-#pragma unroll
-            for (int kt = 0; kt < KT; ++kt) {
-                const size_t at = (size_t)row[t] * a.q_stride + (size_t)head[t] * a.q_head + kt * 32 + quad * 8;
-                if constexpr (QT == 1) {
-                    q[t][kt][0] = __builtin_bit_cast(bf16x8_t, load_global16(static_cast<const uint16_t *>(a.q) + at));
-                } else {
-                    float x[8];
-                    if (a.q_type == EE_FP32)
-                        load8<EE_FP32>(a.q, at, x);
-                    else if (a.q_type == EE_FP16)
-                        load8<EE_FP16>(a.q, at, x);
-                    else
-                        load8<EE_BF16>(a.q, at, x);
-                    split_bf16x8((f32x4_t){x[0], x[1], x[2], x[3]}, (f32x4_t){x[4], x[5], x[6], x[7]}, q[t][kt][0], q[t][kt][1]);
-                }
-            }
-        }
-        attend_pages<HD, TERMS, QT, RT>(it, q, last, max_last, a.scale2, lane, wave, st);
-        attend_join_waves<HD, RT>(st, reinterpret_cast<float *>(lds_raw), min(ATT_W, (it.pg_hi - it.pg_lo + 1) >> 1), a.scale2, lane, wave);
-    }
-    if (wave != 0) return;
-    const int total = a.parts_shared + a.parts_own;
-#pragma unroll
-    for (int t = 0; t < RT; ++t) {
-        if (t * 16 + lm >= it.lines) continue;
-        if (total == 1) {
-            const float inv = st.sum[t] == 0.f ? 0.f : 1.0f / st.sum[t];    // (0: the line saw no position)
-            const size_t to = (size_t)row[t] * a.o_stride + (size_t)head[t] * a.o_head + quad * 4;
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt) store4(a.out_type, a.out, to + nt * 16, st.o[t][nt][0] * inv, st.o[t][nt][1] * inv, st.o[t][nt][2] * inv, st.o[t][nt][3] * inv);
-        } else {
-            const size_t line = (size_t)row[t] * a.n_heads + head[t];
-            if (st.mx[t] != -INFINITY) {                                    // (nothing is read of an empty part)
-                float *o = a.part + (line * total + slot) * HD + quad * 4;
-#pragma unroll
-                for (int nt = 0; nt < NT; ++nt) *as_global_mut(reinterpret_cast<f32x4_t *>(o + nt * 16)) = st.o[t][nt];
-            }
-            if (quad == 0) {
-                float *ml = a.part_ml + (line * total) * 2;
-                as_global_mut(ml)[slot * 2] = st.mx[t];
-                as_global_mut(ml)[slot * 2 + 1] = st.sum[t];
-                if (clear_shared)
-                    for (int s = 0; s < a.parts_shared; ++s) {
-                        as_global_mut(ml)[s * 2] = -INFINITY;
-                        as_global_mut(ml)[s * 2 + 1] = 0.f;
-                    }
-            }
-        }
-    }
-}
-
-// Joins the parts of every line, in order: thread = four dims of a line.
-template <int HD>
-__global__ void __launch_bounds__(256) ee_attend_join_kernel(AttendDev a)
-{
-    constexpr int TPL = HD / 4;                                             // threads of a line
-    const long long line = (long long)blockIdx.x * (256 / TPL) + threadIdx.x / TPL;
-    const int e = (threadIdx.x % TPL) * 4;
-    const long long rows = a.b.start(a.b.n_seqs);
-    if (line >= rows * a.n_heads) return;
-    const int row = (int)(line / a.n_heads), head = (int)(line - (long long)row * a.n_heads);
-    const int total = a.parts_shared + a.parts_own;
-    const float *ml = a.part_ml + line * total * 2;
-    const float *o = a.part + line * total * HD + e;
-    float m = -INFINITY;
-    bool bad = false;
-    for (int p = 0; p < total; ++p) {
-        const float mp = as_global(ml)[2 * p], lp = as_global(ml)[2 * p + 1];
-        m = fmaxf(m, mp);
-        bad |= mp == -INFINITY && lp != 0.f;                                // positions without a softmax
-    }
-    f32x4_t num = {0.f, 0.f, 0.f, 0.f};
-    float den = 0.f;
-    if (m != -INFINITY)
-        for (int p = 0; p < total; ++p) {
-            const float mp = as_global(ml)[2 * p];
-            if (mp == -INFINITY) continue;
-            const float f = __builtin_amdgcn_exp2f((mp - m) * a.scale2);
-            const f32x4_t v = *as_global(reinterpret_cast<const f32x4_t *>(o + (size_t)p * HD));
-#pragma unroll
-            for (int r = 0; r < 4; ++r) num[r] += v[r] * f;
-            den += as_global(ml)[2 * p + 1] * f;
-        }
-    const float inv = m != -INFINITY ? 1.0f / den : bad ? __builtin_nanf("") : 0.f;
-    store4(a.out_type, a.out, (size_t)row * a.o_stride + (size_t)head * a.o_head + e, num[0] * inv, num[1] * inv, num[2] * inv, num[3] * inv);
-}
-
 typedef void (*attend_kernel_t)(AttendDev);
 struct AttendKernel {
     attend_kernel_t f;
     size_t lds;
 };
-template <int HD, int TERMS, int QT>
-static AttendKernel attend_of_tiles(int rt)
+template <int HD, int TERMS, int QT, int PT>
+static AttendKernel attend_of_tiles(int tiles)
 {
-    if (rt == 1) return {ee_attend_kernel<HD, TERMS, QT, 1>, attend_lds<HD, 1>()};
-    if constexpr (HD == 64)
-        if (rt == 4) return {ee_attend_kernel<HD, TERMS, QT, 4>, attend_lds<HD, 4>()};
-    return {ee_attend_kernel<HD, TERMS, QT, 2>, attend_lds<HD, 2>()};
+    if (tiles == 1) return {ee_attend_kernel<HD, TERMS, QT, PT, 1>, attend_lds<HD, 1>()};
+    if constexpr (TERMS == 1 || HD == 64)
+        if (tiles == 2) return {ee_attend_kernel<HD, TERMS, QT, PT, 2>, attend_lds<HD, 2>()};
+    return {ee_attend_wide_kernel<HD, TERMS, QT, PT == 2 && QT == 1 ? 1 : PT>, (size_t)2 * attend_wide_stage<HD, TERMS>()};
 }
-static AttendKernel attend_kernel(int hd, int terms, int q_type, int rt)
+template <int HD>
+static AttendKernel attend_kernel(int terms, int q_type, int out_type, int tiles)
 {
-    if (hd == 64) return terms == 2 ? attend_of_tiles<64, 2, 2>(rt) : q_type == EE_BF16 ? attend_of_tiles<64, 1, 1>(rt) : attend_of_tiles<64, 1, 2>(rt);
-    return terms == 2 ? attend_of_tiles<128, 2, 2>(rt) : q_type == EE_BF16 ? attend_of_tiles<128, 1, 1>(rt) : attend_of_tiles<128, 1, 2>(rt);
+    if (terms == 2) return attend_of_tiles<HD, 2, 3, 3>(tiles);
+    if (out_type == EE_FP32) return q_type == EE_BF16 ? attend_of_tiles<HD, 1, 1, 3>(tiles) : attend_of_tiles<HD, 1, 3, 3>(tiles);
+    if (q_type == EE_FP32) return attend_of_tiles<HD, 1, 3, 3>(tiles);
+    return q_type == EE_BF16 ? attend_of_tiles<HD, 1, 1, 2>(tiles) : attend_of_tiles<HD, 1, 2, 2>(tiles);
 }
 
 // How a call is split; a function of what the host knows (sizes and the caller's bounds).
 struct AttendPlan {
-    int tiles;                        // tiles of 16 lines of an item
-    int chunks_own, parts_own, chunks_shared, parts_shared;
-    size_t part_floats, ml_floats;
+    int tiles;                        // tiles of 16 lines of an item; 8: the kernel for many lines
+    int groups;                       // groups whose common pages are read once
+    int quota, most_own, most_shared;
+    long long items;
+    size_t part_bytes, ml_bytes, lane_bytes;
+    size_t bytes() const { return part_bytes + ml_bytes + lane_bytes; }
 };
 
 // Chunks of `lines` lines that n things with T rows among them can have, each row `per_key` lines: one each, and one more for every `lines` lines behind
 // its first row's (behind its first line, where rows do not fill chunks evenly).
-static int most_chunks(int n, int T, int per_key, int lines)
+static long long most_chunks(int n, int T, int per_key, int lines)
 {
     const long long things = std::min(n, T), all = (long long)T * per_key;
     const int first = lines % per_key == 0 ? per_key : per_key % lines == 0 ? lines : 1;
-    return (int)(things + (all - things * first) / lines);
+    return things + (all - things * first) / lines;
 }
+
+static size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
 
 static AttendPlan plan_attend(const ee_paged_cache &c, const ee_attend_args &p)
 {
-    AttendPlan pl;
+    AttendPlan pl = {};
     const int T = p.n_rows, per_key = p.n_heads / c.n_kv_heads;
     const long long cap = std::min<long long>(c.table_stride, 0x7FFFFFF0 / KV_PAGE);
     const int pages = (int)std::min<long long>(cap, p.max_kv > 0 ? ((long long)p.max_kv + KV_PAGE - 1) / KV_PAGE : cap);
-    const int shared_pages = p.n_groups == 0 ? 0 : (int)std::min<long long>(pages, p.max_shared > 0 ? p.max_shared / KV_PAGE : pages);
-    const int seqs = std::min(c.n_seqs, T), groups = std::min(p.n_groups, seqs);
-    const long long own_lines = (long long)T * per_key / seqs, shared_lines = groups ? (long long)T * per_key / groups : 0;
-    const long long lines = std::max(own_lines, shared_lines);
-    pl.tiles = lines <= 16 ? 1 : lines <= 32 || c.head_dim == 128 ? 2 : 4;
-    pl.chunks_own = most_chunks(seqs, T, per_key, pl.tiles * 16);
-    pl.chunks_shared = groups && shared_pages ? most_chunks(groups, T, per_key, pl.tiles * 16) : 0;
+    int shared_pages = p.n_groups == 0 ? 0 : (int)std::min<long long>(pages, p.max_shared > 0 ? p.max_shared / KV_PAGE : pages);
+    const int seqs = std::min(c.n_seqs, T);
+    const long long own_lines = (long long)T * per_key / seqs;
+    // From 64 lines a sequence on the matrix cores bound the call, and reading common pages once gains nothing.
+    const bool wide = own_lines >= 64;
+    pl.groups = wide || shared_pages == 0 ? 0 : std::min(p.n_groups, seqs);
+    if (pl.groups == 0) shared_pages = 0;
+    const long long lines = pl.groups ? std::max(own_lines, (long long)T * per_key / pl.groups) : own_lines;
+    pl.tiles = wide ? 8 : lines <= 16 || (c.terms == 2 && c.head_dim == 128) ? 1 : 2;
+    const long long chunks_own = most_chunks(seqs, T, per_key, pl.tiles * 16);
+    const long long chunks_shared = pl.groups ? most_chunks(pl.groups, T, per_key, pl.tiles * 16) : 0;
     const int own_pages = std::max(pages - shared_pages, 1);
-    // Parts: enough for two workgroups a compute unit, as long as a part has 8 pages (a pair for each wave).
-    const long long work = (long long)pl.chunks_own * own_pages + (long long)pl.chunks_shared * shared_pages;
-    const long long per_part = std::max<long long>(8, work * c.n_kv_heads / 512);
-    pl.parts_own = (int)std::min<long long>(std::max<long long>(own_pages / per_part, 1), 64);
-    pl.parts_shared = pl.chunks_shared ? (int)std::min<long long>(std::max<long long>(shared_pages / per_part, 1), 64) : 0;
-    const size_t total = (size_t)pl.parts_own + pl.parts_shared;
-    const size_t all = (size_t)T * p.n_heads * total;
-    pl.part_floats = total > 1 ? all * c.head_dim : 0;
-    pl.ml_floats = total > 1 ? all * 2 : 0;
+    // Parts: as many pages each as make about 512 items (two for a compute unit) if sequences are two thirds of the longest on average, in
+    // rounds of 8 (a pair for each wave).
+    const long long work = chunks_own * (seqs > 1 ? (2 * own_pages + 2) / 3 : own_pages) + chunks_shared * shared_pages;
+    pl.quota = (int)(std::max<long long>(8, (work * c.n_kv_heads + 511) / 512) + 7) / 8 * 8;
+    pl.most_own = std::min((own_pages + pl.quota - 1) / pl.quota, 64);
+    pl.most_shared = std::min((shared_pages + pl.quota - 1) / pl.quota, 64);
+    pl.items = chunks_own * pl.most_own + chunks_shared * pl.most_shared;
+    const size_t most = (size_t)pl.most_own + pl.most_shared, all = (size_t)T * p.n_heads;
+    if (most > 1) {
+        pl.part_bytes = align256(all * most * c.head_dim * sizeof(float));
+        pl.ml_bytes = align256(all * (most + 1) * sizeof(float2));
+    }
+    if (pl.groups && (c.n_seqs > 64 || p.n_groups > 64)) pl.lane_bytes = align256(((size_t)c.n_seqs + 2 * (size_t)p.n_groups) * sizeof(int));
     return pl;
 }
 
@@ -305,8 +112,7 @@ extern "C" int ee_attend_workspace(const ee_paged_cache *c, const ee_attend_args
     int rc = check_attend(call, &cs, &ps);
     if (rc != EE_OK) return rc;
     if (c->n_seqs == 0 || p->n_rows == 0) return EE_OK;
-    const AttendPlan pl = plan_attend(*c, *p);
-    *bytes = (pl.part_floats + pl.ml_floats) * sizeof(float);
+    *bytes = plan_attend(*c, *p).bytes();
     return EE_OK;
 }
 
@@ -323,10 +129,10 @@ extern "C" int ee_attend(const ee_paged_cache *c, const ee_attend_args *p, void 
     if (!aligned(p->q, 16) || !aligned(p->out, 16)) return fail(EE_EINVAL, "%s: q and out must be 16-byte aligned", call);
     if (!aligned(p->group_start, 4) || !aligned(p->group_pages, 4)) return fail(EE_EINVAL, "%s: int32 arrays must be 4-byte aligned", call);
     const AttendPlan pl = plan_attend(*c, *p);
-    const size_t need = (pl.part_floats + pl.ml_floats) * sizeof(float);
+    const size_t need = pl.bytes();
     if (need > workspace_bytes || (need && (!workspace || !aligned(workspace, 256))))
         return fail(EE_EINVAL, "%s: the workspace has %zu bytes of %zu, or is not 256-byte aligned", call, workspace_bytes, need);
-    if ((long long)pl.chunks_own * pl.parts_own + (long long)pl.chunks_shared * pl.parts_shared > 0x7FFFFFFF) return fail(EE_EINVAL, "%s: too many rows", call);
+    if (pl.items > 65535) return fail(EE_EINVAL, "%s: %lld chunks of rows and pages are too many for a call", call, pl.items);
 
     AttendDev a;
     a.b = batch_of(*c, p->n_rows, p->row_start, p->kv_len);
@@ -338,27 +144,35 @@ extern "C" int ee_attend(const ee_paged_cache *c, const ee_attend_args *p, void 
     a.o_head = p->out_head_stride;
     a.q_type = p->dtype;
     a.out_type = p->out_dtype;
-    a.n_groups = pl.chunks_shared ? p->n_groups : 0;
+    a.n_groups = pl.groups ? p->n_groups : 0;
     a.group_start = p->group_start;
     a.group_pages = p->group_pages;
-    a.part = static_cast<float *>(workspace);
-    a.part_ml = a.part + pl.part_floats;
+    unsigned char *ws = static_cast<unsigned char *>(workspace);
+    a.part = reinterpret_cast<float *>(ws);
+    a.part_ml = reinterpret_cast<float2 *>(ws + pl.part_bytes);
+    a.from = reinterpret_cast<int *>(ws + pl.part_bytes + pl.ml_bytes);
+    a.common = a.from + c->n_seqs;
+    a.member = a.common + p->n_groups;
     a.n_heads = p->n_heads;
     a.per_key = p->n_heads / c->n_kv_heads;
-    a.parts_own = pl.parts_own;
-    a.parts_shared = pl.parts_shared;
-    a.chunks_shared = pl.chunks_shared;
+    a.quota = pl.quota;
+    a.most_own = pl.most_own;
+    a.most_shared = pl.most_shared;
     a.scale2 = p->scale * 1.44269504f;
     DeviceScope scope(c->device);
     HIP_TRY(scope.status);
-    const AttendKernel k = attend_kernel(c->head_dim, c->terms, p->dtype, pl.tiles);
+    const AttendKernel k = c->head_dim == 64 ? attend_kernel<64>(c->terms, p->dtype, p->out_dtype, pl.tiles) : attend_kernel<128>(c->terms, p->dtype, p->out_dtype, pl.tiles);
     const hipStream_t s = static_cast<hipStream_t>(stream);
-    hipLaunchKernelGGL(k.f, dim3(pl.chunks_own * pl.parts_own + pl.chunks_shared * pl.parts_shared, c->n_kv_heads), dim3(ATT_W * 64), k.lds, s, a);
+    if (pl.lane_bytes) {
+        hipLaunchKernelGGL(ee_attend_plan_kernel, dim3(c->n_seqs + p->n_groups), dim3(64), 0, s, a);
+        HIP_TRY(hipGetLastError());
+    }
+    hipLaunchKernelGGL(k.f, dim3(c->n_kv_heads, (unsigned)pl.items), dim3(ATT_W * 64), k.lds, s, a);
     HIP_TRY(hipGetLastError());
-    if (pl.part_floats) {
-        const int per = 256 / (c->head_dim / 4);
-        const unsigned blocks = (unsigned)(((size_t)p->n_rows * p->n_heads + per - 1) / per);
-        hipLaunchKernelGGL(c->head_dim == 64 ? ee_attend_join_kernel<64> : ee_attend_join_kernel<128>, dim3(blocks), dim3(256), 0, s, a);
+    if (pl.part_bytes) {
+        const int rows = 256 / (c->head_dim / 4), most = pl.most_own + pl.most_shared, spread = most <= 4 ? 1 : most <= 8 ? 4 : rows;
+        const size_t lines = (size_t)p->n_rows * p->n_heads, per = (size_t)(rows / spread);
+        hipLaunchKernelGGL(c->head_dim == 64 ? ee_attend_join_kernel<64> : ee_attend_join_kernel<128>, dim3((unsigned)((lines + per - 1) / per)), dim3(256), 0, s, a, spread);
         HIP_TRY(hipGetLastError());
     }
     return EE_OK;

@@ -4,17 +4,18 @@
 //   maximum m and sum l:  m' = max(m, s_j),  l' = l e^(m - m') + e^(s_j - m'),  o' = o e^(m - m') + e^(s_j - m') v_j;
 //   parts of the positions join by the same rule.
 //
-// Bound by the cache's bytes with few rows (64 flops a byte of a one-term cache with 16 lines), by the matrix cores with
-// many.  A line is a row's query head; the lines that read one key head are taken RT tiles of 16 at a time.  An item is (key head, up to 16 RT
-// lines of one sequence, or of one group over its common pages, a part of their pages) and goes to a workgroup of ATT_W waves,
-// which take pairs of pages in turn; every wave keeps q, the running maximum and sum, and the output in registers:
-//   scores   S[position][line] = K . q^T    v_mfma_f32_16x16x32_bf16, A = 16 positions x 32 values straight from a page's record, B = q
-//   output   O[dim][line] = V^T . P         the same instruction over the pair's 32 positions: its k index may run over them in any order
-//            that both operands share, so P stays in the registers that the scores came in (lane: line l & 15, positions (l >> 4) 4 .. + 3 of
-//            either page), and V, which a record holds transposed, comes as a lane's 4 positions of either page.
-// q of 16 bits beyond bf16 and P are two bf16 terms each (x = hi + lo to 2^-17), products of two lo terms are left out (2^-18); sums are fp32.
-// The waves' results are joined through LDS; where a line has several parts, they go to memory and ee_attend_join_kernel
-// joins them in order, so that results do not depend on who is first.
+// A line is a row's query head.  The lines that read one key head are taken in tiles of 16, an item is (key head, a chunk of lines of one sequence, or of
+// one group over its common pages, a part of their pages) and goes to a workgroup.  Both products are v_mfma_f32_16x16x32_bf16, 32 positions (a
+// pair of pages) at a time:
+//   scores   S[position][line] = K . q^T    A = 16 positions x 32 values, B = q.  Row r of product p is position 8 (r >> 2) + 4 p + (r & 3) of the pair, so that
+//            a lane's scores of both products are the eight positions 8 quad .. 8 quad + 7 (quad = lane >> 4, line = lane & 15) ...
+//   output   O[dim][line] = V^T . P         ... which is the layout of the second product's B: P stays in its registers, and V, which a record holds
+//            transposed, comes as one 16-byte access of eight positions.
+// The output is kept transposed: a line's maximum, sum and output are in the lanes of its column, and rescaling needs no exchange.
+//
+// Precision: sums, maxima and outputs are fp32.  The products' operands are bf16 terms: K and V as the cache has them (TERMS), q in QT terms, exactly for bf16 (1) and
+// fp16 (2) and to 2^-25 for fp32 (3); P in PT: 3 where the results are fp32, 2 (2^-17) for results of 16 bits, 1 (2^-9, as much as the result's
+// own rounding) where the matrix cores bound the call.  Products of the smallest terms are left out (2^-26, or 2^-17 with 2 terms).
 #pragma once
 
 #include "ee_ops.hpp"
@@ -22,7 +23,6 @@
 namespace ee {
 
 constexpr int ATT_W = 4;                       // waves of an item
-constexpr int ATT_ID_PAIRS = 32;               // pairs of pages whose ids a wave holds in its lanes
 
 struct AttendDev {
     BatchDev b;
@@ -30,236 +30,402 @@ struct AttendDev {
     void *out;
     long long q_stride, q_head, o_stride, o_head;
     const int *group_start, *group_pages;
-    float *part;                               // [line of the batch][parts][HD], then [line][parts][2] maxima and sums
-    float *part_ml;
+    float *part;                               // [line of the batch][most_own + most_shared][HD]
+    float2 *part_ml;                           // [line][1 + most_own + most_shared]: first (own parts, common parts) as integers, then maxima and sums
+    int *from, *common, *member;               // per sequence / group, where ee_attend_plan_kernel works them out
     int q_type, out_type;
     int n_groups, n_heads, per_key;            // per_key: query heads of a key head
-    int parts_own, parts_shared, chunks_shared;
+    int quota;                                 // pages of a part
+    int most_own, most_shared;                 // parts at most
     float scale2;                              // scale * log2(e)
 };
 
 // What one item works on.
 struct AttendItem {
-    const uint16_t *k, *v;                     // record of page 0 for the key head
-    size_t page_step;                          // elements from a page's record to the next page's
-    const int *table;
-    int n_pages;
+    int seq;                                   // whose table is read
+    int row0, rows;                            // rows the chunk's lines belong to: of the sequence, or of the group
+    int line0, lines;                          // its lines among them
     int pg_lo, pg_hi;                          // its pages
-    int lines, line0;                          // its lines: line0 .. line0 + lines - 1 of the chunk's rows x heads
-    int first_last;                            // last position that its first line sees (the others see as many or more)
+    int first_pos;                             // position of row0; rows of a group: they see all pages of the item
+    bool shared;
+    int own_parts, common_parts, slot;         // parts of its lines, and which of them this is
 };
+
+constexpr int ALL_SEEN = 0x7FFFFFF0;
+
+__device__ __forceinline__ int group_bound(const AttendDev &a, int g) { return min(max(as_global(a.group_start)[g], 0), a.b.n_seqs); }
+
+// A sequence as its lane holds it.
+struct SeqLane {
+    int r0, n, len, from;                      // first row, rows, positions, pages that its group reads for it
+};
+__device__ __forceinline__ SeqLane seq_lane(const AttendDev &a, int s)
+{
+    SeqLane l = {0, 0, 0, 0};
+    if (s < a.b.n_seqs) {
+        l.r0 = a.b.start(s);
+        l.n = max(a.b.start(s + 1) - l.r0, 0);
+        l.len = a.b.length(s);
+    }
+    return l;
+}
+// pages of which every new row sees all positions
+__device__ __forceinline__ int pages_seen(const SeqLane &l) { return l.n > 0 ? max(l.len - l.n + 1, 0) >> 4 : 0x7FFFFFFF; }
+
+__device__ __forceinline__ int wave_min(int x)
+{
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) x = min(x, __shfl_xor(x, d, 64));
+    return x;
+}
+
+// Pages that a group reads together: the entries its members have in common, as far as every new row of every member sees all of
+// their positions.  `member`: the first one with rows, whose table is read; s1 if there is none.
+__device__ __forceinline__ int common_pages(const AttendDev &a, int group, int lane, int &member)
+{
+    const int s0 = group_bound(a, group), s1 = max(group_bound(a, group + 1), s0);
+    int pages = min(max(as_global(a.group_pages)[group], 0), a.b.table_stride);
+    member = s1;
+    for (int base = s0; base < s1; base += 64) {
+        SeqLane l = seq_lane(a, base + lane);
+        if (base + lane >= s1) l.n = 0;
+        if (const unsigned long long who = __ballot(l.n > 0); who && member == s1) member = base + __builtin_ctzll(who);
+        pages = min(pages, wave_min(pages_seen(l)));
+    }
+    return member < s1 ? __builtin_amdgcn_readfirstlane(pages) : 0;
+}
+
+// Batches of more than 64 sequences: `from`, `common` and `member`, one wave each.
+__global__ void __launch_bounds__(64) ee_attend_plan_kernel(AttendDev a)
+{
+    const int lane = threadIdx.x, i = blockIdx.x;
+    int member;
+    if (i < a.n_groups) {
+        const int pages = common_pages(a, i, lane, member);
+        if (lane == 0) {
+            as_global_mut(a.common)[i] = pages;
+            as_global_mut(a.member)[i] = member;
+        }
+        return;
+    }
+    const int s = i - a.n_groups;
+    int pages = 0;
+    for (int base = 0; base < a.n_groups; base += 64) {
+        const int g = base + lane;
+        const bool in = g < a.n_groups && group_bound(a, g) <= s && s < group_bound(a, g + 1);
+        if (const unsigned long long who = __ballot(in)) {
+            pages = common_pages(a, base + __builtin_ctzll(who), lane, member);
+            break;
+        }
+    }
+    if (lane == 0) as_global_mut(a.from)[s] = pages;
+}
+
+__device__ __forceinline__ int own_parts(const AttendDev &a, int pages) { return min(max((pages + a.quota - 1) / a.quota, 1), a.most_own); }
+__device__ __forceinline__ int common_parts(const AttendDev &a, int pages) { return min((pages + a.quota - 1) / a.quota, a.most_shared); }
+__device__ __forceinline__ int table_pages(const AttendDev &a, int len) { return (min(max(len, 0), a.b.capacity()) + KV_PAGE - 1) >> 4; }
+
+// Item `item` of the launch: the groups' chunks and parts first, then the sequences'.  All lanes get the same; false past the last.
+template <int LINES>
+__device__ __forceinline__ bool attend_item(const AttendDev &a, int item, int lane, AttendItem &it)
+{
+    const int G = a.per_key;
+    const bool small = a.b.n_seqs <= 64 && a.n_groups <= 64;
+    SeqLane mine = seq_lane(a, lane);
+    int g_pages = 0, g_member = 0, g_r0 = 0, g_rows = 0;                    // of group `lane`
+    auto group_rows = [&](int g, int &r0, int &rows) {
+        const int s0 = group_bound(a, g), s1 = max(group_bound(a, g + 1), s0);
+        r0 = a.b.start(s0);
+        rows = max(a.b.start(s1) - r0, 0);
+    };
+    auto shared_count = [&](int pages, int rows) { return pages > 0 ? (rows * G + LINES - 1) / LINES * common_parts(a, pages) : 0; };
+    if (a.n_groups > 0) {
+        int g, place;
+        if (small) {
+            int s0 = 0, declared = 0;
+            if (lane <= a.n_groups) s0 = group_bound(a, lane);
+            if (lane < a.n_groups) {
+                declared = min(max(as_global(a.group_pages)[lane], 0), a.b.table_stride);
+                group_rows(lane, g_r0, g_rows);
+            }
+            const int seen = pages_seen(mine);
+            for (int i = 0; i < a.n_groups; ++i) {
+                const int lo = __builtin_amdgcn_readlane(s0, i), hi = i == 63 ? group_bound(a, 64) : __builtin_amdgcn_readlane(s0, i + 1);
+                const bool in = lane >= lo && lane < hi;
+                const unsigned long long who = __ballot(in && mine.n > 0);
+                const int pages = who ? min(__builtin_amdgcn_readlane(declared, i), wave_min(in ? seen : 0x7FFFFFFF)) : 0;
+                if (in) mine.from = pages;
+                if (lane == i) {
+                    g_pages = pages;
+                    g_member = who ? __builtin_ctzll(who) : 0;
+                }
+            }
+            const int c = shared_count(g_pages, g_rows), incl = wave_scan(c, lane), total = __builtin_amdgcn_readlane(incl, 63);
+            if (item < total) {
+                g = __builtin_ctzll(__ballot(incl > item));
+                place = item - __builtin_amdgcn_readlane(incl - c, g);
+                it.seq = __builtin_amdgcn_readlane(g_member, g);
+                it.row0 = __builtin_amdgcn_readlane(g_r0, g);
+                it.rows = __builtin_amdgcn_readlane(g_rows, g);
+                g_pages = __builtin_amdgcn_readlane(g_pages, g);
+                it.shared = true;
+            } else {
+                item -= total;
+                it.shared = false;
+            }
+        } else {
+            int total = 0;
+            it.shared = find_item(a.n_groups, item, lane, [&](int i) {
+                int r0, rows;
+                group_rows(i, r0, rows);
+                return shared_count(as_global(a.common)[i], rows);
+            }, g, place, &total);
+            if (it.shared) {
+                group_rows(g, it.row0, it.rows);
+                g_pages = as_global(a.common)[g];
+                it.seq = as_global(a.member)[g];
+            } else {
+                item -= total;
+            }
+        }
+        if (it.shared) {
+            const int parts = common_parts(a, g_pages), chunk = place / parts, part = place - chunk * parts;
+            it.line0 = chunk * LINES;
+            it.lines = min(LINES, it.rows * G - it.line0);
+            it.pg_lo = (int)((long long)g_pages * part / parts);
+            it.pg_hi = (int)((long long)g_pages * (part + 1) / parts);
+            it.first_pos = ALL_SEEN;
+            it.own_parts = it.common_parts = 2;                             // (never the only part)
+            it.slot = a.most_own + part;
+            return true;
+        }
+    }
+    it.shared = false;
+    auto own_count = [&](const SeqLane &l) { return l.n > 0 ? (l.n * G + LINES - 1) / LINES * own_parts(a, table_pages(a, l.len) - l.from) : 0; };
+    for (int base = 0;; base += 64) {
+        if (base > 0) mine = seq_lane(a, base + lane);
+        if (!small && a.n_groups > 0 && base + lane < a.b.n_seqs) mine.from = as_global(a.from)[base + lane];
+        const int c = own_count(mine), incl = wave_scan(c, lane), total = __builtin_amdgcn_readlane(incl, 63);
+        if (item < total) {
+            const int l = __builtin_ctzll(__ballot(incl > item)), place = item - __builtin_amdgcn_readlane(incl - c, l);
+            it.seq = base + l;
+            it.row0 = __builtin_amdgcn_readlane(mine.r0, l);
+            it.rows = __builtin_amdgcn_readlane(mine.n, l);
+            const int len = __builtin_amdgcn_readlane(mine.len, l), from = __builtin_amdgcn_readlane(mine.from, l);
+            const int parts = own_parts(a, table_pages(a, len) - from);
+            // the last lines first: they see the most positions
+            const int chunks = (it.rows * G + LINES - 1) / LINES, c_up = place / parts, part = place - c_up * parts;
+            it.line0 = (chunks - 1 - c_up) * LINES;
+            it.lines = min(LINES, it.rows * G - it.line0);
+            it.first_pos = len - it.rows;
+            const int pages = max(table_pages(a, it.first_pos + (it.line0 + it.lines - 1) / G + 1) - from, 0);
+            it.pg_lo = from + (int)((long long)pages * part / parts);
+            it.pg_hi = from + (int)((long long)pages * (part + 1) / parts);
+            it.own_parts = parts;
+            it.common_parts = from > 0 ? common_parts(a, from) : 0;
+            it.slot = part;
+            return true;
+        }
+        item -= total;
+        if (base + 64 >= a.b.n_seqs) return false;
+    }
+}
 
 template <int RT, int NT>
 struct AttendState {
     f32x4_t o[RT][NT];
-    float mx[RT], sum[RT];
+    float mx[RT], sum[RT];                     // of the scores times scale2; the sums are the lane's own until the end
+    unsigned hollow;                           // bit t: this lane saw positions of its line of tile t, but no score above -infinity yet
 };
 
-__device__ __forceinline__ bool nonfinite_bf16(uint32_t w) { return (w & 0x7F80u) == 0x7F80u || (w & 0x7F800000u) == 0x7F800000u; }
-
-// The pages [pg_lo, pg_hi) of an item, pairs of them in turn over the waves.  last[t]: last position that this lane's line of tile t sees.
-template <int HD, int TERMS, int QT, int RT>
-__device__ __forceinline__ void attend_pages(const AttendItem &it, const bf16x8_t (&q)[RT][HD / 32][QT], const int (&last)[RT], int max_last, float scale2, int lane,
-                                             int wave, AttendState<RT, HD / 16> &st)
+template <int RT, int NT>
+__device__ __forceinline__ void attend_clear(AttendState<RT, NT> &st)
 {
-    constexpr int KT = HD / 32, NT = HD / 16;
-    const int lm = lane & 15, quad = lane >> 4;
-    const int pairs = (it.pg_hi - it.pg_lo + 1) >> 1;
-    const int tiles = (it.lines + 15) >> 4;
-    int pr = wave;
-    if (pr >= pairs) return;
-    int ids = -1, ids_from = pr;
-    auto load_ids = [&]() __attribute__((always_inline)) {
-        const int pg = it.pg_lo + 2 * (ids_from + (lane >> 1) * ATT_W) + (lane & 1);
-        ids = pg < it.pg_hi ? as_global(it.table)[pg] : -1;
-        if (ids >= it.n_pages) ids = -1;
-    };
-    unsigned hollow = 0;              // bit t: this lane's line of tile t saw positions, but no score above -infinity yet
-    uint4 kf[2][TERMS][KT];
-    uint2 vf[2][TERMS][NT];
-    int id[2];
-    auto find_ids = [&](int p) __attribute__((always_inline)) {
-        const int i = (p - ids_from) / ATT_W * 2;
-        id[0] = __builtin_amdgcn_readlane(ids, i);
-        id[1] = __builtin_amdgcn_readlane(ids, i + 1);
-    };
-    auto request_k = [&]() __attribute__((always_inline)) {
+    st.hollow = 0;
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const uint16_t *kb = it.k + (size_t)max(id[h], 0) * it.page_step + lm * (TERMS * HD) + quad * 8;
+    for (int t = 0; t < RT; ++t) {
+        st.mx[t] = -INFINITY;
+        st.sum[t] = 0.f;
 #pragma unroll
-            for (int t = 0; t < TERMS; ++t)
+        for (int nt = 0; nt < NT; ++nt) st.o[t][nt] = (f32x4_t){0.f, 0.f, 0.f, 0.f};
+    }
+}
+
+__device__ __forceinline__ bool nonfinite_bf16(uint32_t w) { return (w & 0x7F80u) == 0x7F80u || (w & 0x7F800000u) == 0x7F800000u; }
+__device__ __forceinline__ bool nonfinite_bf16(uint4 v) { return nonfinite_bf16(v.x) || nonfinite_bf16(v.y) || nonfinite_bf16(v.z) || nonfinite_bf16(v.w); }
+// bits of the first `keep` of two elements
+__device__ __forceinline__ uint32_t keep_mask(int keep) { return keep >= 2 ? 0xFFFFFFFFu : keep == 1 ? 0xFFFFu : 0u; }
+__device__ __forceinline__ uint4 keep_first(uint4 v, int keep)
+{
+    return make_uint4(v.x & keep_mask(keep), v.y & keep_mask(keep - 2), v.z & keep_mask(keep - 4), v.w & keep_mask(keep - 6));
+}
+// bits of the elements that are infinite or NaN
+__device__ __forceinline__ uint32_t nonfinite_bits(uint32_t w) { return ((w & 0x7F80u) == 0x7F80u ? 0xFFFFu : 0u) | ((w & 0x7F800000u) == 0x7F800000u ? 0xFFFF0000u : 0u); }
+__device__ __forceinline__ uint4 nonfinite_bits(uint4 v) { return make_uint4(nonfinite_bits(v.x), nonfinite_bits(v.y), nonfinite_bits(v.z), nonfinite_bits(v.w)); }
+
+// eight values as N bf16 terms
+template <int N>
+__device__ __forceinline__ void split_terms(const float (&x)[8], bf16x8_t (&t)[N])
+{
+    uint32_t w[N][4];
 #pragma unroll
-                for (int kt = 0; kt < KT; ++kt) kf[h][t][kt] = load_global16(kb + t * HD + kt * 32);
+    for (int e = 0; e < 4; ++e) {
+        float a = x[2 * e], b = x[2 * e + 1];
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            w[i][e] = pack_bf16(a, b);
+            if (i + 1 < N) {
+                a -= __uint_as_float(w[i][e] << 16);
+                b -= __uint_as_float(w[i][e] & 0xFFFF0000u);
+            }
         }
-    };
-    auto request_v = [&](const int (&of)[2]) __attribute__((always_inline)) {
+    }
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const uint16_t *vb = it.v + (size_t)max(of[h], 0) * it.page_step + lm * KV_PAGE + quad * 4;
+    for (int i = 0; i < N; ++i) t[i] = __builtin_bit_cast(bf16x8_t, make_uint4(w[i][0], w[i][1], w[i][2], w[i][3]));
+}
+
+// What a pair of pages leaves to be seen: positions 8 quad .. of the pair that exist for any line of the item (0 .. 8, the lane's own), and
+// whether anything of the pair is hidden from any line.
+struct PairMask {
+    int keep;
+    bool masked;
+};
+__device__ __forceinline__ PairMask pair_mask(int pos0, bool ok0, bool ok1, int first_last, int max_last, int quad)
+{
+    const int lim0 = ok0 ? min(max(max_last + 1 - pos0, 0), KV_PAGE) : 0, lim1 = ok1 ? min(max(max_last + 1 - pos0 - KV_PAGE, 0), KV_PAGE) : 0;
+    PairMask m;
+    m.keep = min(max((quad < 2 ? lim0 : lim1) - (quad & 1) * 8, 0), 8);
+    m.masked = lim0 < KV_PAGE || lim1 < KV_PAGE || first_last < pos0 + 2 * KV_PAGE - 1;
+    return m;
+}
+
+// Scores of NP pairs of a tile -> weights in s, with the running maximum and sum brought up to date; the output is rescaled where the
+// maximum of any of the wave's lines grew.
+template <int NP, int RT, int NT>
+__device__ __forceinline__ void attend_softmax(AttendState<RT, NT> &st, int t, float (&s)[NP][8], float scale2)
+{
+    float local = -INFINITY;
 #pragma unroll
-            for (int t = 0; t < TERMS; ++t)
+    for (int p = 0; p < NP; ++p)
 #pragma unroll
-                for (int nt = 0; nt < NT; ++nt) vf[h][t][nt] = load_global8(vb + (t * HD + nt * 16) * KV_PAGE);
+        for (int e = 0; e < 8; ++e) local = fmaxf(local, s[p][e]);
+    local = fmaxf(local, __shfl_xor(local, 16, 64));
+    local = fmaxf(local, __shfl_xor(local, 32, 64)) * scale2;
+    if (__any(local > st.mx[t])) {
+        const float m = fmaxf(st.mx[t], local), f = m == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(st.mx[t] - m);
+        st.mx[t] = m;
+        st.sum[t] *= f;
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) st.o[t][nt][r] *= f;
+    }
+    const float base = st.mx[t] == -INFINITY ? 0.f : st.mx[t];
+#pragma unroll
+    for (int p = 0; p < NP; ++p)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            s[p][e] = __builtin_amdgcn_exp2f(fmaf(s[p][e], scale2, -base));
+            st.sum[t] += s[p][e];
         }
-    };
-    load_ids();
-    find_ids(pr);
-    request_k();
-    request_v(id);
-    for (;;) {
-        const int pos0 = (it.pg_lo + 2 * pr) * KV_PAGE;
-        // positions of either page that any line of the item may see
-        int lim[2];
+}
+
+// scores that a lane's line does not see
+__device__ __forceinline__ void attend_hide(float (&s)[8], const PairMask &m, int pos0, int last, int quad)
+{
+    const int seen = min(m.keep, last - pos0 - quad * 8 + 1);
 #pragma unroll
-        for (int h = 0; h < 2; ++h) lim[h] = id[h] < 0 || it.pg_lo + 2 * pr + h >= it.pg_hi ? 0 : min(max(max_last + 1 - pos0 - h * KV_PAGE, 0), KV_PAGE);
-        const bool masked = lim[0] < KV_PAGE || lim[1] < KV_PAGE || it.first_last < pos0 + 2 * KV_PAGE - 1;
-        f32x4_t S[RT][2];
+    for (int e = 0; e < 8; ++e) s[e] = e < seen ? s[e] : -INFINITY;
+}
+
+// A pair of which some lines see a position that others do not, and in which V holds an infinity or NaN: 0 * V would be NaN for the
+// others.  Such elements leave the product (for both of their terms) and make NaN of the lines that see them.  v: the lane's
+// elements of dim nt * 16 + lm.
+template <int TERMS, int RT, int NT>
+__device__ __forceinline__ void attend_odd(AttendState<RT, NT> &st, int nt, uint4 (&v)[TERMS], int pos0, const int (&last)[RT], int quad)
+{
+    uint4 odd = nonfinite_bits(v[0]);
+    if constexpr (TERMS == 2) {
+        const uint4 o = nonfinite_bits(v[1]);
+        odd = make_uint4(odd.x | o.x, odd.y | o.y, odd.z | o.z, odd.w | o.w);
+    }
+#pragma unroll
+    for (int u = 0; u < TERMS; ++u) v[u] = make_uint4(v[u].x & ~odd.x, v[u].y & ~odd.y, v[u].z & ~odd.z, v[u].w & ~odd.w);
+    const uint32_t w[4] = {odd.x, odd.y, odd.z, odd.w};
+    int first = ALL_SEEN + 1;                                               // first such position of the dim
+#pragma unroll
+    for (int e = 7; e >= 0; --e)
+        if (w[e >> 1] >> 16 * (e & 1) & 1) first = pos0 + quad * 8 + e;
+    first = min(first, __shfl_xor(first, 16, 64));
+    first = min(first, __shfl_xor(first, 32, 64));
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+        const int at = __shfl(first, quad * 4 + r, 64);
 #pragma unroll
         for (int t = 0; t < RT; ++t)
-#pragma unroll
-            for (int h = 0; h < 2; ++h) S[t][h] = (f32x4_t){0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int h = 0; h < 2; ++h)
-#pragma unroll
-            for (int kt = 0; kt < KT; ++kt) {
-                const bf16x8_t kh = __builtin_bit_cast(bf16x8_t, kf[h][0][kt]);
-#pragma unroll
-                for (int t = 0; t < RT; ++t) {
-                    if (t >= tiles) continue;
-                    S[t][h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kh, q[t][kt][0], S[t][h], 0, 0, 0);
-                    if constexpr (QT == 2) S[t][h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kh, q[t][kt][1], S[t][h], 0, 0, 0);
-                    if constexpr (TERMS == 2)
-                        S[t][h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, kf[h][1][kt]), q[t][kt][0], S[t][h], 0, 0, 0);
-                }
-            }
-        pr += ATT_W;
-        const bool more = pr < pairs;
-        if (more) {
-            if (pr - ids_from >= ATT_ID_PAIRS * ATT_W) {
-                ids_from = pr;
-                load_ids();
-            }
-            find_ids(pr);
-            request_k();
-        }
-        if (masked) {
-            // what no line sees is taken out of V (it may hold anything), what a line does not see out of its scores
-#pragma unroll
-            for (int h = 0; h < 2; ++h)
-                if (lim[h] < KV_PAGE) {
-                    const int keep = min(max(lim[h] - quad * 4, 0), 4);
-                    const uint32_t m0 = keep >= 2 ? 0xFFFFFFFFu : keep == 1 ? 0xFFFFu : 0u, m1 = keep >= 4 ? 0xFFFFFFFFu : keep == 3 ? 0xFFFFu : 0u;
-#pragma unroll
-                    for (int t = 0; t < TERMS; ++t)
-#pragma unroll
-                        for (int nt = 0; nt < NT; ++nt) {
-                            vf[h][t][nt].x &= m0;
-                            vf[h][t][nt].y &= m1;
-                        }
-                }
-#pragma unroll
-            for (int t = 0; t < RT; ++t)
-#pragma unroll
-                for (int h = 0; h < 2; ++h)
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) {
-                        const int in_page = quad * 4 + r;
-                        if (in_page >= lim[h] || pos0 + h * KV_PAGE + in_page > last[t]) S[t][h][r] = -INFINITY;
-                    }
-        }
-        bf16x8_t Ph[RT], Pl[RT];
-#pragma unroll
-        for (int t = 0; t < RT; ++t) {
-            if (t >= tiles) continue;
-            float m = st.mx[t];
-#pragma unroll
-            for (int h = 0; h < 2; ++h)
-#pragma unroll
-                for (int r = 0; r < 4; ++r) m = fmaxf(m, S[t][h][r]);
-            m = fmaxf(m, __shfl_xor(m, 16, 64));
-            m = fmaxf(m, __shfl_xor(m, 32, 64));
-            const float base = m == -INFINITY ? 0.f : m;
-            const float f = __builtin_amdgcn_exp2f((st.mx[t] - base) * scale2);
-            st.mx[t] = m;
-            if (m == -INFINITY && ((lim[0] > 0 && pos0 <= last[t]) || (lim[1] > 0 && pos0 + KV_PAGE <= last[t]))) hollow |= 1u << t;
-            float sum = 0.f;
-#pragma unroll
-            for (int h = 0; h < 2; ++h)
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    S[t][h][r] = __builtin_amdgcn_exp2f((S[t][h][r] - base) * scale2);
-                    sum += S[t][h][r];
-                }
-            st.sum[t] = st.sum[t] * f + sum;
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                for (int r = 0; r < 4; ++r) st.o[t][nt][r] *= f;
-            split_bf16x8(S[t][0], S[t][1], Ph[t], Pl[t]);
-        }
-        if (masked) {
-            // An infinity or NaN of V in a place that some lines see and others do not: 0 * V would be NaN for those.  A page with such
-            // elements goes position by position, each for the lines that see it, and leaves the product of the pair.
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                bool odd = false;
-#pragma unroll
-                for (int t = 0; t < TERMS; ++t)
-#pragma unroll
-                    for (int nt = 0; nt < NT; ++nt) odd |= nonfinite_bf16(vf[h][t][nt].x) || nonfinite_bf16(vf[h][t][nt].y);
-                if (!__any(odd)) continue;
-#pragma clang loop unroll(disable)
-                for (int j = 0; j < lim[h]; ++j) {
-                    const int mine = quad == j >> 2 ? j & 3 : 4;
-                    const uint32_t m0 = mine == 0 ? 0xFFFFu : mine == 1 ? 0xFFFF0000u : 0u, m1 = mine == 2 ? 0xFFFFu : mine == 3 ? 0xFFFF0000u : 0u;
-#pragma unroll
-                    for (int t = 0; t < RT; ++t) {
-                        if (t >= tiles) continue;
-                        const bool sees = pos0 + h * KV_PAGE + j <= last[t];
-#pragma unroll
-                        for (int nt = 0; nt < NT; ++nt) {
-                            f32x4_t o = st.o[t][nt];
-#pragma unroll
-                            for (int u = 0; u < TERMS; ++u) {
-                                const uint32_t x = vf[h][u][nt].x & m0, y = vf[h][u][nt].y & m1;
-                                const bf16x8_t v = __builtin_bit_cast(bf16x8_t, h == 0 ? make_uint4(x, y, 0u, 0u) : make_uint4(0u, 0u, x, y));
-                                o = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, Ph[t], o, 0, 0, 0);
-                                if (u == 0) o = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, Pl[t], o, 0, 0, 0);
-                            }
-#pragma unroll
-                            for (int r = 0; r < 4; ++r) st.o[t][nt][r] = sees ? o[r] : st.o[t][nt][r];
-                        }
-                    }
-                }
-#pragma unroll
-                for (int t = 0; t < TERMS; ++t)
-#pragma unroll
-                    for (int nt = 0; nt < NT; ++nt) vf[h][t][nt] = make_uint2(0u, 0u);
-            }
-        }
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-            const bf16x8_t vh = __builtin_bit_cast(bf16x8_t, make_uint4(vf[0][0][nt].x, vf[0][0][nt].y, vf[1][0][nt].x, vf[1][0][nt].y));
-#pragma unroll
-            for (int t = 0; t < RT; ++t) {
-                if (t >= tiles) continue;
-                st.o[t][nt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vh, Ph[t], st.o[t][nt], 0, 0, 0);
-                st.o[t][nt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vh, Pl[t], st.o[t][nt], 0, 0, 0);
-                if constexpr (TERMS == 2) {
-                    const bf16x8_t vl = __builtin_bit_cast(bf16x8_t, make_uint4(vf[0][1][nt].x, vf[0][1][nt].y, vf[1][1][nt].x, vf[1][1][nt].y));
-                    st.o[t][nt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vl, Ph[t], st.o[t][nt], 0, 0, 0);
-                }
-            }
-        }
-        if (!more) break;
-        request_v(id);
+            if (last[t] >= at) st.o[t][nt][r] = __builtin_nanf("");
     }
+}
+
+// A lane's q of a line as operands: values 32 kt + 8 quad .. + 7.
+template <int HD, int QT>
+__device__ __forceinline__ void attend_load_q(const AttendDev &a, int row, int head, int quad, bf16x8_t (&q)[HD / 32][QT])
+{
+#pragma unroll
+    for (int kt = 0; kt < HD / 32; ++kt) {
+        const size_t at = (size_t)row * a.q_stride + (size_t)head * a.q_head + kt * 32 + quad * 8;
+        if constexpr (QT == 1) {
+            q[kt][0] = __builtin_bit_cast(bf16x8_t, load_global16(static_cast<const uint16_t *>(a.q) + at));
+        } else {
+            float x[8];
+            if (a.q_type == EE_FP32)
+                load8<EE_FP32>(a.q, at, x);
+            else if (a.q_type == EE_FP16)
+                load8<EE_FP16>(a.q, at, x);
+            else
+                load8<EE_BF16>(a.q, at, x);
+            split_terms<QT>(x, q[kt]);
+        }
+    }
+}
+
+// One line's result: the output where this is its only part, a part of it otherwise.
+template <int RT, int NT>
+__device__ __forceinline__ void attend_store(const AttendDev &a, const AttendItem &it, const AttendState<RT, NT> &st, int t, int row, int head, int quad)
+{
+    constexpr int HD = NT * 16;
+    const size_t line = (size_t)row * a.n_heads + head;
+    const int most = a.most_own + a.most_shared;
+    const bool alone = it.own_parts == 1 && it.common_parts == 0;
+    if (alone) {
+        const float inv = st.sum[t] == 0.f ? 0.f : 1.0f / st.sum[t];        // (0: the line saw no position)
+        const size_t to = (size_t)row * a.o_stride + (size_t)head * a.o_head + quad * 4;
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) store4(a.out_type, a.out, to + nt * 16, st.o[t][nt][0] * inv, st.o[t][nt][1] * inv, st.o[t][nt][2] * inv, st.o[t][nt][3] * inv);
+    } else if (st.mx[t] != -INFINITY) {                                     // (nothing is read of an empty part)
+        float *o = a.part + (line * most + it.slot) * HD + quad * 4;
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) *as_global_mut(reinterpret_cast<f32x4_t *>(o + nt * 16)) = st.o[t][nt];
+    }
+    if (quad == 0 && most > 1) {
+        typedef __attribute__((ext_vector_type(2))) float f32x2_t;
+        f32x2_t *ml = reinterpret_cast<f32x2_t *>(a.part_ml + line * (most + 1));
+        if (!alone) as_global_mut(ml)[1 + it.slot] = (f32x2_t){st.mx[t], st.sum[t]};
+        if (it.slot == 0) as_global_mut(ml)[0] = (f32x2_t){__int_as_float(alone ? 0 : it.own_parts), __int_as_float(it.common_parts)};
+    }
+}
+
+// The sums of a line's lanes, and NaN where it saw positions but no score above -infinity: it has no softmax.
+template <int RT, int NT>
+__device__ __forceinline__ void attend_finish(AttendState<RT, NT> &st)
+{
+    st.hollow |= __shfl_xor(st.hollow, 16, 64);
+    st.hollow |= __shfl_xor(st.hollow, 32, 64);
 #pragma unroll
     for (int t = 0; t < RT; ++t) {
         st.sum[t] += __shfl_xor(st.sum[t], 16, 64);
         st.sum[t] += __shfl_xor(st.sum[t], 32, 64);
-        if (st.mx[t] == -INFINITY && (hollow >> t & 1)) st.sum[t] = __builtin_nanf("");
+        if (st.mx[t] == -INFINITY && (st.hollow >> t & 1)) st.sum[t] = __builtin_nanf("");
     }
 }
 
@@ -269,6 +435,132 @@ __device__ __forceinline__ float join_sums(float m, float m1, float l1, float f1
 {
     if (m == -INFINITY) return l1 + l2;
     return (m1 == -INFINITY ? 0.f : l1 * f1) + (m2 == -INFINITY ? 0.f : l2 * f2);
+}
+
+// ------------------------------------------------------------------ few lines: bound by the cache's bytes
+//
+// The waves take the item's pairs of pages in turn, K and V straight from the records into registers: K of the next pair is requested when this
+// one's scores are done, V when its product is.
+
+template <int HD, int TERMS, int QT, int PT, int RT>
+__device__ __forceinline__ void attend_pages(const AttendDev &a, const AttendItem &it, int kvh, const bf16x8_t (&q)[RT][HD / 32][QT], const int (&last)[RT], int first_last,
+                                             int max_last, int lane, int wave, AttendState<RT, HD / 16> &st)
+{
+    constexpr int KT = HD / 32, NT = HD / 16, ID_PAIRS = 32;
+    const int lm = lane & 15, quad = lane >> 4;
+    const int pairs = (it.pg_hi - it.pg_lo + 1) >> 1, tiles = (it.lines + 15) >> 4;
+    const size_t page_step = (size_t)a.b.n_kv_heads * KV_PAGE * TERMS * HD;
+    const int *table = a.b.table + (size_t)it.seq * a.b.table_stride;
+    int pr = wave;
+    if (pr >= pairs) return;
+    // ids of the wave's next 32 pairs, one page a lane; -1 outside the pools and past the item's last page
+    int ids, ids_from = pr;
+    auto load_ids = [&]() __attribute__((always_inline)) {
+        const int pg = it.pg_lo + 2 * (ids_from + (lane >> 1) * ATT_W) + (lane & 1);
+        ids = pg < it.pg_hi ? as_global(table)[pg] : -1;
+        if (ids >= a.b.n_pages) ids = -1;
+    };
+    int id0, id1;
+    auto find_ids = [&](int p) __attribute__((always_inline)) {
+        const int i = (p - ids_from) / ATT_W * 2;
+        id0 = __builtin_amdgcn_readlane(ids, i);
+        id1 = __builtin_amdgcn_readlane(ids, i + 1);
+    };
+    // operand rows of K: page lm >> 3, position 8 ((lm >> 2) & 1) + 4 p + (lm & 3) of it; V: page quad >> 1, positions 8 (quad & 1) .. + 7
+    const uint16_t *k0 = a.b.kpool + (size_t)kvh * KV_PAGE * TERMS * HD + ((lm >> 2 & 1) * 8 + (lm & 3)) * (TERMS * HD) + quad * 8;
+    const uint16_t *v0 = a.b.vpool + (size_t)kvh * KV_PAGE * TERMS * HD + lm * KV_PAGE + (quad & 1) * 8;
+    uint4 kf[2][TERMS][KT], vf[NT][TERMS];
+    auto request_k = [&]() __attribute__((always_inline)) {
+        const uint16_t *kb = k0 + (size_t)max(lm < 8 ? id0 : id1, 0) * page_step;
+#pragma unroll
+        for (int p = 0; p < 2; ++p)
+#pragma unroll
+            for (int u = 0; u < TERMS; ++u)
+#pragma unroll
+                for (int kt = 0; kt < KT; ++kt) kf[p][u][kt] = load_global16(kb + p * 4 * TERMS * HD + u * HD + kt * 32);
+    };
+    auto request_v = [&]() __attribute__((always_inline)) {
+        const uint16_t *vb = v0 + (size_t)max(quad < 2 ? id0 : id1, 0) * page_step;
+#pragma unroll
+        for (int u = 0; u < TERMS; ++u)
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) vf[nt][u] = load_global16(vb + (u * HD + nt * 16) * KV_PAGE);
+    };
+    load_ids();
+    find_ids(pr);
+    request_k();
+    request_v();
+    for (;;) {
+        const int pos0 = (it.pg_lo + 2 * pr) * KV_PAGE;
+        const PairMask mask = pair_mask(pos0, id0 >= 0, id1 >= 0, first_last, max_last, quad);
+        f32x4_t S[RT][2];
+#pragma unroll
+        for (int t = 0; t < RT; ++t) S[t][0] = S[t][1] = (f32x4_t){0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+            for (int p = 0; p < 2; ++p)
+#pragma unroll
+                for (int u = 0; u < TERMS; ++u) {
+                    const bf16x8_t k = __builtin_bit_cast(bf16x8_t, kf[p][u][kt]);
+#pragma unroll
+                    for (int t = 0; t < RT; ++t) {
+                        if (t >= tiles) continue;
+#pragma unroll
+                        for (int i = 0; i < QT - u; ++i) S[t][p] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, q[t][kt][i], S[t][p], 0, 0, 0);
+                    }
+                }
+        pr += ATT_W;
+        const bool more = pr < pairs;
+        if (more) {
+            if (pr - ids_from >= ID_PAIRS * ATT_W) {
+                ids_from = pr;
+                load_ids();
+            }
+            find_ids(pr);
+            request_k();
+        }
+        bf16x8_t P[RT][PT];
+#pragma unroll
+        for (int t = 0; t < RT; ++t) {
+            if (t >= tiles) continue;
+            float s[1][8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) s[0][e] = S[t][e >> 2][e & 3];
+            if (mask.masked) attend_hide(s[0], mask, pos0, last[t], quad);
+            attend_softmax<1>(st, t, s, a.scale2);
+            if (st.mx[t] == -INFINITY && min(mask.keep, last[t] - pos0 - quad * 8 + 1) > 0) st.hollow |= 1u << t;
+            split_terms<PT>(s[0], P[t]);
+        }
+        if (mask.masked) {
+            // what no line sees may hold anything
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+                bool odd = false;
+#pragma unroll
+                for (int u = 0; u < TERMS; ++u) {
+                    vf[nt][u] = keep_first(vf[nt][u], mask.keep);
+                    odd |= nonfinite_bf16(vf[nt][u]);
+                }
+                if (__any(odd)) attend_odd<TERMS>(st, nt, vf[nt], pos0, last, quad);
+            }
+        }
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int u = 0; u < TERMS; ++u) {
+                const bf16x8_t v = __builtin_bit_cast(bf16x8_t, vf[nt][u]);
+#pragma unroll
+                for (int t = 0; t < RT; ++t) {
+                    if (t >= tiles) continue;
+#pragma unroll
+                    for (int i = 0; i < PT - u; ++i) st.o[t][nt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, P[t][i], st.o[t][nt], 0, 0, 0);
+                }
+            }
+        if (!more) break;
+        request_v();
+    }
+    attend_finish(st);
 }
 
 // floats per lane that a wave hands over
@@ -284,7 +576,7 @@ constexpr size_t attend_lds()
 
 // Joins the waves' results into wave 0's, halves of them at a time; `active`: waves that had pages.
 template <int HD, int RT>
-__device__ __forceinline__ void attend_join_waves(AttendState<RT, HD / 16> &st, float *lds, int active, float scale2, int lane, int wave)
+__device__ __forceinline__ void attend_join_waves(AttendState<RT, HD / 16> &st, float *lds, int active, int lane, int wave)
 {
     constexpr int NT = HD / 16;
 #pragma unroll
@@ -307,7 +599,7 @@ __device__ __forceinline__ void attend_join_waves(AttendState<RT, HD / 16> &st, 
             for (int t = 0; t < RT; ++t) {
                 const float m2 = ml[(2 * t) * 64], l2 = ml[(2 * t + 1) * 64];
                 const float m = fmaxf(st.mx[t], m2), base = m == -INFINITY ? 0.f : m;
-                const float f1 = __builtin_amdgcn_exp2f((st.mx[t] - base) * scale2), f2 = __builtin_amdgcn_exp2f((m2 - base) * scale2);
+                const float f1 = __builtin_amdgcn_exp2f(st.mx[t] - base), f2 = __builtin_amdgcn_exp2f(m2 - base);
                 st.sum[t] = join_sums(m, st.mx[t], st.sum[t], f1, m2, l2, f2);
                 st.mx[t] = m;
 #pragma unroll
@@ -320,6 +612,269 @@ __device__ __forceinline__ void attend_join_waves(AttendState<RT, HD / 16> &st, 
         }
         __syncthreads();
     }
+}
+
+template <int HD, int TERMS, int QT, int PT, int RT>
+__global__ void __launch_bounds__(ATT_W * 64, RT == 1 && TERMS * HD < 256 ? 2 : 1) ee_attend_kernel(AttendDev a)
+{
+    extern __shared__ __align__(16) char lds_raw[];
+    constexpr int KT = HD / 32, NT = HD / 16;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int lm = lane & 15, quad = lane >> 4, kvh = blockIdx.x;
+    AttendItem it;
+    if (!attend_item<RT * 16>(a, blockIdx.y, lane, it)) return;
+    // this lane's lines: row, head, last position seen
+    int row[RT], head[RT], last[RT];
+#pragma unroll
+    for (int t = 0; t < RT; ++t) {
+        const int line = it.line0 + min(t * 16 + lm, it.lines - 1), i = line / a.per_key;
+        row[t] = it.row0 + i;
+        head[t] = kvh * a.per_key + line - i * a.per_key;
+        last[t] = it.shared ? ALL_SEEN : it.first_pos + i;
+    }
+    AttendState<RT, NT> st;
+    attend_clear(st);
+    if (it.pg_hi > it.pg_lo) {
+        const int first_last = it.shared ? ALL_SEEN : it.first_pos + it.line0 / a.per_key;
+        const int max_last = it.shared ? ALL_SEEN : min(it.first_pos + (it.line0 + it.lines - 1) / a.per_key, a.b.capacity() - 1);
+        bf16x8_t q[RT][KT][QT];
+#pragma unroll
+        for (int t = 0; t < RT; ++t)
+            if (t * 16 < it.lines) attend_load_q<HD, QT>(a, row[t], head[t], quad, q[t]);
+        attend_pages<HD, TERMS, QT, PT, RT>(a, it, kvh, q, last, first_last, max_last, lane, wave, st);
+        attend_join_waves<HD, RT>(st, reinterpret_cast<float *>(lds_raw), min(ATT_W, (it.pg_hi - it.pg_lo + 1) >> 1), lane, wave);
+    }
+    if (wave != 0) return;
+#pragma unroll
+    for (int t = 0; t < RT; ++t)
+        if (t * 16 + lm < it.lines) attend_store(a, it, st, t, row[t], head[t], quad);
+}
+
+// ------------------------------------------------------------------ many lines: bound by the matrix cores
+//
+// Each of the waves has 32 lines of its own, K and V of POS positions go through LDS for all of them, straight from the records (K gathered into
+// operand order), the next ones on their way while these are multiplied.
+
+constexpr int ATT_WIDE = ATT_W * 32;           // lines of an item
+template <int HD, int TERMS>
+constexpr int attend_wide_pos() { return TERMS == 1 ? 64 : 32; }
+template <int HD, int TERMS>
+constexpr int attend_wide_stage() { return attend_wide_pos<HD, TERMS>() * TERMS * HD * 4; }   // bytes of K and V
+
+template <int HD, int TERMS, int QT, int PT>
+__global__ void __launch_bounds__(ATT_W * 64, QT == 1 ? 2 : 1) ee_attend_wide_kernel(AttendDev a)
+{
+    extern __shared__ __align__(16) char lds[];
+    constexpr int KT = HD / 32, NT = HD / 16, RT = 2, POS = attend_wide_pos<HD, TERMS>(), PAGES = POS / KV_PAGE, NP = POS / 32;
+    constexpr int REC = KV_PAGE * TERMS * HD * 2;            // bytes of a (page, head) record of K or of V
+    constexpr int STAGE = attend_wide_stage<HD, TERMS>();    // [page][K, V][REC]
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int lm = lane & 15, quad = lane >> 4, kvh = blockIdx.x;
+    AttendItem it;
+    if (!attend_item<ATT_WIDE>(a, blockIdx.y, lane, it)) return;
+    const int line_w = it.line0 + wave * 32, lines = min(max(it.lines - wave * 32, 0), 32);
+    int row[RT], head[RT], last[RT];
+    bf16x8_t q[RT][KT][QT];
+#pragma unroll
+    for (int t = 0; t < RT; ++t) {
+        const int line = min(line_w + t * 16 + lm, it.line0 + it.lines - 1), i = line / a.per_key;
+        row[t] = it.row0 + i;
+        head[t] = kvh * a.per_key + line - i * a.per_key;
+        last[t] = it.first_pos + i;
+        attend_load_q<HD, QT>(a, row[t], head[t], quad, q[t]);
+    }
+    const int first_last = it.first_pos + line_w / a.per_key;                                       // of the wave
+    const int wave_last = lines > 0 ? min(it.first_pos + (line_w + lines - 1) / a.per_key, a.b.capacity() - 1) : -1;
+    const int n_pg = it.pg_hi - it.pg_lo, steps = (n_pg + PAGES - 1) / PAGES;
+    const int *table = a.b.table + (size_t)it.seq * a.b.table_stride;
+    const unsigned lds0 = lds_offset(lds);
+    // ids of 64 pages in the lanes, from page ids_from of the item on
+    int ids = -1, ids_from = -64;
+    auto id_of = [&](int pg) __attribute__((always_inline)) { return pg < n_pg ? __builtin_amdgcn_readlane(ids, pg - ids_from) : -1; };
+    auto load_ids = [&](int pg) __attribute__((always_inline)) {
+        if (pg < ids_from + 64) return;
+        ids_from = pg;
+        ids = pg + lane < n_pg ? as_global(table)[it.pg_lo + pg + lane] : -1;
+        if (ids >= a.b.n_pages) ids = -1;
+    };
+    // A wave brings its share of a step's records.  K in operand order: kilobyte (kt, term) holds lane (position lm, values 8 quad ..)'s 16 bytes in turn.
+    auto request = [&](int step, int buf) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < 2 * PAGES / ATT_W; ++i) {
+            const int which = wave + i * ATT_W, pg = which >> 1;
+            const bool is_v = which & 1;
+            const int id = max(id_of(step * PAGES + pg), 0);
+            const char *src = reinterpret_cast<const char *>(is_v ? a.b.vpool : a.b.kpool) + ((size_t)id * a.b.n_kv_heads + kvh) * REC;
+            const unsigned dst = lds0 + buf * STAGE + which * REC;
+            const int off = is_v ? lane * 16 : lm * (TERMS * HD * 2) + quad * 16;
+#pragma unroll
+            for (int f = 0; f < REC / 1024; ++f) load_lds_kb(uniform_ptr(src + (is_v ? f * 1024 : (f % TERMS) * HD * 2 + f / TERMS * 64)), off, dst + f * 1024);
+        }
+    };
+    AttendState<RT, NT> st;
+    attend_clear(st);
+    if (steps > 0) {
+        load_ids(0);
+        wait_vmem();
+        request(0, 0);
+    }
+    const int koff = (lm >> 3) * 2 * REC + (quad * 16 + (lm >> 2 & 1) * 8 + (lm & 3)) * 16;
+    const int voff = REC + (quad >> 1) * 2 * REC + lm * 32 + (quad & 1) * 16;
+    for (int step = 0; step < steps; ++step) {
+        int id[PAGES];
+#pragma unroll
+        for (int i = 0; i < PAGES; ++i) id[i] = id_of(step * PAGES + i);
+        if (step + 1 < steps) load_ids((step + 1) * PAGES);
+        wait_pending<0>();
+        lds_barrier();
+        if (step + 1 < steps) request(step + 1, (step + 1) & 1);
+        const int pos0 = (it.pg_lo + step * PAGES) * KV_PAGE;
+        if (pos0 > wave_last) continue;
+        const char *buf = lds + (step & 1) * STAGE;
+        float s[RT][NP][8];
+#pragma unroll
+        for (int p = 0; p < NP; ++p) {
+            f32x4_t S[RT][2];
+#pragma unroll
+            for (int t = 0; t < RT; ++t) S[t][0] = S[t][1] = (f32x4_t){0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+#pragma unroll
+                    for (int u = 0; u < TERMS; ++u) {
+                        const bf16x8_t k = *reinterpret_cast<const bf16x8_t *>(buf + p * 4 * REC + koff + h * 64 + (kt * TERMS + u) * 1024);
+#pragma unroll
+                        for (int t = 0; t < RT; ++t)
+#pragma unroll
+                            for (int i = 0; i < QT - u; ++i) S[t][h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, q[t][kt][i], S[t][h], 0, 0, 0);
+                    }
+#pragma unroll
+            for (int t = 0; t < RT; ++t)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) s[t][p][e] = S[t][e >> 2][e & 3];
+        }
+        PairMask mask[NP];
+        bool masked = false;
+#pragma unroll
+        for (int p = 0; p < NP; ++p) {
+            mask[p] = pair_mask(pos0 + p * 32, id[2 * p] >= 0, id[2 * p + 1] >= 0, first_last, wave_last, quad);
+            masked |= mask[p].masked;
+        }
+        bf16x8_t P[NP][RT][PT];
+#pragma unroll
+        for (int t = 0; t < RT; ++t) {
+            if (masked) {
+#pragma unroll
+                for (int p = 0; p < NP; ++p) attend_hide(s[t][p], mask[p], pos0 + p * 32, last[t], quad);
+            }
+            attend_softmax<NP>(st, t, s[t], a.scale2);
+            if (st.mx[t] == -INFINITY) {
+#pragma unroll
+                for (int p = 0; p < NP; ++p)
+                    if (min(mask[p].keep, last[t] - pos0 - p * 32 - quad * 8 + 1) > 0) st.hollow |= 1u << t;
+            }
+#pragma unroll
+            for (int p = 0; p < NP; ++p) split_terms<PT>(s[t][p], P[p][t]);
+        }
+#pragma unroll
+        for (int p = 0; p < NP; ++p) {
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+                uint4 v[TERMS];
+#pragma unroll
+                for (int u = 0; u < TERMS; ++u) v[u] = *reinterpret_cast<const uint4 *>(buf + p * 4 * REC + voff + u * HD * 32 + nt * 512);
+                if (mask[p].masked) {
+                    // what no line sees may hold anything
+                    bool odd = false;
+#pragma unroll
+                    for (int u = 0; u < TERMS; ++u) {
+                        v[u] = keep_first(v[u], mask[p].keep);
+                        odd |= nonfinite_bf16(v[u]);
+                    }
+                    if (__any(odd)) attend_odd<TERMS>(st, nt, v, pos0 + p * 32, last, quad);
+                }
+#pragma unroll
+                for (int u = 0; u < TERMS; ++u)
+#pragma unroll
+                    for (int t = 0; t < RT; ++t)
+#pragma unroll
+                        for (int i = 0; i < PT - u; ++i)
+                            st.o[t][nt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, v[u]), P[p][t][i], st.o[t][nt], 0, 0, 0);
+            }
+        }
+    }
+    attend_finish(st);
+#pragma unroll
+    for (int t = 0; t < RT; ++t)
+        if (t * 16 + lm < lines) attend_store(a, it, st, t, row[t], head[t], quad);
+}
+
+// ------------------------------------------------------------------ parts
+//
+// Joins the parts of every line that has several, in order.  thread = four dims of a line and every 256 / (HD / 4)-th of its parts where there are many
+// (`spread` of them side by side), of several lines otherwise.
+template <int HD>
+__global__ void __launch_bounds__(256) ee_attend_join_kernel(AttendDev a, int spread)
+{
+    constexpr int TPL = HD / 4, ROWS = 256 / TPL;
+    typedef __attribute__((ext_vector_type(2))) float f32x2_t;
+    __shared__ f32x4_t nums[ROWS][TPL];
+    __shared__ float dens[ROWS], maxs[ROWS], bads[ROWS];
+    const int tr = threadIdx.x / TPL, td = threadIdx.x % TPL, sub = tr % spread;
+    const long long line = (long long)blockIdx.x * (ROWS / spread) + tr / spread;
+    const long long rows = a.b.start(a.b.n_seqs);
+    const int most = a.most_own + a.most_shared;
+    int own = 0, shared = 0;
+    const f32x2_t *ml = reinterpret_cast<const f32x2_t *>(a.part_ml + line * (most + 1));
+    if (line < rows * a.n_heads) {
+        const f32x2_t n = as_global(ml)[0];
+        own = __float_as_int(n[0]);
+        shared = __float_as_int(n[1]);
+    }
+    if (own == 0) own = shared = 0;                                         // (written already, or padding)
+    const float *o = a.part + line * most * HD + td * 4;
+    f32x4_t num = {0.f, 0.f, 0.f, 0.f};
+    float m = -INFINITY, den = 0.f, bad = 0.f;
+    for (int p = sub; p < own + shared; p += spread) {
+        const int slot = p < own ? p : a.most_own + p - own;
+        const f32x2_t x = as_global(ml)[1 + slot];
+        if (x[0] == -INFINITY) {
+            bad = x[1] != 0.f ? 1.f : bad;                                  // positions without a softmax
+            continue;
+        }
+        const f32x4_t v = *as_global(reinterpret_cast<const f32x4_t *>(o + (size_t)slot * HD));
+        const float m_new = fmaxf(m, x[0]), f0 = __builtin_amdgcn_exp2f(m - m_new), f1 = __builtin_amdgcn_exp2f(x[0] - m_new);
+        m = m_new;
+        den = den * f0 + x[1] * f1;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) num[r] = num[r] * f0 + v[r] * f1;
+    }
+    if (spread > 1) {
+        nums[tr][td] = num;
+        if (td == 0) {
+            dens[tr] = den;
+            maxs[tr] = m;
+            bads[tr] = bad;
+        }
+        __syncthreads();
+        if (sub != 0) return;
+        for (int i = 1; i < spread; ++i) {
+            const float m2 = maxs[tr + i];
+            bad = fmaxf(bad, bads[tr + i]);
+            if (m2 == -INFINITY) continue;
+            const float m_new = fmaxf(m, m2), f0 = __builtin_amdgcn_exp2f(m - m_new), f1 = __builtin_amdgcn_exp2f(m2 - m_new);
+            m = m_new;
+            den = den * f0 + dens[tr + i] * f1;
+            const f32x4_t v = nums[tr + i][td];
+#pragma unroll
+            for (int r = 0; r < 4; ++r) num[r] = num[r] * f0 + v[r] * f1;
+        }
+    }
+    if (own == 0) return;
+    const int row = (int)(line / a.n_heads), head = (int)(line - (long long)row * a.n_heads);
+    const float inv = m != -INFINITY ? 1.0f / den : bad != 0.f ? __builtin_nanf("") : 0.f;
+    store4(a.out_type, a.out, (size_t)row * a.o_stride + (size_t)head * a.o_head + td * 4, num[0] * inv, num[1] * inv, num[2] * inv, num[3] * inv);
 }
 
 }  // namespace ee

@@ -39,10 +39,11 @@ __device__ __forceinline__ int wave_scan(int x, int lane)
 }
 
 // Which of n things item `item` belongs to when thing i has count(i) items, and its place there; false past the last.  All
-// lanes of a wave call it and get the same answer; 64 things a round.
+// lanes of a wave call it and get the same answer; 64 things a round.  Where there is no such item, *all is the number of items.
 template <typename F>
-__device__ __forceinline__ bool find_item(int n, int item, int lane, F count, int &index, int &place)
+__device__ __forceinline__ bool find_item(int n, int item, int lane, F count, int &index, int &place, int *all = nullptr)
 {
+    int before = 0;
     for (int base = 0; base < n; base += 64) {
         const int c = base + lane < n ? count(base + lane) : 0;
         const int incl = wave_scan(c, lane), total = __shfl(incl, 63, 64);
@@ -53,7 +54,9 @@ __device__ __forceinline__ bool find_item(int n, int item, int lane, F count, in
             return true;
         }
         item -= total;
+        before += total;
     }
+    if (all) *all = before;
     return false;
 }
 
