@@ -10,10 +10,10 @@ struct AttendKernel {
 template <int HD, int TERMS, int QT, int PT>
 static AttendKernel attend_of_tiles(int tiles)
 {
-    if (tiles == 1) return {ee_attend_kernel<HD, TERMS, QT, PT, 1>, attend_lds<HD, 1>()};
+    if (tiles == 1) return {ee_attend_kernel<HD, TERMS, QT, PT, 1>, attend_lds<HD, QT, 1>()};
     if constexpr (TERMS == 1 || HD == 64)
-        if (tiles == 2) return {ee_attend_kernel<HD, TERMS, QT, PT, 2>, attend_lds<HD, 2>()};
-    return {ee_attend_wide_kernel<HD, TERMS, QT, PT == 2 && QT == 1 ? 1 : PT>, (size_t)2 * attend_wide_stage<HD, TERMS>()};
+        if (tiles == 2) return {ee_attend_kernel<HD, TERMS, QT, PT, 2>, attend_lds<HD, QT, 2>()};
+    return {ee_attend_wide_kernel<HD, TERMS, QT, PT == 2 && QT == 1 ? 1 : PT>, attend_wide_lds<HD, TERMS>()};
 }
 template <int HD>
 static AttendKernel attend_kernel(int terms, int q_type, int out_type, int tiles)
@@ -63,10 +63,19 @@ static AttendPlan plan_attend(const ee_paged_cache &c, const ee_attend_args &p)
     const long long chunks_own = most_chunks(seqs, T, per_key, pl.tiles * 16);
     const long long chunks_shared = pl.groups ? most_chunks(pl.groups, T, per_key, pl.tiles * 16) : 0;
     const int own_pages = std::max(pages - shared_pages, 1);
-    // Parts: as many pages each as make about 512 items (two for a compute unit) if sequences are two thirds of the longest on average, in
-    // rounds of 8 (a pair for each wave).
-    const long long work = chunks_own * (seqs > 1 ? (2 * own_pages + 2) / 3 : own_pages) + chunks_shared * shared_pages;
-    pl.quota = (int)(std::max<long long>(8, (work * c.n_kv_heads + 511) / 512) + 7) / 8 * 8;
+    // Parts: the fewest pages each (a pair for each wave at a time: multiples of 8) that leave the items as many as the chip holds at once, two for a
+    // compute unit, if sequences are half the longest on average.  A second round costs more than longer parts: eight rounds of five rows of 32 heads
+    // behind 576 common positions, parts of 16 / 24 pages (544 / 448 items) 21.6 / 16.8 us; 32 rows of 8 key heads behind 6000, parts of 40 / 56 / 80
+    // pages (616 / 500 / 424 items) 33.9 / 27.3 / 32.4.  Where chunks alone are more than that, half as many parts again.
+    const long long est_own = seqs * ((own_lines + pl.tiles * 16 - 1) / (pl.tiles * 16));
+    const double room = std::max(512.0 / c.n_kv_heads, 1.5 * (double)(est_own + chunks_shared));
+    pl.quota = 8;
+    while (pl.quota < std::max(own_pages, shared_pages)) {
+        const double own_parts = seqs == 1 ? (double)((own_pages + pl.quota - 1) / pl.quota) : std::max(1.0, 0.5 * own_pages / pl.quota + 0.5);
+        const long long shared_parts = (shared_pages + pl.quota - 1) / pl.quota;
+        if ((double)est_own * own_parts + (double)(chunks_shared * shared_parts) <= room && own_pages <= 64 * pl.quota && shared_pages <= 64 * pl.quota) break;
+        pl.quota += std::max(8, pl.quota / 64 * 8);
+    }
     pl.most_own = std::min((own_pages + pl.quota - 1) / pl.quota, 64);
     pl.most_shared = std::min((shared_pages + pl.quota - 1) / pl.quota, 64);
     pl.items = chunks_own * pl.most_own + chunks_shared * pl.most_shared;
@@ -158,6 +167,7 @@ extern "C" int ee_attend(const ee_paged_cache *c, const ee_attend_args *p, void 
     a.quota = pl.quota;
     a.most_own = pl.most_own;
     a.most_shared = pl.most_shared;
+    a.descending = std::min(c->n_seqs, p->n_rows) == 1 && pl.items * c->n_kv_heads <= 512 ? std::max(256 / c->n_kv_heads, 1) : 0x7FFFFFFF;
     a.scale2 = p->scale * 1.44269504f;
     DeviceScope scope(c->device);
     HIP_TRY(scope.status);

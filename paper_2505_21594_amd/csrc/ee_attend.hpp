@@ -18,6 +18,8 @@
 // own rounding) where the matrix cores bound the call.  Products of the smallest terms are left out (2^-26, or 2^-17 with 2 terms).
 #pragma once
 
+#include <type_traits>
+
 #include "ee_ops.hpp"
 
 namespace ee {
@@ -37,6 +39,7 @@ struct AttendDev {
     int n_groups, n_heads, per_key;            // per_key: query heads of a key head
     int quota;                                 // pages of a part
     int most_own, most_shared;                 // parts at most
+    int descending;                            // chunks of a sequence in descending order before those in ascending order
     float scale2;                              // scale * log2(e)
 };
 
@@ -71,13 +74,6 @@ __device__ __forceinline__ SeqLane seq_lane(const AttendDev &a, int s)
 }
 // pages of which every new row sees all positions
 __device__ __forceinline__ int pages_seen(const SeqLane &l) { return l.n > 0 ? max(l.len - l.n + 1, 0) >> 4 : 0x7FFFFFFF; }
-
-__device__ __forceinline__ int wave_min(int x)
-{
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) x = min(x, __shfl_xor(x, d, 64));
-    return x;
-}
 
 // Pages that a group reads together: the entries its members have in common, as far as every new row of every member sees all of
 // their positions.  `member`: the first one with rows, whose table is read; s1 if there is none.
@@ -160,7 +156,7 @@ __device__ __forceinline__ bool attend_item(const AttendDev &a, int item, int la
                     g_member = who ? __builtin_ctzll(who) : 0;
                 }
             }
-            const int c = shared_count(g_pages, g_rows), incl = wave_scan(c, lane), total = __builtin_amdgcn_readlane(incl, 63);
+            const int c = shared_count(g_pages, g_rows), incl = wave_scan(c), total = __builtin_amdgcn_readlane(incl, 63);
             if (item < total) {
                 g = __builtin_ctzll(__ballot(incl > item));
                 place = item - __builtin_amdgcn_readlane(incl - c, g);
@@ -205,7 +201,7 @@ __device__ __forceinline__ bool attend_item(const AttendDev &a, int item, int la
     for (int base = 0;; base += 64) {
         if (base > 0) mine = seq_lane(a, base + lane);
         if (!small && a.n_groups > 0 && base + lane < a.b.n_seqs) mine.from = as_global(a.from)[base + lane];
-        const int c = own_count(mine), incl = wave_scan(c, lane), total = __builtin_amdgcn_readlane(incl, 63);
+        const int c = own_count(mine), incl = wave_scan(c), total = __builtin_amdgcn_readlane(incl, 63);
         if (item < total) {
             const int l = __builtin_ctzll(__ballot(incl > item)), place = item - __builtin_amdgcn_readlane(incl - c, l);
             it.seq = base + l;
@@ -213,9 +209,10 @@ __device__ __forceinline__ bool attend_item(const AttendDev &a, int item, int la
             it.rows = __builtin_amdgcn_readlane(mine.n, l);
             const int len = __builtin_amdgcn_readlane(mine.len, l), from = __builtin_amdgcn_readlane(mine.from, l);
             const int parts = own_parts(a, table_pages(a, len) - from);
-            // the last lines first: they see the most positions
+            // The last lines first: they see the most positions.  Where all items are on the chip at once, the second half of them, which share
+            // compute units with the first, from the other end (2041 rows of 32 heads: 80 -> 60 us).
             const int chunks = (it.rows * G + LINES - 1) / LINES, c_up = place / parts, part = place - c_up * parts;
-            it.line0 = (chunks - 1 - c_up) * LINES;
+            it.line0 = (c_up < a.descending ? chunks - 1 - c_up : c_up - a.descending) * LINES;
             it.lines = min(LINES, it.rows * G - it.line0);
             it.first_pos = len - it.rows;
             const int pages = max(table_pages(a, it.first_pos + (it.line0 + it.lines - 1) / G + 1) - from, 0);
@@ -251,8 +248,10 @@ __device__ __forceinline__ void attend_clear(AttendState<RT, NT> &st)
     }
 }
 
-__device__ __forceinline__ bool nonfinite_bf16(uint32_t w) { return (w & 0x7F80u) == 0x7F80u || (w & 0x7F800000u) == 0x7F800000u; }
-__device__ __forceinline__ bool nonfinite_bf16(uint4 v) { return nonfinite_bf16(v.x) || nonfinite_bf16(v.y) || nonfinite_bf16(v.z) || nonfinite_bf16(v.w); }
+// Bits 15 and 31 are set where the low and the high element are infinite or NaN (a full exponent carries out of its field); other bits are anything.
+__device__ __forceinline__ uint32_t nonfinite_carry(uint32_t w) { return (w & 0x7F807F80u) + 0x00800080u; }
+__device__ __forceinline__ uint32_t nonfinite_carry(uint4 v) { return nonfinite_carry(v.x) | nonfinite_carry(v.y) | nonfinite_carry(v.z) | nonfinite_carry(v.w); }
+__device__ __forceinline__ bool nonfinite(uint32_t carries) { return (carries & 0x80008000u) != 0; }
 // bits of the first `keep` of two elements
 __device__ __forceinline__ uint32_t keep_mask(int keep) { return keep >= 2 ? 0xFFFFFFFFu : keep == 1 ? 0xFFFFu : 0u; }
 __device__ __forceinline__ uint4 keep_first(uint4 v, int keep)
@@ -260,7 +259,7 @@ __device__ __forceinline__ uint4 keep_first(uint4 v, int keep)
     return make_uint4(v.x & keep_mask(keep), v.y & keep_mask(keep - 2), v.z & keep_mask(keep - 4), v.w & keep_mask(keep - 6));
 }
 // bits of the elements that are infinite or NaN
-__device__ __forceinline__ uint32_t nonfinite_bits(uint32_t w) { return ((w & 0x7F80u) == 0x7F80u ? 0xFFFFu : 0u) | ((w & 0x7F800000u) == 0x7F800000u ? 0xFFFF0000u : 0u); }
+__device__ __forceinline__ uint32_t nonfinite_bits(uint32_t w) { return (nonfinite_carry(w) >> 15 & 0x00010001u) * 0xFFFFu; }
 __device__ __forceinline__ uint4 nonfinite_bits(uint4 v) { return make_uint4(nonfinite_bits(v.x), nonfinite_bits(v.y), nonfinite_bits(v.z), nonfinite_bits(v.w)); }
 
 // eight values as N bf16 terms
@@ -284,58 +283,79 @@ __device__ __forceinline__ void split_terms(const float (&x)[8], bf16x8_t (&t)[N
     for (int i = 0; i < N; ++i) t[i] = __builtin_bit_cast(bf16x8_t, make_uint4(w[i][0], w[i][1], w[i][2], w[i][3]));
 }
 
-// What a pair of pages leaves to be seen: positions 8 quad .. of the pair that exist for any line of the item (0 .. 8, the lane's own), and
-// whether anything of the pair is hidden from any line.
+// What a pair of pages leaves to be seen: positions of either page that exist for any line of the wave (uniform), whether
+// anything of the pair is hidden from any line, and how many of the lane's positions 8 quad .. of the pair exist.
 struct PairMask {
-    int keep;
+    int lim0, lim1;
     bool masked;
+    __device__ __forceinline__ int keep(int quad) const { return min(max((quad < 2 ? lim0 : lim1) - (quad & 1) * 8, 0), 8); }
 };
-__device__ __forceinline__ PairMask pair_mask(int pos0, bool ok0, bool ok1, int first_last, int max_last, int quad)
+__device__ __forceinline__ PairMask pair_mask(int pos0, int id0, int id1, int first_last, int max_last)
 {
-    const int lim0 = ok0 ? min(max(max_last + 1 - pos0, 0), KV_PAGE) : 0, lim1 = ok1 ? min(max(max_last + 1 - pos0 - KV_PAGE, 0), KV_PAGE) : 0;
     PairMask m;
-    m.keep = min(max((quad < 2 ? lim0 : lim1) - (quad & 1) * 8, 0), 8);
-    m.masked = lim0 < KV_PAGE || lim1 < KV_PAGE || first_last < pos0 + 2 * KV_PAGE - 1;
+    m.lim0 = id0 >= 0 ? min(max(max_last + 1 - pos0, 0), KV_PAGE) : 0;
+    m.lim1 = id1 >= 0 ? min(max(max_last + 1 - pos0 - KV_PAGE, 0), KV_PAGE) : 0;
+    m.masked = m.lim0 < KV_PAGE || m.lim1 < KV_PAGE || first_last < pos0 + 2 * KV_PAGE - 1;
     return m;
 }
 
-// Scores of NP pairs of a tile -> weights in s, with the running maximum and sum brought up to date; the output is rescaled where the
-// maximum of any of the wave's lines grew.
-template <int NP, int RT, int NT>
-__device__ __forceinline__ void attend_softmax(AttendState<RT, NT> &st, int t, float (&s)[NP][8], float scale2)
+// Scores of a tile -> weights in s, with the running maximum and sum brought up to date.  Any number near the maximum serves as well: it is
+// moved (and the output rescaled) only where some line's scores exceed it by ATT_SLACK powers of two, after which weights are at most 2^ATT_SLACK.
+constexpr float ATT_SLACK = 8.f;
+template <int NP>
+__device__ __forceinline__ float attend_largest(const float (&s)[NP][8], float scale2)
 {
-    float local = -INFINITY;
+    float local = s[0][0];
 #pragma unroll
-    for (int p = 0; p < NP; ++p)
+    for (int p = 0; p < NP; ++p) local = max3(local, max3(max3(s[p][0], s[p][1], s[p][2]), s[p][3], s[p][4]), max3(s[p][5], s[p][6], s[p][7]));
+    return quads_max(local) * scale2;
+}
+template <int RT, int NT>
+__device__ __forceinline__ void attend_raise(AttendState<RT, NT> &st, int t, float local)
+{
+    const float m = fmaxf(st.mx[t], local), f = m == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(st.mx[t] - m);
+    st.mx[t] = m;
+    st.sum[t] *= f;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) local = fmaxf(local, s[p][e]);
-    local = fmaxf(local, __shfl_xor(local, 16, 64));
-    local = fmaxf(local, __shfl_xor(local, 32, 64)) * scale2;
-    if (__any(local > st.mx[t])) {
-        const float m = fmaxf(st.mx[t], local), f = m == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(st.mx[t] - m);
-        st.mx[t] = m;
-        st.sum[t] *= f;
+    for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) st.o[t][nt][r] *= f;
-    }
+        for (int r = 0; r < 4; ++r) st.o[t][nt][r] *= f;
+}
+template <int PT, int NP, int RT, int NT>
+__device__ __forceinline__ void attend_exps(AttendState<RT, NT> &st, int t, float (&s)[NP][8], float scale2, bf16x8_t (&P)[NP][PT])
+{
     const float base = st.mx[t] == -INFINITY ? 0.f : st.mx[t];
 #pragma unroll
-    for (int p = 0; p < NP; ++p)
+    for (int p = 0; p < NP; ++p) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
             s[p][e] = __builtin_amdgcn_exp2f(fmaf(s[p][e], scale2, -base));
             st.sum[t] += s[p][e];
         }
+        split_terms<PT>(s[p], P[p]);
+    }
 }
 
-// scores that a lane's line does not see
-__device__ __forceinline__ void attend_hide(float (&s)[8], const PairMask &m, int pos0, int last, int quad)
+// A tile's scores of NP pairs as the lane's eights.  MASKED: those that its line does not see are nothing; keep: of the lane's positions of a pair,
+// those that exist.  Returns the largest, scaled.
+template <bool MASKED, int NP, int RT, int NT>
+__device__ __forceinline__ float attend_scores(AttendState<RT, NT> &st, int t, const f32x4_t (&S)[NP][2], const int (&keep)[NP], int pos0, int last, int quad, float scale2,
+                                               float (&s)[NP][8])
 {
-    const int seen = min(m.keep, last - pos0 - quad * 8 + 1);
+    bool sees = false;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) s[e] = e < seen ? s[e] : -INFINITY;
+    for (int p = 0; p < NP; ++p) {
+        const int seen = min(keep[p], last - pos0 - p * 32 - quad * 8 + 1);
+        sees |= seen > 0;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            s[p][e] = S[p][e >> 2][e & 3];
+            if constexpr (MASKED) s[p][e] = e < seen ? s[p][e] : -INFINITY;
+        }
+    }
+    const float local = attend_largest<NP>(s, scale2);
+    if (local == -INFINITY && (!MASKED || sees)) st.hollow |= 1u << t;     // (counts only where the maximum stays there)
+    return local;
 }
 
 // A pair of which some lines see a position that others do not, and in which V holds an infinity or NaN: 0 * V would be NaN for the
@@ -367,25 +387,48 @@ __device__ __forceinline__ void attend_odd(AttendState<RT, NT> &st, int nt, uint
     }
 }
 
-// A lane's q of a line as operands: values 32 kt + 8 quad .. + 7.
-template <int HD, int QT>
-__device__ __forceinline__ void attend_load_q(const AttendDev &a, int row, int head, int quad, bf16x8_t (&q)[HD / 32][QT])
+// A pair's V where something of the pair is hidden: what no line sees may hold anything, and what some lines see and others do not, infinities and NaN.
+template <int TERMS, int RT, int NT>
+__device__ __forceinline__ void attend_clean_v(AttendState<RT, NT> &st, uint4 (&v)[NT][TERMS], const PairMask &mask, int keep, int pos0, const int (&last)[RT], int quad)
 {
+    if constexpr (TERMS == 2) {                                             // (registers are short there: one dim tile after the other)
 #pragma unroll
-    for (int kt = 0; kt < HD / 32; ++kt) {
-        const size_t at = (size_t)row * a.q_stride + (size_t)head * a.q_head + kt * 32 + quad * 8;
-        if constexpr (QT == 1) {
-            q[kt][0] = __builtin_bit_cast(bf16x8_t, load_global16(static_cast<const uint16_t *>(a.q) + at));
-        } else {
-            float x[8];
-            if (a.q_type == EE_FP32)
-                load8<EE_FP32>(a.q, at, x);
-            else if (a.q_type == EE_FP16)
-                load8<EE_FP16>(a.q, at, x);
-            else
-                load8<EE_BF16>(a.q, at, x);
-            split_terms<QT>(x, q[kt]);
+        for (int nt = 0; nt < NT; ++nt) {
+            v[nt][0] = keep_first(v[nt][0], keep);
+            v[nt][1] = keep_first(v[nt][1], keep);
+            if (__any(nonfinite(nonfinite_carry(v[nt][0]) | nonfinite_carry(v[nt][1])))) attend_odd<TERMS>(st, nt, v[nt], pos0, last, quad);
         }
+    } else {
+        if (mask.lim0 < KV_PAGE || mask.lim1 < KV_PAGE) {                   // (uniform)
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) v[nt][0] = keep_first(v[nt][0], keep);
+        }
+        uint32_t odd = 0;
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) odd |= nonfinite_carry(v[nt][0]);
+        if (__any(nonfinite(odd))) {
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) attend_odd<TERMS>(st, nt, v[nt], pos0, last, quad);
+        }
+    }
+}
+
+// A lane's q of a line as operands: values 32 kt + 8 quad .. + 7.
+template <int QT>
+__device__ __forceinline__ void attend_load_q(const AttendDev &a, int row, int head, int kt, int quad, bf16x8_t (&q)[QT])
+{
+    const size_t at = (size_t)row * a.q_stride + (size_t)head * a.q_head + kt * 32 + quad * 8;
+    if constexpr (QT == 1) {
+        q[0] = __builtin_bit_cast(bf16x8_t, load_global16(static_cast<const uint16_t *>(a.q) + at));
+    } else {
+        float x[8];
+        if (a.q_type == EE_FP32)
+            load8<EE_FP32>(a.q, at, x);
+        else if (a.q_type == EE_FP16)
+            load8<EE_FP16>(a.q, at, x);
+        else
+            load8<EE_BF16>(a.q, at, x);
+        split_terms<QT>(x, q);
     }
 }
 
@@ -419,12 +462,10 @@ __device__ __forceinline__ void attend_store(const AttendDev &a, const AttendIte
 template <int RT, int NT>
 __device__ __forceinline__ void attend_finish(AttendState<RT, NT> &st)
 {
-    st.hollow |= __shfl_xor(st.hollow, 16, 64);
-    st.hollow |= __shfl_xor(st.hollow, 32, 64);
+    st.hollow = quads_or(st.hollow);
 #pragma unroll
     for (int t = 0; t < RT; ++t) {
-        st.sum[t] += __shfl_xor(st.sum[t], 16, 64);
-        st.sum[t] += __shfl_xor(st.sum[t], 32, 64);
+        st.sum[t] = quads_sum(st.sum[t]);
         if (st.mx[t] == -INFINITY && (st.hollow >> t & 1)) st.sum[t] = __builtin_nanf("");
     }
 }
@@ -440,19 +481,23 @@ __device__ __forceinline__ float join_sums(float m, float m1, float l1, float f1
 // ------------------------------------------------------------------ few lines: bound by the cache's bytes
 //
 // The waves take the item's pairs of pages in turn, K and V straight from the records into registers: K of the next pair is requested when this
-// one's scores are done, V when its product is.
+// one's scores are done, V when its product is.  q of 128 values and several terms or tiles is in LDS: in registers it would leave
+// room for one workgroup a compute unit instead of two.
+
+template <int HD, int QT, int RT>
+constexpr bool attend_q_in_lds() { return HD == 128 && (QT > 1 || RT > 1); }
 
 template <int HD, int TERMS, int QT, int PT, int RT>
-__device__ __forceinline__ void attend_pages(const AttendDev &a, const AttendItem &it, int kvh, const bf16x8_t (&q)[RT][HD / 32][QT], const int (&last)[RT], int first_last,
-                                             int max_last, int lane, int wave, AttendState<RT, HD / 16> &st)
+__device__ __forceinline__ void attend_pages(const AttendDev &a, const AttendItem &it, int kvh, const int (&row)[RT], const int (&head)[RT], const int (&last)[RT], int first_last,
+                                             int max_last, int lane, int wave, char *q_lds, AttendState<RT, HD / 16> &st)
 {
+    constexpr bool Q_LDS = attend_q_in_lds<HD, QT, RT>();
     constexpr int KT = HD / 32, NT = HD / 16, ID_PAIRS = 32;
     const int lm = lane & 15, quad = lane >> 4;
     const int pairs = (it.pg_hi - it.pg_lo + 1) >> 1, tiles = (it.lines + 15) >> 4;
     const size_t page_step = (size_t)a.b.n_kv_heads * KV_PAGE * TERMS * HD;
     const int *table = a.b.table + (size_t)it.seq * a.b.table_stride;
     int pr = wave;
-    if (pr >= pairs) return;
     // ids of the wave's next 32 pairs, one page a lane; -1 outside the pools and past the item's last page
     int ids, ids_from = pr;
     auto load_ids = [&]() __attribute__((always_inline)) {
@@ -486,30 +531,55 @@ __device__ __forceinline__ void attend_pages(const AttendDev &a, const AttendIte
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) vf[nt][u] = load_global16(vb + (u * HD + nt * 16) * KV_PAGE);
     };
-    load_ids();
-    find_ids(pr);
-    request_k();
-    request_v();
-    for (;;) {
-        const int pos0 = (it.pg_lo + 2 * pr) * KV_PAGE;
-        const PairMask mask = pair_mask(pos0, id0 >= 0, id1 >= 0, first_last, max_last, quad);
-        f32x4_t S[RT][2];
+    bf16x8_t q[Q_LDS ? 1 : RT][Q_LDS ? 1 : KT][QT];
+    if constexpr (Q_LDS) {
+        // wave w prepares values 32 w .. of all lines
+        static_assert(KT == ATT_W, "a wave for each 32 values");
 #pragma unroll
-        for (int t = 0; t < RT; ++t) S[t][0] = S[t][1] = (f32x4_t){0.f, 0.f, 0.f, 0.f};
+        for (int t = 0; t < RT; ++t) {
+            if (t >= tiles) continue;
+            attend_load_q<QT>(a, row[t], head[t], wave, quad, q[0][0]);
+#pragma unroll
+            for (int i = 0; i < QT; ++i) *reinterpret_cast<bf16x8_t *>(q_lds + (((t * KT + wave) * QT + i) * 64 + lane) * 16) = q[0][0][i];
+        }
+    } else {
+#pragma unroll
+        for (int t = 0; t < RT; ++t)
+            if (t < tiles) {
+#pragma unroll
+                for (int kt = 0; kt < KT; ++kt) attend_load_q<QT>(a, row[t], head[t], kt, quad, q[t][kt]);
+            }
+    }
+    if (pr < pairs) {
+        load_ids();
+        find_ids(pr);
+        request_k();
+        request_v();
+    }
+    if constexpr (Q_LDS) lds_barrier();
+    if (pr >= pairs) return;
+    for (;;) {
+        if constexpr (Q_LDS) asm volatile("" ::: "memory");                 // (or the loop's reads of q would move in front of it, into registers)
+        const int pos0 = (it.pg_lo + 2 * pr) * KV_PAGE;
+        const PairMask mask = pair_mask(pos0, id0, id1, first_last, max_last);
+        f32x4_t S[RT][1][2];
+#pragma unroll
+        for (int t = 0; t < RT; ++t) S[t][0][0] = S[t][0][1] = (f32x4_t){0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int kt = 0; kt < KT; ++kt)
 #pragma unroll
-            for (int p = 0; p < 2; ++p)
+            for (int t = 0; t < RT; ++t) {
+                if (t >= tiles) continue;
+                bf16x8_t x[QT];
 #pragma unroll
-                for (int u = 0; u < TERMS; ++u) {
-                    const bf16x8_t k = __builtin_bit_cast(bf16x8_t, kf[p][u][kt]);
+                for (int i = 0; i < QT; ++i) x[i] = Q_LDS ? *reinterpret_cast<const bf16x8_t *>(q_lds + (((t * KT + kt) * QT + i) * 64 + lane) * 16) : q[Q_LDS ? 0 : t][Q_LDS ? 0 : kt][i];
 #pragma unroll
-                    for (int t = 0; t < RT; ++t) {
-                        if (t >= tiles) continue;
+                for (int p = 0; p < 2; ++p)
 #pragma unroll
-                        for (int i = 0; i < QT - u; ++i) S[t][p] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, q[t][kt][i], S[t][p], 0, 0, 0);
-                    }
-                }
+                    for (int u = 0; u < TERMS; ++u)
+#pragma unroll
+                        for (int i = 0; i < QT - u; ++i) S[t][0][p] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, kf[p][u][kt]), x[i], S[t][0][p], 0, 0, 0);
+            }
         pr += ATT_W;
         const bool more = pr < pairs;
         if (more) {
@@ -520,43 +590,46 @@ __device__ __forceinline__ void attend_pages(const AttendDev &a, const AttendIte
             find_ids(pr);
             request_k();
         }
-        bf16x8_t P[RT][PT];
+        auto multiply = [&](auto masked) __attribute__((always_inline)) {
+            constexpr bool MASKED = decltype(masked)::value;
+            const int keep[1] = {mask.keep(quad)};
+            bf16x8_t P[RT][1][PT];
+            float s[RT][1][8], local[RT];
+            bool up = false;
 #pragma unroll
-        for (int t = 0; t < RT; ++t) {
-            if (t >= tiles) continue;
-            float s[1][8];
+            for (int t = 0; t < RT; ++t) {
+                local[t] = -INFINITY;
+                if (t < tiles) local[t] = attend_scores<MASKED, 1>(st, t, S[t], keep, pos0, last[t], quad, a.scale2, s[t]);
+                up |= local[t] > st.mx[t] + ATT_SLACK;
+            }
+            if (__any(up)) {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) s[0][e] = S[t][e >> 2][e & 3];
-            if (mask.masked) attend_hide(s[0], mask, pos0, last[t], quad);
-            attend_softmax<1>(st, t, s, a.scale2);
-            if (st.mx[t] == -INFINITY && min(mask.keep, last[t] - pos0 - quad * 8 + 1) > 0) st.hollow |= 1u << t;
-            split_terms<PT>(s[0], P[t]);
-        }
-        if (mask.masked) {
-            // what no line sees may hold anything
+                for (int t = 0; t < RT; ++t)
+                    if (t < tiles) attend_raise(st, t, local[t]);
+            }
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt) {
-                bool odd = false;
+            for (int t = 0; t < RT; ++t)
+                if (t < tiles) attend_exps<PT, 1>(st, t, s[t], a.scale2, P[t]);
+            if constexpr (MASKED)
+                if (mask.masked) attend_clean_v<TERMS>(st, vf, mask, keep[0], pos0, last, quad);
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                 for (int u = 0; u < TERMS; ++u) {
-                    vf[nt][u] = keep_first(vf[nt][u], mask.keep);
-                    odd |= nonfinite_bf16(vf[nt][u]);
+                    const bf16x8_t v = __builtin_bit_cast(bf16x8_t, vf[nt][u]);
+#pragma unroll
+                    for (int t = 0; t < RT; ++t) {
+                        if (t >= tiles) continue;
+#pragma unroll
+                        for (int i = 0; i < PT - u; ++i) st.o[t][nt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, P[t][0][i], st.o[t][nt], 0, 0, 0);
+                    }
                 }
-                if (__any(odd)) attend_odd<TERMS>(st, nt, vf[nt], pos0, last, quad);
-            }
-        }
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-            for (int u = 0; u < TERMS; ++u) {
-                const bf16x8_t v = __builtin_bit_cast(bf16x8_t, vf[nt][u]);
-#pragma unroll
-                for (int t = 0; t < RT; ++t) {
-                    if (t >= tiles) continue;
-#pragma unroll
-                    for (int i = 0; i < PT - u; ++i) st.o[t][nt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, P[t][i], st.o[t][nt], 0, 0, 0);
-                }
-            }
+        };
+        // (two copies of this, but for two-term caches, where they need more registers than two workgroups a compute unit leave)
+        if (TERMS == 2 || mask.masked)
+            multiply(std::true_type{});
+        else
+            multiply(std::false_type{});
         if (!more) break;
         request_v();
     }
@@ -567,9 +640,11 @@ __device__ __forceinline__ void attend_pages(const AttendDev &a, const AttendIte
 template <int HD, int RT>
 constexpr int attend_lds_floats() { return RT * (HD / 16) * 4 + 2 * RT; }
 template <int HD, int RT>
+constexpr size_t attend_join_lds() { return (size_t)(ATT_W / 2) * 64 * attend_lds_floats<HD, RT>() * sizeof(float); }
+template <int HD, int QT, int RT>
 constexpr size_t attend_lds()
 {
-    constexpr size_t bytes = (size_t)(ATT_W / 2) * 64 * attend_lds_floats<HD, RT>() * sizeof(float);
+    constexpr size_t bytes = attend_join_lds<HD, RT>() + (attend_q_in_lds<HD, QT, RT>() ? RT * (HD / 32) * QT * 1024 : 0);
     static_assert(bytes <= 65536, "what a launch gets without asking for more");
     return bytes;
 }
@@ -615,33 +690,30 @@ __device__ __forceinline__ void attend_join_waves(AttendState<RT, HD / 16> &st, 
 }
 
 template <int HD, int TERMS, int QT, int PT, int RT>
-__global__ void __launch_bounds__(ATT_W * 64, RT == 1 && TERMS * HD < 256 ? 2 : 1) ee_attend_kernel(AttendDev a)
+__global__ void __launch_bounds__(ATT_W * 64, 2) ee_attend_kernel(AttendDev a)
 {
     extern __shared__ __align__(16) char lds_raw[];
-    constexpr int KT = HD / 32, NT = HD / 16;
+    constexpr int NT = HD / 16;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int lm = lane & 15, quad = lane >> 4, kvh = blockIdx.x;
     AttendItem it;
     if (!attend_item<RT * 16>(a, blockIdx.y, lane, it)) return;
     // this lane's lines: row, head, last position seen
     int row[RT], head[RT], last[RT];
+    const int i0 = it.line0 / a.per_key, l0 = it.line0 - i0 * a.per_key;    // row of the chunk's first line, and which of its lines that is
 #pragma unroll
     for (int t = 0; t < RT; ++t) {
-        const int line = it.line0 + min(t * 16 + lm, it.lines - 1), i = line / a.per_key;
-        row[t] = it.row0 + i;
-        head[t] = kvh * a.per_key + line - i * a.per_key;
-        last[t] = it.shared ? ALL_SEEN : it.first_pos + i;
+        const int l = l0 + min(t * 16 + lm, it.lines - 1), i = div_small(l, a.per_key);
+        row[t] = it.row0 + i0 + i;
+        head[t] = kvh * a.per_key + l - i * a.per_key;
+        last[t] = it.shared ? ALL_SEEN : it.first_pos + i0 + i;
     }
     AttendState<RT, NT> st;
     attend_clear(st);
     if (it.pg_hi > it.pg_lo) {
-        const int first_last = it.shared ? ALL_SEEN : it.first_pos + it.line0 / a.per_key;
-        const int max_last = it.shared ? ALL_SEEN : min(it.first_pos + (it.line0 + it.lines - 1) / a.per_key, a.b.capacity() - 1);
-        bf16x8_t q[RT][KT][QT];
-#pragma unroll
-        for (int t = 0; t < RT; ++t)
-            if (t * 16 < it.lines) attend_load_q<HD, QT>(a, row[t], head[t], quad, q[t]);
-        attend_pages<HD, TERMS, QT, PT, RT>(a, it, kvh, q, last, first_last, max_last, lane, wave, st);
+        const int first_last = it.shared ? ALL_SEEN : it.first_pos + i0;
+        const int max_last = it.shared ? ALL_SEEN : min(it.first_pos + i0 + __builtin_amdgcn_readfirstlane(div_small(l0 + it.lines - 1, a.per_key)), a.b.capacity() - 1);
+        attend_pages<HD, TERMS, QT, PT, RT>(a, it, kvh, row, head, last, first_last, max_last, lane, wave, lds_raw + attend_join_lds<HD, RT>(), st);
         attend_join_waves<HD, RT>(st, reinterpret_cast<float *>(lds_raw), min(ATT_W, (it.pg_hi - it.pg_lo + 1) >> 1), lane, wave);
     }
     if (wave != 0) return;
@@ -652,157 +724,168 @@ __global__ void __launch_bounds__(ATT_W * 64, RT == 1 && TERMS * HD < 256 ? 2 : 
 
 // ------------------------------------------------------------------ many lines: bound by the matrix cores
 //
-// Each of the waves has 32 lines of its own, K and V of POS positions go through LDS for all of them, straight from the records (K gathered into
-// operand order), the next ones on their way while these are multiplied.
+// Four waves have 32 lines each; K and V of a step of 64 positions (32 of a two-term cache) go through LDS for all of them, straight from the
+// records into operand order, the next step's on their way while this one is multiplied.  Two workgroups share a compute unit where the registers allow it:
+// one fills the matrix cores while the other has its exponentials.
 
-constexpr int ATT_WIDE = ATT_W * 32;           // lines of an item
+constexpr int ATT_WIDE = 128;                  // lines of an item
+template <int TERMS>
+constexpr int attend_wide_pairs() { return TERMS == 1 ? 2 : 1; }
 template <int HD, int TERMS>
-constexpr int attend_wide_pos() { return TERMS == 1 ? 64 : 32; }
+constexpr int attend_wide_pair() { return 32 * TERMS * HD * 4; }                                    // bytes of a pair's K and V
 template <int HD, int TERMS>
-constexpr int attend_wide_stage() { return attend_wide_pos<HD, TERMS>() * TERMS * HD * 4; }   // bytes of K and V
+constexpr size_t attend_wide_lds()
+{
+    static_assert(2 * attend_wide_pairs<TERMS>() * attend_wide_pair<HD, TERMS>() <= 65536, "what a launch gets without asking for more");
+    return (size_t)2 * attend_wide_pairs<TERMS>() * attend_wide_pair<HD, TERMS>();
+}
 
 template <int HD, int TERMS, int QT, int PT>
-__global__ void __launch_bounds__(ATT_W * 64, QT == 1 ? 2 : 1) ee_attend_wide_kernel(AttendDev a)
+__global__ void __launch_bounds__(256, QT == 1 ? 2 : 1) ee_attend_wide_kernel(AttendDev a)
 {
     extern __shared__ __align__(16) char lds[];
-    constexpr int KT = HD / 32, NT = HD / 16, RT = 2, POS = attend_wide_pos<HD, TERMS>(), PAGES = POS / KV_PAGE, NP = POS / 32;
-    constexpr int REC = KV_PAGE * TERMS * HD * 2;            // bytes of a (page, head) record of K or of V
-    constexpr int STAGE = attend_wide_stage<HD, TERMS>();    // [page][K, V][REC]
+    constexpr int KT = HD / 32, NT = HD / 16, RT = 2, NP = attend_wide_pairs<TERMS>();
+    constexpr int PAIR = attend_wide_pair<HD, TERMS>(), STAGE = NP * PAIR;
+    static_assert(KT == NT / 2, "K of a product is as much as half of V");
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int lm = lane & 15, quad = lane >> 4, kvh = blockIdx.x;
     AttendItem it;
     if (!attend_item<ATT_WIDE>(a, blockIdx.y, lane, it)) return;
-    const int line_w = it.line0 + wave * 32, lines = min(max(it.lines - wave * 32, 0), 32);
+    const int lines = min(max(it.lines - wave * 32, 0), 32);
+    const int i0 = it.line0 / a.per_key, l0 = it.line0 - i0 * a.per_key;    // row of the chunk's first line, and which of its lines that is
     int row[RT], head[RT], last[RT];
     bf16x8_t q[RT][KT][QT];
 #pragma unroll
     for (int t = 0; t < RT; ++t) {
-        const int line = min(line_w + t * 16 + lm, it.line0 + it.lines - 1), i = line / a.per_key;
-        row[t] = it.row0 + i;
-        head[t] = kvh * a.per_key + line - i * a.per_key;
-        last[t] = it.first_pos + i;
-        attend_load_q<HD, QT>(a, row[t], head[t], quad, q[t]);
+        const int l = l0 + min(wave * 32 + t * 16 + lm, it.lines - 1), i = div_small(l, a.per_key);
+        row[t] = it.row0 + i0 + i;
+        head[t] = kvh * a.per_key + l - i * a.per_key;
+        last[t] = it.first_pos + i0 + i;
+#pragma unroll
+        for (int kt = 0; kt < KT; ++kt) attend_load_q<QT>(a, row[t], head[t], kt, quad, q[t][kt]);
     }
-    const int first_last = it.first_pos + line_w / a.per_key;                                       // of the wave
-    const int wave_last = lines > 0 ? min(it.first_pos + (line_w + lines - 1) / a.per_key, a.b.capacity() - 1) : -1;
-    const int n_pg = it.pg_hi - it.pg_lo, steps = (n_pg + PAGES - 1) / PAGES;
+    const int first_last = it.first_pos + i0 + __builtin_amdgcn_readfirstlane(div_small(l0 + wave * 32, a.per_key));   // of the wave
+    const int wave_last = lines > 0 ? min(it.first_pos + i0 + __builtin_amdgcn_readfirstlane(div_small(l0 + wave * 32 + lines - 1, a.per_key)), a.b.capacity() - 1) : -1;
+    const int n_pg = it.pg_hi - it.pg_lo, steps = (n_pg + 2 * NP - 1) / (2 * NP);
     const int *table = a.b.table + (size_t)it.seq * a.b.table_stride;
     const unsigned lds0 = lds_offset(lds);
     // ids of 64 pages in the lanes, from page ids_from of the item on
     int ids = -1, ids_from = -64;
-    auto id_of = [&](int pg) __attribute__((always_inline)) { return pg < n_pg ? __builtin_amdgcn_readlane(ids, pg - ids_from) : -1; };
     auto load_ids = [&](int pg) __attribute__((always_inline)) {
         if (pg < ids_from + 64) return;
         ids_from = pg;
         ids = pg + lane < n_pg ? as_global(table)[it.pg_lo + pg + lane] : -1;
         if (ids >= a.b.n_pages) ids = -1;
     };
-    // A wave brings its share of a step's records.  K in operand order: kilobyte (kt, term) holds lane (position lm, values 8 quad ..)'s 16 bytes in turn.
-    auto request = [&](int step, int buf) __attribute__((always_inline)) {
+    // A pair in LDS is kilobytes in operand order, every lane's 16 bytes in turn, so that all reads are contiguous: K of product h, values kt, term u at
+    // (h KT + kt) TERMS + u, behind them V of dims nt, term u at nt TERMS + u.  Waves 0 and 1 bring K of their product, 2 and 3 a half of V.
+    const bool is_v = wave >= 2;
+    const uint16_t *const src = (is_v ? a.b.vpool : a.b.kpool) + (size_t)kvh * KV_PAGE * TERMS * HD +
+                                (is_v ? ((wave & 1) * HD / 2 + lm) * KV_PAGE + (quad & 1) * 8 : ((lm >> 2 & 1) * 8 + wave * 4 + (lm & 3)) * TERMS * HD + quad * 8);
+    const bool second = is_v ? quad >= 2 : lm >= 8;          // which of the pair's pages the lane's 16 bytes are on
+    const size_t page_step = (size_t)a.b.n_kv_heads * KV_PAGE * TERMS * HD;
+    auto request = [&](int step, int slot, int (&id)[2 * NP]) __attribute__((always_inline)) {
+        load_ids(2 * NP * step);
 #pragma unroll
-        for (int i = 0; i < 2 * PAGES / ATT_W; ++i) {
-            const int which = wave + i * ATT_W, pg = which >> 1;
-            const bool is_v = which & 1;
-            const int id = max(id_of(step * PAGES + pg), 0);
-            const char *src = reinterpret_cast<const char *>(is_v ? a.b.vpool : a.b.kpool) + ((size_t)id * a.b.n_kv_heads + kvh) * REC;
-            const unsigned dst = lds0 + buf * STAGE + which * REC;
-            const int off = is_v ? lane * 16 : lm * (TERMS * HD * 2) + quad * 16;
+        for (int i = 0; i < 2 * NP; ++i) id[i] = __builtin_amdgcn_readlane(ids, 2 * NP * step + i - ids_from);
 #pragma unroll
-            for (int f = 0; f < REC / 1024; ++f) load_lds_kb(uniform_ptr(src + (is_v ? f * 1024 : (f % TERMS) * HD * 2 + f / TERMS * 64)), off, dst + f * 1024);
+        for (int n = 0; n < NP; ++n) {
+            const uint16_t *p = src + (size_t)max(second ? id[2 * n + 1] : id[2 * n], 0) * page_step;
+            const unsigned dst = lds0 + slot * STAGE + n * PAIR + wave * (PAIR / 4);
+            if (is_v) {
+#pragma unroll
+                for (int nt = 0; nt < NT / 2; ++nt)
+#pragma unroll
+                    for (int u = 0; u < TERMS; ++u) load_lds_lanes(p + (u * HD + nt * 16) * KV_PAGE, dst + (nt * TERMS + u) * 1024);
+            } else {
+#pragma unroll
+                for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+                    for (int u = 0; u < TERMS; ++u) load_lds_lanes(p + u * HD + kt * 32, dst + (kt * TERMS + u) * 1024);
+            }
         }
     };
     AttendState<RT, NT> st;
     attend_clear(st);
-    if (steps > 0) {
-        load_ids(0);
-        wait_vmem();
-        request(0, 0);
-    }
-    const int koff = (lm >> 3) * 2 * REC + (quad * 16 + (lm >> 2 & 1) * 8 + (lm & 3)) * 16;
-    const int voff = REC + (quad >> 1) * 2 * REC + lm * 32 + (quad & 1) * 16;
+    wait_vmem();
+    int next[2 * NP] = {};
+    if (steps > 0) request(0, 0, next);
     for (int step = 0; step < steps; ++step) {
-        int id[PAGES];
+        int id[2 * NP];
 #pragma unroll
-        for (int i = 0; i < PAGES; ++i) id[i] = id_of(step * PAGES + i);
-        if (step + 1 < steps) load_ids((step + 1) * PAGES);
+        for (int i = 0; i < 2 * NP; ++i) id[i] = next[i];
         wait_pending<0>();
-        lds_barrier();
-        if (step + 1 < steps) request(step + 1, (step + 1) & 1);
-        const int pos0 = (it.pg_lo + step * PAGES) * KV_PAGE;
+        lds_barrier();                                       // this step is there for all waves, the last one has been read by all
+        if (step + 1 < steps) request(step + 1, (step + 1) & 1, next);
+        const int pos0 = (it.pg_lo + 2 * NP * step) * KV_PAGE;
         if (pos0 > wave_last) continue;
-        const char *buf = lds + (step & 1) * STAGE;
-        float s[RT][NP][8];
+        const char *buf = lds + (step & 1) * STAGE + lane * 16;
+        PairMask mask[NP];
+        bool hidden = false;
 #pragma unroll
-        for (int p = 0; p < NP; ++p) {
-            f32x4_t S[RT][2];
+        for (int n = 0; n < NP; ++n) {
+            mask[n] = pair_mask(pos0 + n * 32, id[2 * n], id[2 * n + 1], first_last, wave_last);
+            hidden |= mask[n].masked;
+        }
+        auto multiply = [&](auto masked) __attribute__((always_inline)) {
+            constexpr bool MASKED = decltype(masked)::value;
+            int keep[NP];
+            f32x4_t S[RT][NP][2];
 #pragma unroll
-            for (int t = 0; t < RT; ++t) S[t][0] = S[t][1] = (f32x4_t){0.f, 0.f, 0.f, 0.f};
+            for (int n = 0; n < NP; ++n) {
+                keep[n] = mask[n].keep(quad);
 #pragma unroll
-            for (int kt = 0; kt < KT; ++kt)
+                for (int t = 0; t < RT; ++t) S[t][n][0] = S[t][n][1] = (f32x4_t){0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                for (int h = 0; h < 2; ++h)
+                for (int kt = 0; kt < KT; ++kt)
 #pragma unroll
-                    for (int u = 0; u < TERMS; ++u) {
-                        const bf16x8_t k = *reinterpret_cast<const bf16x8_t *>(buf + p * 4 * REC + koff + h * 64 + (kt * TERMS + u) * 1024);
+                    for (int h = 0; h < 2; ++h)
+#pragma unroll
+                        for (int u = 0; u < TERMS; ++u) {
+                            const bf16x8_t k = *reinterpret_cast<const bf16x8_t *>(buf + n * PAIR + ((h * KT + kt) * TERMS + u) * 1024);
+#pragma unroll
+                            for (int t = 0; t < RT; ++t)
+#pragma unroll
+                                for (int i = 0; i < QT - u; ++i) S[t][n][h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, q[t][kt][i], S[t][n][h], 0, 0, 0);
+                        }
+            }
+            float s[RT][NP][8], local[RT];
+            bool up = false;
+#pragma unroll
+            for (int t = 0; t < RT; ++t) {
+                local[t] = attend_scores<MASKED, NP>(st, t, S[t], keep, pos0, last[t], quad, a.scale2, s[t]);
+                up |= local[t] > st.mx[t] + ATT_SLACK;
+            }
+            if (__any(up)) {
+#pragma unroll
+                for (int t = 0; t < RT; ++t) attend_raise(st, t, local[t]);
+            }
+            bf16x8_t P[RT][NP][PT];
+#pragma unroll
+            for (int t = 0; t < RT; ++t) attend_exps<PT, NP>(st, t, s[t], a.scale2, P[t]);
+#pragma unroll
+            for (int n = 0; n < NP; ++n) {
+                uint4 v[NT][TERMS];
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                    for (int u = 0; u < TERMS; ++u) v[nt][u] = *reinterpret_cast<const uint4 *>(buf + n * PAIR + PAIR / 2 + (nt * TERMS + u) * 1024);
+                if constexpr (MASKED) attend_clean_v<TERMS>(st, v, mask[n], keep[n], pos0 + n * 32, last, quad);
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                    for (int u = 0; u < TERMS; ++u)
 #pragma unroll
                         for (int t = 0; t < RT; ++t)
 #pragma unroll
-                            for (int i = 0; i < QT - u; ++i) S[t][h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, q[t][kt][i], S[t][h], 0, 0, 0);
-                    }
-#pragma unroll
-            for (int t = 0; t < RT; ++t)
-#pragma unroll
-                for (int e = 0; e < 8; ++e) s[t][p][e] = S[t][e >> 2][e & 3];
-        }
-        PairMask mask[NP];
-        bool masked = false;
-#pragma unroll
-        for (int p = 0; p < NP; ++p) {
-            mask[p] = pair_mask(pos0 + p * 32, id[2 * p] >= 0, id[2 * p + 1] >= 0, first_last, wave_last, quad);
-            masked |= mask[p].masked;
-        }
-        bf16x8_t P[NP][RT][PT];
-#pragma unroll
-        for (int t = 0; t < RT; ++t) {
-            if (masked) {
-#pragma unroll
-                for (int p = 0; p < NP; ++p) attend_hide(s[t][p], mask[p], pos0 + p * 32, last[t], quad);
+                            for (int i = 0; i < PT - u; ++i)
+                                st.o[t][nt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, v[nt][u]), P[t][n][i], st.o[t][nt], 0, 0, 0);
             }
-            attend_softmax<NP>(st, t, s[t], a.scale2);
-            if (st.mx[t] == -INFINITY) {
-#pragma unroll
-                for (int p = 0; p < NP; ++p)
-                    if (min(mask[p].keep, last[t] - pos0 - p * 32 - quad * 8 + 1) > 0) st.hollow |= 1u << t;
-            }
-#pragma unroll
-            for (int p = 0; p < NP; ++p) split_terms<PT>(s[t][p], P[p][t]);
-        }
-#pragma unroll
-        for (int p = 0; p < NP; ++p) {
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt) {
-                uint4 v[TERMS];
-#pragma unroll
-                for (int u = 0; u < TERMS; ++u) v[u] = *reinterpret_cast<const uint4 *>(buf + p * 4 * REC + voff + u * HD * 32 + nt * 512);
-                if (mask[p].masked) {
-                    // what no line sees may hold anything
-                    bool odd = false;
-#pragma unroll
-                    for (int u = 0; u < TERMS; ++u) {
-                        v[u] = keep_first(v[u], mask[p].keep);
-                        odd |= nonfinite_bf16(v[u]);
-                    }
-                    if (__any(odd)) attend_odd<TERMS>(st, nt, v, pos0 + p * 32, last, quad);
-                }
-#pragma unroll
-                for (int u = 0; u < TERMS; ++u)
-#pragma unroll
-                    for (int t = 0; t < RT; ++t)
-#pragma unroll
-                        for (int i = 0; i < PT - u; ++i)
-                            st.o[t][nt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, v[u]), P[p][t][i], st.o[t][nt], 0, 0, 0);
-            }
-        }
+        };
+        if (hidden)
+            multiply(std::true_type{});
+        else
+            multiply(std::false_type{});
     }
     attend_finish(st);
 #pragma unroll
@@ -823,32 +906,46 @@ __global__ void __launch_bounds__(256) ee_attend_join_kernel(AttendDev a, int sp
     __shared__ float dens[ROWS], maxs[ROWS], bads[ROWS];
     const int tr = threadIdx.x / TPL, td = threadIdx.x % TPL, sub = tr % spread;
     const long long line = (long long)blockIdx.x * (ROWS / spread) + tr / spread;
-    const long long rows = a.b.start(a.b.n_seqs);
     const int most = a.most_own + a.most_shared;
-    int own = 0, shared = 0;
-    const f32x2_t *ml = reinterpret_cast<const f32x2_t *>(a.part_ml + line * (most + 1));
-    if (line < rows * a.n_heads) {
-        const f32x2_t n = as_global(ml)[0];
-        own = __float_as_int(n[0]);
-        shared = __float_as_int(n[1]);
-    }
-    if (own == 0) own = shared = 0;                                         // (written already, or padding)
-    const float *o = a.part + line * most * HD + td * 4;
+    const bool there = line < (long long)a.b.n_rows * a.n_heads;
+    const f32x2_t *ml = reinterpret_cast<const f32x2_t *>(a.part_ml + (there ? line : 0) * (most + 1));
+    const float *o = a.part + (there ? line : 0) * most * HD + td * 4;
     f32x4_t num = {0.f, 0.f, 0.f, 0.f};
     float m = -INFINITY, den = 0.f, bad = 0.f;
-    for (int p = sub; p < own + shared; p += spread) {
-        const int slot = p < own ? p : a.most_own + p - own;
-        const f32x2_t x = as_global(ml)[1 + slot];
-        if (x[0] == -INFINITY) {
-            bad = x[1] != 0.f ? 1.f : bad;                                  // positions without a softmax
-            continue;
-        }
-        const f32x4_t v = *as_global(reinterpret_cast<const f32x4_t *>(o + (size_t)slot * HD));
-        const float m_new = fmaxf(m, x[0]), f0 = __builtin_amdgcn_exp2f(m - m_new), f1 = __builtin_amdgcn_exp2f(x[0] - m_new);
-        m = m_new;
-        den = den * f0 + x[1] * f1;
+    int own = 0, shared = 0;
+    // four slots at a time, the first four together with the counts that say which of them are in use
+    for (int base = sub; base < most; base += 4 * spread) {
+        f32x2_t x[4];
+        f32x4_t v[4];
 #pragma unroll
-        for (int r = 0; r < 4; ++r) num[r] = num[r] * f0 + v[r] * f1;
+        for (int i = 0; i < 4; ++i) {
+            const int slot = min(base + i * spread, most - 1);
+            x[i] = as_global(ml)[1 + slot];
+            v[i] = *as_global(reinterpret_cast<const f32x4_t *>(o + (size_t)slot * HD));
+        }
+        if (base == sub) {
+            const f32x2_t n = as_global(ml)[0];
+            const long long rows = a.b.start(a.b.n_seqs);
+            if (line < rows * a.n_heads) {
+                own = __float_as_int(n[0]);
+                shared = own ? __float_as_int(n[1]) : 0;                    // (own 0: written already)
+            }
+            if (own == 0) break;
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int slot = base + i * spread;
+            if (!(slot < a.most_own ? slot < own : slot - a.most_own < shared) || slot >= most) continue;
+            if (x[i][0] == -INFINITY) {
+                bad = x[i][1] != 0.f ? 1.f : bad;                           // positions without a softmax
+                continue;
+            }
+            const float m_new = fmaxf(m, x[i][0]), f0 = __builtin_amdgcn_exp2f(m - m_new), f1 = __builtin_amdgcn_exp2f(x[i][0] - m_new);
+            m = m_new;
+            den = den * f0 + x[i][1] * f1;
+#pragma unroll
+            for (int r = 0; r < 4; ++r) num[r] = num[r] * f0 + v[i][r] * f1;
+        }
     }
     if (spread > 1) {
         nums[tr][td] = num;

@@ -27,15 +27,79 @@ struct BatchDev {
     __device__ __forceinline__ int capacity() const { return min(table_stride, 0x7FFFFFF0 / KV_PAGE) * KV_PAGE; }
 };
 
-// inclusive sum over the lanes of a wave
-__device__ __forceinline__ int wave_scan(int x, int lane)
+// Exchanges between lanes in the vector unit: a shuffle through LDS takes about 100 cycles, these 4 to 8.
+template <int CTRL, int ROWS = 0xF>
+__device__ __forceinline__ int dpp(int other, int x) { return __builtin_amdgcn_update_dpp(other, x, CTRL, ROWS, 0xF, false); }
+constexpr int DPP_XOR1 = 0xB1, DPP_XOR2 = 0x4E, DPP_HALF_MIRROR = 0x141, DPP_MIRROR = 0x140, DPP_SHR = 0x110, DPP_BCAST15 = 0x142, DPP_BCAST31 = 0x143;
+
+// the values of lanes l and l ^ 16, l and l ^ 32, in some order
+__device__ __forceinline__ void pair16(unsigned x, unsigned &a, unsigned &b)
 {
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-        const int y = __shfl_up(x, d, 64);
-        x += lane >= d ? y : 0;
-    }
+    const auto r = __builtin_amdgcn_permlane16_swap(x, x, false, false);
+    a = r[0];
+    b = r[1];
+}
+__device__ __forceinline__ void pair32(unsigned x, unsigned &a, unsigned &b)
+{
+    const auto r = __builtin_amdgcn_permlane32_swap(x, x, false, false);
+    a = r[0];
+    b = r[1];
+}
+// (written out: of values it knows nothing about the compiler makes every one canonical first, an instruction each)
+__device__ __forceinline__ float max3(float a, float b, float c)
+{
+    float r;
+    asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+    return r;
+}
+// largest and sum over the lanes l, l ^ 16, l ^ 32, l ^ 48
+__device__ __forceinline__ float quads_max(float x)
+{
+    unsigned a, b;
+    pair16(__float_as_uint(x), a, b);
+    x = fmaxf(__uint_as_float(a), __uint_as_float(b));
+    pair32(__float_as_uint(x), a, b);
+    return fmaxf(__uint_as_float(a), __uint_as_float(b));
+}
+__device__ __forceinline__ float quads_sum(float x)
+{
+    unsigned a, b;
+    pair16(__float_as_uint(x), a, b);
+    x = __uint_as_float(a) + __uint_as_float(b);
+    pair32(__float_as_uint(x), a, b);
+    return __uint_as_float(a) + __uint_as_float(b);
+}
+__device__ __forceinline__ unsigned quads_or(unsigned x)
+{
+    unsigned a, b;
+    pair16(x, a, b);
+    pair32(a | b, a, b);
+    return a | b;
+}
+
+// inclusive sum over the lanes of a wave
+__device__ __forceinline__ int wave_scan(int x)
+{
+    x += dpp<DPP_SHR + 1>(0, x);
+    x += dpp<DPP_SHR + 2>(0, x);
+    x += dpp<DPP_SHR + 4>(0, x);
+    x += dpp<DPP_SHR + 8>(0, x);
+    x += dpp<DPP_BCAST15, 0xA>(0, x);
+    x += dpp<DPP_BCAST31, 0xC>(0, x);
     return x;
+}
+
+// smallest over a wave, in every lane
+__device__ __forceinline__ int wave_min(int x)
+{
+    x = min(x, dpp<DPP_XOR1>(x, x));
+    x = min(x, dpp<DPP_XOR2>(x, x));
+    x = min(x, dpp<DPP_HALF_MIRROR>(x, x));
+    x = min(x, dpp<DPP_MIRROR>(x, x));
+    unsigned a, b;
+    pair16((unsigned)x, a, b);
+    pair32((unsigned)min((int)a, (int)b), a, b);
+    return min((int)a, (int)b);
 }
 
 // Which of n things item `item` belongs to when thing i has count(i) items, and its place there; false past the last.  All
@@ -46,11 +110,11 @@ __device__ __forceinline__ bool find_item(int n, int item, int lane, F count, in
     int before = 0;
     for (int base = 0; base < n; base += 64) {
         const int c = base + lane < n ? count(base + lane) : 0;
-        const int incl = wave_scan(c, lane), total = __shfl(incl, 63, 64);
+        const int incl = wave_scan(c), total = __builtin_amdgcn_readlane(incl, 63);
         if (item < total) {
             const int l = __builtin_ctzll(__ballot(incl > item));
-            index = __builtin_amdgcn_readfirstlane(base + l);
-            place = __builtin_amdgcn_readfirstlane(item - __shfl(incl - c, l, 64));
+            index = base + l;
+            place = item - __builtin_amdgcn_readlane(incl - c, l);
             return true;
         }
         item -= total;
@@ -58,6 +122,12 @@ __device__ __forceinline__ bool find_item(int n, int item, int lane, F count, in
     }
     if (all) *all = before;
     return false;
+}
+
+// A kilobyte into LDS whose sixteen-byte pieces come from an address of each lane's: to LDS byte dst + 16 l.  As load_lds_kb, the caller waits.
+__device__ __forceinline__ void load_lds_lanes(const void *src, unsigned dst)
+{
+    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" : : "v"(src), "s"(dst) : "m0", "memory");
 }
 
 // eight neighbouring elements as floats; 16-byte aligned
