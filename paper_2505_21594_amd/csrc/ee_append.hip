@@ -2,18 +2,18 @@
 //
 // Bound by bytes (a row's queries, keys and values once in, once out) where there are many rows, by the chain of
 // dependent loads (row -> sequence -> page -> data) where there are few.
-// A block is up to 16 new rows of one sequence that lie on one page.  Its work is dealt to waves in units: APP_HEADS heads of queries,
-// of keys, or of values.  Queries and keys: a row's head is HD / 16 lanes, each with eight neighbouring elements of either half, so that the partners of
-// a rotation (x_j and x_{j + HD/2}, or neighbours) are in one lane, every access is 16 bytes wide, and a row's cosines and sines are
-// fetched once for a unit's heads.  Values: the cache holds them transposed ([dim][position]), so a lane takes two dims of all 16 rows and
-// writes whole 32-byte runs of positions; pages that the new rows cover only partly are written position by position, so that the
-// others stay as they are.
+// A block is up to 16 new rows of one sequence that lie on one page.  Its work is dealt to waves in units: a head of queries or keys of 64 / (HD / 16) rows, or a
+// head of values (two of 64).  Queries and keys: a row's head is HD / 16 lanes, each with eight neighbouring elements of either half, so that the partners of
+// a rotation (x_j and x_{j + HD/2}, or neighbours) are in one lane and every access is 16 bytes wide.  Values: the cache holds them transposed ([dim][position]), so a lane takes two dims of all 16 rows, and the
+// wave turns its 64-byte pieces into whole kilobytes through LDS; pages that the new rows cover only partly are written position by position,
+// so that the others stay as they are.
+// (Units of four heads, which fetch a row's cosines and sines once for all: eight rounds of five rows 7.7 -> 10.1 us, 2041 rows of 32 heads 26.2 -> 28.8.)
 #include "ee_ops.hpp"
 
 namespace ee {
 
-constexpr int APP_HEADS = 4;      // heads of a unit
 constexpr int APP_WAVES = 4;
+constexpr int append_value_heads(int hd) { return 128 / hd; }   // heads of a unit of values: a lane has two dims
 
 struct AppendDev {
     BatchDev b;
@@ -63,99 +63,87 @@ __device__ __forceinline__ bool append_block(const BatchDev &b, int block, int l
 }
 
 template <int HD, int TERMS, int IN>
-__device__ __forceinline__ void append_normed(const AppendDev &a, const AppendBlock &at, int page, bool is_k, int h0, int lane)
+__device__ __forceinline__ void append_normed(const AppendDev &a, const AppendBlock &at, int page, bool is_k, int h, int it, int lane)
 {
     constexpr int LANES = HD / 16, ROWS = 64 / LANES;
     const int sub = lane % LANES, i0 = sub * 8;
     const void *src = is_k ? a.k : a.q;
     const long long stride = is_k ? a.k_stride : a.q_stride, head = is_k ? a.k_head : a.q_head;
     const float *gain = is_k ? a.k_gain : a.q_gain;
-    const int nh = min(APP_HEADS, (is_k ? a.b.n_kv_heads : a.n_heads) - h0);
+    if (at.hi <= it || at.lo >= it + ROWS) return;
     float g[2][8];
     if (gain) {
         load8<EE_FP32>(gain, i0, g[0]);
         load8<EE_FP32>(gain, HD / 2 + i0, g[1]);
     }
-    for (int it = 0; it < KV_PAGE; it += ROWS) {
-        if (at.hi <= it || at.lo >= it + ROWS) continue;
-        const int slot = it + lane / LANES;
-        const bool row_ok = slot >= at.lo && slot < at.hi;
-        const bool placed = row_ok && slot < at.usable;
-        const int row = at.row0 + (row_ok ? slot : max(at.lo, it));          // (lanes without a row repeat one)
-        float x[APP_HEADS][2][8];
+    const int slot = it + lane / LANES;
+    const bool row_ok = slot >= at.lo && slot < at.hi;
+    const bool placed = row_ok && slot < at.usable;
+    const int row = at.row0 + (row_ok ? slot : max(at.lo, it));          // (lanes without a row repeat one)
+    float y[2][8];
+    const size_t from = (size_t)row * stride + (size_t)h * head + i0;
+    load8<IN>(src, from, y[0]);
+    load8<IN>(src, from + HD / 2, y[1]);
+    // cosines and sines: of pairs (j, j + HD/2) the lane has j = i0 .. i0 + 7; of neighbours i0 / 2 .. + 3 and HD / 4 more
+    float cs[2][8];
+    if (a.rope) {
+        const int pos = placed ? (at.page << 4) + slot : 0;
+        const float *t = a.rope + (size_t)pos * HD;
+        const int c0 = a.rope_pairs ? i0 : 2 * i0, c1 = a.rope_pairs ? HD / 2 + i0 : 2 * i0 + 8;
+        load8<EE_FP32>(t, c0, cs[0]);
+        load8<EE_FP32>(t, c1, cs[1]);
+    }
+    if (gain) {
+        float ss = 0.f;
 #pragma unroll
-        for (int h = 0; h < APP_HEADS; ++h) {
-            const size_t from = (size_t)row * stride + (size_t)(h0 + min(h, nh - 1)) * head + i0;
-            load8<IN>(src, from, x[h][0]);
-            load8<IN>(src, from + HD / 2, x[h][1]);
+        for (int e = 0; e < 8; ++e) ss += y[0][e] * y[0][e] + y[1][e] * y[1][e];
+#pragma unroll
+        for (int d = 1; d < LANES; d <<= 1) ss += __shfl_xor(ss, d, 64);
+        const float r = 1.0f / sqrtf(ss * (1.0f / HD) + a.eps);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            y[0][e] = y[0][e] * r * g[0][e];
+            y[1][e] = y[1][e] * r * g[1][e];
         }
-        // cosines and sines: of pairs (j, j + HD/2) the lane has j = i0 .. i0 + 7; of neighbours i0 / 2 .. + 3 and HD / 4 more
-        float cs[2][8];
-        if (a.rope) {
-            const int pos = placed ? (at.page << 4) + slot : 0;
-            const float *t = a.rope + (size_t)pos * HD;
-            const int c0 = a.rope_pairs ? i0 : 2 * i0, c1 = a.rope_pairs ? HD / 2 + i0 : 2 * i0 + 8;
-            load8<EE_FP32>(t, c0, cs[0]);
-            load8<EE_FP32>(t, c1, cs[1]);
+    }
+    if (a.rope) {
+        if (a.rope_pairs) {
+#pragma unroll
+            for (int p = 0; p < 2; ++p)
+#pragma unroll
+                for (int e = 0; e < 8; e += 2) {
+                    const float u = y[p][e], w = y[p][e + 1], c = cs[p][e], s = cs[p][e + 1];
+                    y[p][e] = u * c - w * s;
+                    y[p][e + 1] = w * c + u * s;
+                }
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const float u = y[0][e], w = y[1][e], c = cs[e >> 2][2 * (e & 3)], s = cs[e >> 2][2 * (e & 3) + 1];
+                y[0][e] = u * c - w * s;
+                y[1][e] = w * c + u * s;
+            }
         }
+    }
+    if (!is_k) {
+        if (row_ok) {
+            const size_t to = (size_t)row * a.o_stride + (size_t)h * a.o_head + i0;
 #pragma unroll
-        for (int h = 0; h < APP_HEADS; ++h) {
-            if (h >= nh) break;
-            float (&y)[2][8] = x[h];
-            if (gain) {
-                float ss = 0.f;
+            for (int p = 0; p < 2; ++p) {
 #pragma unroll
-                for (int e = 0; e < 8; ++e) ss += y[0][e] * y[0][e] + y[1][e] * y[1][e];
-#pragma unroll
-                for (int d = 1; d < LANES; d <<= 1) ss += __shfl_xor(ss, d, 64);
-                const float r = 1.0f / sqrtf(ss * (1.0f / HD) + a.eps);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    y[0][e] = y[0][e] * r * g[0][e];
-                    y[1][e] = y[1][e] * r * g[1][e];
-                }
+                for (int e = 0; e < 8; ++e) y[p][e] = placed ? y[p][e] : 0.f;
+                store8(a.out_type, a.q_out, to + p * (HD / 2), y[p]);
             }
-            if (a.rope) {
-                if (a.rope_pairs) {
+        }
+    } else if (placed && page >= 0) {
+        uint16_t *rec = a.b.kpool + ((((size_t)page * a.b.n_kv_heads + h) * KV_PAGE + slot) * TERMS) * HD + i0;
 #pragma unroll
-                    for (int p = 0; p < 2; ++p)
+        for (int p = 0; p < 2; ++p) {
+            uint32_t hi[4], lo[4];
 #pragma unroll
-                        for (int e = 0; e < 8; e += 2) {
-                            const float u = y[p][e], w = y[p][e + 1], c = cs[p][e], s = cs[p][e + 1];
-                            y[p][e] = u * c - w * s;
-                            y[p][e + 1] = w * c + u * s;
-                        }
-                } else {
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        const float u = y[0][e], w = y[1][e], c = cs[e >> 2][2 * (e & 3)], s = cs[e >> 2][2 * (e & 3) + 1];
-                        y[0][e] = u * c - w * s;
-                        y[1][e] = w * c + u * s;
-                    }
-                }
-            }
-            if (!is_k) {
-                if (row_ok) {
-                    const size_t to = (size_t)row * a.o_stride + (size_t)(h0 + h) * a.o_head + i0;
-#pragma unroll
-                    for (int p = 0; p < 2; ++p)
-#pragma unroll
-                        for (int e = 0; e < 8; e += 4) {
-                            const bool z = !placed;
-                            store4(a.out_type, a.q_out, to + p * (HD / 2) + e, z ? 0.f : y[p][e], z ? 0.f : y[p][e + 1], z ? 0.f : y[p][e + 2], z ? 0.f : y[p][e + 3]);
-                        }
-                }
-            } else if (placed && page >= 0) {
-                uint16_t *rec = a.b.kpool + ((((size_t)page * a.b.n_kv_heads + h0 + h) * KV_PAGE + slot) * TERMS) * HD + i0;
-#pragma unroll
-                for (int p = 0; p < 2; ++p) {
-                    uint32_t hi[4], lo[4];
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) split_bf16(y[p][2 * e], y[p][2 * e + 1], hi[e], lo[e]);
-                    *as_global_mut(reinterpret_cast<u32x4_t *>(rec + p * (HD / 2))) = (u32x4_t){hi[0], hi[1], hi[2], hi[3]};
-                    if constexpr (TERMS == 2) *as_global_mut(reinterpret_cast<u32x4_t *>(rec + HD + p * (HD / 2))) = (u32x4_t){lo[0], lo[1], lo[2], lo[3]};
-                }
-            }
+            for (int e = 0; e < 4; ++e) split_bf16(y[p][2 * e], y[p][2 * e + 1], hi[e], lo[e]);
+            *as_global_mut(reinterpret_cast<u32x4_t *>(rec + p * (HD / 2))) = (u32x4_t){hi[0], hi[1], hi[2], hi[3]};
+            if constexpr (TERMS == 2) *as_global_mut(reinterpret_cast<u32x4_t *>(rec + HD + p * (HD / 2))) = (u32x4_t){lo[0], lo[1], lo[2], lo[3]};
         }
     }
 }
@@ -182,42 +170,59 @@ __device__ __forceinline__ void load2(const void *base, size_t at, float &a, flo
 }
 
 template <int HD, int TERMS, int IN>
-__device__ __forceinline__ void append_values(const AppendDev &a, const AppendBlock &at, int page, int h0, int lane)
+__device__ __forceinline__ void append_values(const AppendDev &a, const AppendBlock &at, int page, int h0, int lane, char *lds)
 {
-    constexpr int LANES = HD / 2, HEADS = 64 / LANES;       // lanes of a head, heads at a time
-    const int d0 = (lane % LANES) * 2;
+    constexpr int LANES = HD / 2;                                           // of a head: two dims each
+    const int d0 = (lane % LANES) * 2, h = h0 + lane / LANES;
     const int lo = at.lo, hi = min(at.hi, at.usable);
     if (page < 0 || lo >= hi) return;
-    const int end = min(h0 + APP_HEADS, a.b.n_kv_heads);
-    for (int hb = h0; hb < end; hb += HEADS) {
-        const int h = hb + lane / LANES;
-        const bool ok = h < end;
-        float x[KV_PAGE][2];
+    float x[KV_PAGE][2];
 #pragma unroll
-        for (int r = 0; r < KV_PAGE; ++r) {
-            const int row = at.row0 + min(max(r, lo), hi - 1);
-            load2<IN>(a.v, (size_t)row * a.v_stride + (size_t)(ok ? h : h0) * a.v_head + d0, x[r][0], x[r][1]);
-        }
-        if (!ok) continue;
-        uint16_t *rec = a.b.vpool + ((size_t)page * a.b.n_kv_heads + h) * (size_t)(TERMS * HD * KV_PAGE) + d0 * KV_PAGE;
+    for (int r = 0; r < KV_PAGE; ++r) {
+        const int row = at.row0 + min(max(r, lo), hi - 1);
+        load2<IN>(a.v, (size_t)row * a.v_stride + (size_t)min(h, a.b.n_kv_heads - 1) * a.v_head + d0, x[r][0], x[r][1]);
+    }
+    uint16_t *const recs = a.b.vpool + ((size_t)page * a.b.n_kv_heads + h0) * (size_t)(TERMS * HD * KV_PAGE);
+    uint32_t w[2][2][KV_PAGE / 2];
 #pragma unroll
-        for (int e = 0; e < 2; ++e) {
-            uint32_t th[KV_PAGE / 2], tl[KV_PAGE / 2];
+    for (int e = 0; e < 2; ++e)
 #pragma unroll
-            for (int r = 0; r < KV_PAGE / 2; ++r) split_bf16(x[2 * r][e], x[2 * r + 1][e], th[r], tl[r]);
+        for (int r = 0; r < KV_PAGE / 2; ++r) split_bf16(x[2 * r][e], x[2 * r + 1][e], w[0][e][r], w[1][e][r]);
 #pragma unroll
-            for (int t = 0; t < TERMS; ++t) {
-                const uint32_t (&w)[KV_PAGE / 2] = t ? tl : th;
-                uint16_t *out = rec + t * HD * KV_PAGE + e * KV_PAGE;
-                if (lo == 0 && hi == KV_PAGE) {
-                    *as_global_mut(reinterpret_cast<u32x4_t *>(out)) = (u32x4_t){w[0], w[1], w[2], w[3]};
-                    *as_global_mut(reinterpret_cast<u32x4_t *>(out + 8)) = (u32x4_t){w[4], w[5], w[6], w[7]};
-                } else {
+    for (int t = 0; t < TERMS; ++t) {
+        if (lo == 0 && hi == KV_PAGE) {
+            // the lane's 64 bytes (two dims of 16 positions) -> the wave's four kilobytes, sixteen bytes a lane and turn
+            u32x4_t *mine = reinterpret_cast<u32x4_t *>(lds) + lane * 4;
 #pragma unroll
-                    for (int r = 0; r < KV_PAGE; ++r)
-                        if (r >= lo && r < hi) as_global_mut(out)[r] = (uint16_t)(w[r >> 1] >> (16 * (r & 1)));
-                }
+            for (int e = 0; e < 2; ++e)
+#pragma unroll
+                for (int k = 0; k < 2; ++k)                                 // (turned by the lane, or all would meet in the same banks)
+                    mine[(e * 2 + k + (lane >> 1)) & 3] = (u32x4_t){w[t][e][4 * k], w[t][e][4 * k + 1], w[t][e][4 * k + 2], w[t][e][4 * k + 3]};
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");              // (one wave's own LDS: no barrier)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const int piece = k * 64 + lane, from = piece >> 2;         // of lane `from`
+                const u32x4_t v = reinterpret_cast<const u32x4_t *>(lds)[from * 4 + ((piece + (from >> 1)) & 3)];
+                const int head = from / LANES, in = piece - head * LANES * 4;
+                if (h0 + head < a.b.n_kv_heads) *as_global_mut(reinterpret_cast<u32x4_t *>(recs + (size_t)head * (TERMS * HD * KV_PAGE) + t * HD * KV_PAGE) + in) = v;
             }
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        } else if (h < a.b.n_kv_heads) {
+            uint16_t *out = recs + (size_t)(lane / LANES) * (TERMS * HD * KV_PAGE) + (t * HD + d0) * KV_PAGE;
+#pragma unroll
+            for (int e = 0; e < 2; ++e)
+#pragma unroll
+                for (int r = 0; r < KV_PAGE; r += 2) {
+                    uint16_t *o = out + e * KV_PAGE + r;
+                    const uint32_t two = w[t][e][r >> 1];
+                    const bool first = r >= lo && r < hi, second = r + 1 >= lo && r + 1 < hi;
+                    if (first && second)
+                        *as_global_mut(reinterpret_cast<uint32_t *>(o)) = two;
+                    else if (first)
+                        as_global_mut(o)[0] = (uint16_t)two;
+                    else if (second)
+                        as_global_mut(o)[1] = (uint16_t)(two >> 16);
+                }
         }
     }
 }
@@ -225,6 +230,8 @@ __device__ __forceinline__ void append_values(const AppendDev &a, const AppendBl
 template <int HD, int TERMS, int IN>
 __global__ void __launch_bounds__(APP_WAVES * 64) ee_append_kernel(AppendDev a)
 {
+    __shared__ __align__(16) char lds[APP_WAVES][4096];
+    constexpr int ROWS = 64 / (HD / 16), ROUNDS = KV_PAGE / ROWS;            // rows of a unit of queries or keys, units for a page
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int unit = blockIdx.y * APP_WAVES + wave;
     AppendBlock at;
@@ -234,12 +241,13 @@ __global__ void __launch_bounds__(APP_WAVES * 64) ee_append_kernel(AppendDev a)
         page = as_global(a.b.table)[(size_t)at.seq * a.b.table_stride + at.page];
         if (page >= a.b.n_pages) page = -1;
     }
-    if (unit < a.q_units)
-        append_normed<HD, TERMS, IN>(a, at, page, false, unit * APP_HEADS, lane);
-    else if (unit < a.k_units)
-        append_normed<HD, TERMS, IN>(a, at, page, true, (unit - a.q_units) * APP_HEADS, lane);
-    else
-        append_values<HD, TERMS, IN>(a, at, page, (unit - a.k_units) * APP_HEADS, lane);
+    if (unit < a.k_units) {
+        const bool is_k = unit >= a.q_units;
+        const int u = is_k ? unit - a.q_units : unit;
+        append_normed<HD, TERMS, IN>(a, at, page, is_k, u / ROUNDS, u % ROUNDS * ROWS, lane);
+    } else {
+        append_values<HD, TERMS, IN>(a, at, page, (unit - a.k_units) * append_value_heads(HD), lane, lds[wave]);
+    }
 }
 
 typedef void (*append_kernel_t)(AppendDev);
@@ -334,19 +342,21 @@ extern "C" int ee_kv_append(const ee_paged_cache *c, const ee_append_args *p, vo
     a.rope_pairs = p->rope_pairs;
     a.out_type = p->q_out_dtype;
     a.eps = p->eps;
-    const int kvu = (c->n_kv_heads + APP_HEADS - 1) / APP_HEADS;
-    a.q_units = (p->n_heads + APP_HEADS - 1) / APP_HEADS;
-    a.k_units = a.q_units + kvu;
-    a.units = a.k_units + kvu;
     // A sequence's n rows touch at most 1 + (n + 14) / 16 pages, one if there is one row: with T rows in s sequences, of which t have more
     // than one, at most s + (T - s + 15 t) / 16.
     const int s = std::min(c->n_seqs, p->n_rows), t = std::min(s, p->n_rows - s);
     const unsigned blocks = (unsigned)(s + (p->n_rows - s + 15 * t) / KV_PAGE);
+    const int rounds = c->head_dim == 64 ? 1 : 2, of_values = append_value_heads(c->head_dim);
+    a.q_units = p->n_heads * rounds;
+    a.k_units = a.q_units + c->n_kv_heads * rounds;
+    a.units = a.k_units + (c->n_kv_heads + of_values - 1) / of_values;
+    const unsigned groups = (a.units + APP_WAVES - 1) / APP_WAVES;
+    if (groups > OPS_MAX_GRID_Y) return fail(EE_EINVAL, "%s: %d heads are too many for a call", call, p->n_heads);
     DeviceScope scope(c->device);
     HIP_TRY(scope.status);
     append_kernel_t kernel = c->head_dim == 64 ? (c->terms == 1 ? append_kernel<64, 1>(p->dtype) : append_kernel<64, 2>(p->dtype))
                                                : (c->terms == 1 ? append_kernel<128, 1>(p->dtype) : append_kernel<128, 2>(p->dtype));
-    hipLaunchKernelGGL(kernel, dim3(blocks, (a.units + APP_WAVES - 1) / APP_WAVES), dim3(APP_WAVES * 64), 0, static_cast<hipStream_t>(stream), a);
+    hipLaunchKernelGGL(kernel, dim3(blocks, groups), dim3(APP_WAVES * 64), 0, static_cast<hipStream_t>(stream), a);
     HIP_TRY(hipGetLastError());
     return EE_OK;
 }

@@ -176,6 +176,20 @@ __device__ __forceinline__ void store4(int type, void *base, size_t at, float a,
     }
 }
 
+// eight neighbouring elements of the type, rounded once; 16-byte aligned
+__device__ __forceinline__ void store8(int type, void *base, size_t at, const float (&x)[8])
+{
+    if (type == EE_FP32) {
+        store4(type, base, at, x[0], x[1], x[2], x[3]);
+        store4(type, base, at + 4, x[4], x[5], x[6], x[7]);
+    } else {
+        u32x4_t v;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = type == EE_BF16 ? pack_bf16(x[2 * e], x[2 * e + 1]) : pack_fp16(x[2 * e], x[2 * e + 1]);
+        *as_global_mut(reinterpret_cast<u32x4_t *>(static_cast<uint16_t *>(base) + at)) = v;
+    }
+}
+
 // ------------------------------------------------------------------ host
 
 inline size_t size_of_type(int type) { return type == EE_FP32 ? 4 : 2; }
