@@ -71,6 +71,7 @@ extern "C" {
 
 /* ee_prefill flags */
 #define EE_HOLD_LAST 1u       /* cache n-1 tokens, pending = tokens[n-1], no logits     */
+#define EE_CONTINUE 2u        /* the rows follow the session's cached positions         */
 /* ee_session_create flags */
 #define EE_KEEP_LOGITS 1u     /* keep every head's logits of the last pass (debug)      */
 #define EE_NO_AUTOCOMMIT 2u   /* final accept does not move kv_len / pending            */
@@ -175,7 +176,8 @@ int ee_session_free(ee_session *s);
    pending = *first_token = argmax of the final head at the last prompt row,
    kv_len = n.  With EE_HOLD_LAST (the paper's first round, where the drafts
    follow the prompt directly): kv_len = n-1, pending = tokens[n-1], no head is
-   evaluated and *first_token is left alone.  Resets the session first.
+   evaluated and *first_token is left alone.  Resets the session first; with EE_CONTINUE the rows follow the
+   kv_len positions that it has instead (all n of them: a pending token that is to stay is the first of the new ones).
    tokens: n ids in [0, vocab). */
 int ee_prefill(ee_session *s, const int32_t *tokens, int n, unsigned flags, int32_t *first_token);
 /* Same, with n_emb rows of bf16[d_model] (raw uint16, row-major) placed before
@@ -183,6 +185,13 @@ int ee_prefill(ee_session *s, const int32_t *tokens, int n, unsigned flags, int3
    vision-language experiment. */
 int ee_prefill_embeds(ee_session *s, const uint16_t *emb_bf16, int n_emb, const int32_t *tokens,
                       int n, unsigned flags, int32_t *first_token);
+
+/* Many clients behind one prompt (a system prompt, an image): resets `to`, a session of the same model, and gives it the first n
+   of `from`'s cached positions (1 <= n <= kv_len; synchronous, a copy in device memory).  kv_len of `to` is then n, and it has no pending token:
+   ee_prefill with EE_CONTINUE or ee_set_pending comes next.  `from` stays as it is, and either can be freed before the other.
+   ee_verify_batch and ee_verify_sampled_batch read the whole pages that sessions have in common through forks (also forks of forks, down to what no
+   ee_kv_truncate has cut) once for all of them, where that is faster; results are the same up to the order of the fp32 sums. */
+int ee_session_fork(ee_session *from, int n, ee_session *to);
 
 /* Asynchronous: enqueues one pass over [pending, draft_tokens[0..gamma-1]] and
    returns.  exit_layers: n_exits strictly increasing values in [1, L-1], each
@@ -343,12 +352,15 @@ int ee_device_synchronize(int device);
      to what K and the partial tiles' room allow); 0 = chosen per GEMM from estimated times (the default).  Results
      are the same up to the order of the fp32 sums.
    EE_OPT_PREFILL_ATT_ROWS: query rows per workgroup of such a prompt's attention (64 or 128); 0 = chosen from
-     the heads, the rows and the number of compute units (the default). */
+     the heads, the rows and the number of compute units (the default).
+   EE_OPT_SHARED_ATT (of the session that leads a batch): 1 = pages in common are read for every session, 2 = once wherever there are
+     any, 0 = once where reading them for every session would take longer (the default).  EE_OPT_ATT_SPLITS other than 0 goes before it. */
 #define EE_OPT_ATT_SPLITS 1
 #define EE_OPT_SCATTER_PAGES 2
 #define EE_OPT_HEAD_BATCH 3
 #define EE_OPT_PREFILL_GEMM 4
 #define EE_OPT_PREFILL_ATT_ROWS 5
+#define EE_OPT_SHARED_ATT 6
 int ee_session_option(ee_session *s, int option, int value);
 
 /* Measurement (EE_TIME_LAUNCHES sessions, pass led by `s`): for every kernel launch of the

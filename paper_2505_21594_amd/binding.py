@@ -24,19 +24,19 @@ EE_MAX_ROWS = 48
 EE_OK, EE_NOT_READY, EE_DONE = 0, 1, 2
 EE_EINVAL, EE_ESTATE, EE_ECAPACITY, EE_EIO, EE_EFORMAT, EE_EDEVICE = -1, -2, -3, -4, -5, -6
 
-HOLD_LAST = 1
+HOLD_LAST, CONTINUE = 1, 2
 KEEP_LOGITS = 1
 NO_AUTOCOMMIT = 2
 SAMPLING = 4
 TIME_LAUNCHES = 16
 FORM_AUTO, FORM_PLAIN, FORM_PACKED = 0, 1, 2
-OPT_ATT_SPLITS, OPT_SCATTER_PAGES, OPT_HEAD_BATCH, OPT_PREFILL_GEMM, OPT_PREFILL_ATT_ROWS = 1, 2, 3, 4, 5
+OPT_ATT_SPLITS, OPT_SCATTER_PAGES, OPT_HEAD_BATCH, OPT_PREFILL_GEMM, OPT_PREFILL_ATT_ROWS, OPT_SHARED_ATT = 1, 2, 3, 4, 5, 6
 BF16, FP16, FP32 = 0, 1, 2
 LAUNCH_NAMES = ("qkv", "o", "gu", "dn", "head", "adapter_down", "adapter_up", "embed", "att", "sample")
 
 EXPORTS = [
     "ee_last_error", "ee_model_load", "ee_model_load_ex", "ee_model_load_form", "ee_model_free", "ee_model_info", "ee_model_packed_bytes",
-    "ee_session_create", "ee_session_free", "ee_prefill", "ee_prefill_embeds", "ee_verify",
+    "ee_session_create", "ee_session_free", "ee_session_fork", "ee_prefill", "ee_prefill_embeds", "ee_verify",
     "ee_verify_batch", "ee_verify_static", "ee_verify_sampled", "ee_wait_exit", "ee_query_exit", "ee_wait_final", "ee_query_final",
     "ee_pass_time_ms", "ee_kv_truncate", "ee_set_pending", "ee_kv_len", "ee_pending",
     "ee_verify_sampled_batch", "ee_debug_logits", "ee_debug_mfma_layout", "ee_debug_div_small", "ee_tune_k_split", "ee_device_synchronize", "ee_session_option",
@@ -137,6 +137,7 @@ def load_library():
     lib.ee_model_info.argtypes = [vp, P(ModelConfigC)]
     lib.ee_session_create.argtypes = [vp, ci, ci, ctypes.c_uint, P(vp)]
     lib.ee_session_free.argtypes = [vp]
+    lib.ee_session_fork.argtypes = [vp, ci, vp]
     lib.ee_prefill.argtypes = [vp, i32p, ci, ctypes.c_uint, i32p]
     lib.ee_prefill_embeds.argtypes = [vp, vp, ci, i32p, ci, ctypes.c_uint, i32p]
     lib.ee_verify.argtypes = [vp, i32p, ci, i32p, ci, P(P(VerifyResultC))]
@@ -297,6 +298,10 @@ class Session:
         if self._h:
             self._l.ee_session_free(self._h)
             self._h = None
+
+    def ee_session_fork(self, n: int, to: "Session") -> None:
+        """`to` gets this session's first n cached positions."""
+        _check(self._l.ee_session_fork(self._h, n, to._h))
 
     def ee_prefill(self, tokens: Sequence[int], flags: int = 0, emb: Optional[np.ndarray] = None) -> Optional[int]:
         t = _i32(tokens)

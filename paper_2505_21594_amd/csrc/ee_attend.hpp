@@ -92,7 +92,7 @@ __device__ __forceinline__ int common_pages(const AttendDev &a, int group, int l
 }
 
 // Batches of more than 64 sequences: `from`, `common` and `member`, one wave each.
-__global__ void __launch_bounds__(64) ee_attend_plan_kernel(AttendDev a)
+static __global__ void __launch_bounds__(64) ee_attend_plan_kernel(AttendDev a)
 {
     const int lane = threadIdx.x, i = blockIdx.x;
     int member;

@@ -256,6 +256,29 @@ struct PassArgs {
     SampleDev sm;
 };
 
+// Attention of a batch some of whose sessions have their first pages in common (ee_session_fork): those are read once for all of a
+// group's sessions, from its first member's pool (ee_shared_att_kernel).
+constexpr int ATT_MAX_GROUPS = EE_MAX_BATCH / 2;
+struct SharedAtt {
+    const SessDev *sess;                 // device array
+    const float *q;                      // Scratch::q
+    uint16_t *attn;                      // Scratch::attn
+    float *part;                         // [row][head][most_own + most_shared][hd] parts of a row's head, ...
+    float *ml;                           // ... [row][head][most_own + most_shared][2] their maxima and sums
+    float scale2;                        // scale of the scores * log2(e)
+    int layer, n_sess, M, rows, H, d;
+    int n_groups, most_own, most_shared;
+    int group_items;                     // items of the groups, in front of the sessions'
+    struct Group {
+        unsigned long long members;      // sessions, four bits each
+        int n, pages, parts;             // members, pages in common, parts these are split into
+    } group[ATT_MAX_GROUPS];
+    struct Own {
+        short group, from, parts, first; // group or -1; pages that it reads for the session; parts of the others; items of the sessions before
+    } own[EE_MAX_BATCH];
+};
+void launch_shared_attention(const SharedAtt &a, int hd, int own_items, hipStream_t stream);
+
 typedef void (*pass_kernel_t)(PassArgs);
 // The kernel of a GEMM kind for so many rows.  Defined per kind in a translation unit of its own (ee_gemm_*.hip): they are compiled side by side.
 template <int KIND>

@@ -37,7 +37,7 @@ struct PfScratch {
 struct PfArgs {
     PfScratch b;
     int rows;                 // rows of this chunk
-    int pos0;                 // position of row 0 (a multiple of KV_PAGE)
+    int pos0;                 // position of row 0
     int layer;
     int d, F, H, hd;
     float eps, att_scale;

@@ -10,6 +10,7 @@
 #include <unistd.h>
 
 #include <algorithm>
+#include <atomic>
 #include <climits>
 #include <new>
 #include <tuple>
@@ -112,6 +113,10 @@ struct ee_session {
     int att_splits_opt;              // EE_OPT_ATT_SPLITS (0: chosen per pass)
     int head_batch;                  // EE_OPT_HEAD_BATCH: exit heads per launch of the LM head
     bool scatter_pages;              // EE_OPT_SCATTER_PAGES
+    int shared_att_opt;              // EE_OPT_SHARED_ATT
+    // What the session has in common with others: (id, n) for every fork its cache has gone through, n ascending.  Sessions that hold the same
+    // id hold the same keys and values at positions 0 .. n - 1 (nothing writes below kv_len; what takes kv_len below n takes the mark away).
+    std::vector<std::pair<unsigned long long, int>> marks;
     int pf_gemm_opt, pf_att_opt;     // EE_OPT_PREFILL_GEMM, EE_OPT_PREFILL_ATT_ROWS (0: chosen per launch)
     int flight_row0;                 // first row of this session in the pass in flight
     unsigned long long popped_mask;  // exits of the pass in flight that ee_exit_pop has handed out
@@ -970,6 +975,13 @@ static int attention_splits(const ee_session *lead, int items_cap, int n_sess, i
     return std::min(s, cap);
 }
 
+// What reading common pages once has to save, in pages times heads times values of a head, to be worth its second launch.
+// us a layer, pages read for every session / once (five rows a session, 41 own positions each):
+//   32 heads of 128   2 sessions, 512 in common (131072 saved) 14.0 / 15.7, 2048 (524288) 30.6 / 24.8
+//                     8 sessions, 128 (229376) 14.4 / 16.9, 256 (458752) 19.6 / 17.1, 1024 52.6 / 24.9, 4096 197 / 59
+//   20 heads of 64    4 sessions, 512 (122880) 11.1 / 12.7, 2048 (491520) 19.4 / 17.2;  8 sessions, 512 (286720) 13.0 / 14.4, 1024 18.5 / 15.2, 4096 65 / 30
+constexpr int SHARED_ATT_MIN = 64 * 32 * 128;
+
 // Splits of a batch by session: pages per split are the same for all, so that a session has as many splits as its own pages ask for,
 // instead of the number that attention_splits gives all of them.  Taken where the launch's estimated time is lower by 5 %: a
 // start, an exchange if anything is split (its merge takes eight at a time), the pages of the largest workgroup and a compute unit's share of
@@ -1014,6 +1026,107 @@ static void attention_splits_by_session(const ee_session *lead, int items_cap, e
         best = t;
         a.att_splits = s;
         a.att_starts = starts | 1ull << total;
+    }
+}
+
+// Groups of a batch's sessions that have at least a page in common, most pages saved first; fills g's groups and own[].group / from.
+static void shared_groups(ee_session *const *sessions, int n_sess, SharedAtt &g)
+{
+    for (int i = 0; i < n_sess; ++i) {
+        g.own[i].group = -1;
+        g.own[i].from = 0;
+    }
+    g.n_groups = 0;
+    while (g.n_groups < ATT_MAX_GROUPS) {
+        unsigned long long best = 0;
+        int best_pages = 0, best_n = 0;
+        for (int i = 0; i < n_sess; ++i) {
+            if (g.own[i].group >= 0) continue;
+            for (const auto &mark : sessions[i]->marks) {
+                int n = 0;
+                for (int j = 0; j < n_sess; ++j)
+                    n += g.own[j].group < 0 && std::find(sessions[j]->marks.begin(), sessions[j]->marks.end(), mark) != sessions[j]->marks.end();
+                const int pages = mark.second / KV_PAGE;
+                if ((n - 1) * pages > (best_n - 1) * best_pages && n > 1) {
+                    best = mark.first;
+                    best_pages = pages;
+                    best_n = n;
+                }
+            }
+        }
+        if (!best) break;
+        SharedAtt::Group &grp = g.group[g.n_groups];
+        grp.members = 0;
+        grp.n = 0;
+        grp.pages = best_pages;
+        for (int i = 0; i < n_sess; ++i) {
+            bool has = false;
+            for (const auto &mark : sessions[i]->marks) has |= mark.first == best;
+            if (g.own[i].group >= 0 || !has) continue;
+            grp.members |= (unsigned long long)i << (4 * grp.n++);
+            g.own[i].group = (short)g.n_groups;
+            g.own[i].from = (short)best_pages;
+        }
+        ++g.n_groups;
+    }
+}
+
+// Attention of a batch with pages in common (ee_shared_att_kernel).  Returns the sessions' items, 0: not taken.
+static int plan_shared_attention(const ee_session *lead, int items_cap, ee_session *const *sessions, int n_sess, int M, const PassArgs &a, SharedAtt &g)
+{
+    const ee_model *m = lead->m;
+    const int H = m->cfg.n_heads, hd = m->cfg.head_dim;
+    if (n_sess < 2 || lead->att_splits_opt > 0 || lead->shared_att_opt == 1) return 0;
+    shared_groups(sessions, n_sess, g);
+    if (g.n_groups == 0) return 0;
+    int own_pages[EE_MAX_BATCH], all = 0, read = 0, longest = 0;
+    for (int i = 0; i < n_sess; ++i) {
+        const int pages = (sessions[i]->kv_len + M + KV_PAGE - 1) / KV_PAGE;
+        own_pages[i] = pages - g.own[i].from;
+        all += pages;
+        read += own_pages[i];
+        longest = std::max(longest, own_pages[i]);
+    }
+    for (int i = 0; i < g.n_groups; ++i) {
+        read += g.group[i].pages;
+        longest = std::max(longest, g.group[i].pages);
+    }
+    if (lead->shared_att_opt == 0 && (all - read) * H * hd < SHARED_ATT_MIN) return 0;
+    // parts: the fewest pages each (multiples of 8: a pair for each wave) that leave at most two items for a compute unit, as the partials' room allows
+    const size_t room = (size_t)items_cap * att_item(hd);
+    for (int quota = 8;; quota += 8) {
+        int items = 0;
+        g.most_own = g.most_shared = 1;
+        g.group_items = 0;
+        for (int i = 0; i < g.n_groups; ++i) {
+            SharedAtt::Group &grp = g.group[i];
+            grp.parts = (grp.pages + quota - 1) / quota;
+            g.most_shared = std::max(g.most_shared, grp.parts);
+            g.group_items += (grp.n * M + 15) / 16 * grp.parts;
+        }
+        for (int i = 0; i < n_sess; ++i) {
+            g.own[i].first = (short)items;
+            g.own[i].parts = (short)((own_pages[i] + quota - 1) / quota);
+            g.most_own = std::max<int>(g.most_own, g.own[i].parts);
+            items += g.own[i].parts;
+        }
+        const size_t need = (size_t)n_sess * M * H * (g.most_own + g.most_shared) * (hd + 2);
+        const bool fits = need <= room;
+        if ((fits && (items + g.group_items) * H <= 2 * m->nwg) || quota >= longest) {
+            if (!fits) return 0;
+            g.n_sess = n_sess;
+            g.M = M;
+            g.rows = n_sess * M;
+            g.H = H;
+            g.d = a.d;
+            g.sess = lead->dev_sessdev;
+            g.q = a.sc.q;
+            g.attn = a.sc.attn;
+            g.part = a.sc.att_part;
+            g.ml = g.part + (size_t)g.rows * H * (g.most_own + g.most_shared) * hd;
+            g.scale2 = a.att_scale * 1.44269504f;
+            return items;
+        }
     }
 }
 
@@ -1248,6 +1361,11 @@ static void fill_sessdev(SessDev &sd, const ee_session *s)
         }
 }
 
+static void drop_marks(ee_session *s, int keep_positions)
+{
+    while (!s->marks.empty() && s->marks.back().second > keep_positions) s->marks.pop_back();
+}
+
 // host mirror of the kernels' stage list: [EMBED] { QKV ATT O GU DN } x layers [AD AU] [HEAD];
 // returns the stage's EE_LAUNCH_* code (for a GEMM stage: its GemmKind), or -1 past the end
 static int launch_code(const PassArgs &a, int ph)
@@ -1320,7 +1438,9 @@ static bool packed_pays(int kind, const GemmPlan &p, int rows) { return rows <= 
 
 // Enqueues the stages of one segment, one launch each, on the leader's stream.
 // `many`: the adapters of the group's n_heads exits in one launch each, from stored exit adapter_slot on, `adapter_step` apart.
-static int launch_segment(ee_session *lead, PassArgs &a, int adapter_slot, SampleUpload *up = nullptr, bool many = false, int adapter_step = 0)
+// own_items > 0: attention of a batch with pages in common, as `shared` says.
+static int launch_segment(ee_session *lead, PassArgs &a, int adapter_slot, SampleUpload *up = nullptr, bool many = false, int adapter_step = 0, SharedAtt *shared = nullptr,
+                          int own_items = 0)
 {
     const ee_model *m = lead->m;
     const int per_layer = 5;
@@ -1404,7 +1524,10 @@ static int launch_segment(ee_session *lead, PassArgs &a, int adapter_slot, Sampl
             lead->lt_codes.push_back(code);
             HIP_TRY(hipEventRecord(lead->lt_events[2 * i], lead->run_stream));
         }
-        if (code == EE_LAUNCH_ATT)
+        if (code == EE_LAUNCH_ATT && own_items > 0) {
+            shared->layer = a.layer;
+            launch_shared_attention(*shared, m->cfg.head_dim, own_items, lead->run_stream);
+        } else if (code == EE_LAUNCH_ATT)
             hipLaunchKernelGGL(k, a.att_starts ? dim3(a.H, 63 - __builtin_clzll(a.att_starts)) : dim3(a.att_splits, a.H, a.mode == 1 ? (a.M + ATT_ROWS - 1) / ATT_ROWS : a.n_sess),
                                dim3(WG_THREADS), att_lds(m->cfg.head_dim, a.M), lead->run_stream, a);
         else
@@ -1466,6 +1589,18 @@ static int finish_flight(ee_session *s)
         s->pending = s->result->next_token;
     }
     return EE_OK;
+}
+
+// An empty cache; no pass of the session is in flight.
+static void reset_cache(ee_session *s)
+{
+    release_pages(s, 0);
+    // all pages are free here: hand them out in ascending order (a fresh session's pages are then
+    // consecutive and the kernels skip the table lookup) or, as a test aid, in descending order
+    std::sort(s->free_pages.begin(), s->free_pages.end());
+    if (!s->scatter_pages) std::reverse(s->free_pages.begin(), s->free_pages.end());
+    drop_marks(s, 0);
+    s->kv_len = 0;
 }
 
 // ------------------------------------------------------------------ prefill
@@ -1559,26 +1694,24 @@ extern "C" int ee_prefill_embeds(ee_session *s, const uint16_t *emb_bf16, int n_
     int rc = finish_flight(s);
     if (rc != EE_OK && rc != EE_EDEVICE) return rc;
     HIP_TRY(hipStreamSynchronize(s->stream));
-    // reset
     s->run_stream = s->stream;
-    release_pages(s, 0);
-    // all pages are free here: hand them out in ascending order (a fresh session's pages are then
-    // consecutive and the kernels skip the table lookup) or, as a test aid, in descending order
-    std::sort(s->free_pages.begin(), s->free_pages.end());
-    if (!s->scatter_pages) std::reverse(s->free_pages.begin(), s->free_pages.end());
-    s->kv_len = 0;
+    const bool more = (flags & EE_CONTINUE) != 0;
+    if (!more) reset_cache(s);
+    const int base = s->kv_len;   // the first row's position
+    if (base + total + 1 > s->max_ctx) return fail(EE_ECAPACITY, "ee_prefill: %d rows behind %d positions do not fit max_ctx %d", total, base, s->max_ctx);
     s->has_pending = false;
     s->leader = s;
     s->flight_gamma = 0;
     s->flight_exits = 0;
     s->result->device_status = 0;
-    if ((rc = ensure_pages(s, total + 1, s->stream)) != EE_OK) return rc;
+    if ((rc = ensure_pages(s, base + total + 1, s->stream)) != EE_OK) return rc;
 
     fill_sessdev(s->host_sessdev[0], s);
     // More rows than a pass of this model carries: the many-row kernels, in chunks of nearly equal size.  us with
     // them / in streamed chunks of 16 rows: 7B shape, 4 layers, 24 rows 646 / 816, 48 rows 673 / 1238; 1280-wide model, 3
     // layers, 24 rows 204 / 233.  (A streamed pass of 48 rows takes 600: models loaded for that many keep it.)
-    const bool many = total > c.max_rows;
+    // (Rows behind cached positions always take them: a pass's prompt kernels start at position 0.)
+    const bool many = total > c.max_rows || (base > 0 && total > 0);
     const int n_chunks = (total + s->pf_cap - 1) / s->pf_cap;
     const int chunk = many ? std::min(s->pf_cap, (int)align_up((size_t)((total + n_chunks - 1) / n_chunks), 128)) : total;
     const size_t d = (size_t)c.d_model;
@@ -1620,7 +1753,7 @@ extern "C" int ee_prefill_embeds(ee_session *s, const uint16_t *emb_bf16, int n_
             a.att_splits = attention_splits(s, s->att_items_cap, 1, rows, rows);
             if (a.att_splits == 0) return fail(EE_ECAPACITY, "ee_prefill: context too long for the session's attention scratch");
         } else {
-            if ((rc = prefill_chunk(s, start, rows)) != EE_OK) return rc;
+            if ((rc = prefill_chunk(s, base + start, rows)) != EE_OK) return rc;
             if (!last) continue;
             PfArgs p;
             memset(&p, 0, sizeof p);
@@ -1636,7 +1769,7 @@ extern "C" int ee_prefill_embeds(ee_session *s, const uint16_t *emb_bf16, int n_
         if ((rc = launch_segment(s, a, 0)) != EE_OK) return rc;
     }
     HIP_TRY(hipStreamSynchronize(s->stream));
-    s->kv_len = total;
+    s->kv_len = base + total;
     if (hold) {
         s->pending = tokens[n - 1];
     } else {
@@ -1841,6 +1974,8 @@ static int verify_impl(ee_session *const *sessions, int n_sessions, const int32_
                                       "(list the session with the largest max_ctx first)", n_pos_max);
         attention_splits_by_session(lead, lead->att_items_cap, sessions, n_sessions, M, a);
     }
+    SharedAtt shared;
+    const int own_items = static_scratch ? 0 : plan_shared_attention(lead, lead->att_items_cap, sessions, n_sessions, M, a, shared);
     // everything below is enqueued on the leader's stream; other sessions' own
     // streams are idle here (their last pass has been waited for)
     for (int i = 0; i < n_sessions; ++i) {
@@ -1918,7 +2053,7 @@ static int verify_impl(ee_session *const *sessions, int n_sessions, const int32_
         } else {
             a.ad_gain = a.head_gain;
         }
-        if ((rc = launch_segment(lead, a, slot, &upload, many, step)) != EE_OK) return rc;
+        if ((rc = launch_segment(lead, a, slot, &upload, many, step, &shared, own_items)) != EE_OK) return rc;
         if (fin) {
             HIP_TRY(hipEventRecord(lead->ev_final, lead->run_stream));
         } else if (a.head_stage) {
@@ -2153,6 +2288,59 @@ extern "C" int ee_kv_truncate(ee_session *s, int new_len)
     if (new_len < 0 || new_len > s->kv_len) return fail(EE_EINVAL, "ee_kv_truncate: %d not in [0, kv_len=%d]", new_len, s->kv_len);
     s->kv_len = new_len;
     release_pages(s, new_len);
+    drop_marks(s, new_len);
+    return EE_OK;
+}
+
+// The first pages of a session's cache into another's pools: a workgroup copies one layer's records of one page.
+static __global__ void __launch_bounds__(256) fork_pages_kernel(const uint16_t *k, const uint16_t *v, const int *table, int n_pages, uint16_t *to_k, uint16_t *to_v,
+                                                                const int *to_table, int to_pages, int record)
+{
+    const size_t from = ((size_t)blockIdx.y * n_pages + table[blockIdx.x]) * record, to = ((size_t)blockIdx.y * to_pages + to_table[blockIdx.x]) * record;
+    const uint4 *src = reinterpret_cast<const uint4 *>((blockIdx.z ? v : k) + from);
+    uint4 *dst = reinterpret_cast<uint4 *>((blockIdx.z ? to_v : to_k) + to);
+    for (int i = threadIdx.x; i < record / 8; i += blockDim.x) dst[i] = src[i];
+}
+
+extern "C" int ee_session_fork(ee_session *from, int n, ee_session *to)
+{
+    if (!from || !to || from == to) return fail(EE_EINVAL, "ee_session_fork: two sessions are needed");
+    if (from->m != to->m) return fail(EE_EINVAL, "ee_session_fork: sessions of different models");
+    const ee_model *m = from->m;
+    HIP_TRY(hipSetDevice(m->device));
+    int rc = finish_flight(from);
+    if (rc != EE_OK) return rc;
+    rc = finish_flight(to);
+    if (rc != EE_OK && rc != EE_EDEVICE) return rc;   // (what failed there is given up)
+    if (n < 1 || n > from->kv_len) return fail(EE_EINVAL, "ee_session_fork: %d not in [1, kv_len=%d]", n, from->kv_len);
+    if (n + 1 > to->max_ctx) return fail(EE_ECAPACITY, "ee_session_fork: %d positions do not fit max_ctx %d", n, to->max_ctx);
+    HIP_TRY(hipStreamSynchronize(from->stream));
+    HIP_TRY(hipStreamSynchronize(to->stream));
+    to->run_stream = to->stream;
+    reset_cache(to);
+    to->has_pending = false;
+    to->leader = to;
+    to->flight_gamma = 0;
+    to->flight_exits = 0;
+    to->result->device_status = 0;
+    if ((rc = ensure_pages(to, n, to->stream)) != EE_OK) return rc;
+    const int pages = (n + KV_PAGE - 1) / KV_PAGE, record = m->cfg.n_heads * KV_PAGE * 2 * m->cfg.head_dim;
+    hipLaunchKernelGGL(fork_pages_kernel, dim3(pages, m->cfg.n_layers, 2), dim3(256), 0, to->stream, from->kpool, from->vpool, from->dev_page_table, from->n_pages,
+                       to->kpool, to->vpool, to->dev_page_table, to->n_pages, record);
+    HIP_TRY(hipGetLastError());
+    HIP_TRY(hipStreamSynchronize(to->stream));
+    to->kv_len = n;
+    // a mark of this fork, unless the session has one at this length already (without memory for it the sessions only share nothing)
+    try {
+        auto at = std::lower_bound(from->marks.begin(), from->marks.end(), n, [](const std::pair<unsigned long long, int> &x, int len) { return x.second < len; });
+        if (at == from->marks.end() || at->second != n) {
+            static std::atomic<unsigned long long> forks{0};
+            at = from->marks.insert(at, {++forks, n});
+        }
+        to->marks.assign(from->marks.begin(), at + 1);
+    } catch (const std::bad_alloc &) {
+        to->marks.clear();
+    }
     return EE_OK;
 }
 
@@ -2238,6 +2426,10 @@ extern "C" int ee_session_option(ee_session *s, int option, int value)
     case EE_OPT_PREFILL_ATT_ROWS:
         if (value != 0 && value != 64 && value != 128) return fail(EE_EINVAL, "EE_OPT_PREFILL_ATT_ROWS: %d not 0, 64 or 128", value);
         s->pf_att_opt = value;
+        return EE_OK;
+    case EE_OPT_SHARED_ATT:
+        if (value < 0 || value > 2) return fail(EE_EINVAL, "EE_OPT_SHARED_ATT: %d not in [0,2]", value);
+        s->shared_att_opt = value;
         return EE_OK;
     default:
         return fail(EE_EINVAL, "ee_session_option: unknown option %d", option);
