@@ -7,13 +7,13 @@ struct AttendKernel {
     attend_kernel_t f;
     size_t lds;
 };
-template <int HD, int TERMS, int QT, int PT>
+template <int HD, int TERMS, int QT, int PT, int PT_WIDE = PT>
 static AttendKernel attend_of_tiles(int tiles)
 {
     if (tiles == 1) return {ee_attend_kernel<HD, TERMS, QT, PT, 1>, attend_lds<HD, QT, 1>()};
     if constexpr (TERMS == 1 || HD == 64)
         if (tiles == 2) return {ee_attend_kernel<HD, TERMS, QT, PT, 2>, attend_lds<HD, QT, 2>()};
-    return {ee_attend_wide_kernel<HD, TERMS, QT, PT == 2 && QT == 1 ? 1 : PT>, attend_wide_lds<HD, TERMS>()};
+    return {ee_attend_wide_kernel<HD, TERMS, QT, PT_WIDE>, attend_wide_lds<HD, TERMS>()};
 }
 template <int HD>
 static AttendKernel attend_kernel(int terms, int q_type, int out_type, int tiles)
@@ -21,7 +21,8 @@ static AttendKernel attend_kernel(int terms, int q_type, int out_type, int tiles
     if (terms == 2) return attend_of_tiles<HD, 2, 3, 3>(tiles);
     if (out_type == EE_FP32) return q_type == EE_BF16 ? attend_of_tiles<HD, 1, 1, 3>(tiles) : attend_of_tiles<HD, 1, 3, 3>(tiles);
     if (q_type == EE_FP32) return attend_of_tiles<HD, 1, 3, 3>(tiles);
-    return q_type == EE_BF16 ? attend_of_tiles<HD, 1, 1, 2>(tiles) : attend_of_tiles<HD, 1, 2, 2>(tiles);
+    if (q_type == EE_FP16) return attend_of_tiles<HD, 1, 2, 2>(tiles);
+    return out_type == EE_BF16 ? attend_of_tiles<HD, 1, 1, 2, 1>(tiles) : attend_of_tiles<HD, 1, 1, 2>(tiles);
 }
 
 // How a call is split; a function of what the host knows (sizes and the caller's bounds).
@@ -45,6 +46,29 @@ static long long most_chunks(int n, int T, int per_key, int lines)
 
 static size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
 
+// Pages of a part for the kernel for many lines: as many parts as give the least time by this estimate, the fewest of those within 5 %.  The largest
+// item's pages, at 0.22 us for each matrix product of a page, or all pages, at two items for a compute unit; parts are written and read again at 1.25
+// MB a microsecond, behind a launch.  us, 32 heads of 128, bf16, 1 / 2 / about 5 parts: 350 rows 16.4 / 20.8 / 23.5, 500 19.8 / 24.5 / 26.8, 350 behind 2000 cached
+// positions 61.5 / 41.6 / 41.4; 700 and 1000 rows behind 2000 69.7 and 76.6 / 58.2 and 67.2 (two parts).
+static int wide_quota(const ee_paged_cache &c, const ee_attend_args &p, int own_pages, long long chunks, int seqs)
+{
+    const int step = c.terms == 1 ? 4 : 2;
+    const int products = c.terms == 2 ? 10 : p.dtype == EE_BF16 ? 2 : 5;
+    const double page = 0.22 * products * c.head_dim / 128, all = (double)chunks * c.n_kv_heads * own_pages * (seqs == 1 ? 1.0 : 0.5) / 512;
+    const double part = (double)p.n_rows * p.n_heads * c.head_dim * 4 / 1.25e6;
+    int best_quota = 0;
+    double best = 0;
+    for (int n = 1; n <= 64; ++n) {
+        const int quota = ((own_pages + n - 1) / n + step - 1) / step * step, parts = (own_pages + quota - 1) / quota;
+        const double t = page * std::max<double>(quota, all) + (parts > 1 ? 3 + part * parts : 0);
+        if (best_quota == 0 || t < 0.95 * best) {
+            best_quota = quota;
+            best = t;
+        }
+    }
+    return best_quota;
+}
+
 static AttendPlan plan_attend(const ee_paged_cache &c, const ee_attend_args &p)
 {
     AttendPlan pl = {};
@@ -54,8 +78,13 @@ static AttendPlan plan_attend(const ee_paged_cache &c, const ee_attend_args &p)
     int shared_pages = p.n_groups == 0 ? 0 : (int)std::min<long long>(pages, p.max_shared > 0 ? p.max_shared / KV_PAGE : pages);
     const int seqs = std::min(c.n_seqs, T);
     const long long own_lines = (long long)T * per_key / seqs;
-    // From 64 lines a sequence on the matrix cores bound the call, and reading common pages once gains nothing.
-    const bool wide = own_lines >= 64;
+    // Many lines of a key head a sequence: the kernel that reads keys and values for 128 of them at a time (ee_attend_wide_kernel).  us, it / the others,
+    // heads of 128, one term, 8 sequences of 2000 positions, 32 heads on 8 / on 32: 32 lines 23.3 / 23.6, 61.1 / 60.0, 48 lines 25.8 / 33.6, 67.1 / 64.7,
+    // 64 lines 27.6 / 33.2, 68.0 / 68.9, 128 lines 35.2 / 44.9, 85.9 / 126; one sequence of 8000: 32 lines 18.4 / 19.1, 48 lines 20.6 / 20.3, 35.6 / 47.0.
+    // Two terms, 32 heads on 32: 48 lines 184 / 163, 64 lines 186 / 187, 96 lines 193 / 262; one sequence of 2000: 64 lines 41 / 32, 96 lines 46 / 48.
+    // It reads common pages for every sequence, which from here on is no loss: 8 sequences with 3840 of 4000 positions in common, every page for every
+    // sequence / once, 8 and 32 key heads: 48 lines 34.8 / 35.1, 85 / 92, 64 lines 36 / 39, 89 / 107, 128 lines 44 / 60, 100 / 202.
+    const bool wide = own_lines > (c.terms == 1 ? 32 : 64);
     pl.groups = wide || shared_pages == 0 ? 0 : std::min(p.n_groups, seqs);
     if (pl.groups == 0) shared_pages = 0;
     const long long lines = pl.groups ? std::max(own_lines, (long long)T * per_key / pl.groups) : own_lines;
@@ -63,18 +92,22 @@ static AttendPlan plan_attend(const ee_paged_cache &c, const ee_attend_args &p)
     const long long chunks_own = most_chunks(seqs, T, per_key, pl.tiles * 16);
     const long long chunks_shared = pl.groups ? most_chunks(pl.groups, T, per_key, pl.tiles * 16) : 0;
     const int own_pages = std::max(pages - shared_pages, 1);
-    // Parts: the fewest pages each (a pair for each wave at a time: multiples of 8) that leave the items as many as the chip holds at once, two for a
-    // compute unit, if sequences are half the longest on average.  A second round costs more than longer parts: eight rounds of five rows of 32 heads
-    // behind 576 common positions, parts of 16 / 24 pages (544 / 448 items) 21.6 / 16.8 us; 32 rows of 8 key heads behind 6000, parts of 40 / 56 / 80
-    // pages (616 / 500 / 424 items) 33.9 / 27.3 / 32.4.  Where chunks alone are more than that, half as many parts again.
     const long long est_own = seqs * ((own_lines + pl.tiles * 16 - 1) / (pl.tiles * 16));
-    const double room = std::max(512.0 / c.n_kv_heads, 1.5 * (double)(est_own + chunks_shared));
-    pl.quota = 8;
-    while (pl.quota < std::max(own_pages, shared_pages)) {
-        const double own_parts = seqs == 1 ? (double)((own_pages + pl.quota - 1) / pl.quota) : std::max(1.0, 0.5 * own_pages / pl.quota + 0.5);
-        const long long shared_parts = (shared_pages + pl.quota - 1) / pl.quota;
-        if ((double)est_own * own_parts + (double)(chunks_shared * shared_parts) <= room && own_pages <= 64 * pl.quota && shared_pages <= 64 * pl.quota) break;
-        pl.quota += std::max(8, pl.quota / 64 * 8);
+    if (wide) {
+        pl.quota = wide_quota(c, p, own_pages, est_own, seqs);
+    } else {
+        // Parts: the fewest pages each (a pair for each wave at a time: multiples of 8) that leave the items as many as the chip holds at once, two for a
+        // compute unit, if sequences are half the longest on average.  A second round costs more than longer parts: eight rounds of five rows of 32 heads
+        // behind 576 common positions, parts of 16 / 24 pages (544 / 448 items) 21.6 / 16.8 us; 32 rows of 8 key heads behind 6000, parts of 40 / 56 / 80
+        // pages (616 / 500 / 424 items) 33.9 / 27.3 / 32.4.  Where chunks alone are more than that, half as many parts again.
+        const double room = std::max(512.0 / c.n_kv_heads, 1.5 * (double)(est_own + chunks_shared));
+        pl.quota = 8;
+        while (pl.quota < std::max(own_pages, shared_pages)) {
+            const double own_parts = seqs == 1 ? (double)((own_pages + pl.quota - 1) / pl.quota) : std::max(1.0, 0.5 * own_pages / pl.quota + 0.5);
+            const long long shared_parts = (shared_pages + pl.quota - 1) / pl.quota;
+            if ((double)est_own * own_parts + (double)(chunks_shared * shared_parts) <= room && own_pages <= 64 * pl.quota && shared_pages <= 64 * pl.quota) break;
+            pl.quota += std::max(8, pl.quota / 64 * 8);
+        }
     }
     pl.most_own = std::min((own_pages + pl.quota - 1) / pl.quota, 64);
     pl.most_shared = std::min((shared_pages + pl.quota - 1) / pl.quota, 64);
@@ -167,7 +200,6 @@ extern "C" int ee_attend(const ee_paged_cache *c, const ee_attend_args *p, void 
     a.quota = pl.quota;
     a.most_own = pl.most_own;
     a.most_shared = pl.most_shared;
-    a.descending = std::min(c->n_seqs, p->n_rows) == 1 && pl.items * c->n_kv_heads <= 512 ? std::max(256 / c->n_kv_heads, 1) : 0x7FFFFFFF;
     a.scale2 = p->scale * 1.44269504f;
     DeviceScope scope(c->device);
     HIP_TRY(scope.status);

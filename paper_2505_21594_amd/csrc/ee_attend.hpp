@@ -14,8 +14,8 @@
 // The output is kept transposed: a line's maximum, sum and output are in the lanes of its column, and rescaling needs no exchange.
 //
 // Precision: sums, maxima and outputs are fp32.  The products' operands are bf16 terms: K and V as the cache has them (TERMS), q in QT terms, exactly for bf16 (1) and
-// fp16 (2) and to 2^-25 for fp32 (3); P in PT: 3 where the results are fp32, 2 (2^-17) for results of 16 bits, 1 (2^-9, as much as the result's
-// own rounding) where the matrix cores bound the call.  Products of the smallest terms are left out (2^-26, or 2^-17 with 2 terms).
+// fp16 (2) and to 2^-24 for fp32 (3); P in PT: 3 where the results are fp32, 2 (2^-16) for results of 16 bits, 1 (2^-8, as much as the result's
+// own rounding) for bf16 queries and results of many lines, where the matrix cores bound the call.  Products of the smallest terms are left out (2^-24, or 2^-16 with 2 terms).
 #pragma once
 
 #include <type_traits>
@@ -39,7 +39,6 @@ struct AttendDev {
     int n_groups, n_heads, per_key;            // per_key: query heads of a key head
     int quota;                                 // pages of a part
     int most_own, most_shared;                 // parts at most
-    int descending;                            // chunks of a sequence in descending order before those in ascending order
     float scale2;                              // scale * log2(e)
 };
 
@@ -209,10 +208,9 @@ __device__ __forceinline__ bool attend_item(const AttendDev &a, int item, int la
             it.rows = __builtin_amdgcn_readlane(mine.n, l);
             const int len = __builtin_amdgcn_readlane(mine.len, l), from = __builtin_amdgcn_readlane(mine.from, l);
             const int parts = own_parts(a, table_pages(a, len) - from);
-            // The last lines first: they see the most positions.  Where all items are on the chip at once, the second half of them, which share
-            // compute units with the first, from the other end (2041 rows of 32 heads: 80 -> 60 us).
+            // the last lines first: they see the most positions
             const int chunks = (it.rows * G + LINES - 1) / LINES, c_up = place / parts, part = place - c_up * parts;
-            it.line0 = (c_up < a.descending ? chunks - 1 - c_up : c_up - a.descending) * LINES;
+            it.line0 = (chunks - 1 - c_up) * LINES;
             it.lines = min(LINES, it.rows * G - it.line0);
             it.first_pos = len - it.rows;
             const int pages = max(table_pages(a, it.first_pos + (it.line0 + it.lines - 1) / G + 1) - from, 0);
@@ -336,13 +334,25 @@ __device__ __forceinline__ void attend_exps(AttendState<RT, NT> &st, int t, floa
     }
 }
 
+// max3 is not an instruction the compiler knows to keep away from a matrix product's results while they are on their way (NaN in a call of many rows
+// showed it): this waits for them.  A 16x16x32 product needs at most 12 wait states; where a select reads the scores first (MASKED) the compiler has seen to it.
+template <int NP>
+__device__ __forceinline__ void products_done(f32x4_t (&S)[NP][2])
+{
+    if constexpr (NP == 1)
+        asm("s_nop 15" : "+v"(S[0][0]), "+v"(S[0][1]));
+    else
+        asm("s_nop 15" : "+v"(S[0][0]), "+v"(S[0][1]), "+v"(S[1][0]), "+v"(S[1][1]));
+}
+
 // A tile's scores of NP pairs as the lane's eights.  MASKED: those that its line does not see are nothing; keep: of the lane's positions of a pair,
 // those that exist.  Returns the largest, scaled.
 template <bool MASKED, int NP, int RT, int NT>
-__device__ __forceinline__ float attend_scores(AttendState<RT, NT> &st, int t, const f32x4_t (&S)[NP][2], const int (&keep)[NP], int pos0, int last, int quad, float scale2,
+__device__ __forceinline__ float attend_scores(AttendState<RT, NT> &st, int t, f32x4_t (&S)[NP][2], const int (&keep)[NP], int pos0, int last, int quad, float scale2,
                                                float (&s)[NP][8])
 {
     bool sees = false;
+    if constexpr (!MASKED) products_done<NP>(S);
 #pragma unroll
     for (int p = 0; p < NP; ++p) {
         const int seen = min(keep[p], last - pos0 - p * 32 - quad * 8 + 1);

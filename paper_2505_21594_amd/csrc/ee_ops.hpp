@@ -45,7 +45,8 @@ __device__ __forceinline__ void pair32(unsigned x, unsigned &a, unsigned &b)
     a = r[0];
     b = r[1];
 }
-// (written out: of values it knows nothing about the compiler makes every one canonical first, an instruction each)
+// (written out: of values it knows nothing about the compiler makes every one canonical first, an instruction each.  No operand may come straight
+// from a matrix product: the compiler adds the wait states that this needs only in front of instructions it chose itself)
 __device__ __forceinline__ float max3(float a, float b, float c)
 {
     float r;

@@ -1,4 +1,5 @@
 """The operators on device memory against plain 64-bit forms: ee_kv_append, ee_attend, ee_accept_drafts."""
+import copy
 import ctypes
 
 import numpy as np
@@ -34,7 +35,8 @@ def close(got, want, tol, what):
 
 # ---------------------------------------------------------------- ee_attend
 
-def run_attend(c, heads, kind, out_kind, groups=True, scale=None, layout="plain", max_kv=None, hint_shared=None, stream=0):
+def run_attend(c, heads, kind, out_kind, groups=True, scale=None, layout="plain", max_kv=None, hint_shared=None, stream=0, weight_step=0.0):
+    """weight_step: how far one term of a softmax weight may be off, relative to it, where that is more than the tolerance of ref.attend has."""
     q = np.zeros((c.cap, heads, c.dim), np.float32)
     q[:] = c.rng.standard_normal(q.shape)
     enc = encode(q, kind)
@@ -71,6 +73,10 @@ def run_attend(c, heads, kind, out_kind, groups=True, scale=None, layout="plain"
         out = out[:, 1: heads + 1]
     assert (out[c.T:] == fill).all(), "padding rows were written"
     want, tol = ref.attend(c, decode(enc)[: c.T], scale, kind, out_kind)
+    if weight_step:
+        magnitudes = copy.copy(c)
+        magnitudes.values = lambda s: np.abs(c.values(s))
+        tol = tol + weight_step * ref.attend(magnitudes, decode(enc)[: c.T], scale, kind, out_kind)[0]
     return decode(out)[: c.T], want, tol
 
 
@@ -99,6 +105,34 @@ def test_attend(i, layout):
     c = ref.Case(100 + i, rows, lens, kv_heads, dim, terms, pad=i % 3).fill_fast()
     got, want, tol = run_attend(c, heads, kind, out_kind, layout=layout)
     close(got, want, tol, "attention")
+
+
+MANY = [
+    # rows, lens, heads, kv_heads, dim, terms, kind, out, groups, shared pages: more than 32 lines of a key head a sequence
+    ([33], [33], 1, 1, 64, 1, "bf16", "bf16", (), ()),
+    ([128], [128], 4, 4, 64, 1, "bf16", "bf16", (), ()),
+    ([200], [1500], 4, 4, 128, 1, "bf16", "bf16", (), ()),                 # parts
+    ([300], [120], 2, 2, 64, 1, "bf16", "bf16", (), ()),                   # rows in front of position 0
+    ([65, 0, 100, 3], [65, 10, 900, 400], 8, 2, 128, 1, "bf16", "fp16", (), ()),
+    ([40, 30], [300, 31], 2, 1, 64, 1, "fp16", "fp16", (), ()),
+    ([129], [2049], 2, 2, 128, 1, "fp16", "fp32", (), ()),
+    ([40] * 3, [100, 500, 3001], 4, 4, 128, 1, "fp32", "fp32", (), ()),
+    ([50, 1], [1600, 1700], 3, 1, 64, 1, "bf16", "fp32", (), ()),
+    ([150], [150], 2, 2, 64, 2, "fp32", "fp32", (), ()),
+    ([70, 70, 70], [2000, 71, 500], 2, 2, 128, 2, "fp32", "bf16", (), ()),
+    ([66, 70, 1], [300, 290, 220], 4, 4, 128, 1, "bf16", "bf16", [(0, 3)], [13]),
+    ([90, 66], [700, 90], 2, 2, 64, 2, "fp32", "fp32", [(0, 2)], [1]),
+]
+
+
+@pytest.mark.parametrize("layout", ["plain", "strided"])
+@pytest.mark.parametrize("i", range(len(MANY)))
+def test_attend_many_rows(i, layout):
+    """For bf16 queries and results of one-term caches a weight is one bf16 term, off by half a step: 2^-8 of it."""
+    rows, lens, heads, kv_heads, dim, terms, kind, out_kind, groups, shared = MANY[i]
+    c = ref.Case(600 + i, rows, lens, kv_heads, dim, terms, groups, shared, pad=i % 3).fill_fast()
+    got, want, tol = run_attend(c, heads, kind, out_kind, layout=layout, weight_step=2.0 ** -8 if (kind, out_kind, terms) == ("bf16", "bf16", 1) else 0)
+    close(got, want, tol, "many rows")
 
 
 GROUPS = [
