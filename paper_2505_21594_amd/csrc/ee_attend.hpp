@@ -468,7 +468,8 @@ __device__ __forceinline__ void attend_store(const AttendDev &a, const AttendIte
     }
 }
 
-// The sums of a line's lanes, and NaN where it saw positions but no score above -infinity: it has no softmax.
+// The sums of a line's lanes, and NaN where it saw positions but no score above -infinity: it has no softmax.  Scores of NaN have left NaN in the sum,
+// but no maximum: with any maximum the part counts, and the line becomes NaN.
 template <int RT, int NT>
 __device__ __forceinline__ void attend_finish(AttendState<RT, NT> &st)
 {
@@ -476,7 +477,11 @@ __device__ __forceinline__ void attend_finish(AttendState<RT, NT> &st)
 #pragma unroll
     for (int t = 0; t < RT; ++t) {
         st.sum[t] = quads_sum(st.sum[t]);
-        if (st.mx[t] == -INFINITY && (st.hollow >> t & 1)) st.sum[t] = __builtin_nanf("");
+        if (st.mx[t] != -INFINITY) continue;
+        if (st.sum[t] != st.sum[t])
+            st.mx[t] = 0.f;
+        else if (st.hollow >> t & 1)
+            st.sum[t] = __builtin_nanf("");
     }
 }
 

@@ -236,6 +236,69 @@ def test_attend_infinite_scores(kind):
             assert np.abs(out[0, 0] - e @ V / e.sum()).max() < 1e-4
 
 
+@pytest.mark.parametrize("kind", ["bf16", "fp32"])
+@pytest.mark.parametrize("terms", [1, 2])
+@pytest.mark.parametrize("dim", [64, 128])
+def test_attend_many_rows_nan_where_a_row_does_not_look(dim, terms, kind):
+    c, clean = (ref.Case(14, [120, 70], [700, 75], 2, dim, terms).fill_fast() for _ in range(2))
+    for s, p, bits in ((0, 640, 0x7F80), (0, 699, 0x7FC0), (1, 40, 0xFF80)):
+        page, slot = c.table[s, p // 16], p % 16
+        c.k_pool[page, :, slot] = 0x7FC0
+        c.v_pool[page, :, :, 5:9, slot] = bits
+    c.rng, clean.rng = np.random.default_rng(4), np.random.default_rng(4)
+    got, _, _ = run_attend(c, 2, kind, "fp32")
+    _, want, tol = run_attend(clean, 2, kind, "fp32")
+    blind = np.concatenate([580 + np.arange(120) < 640, 5 + np.arange(70) < 40])
+    close(got[blind], want[blind], tol[blind], "rows in front")
+    assert np.isnan(got[~blind]).any(axis=(1, 2)).all()
+
+
+@pytest.mark.parametrize("kind", ["bf16", "fp32"])
+@pytest.mark.parametrize("terms", [1, 2])
+@pytest.mark.parametrize("at", [0, 128, 256, 1023, 1024])
+def test_attend_nan_score_alone_in_a_part(at, terms, kind):
+    """A key of NaN makes its row NaN, also where a part of the positions, or a wave of it, has no other score above -infinity."""
+    c = ref.Case(17, [1], [1025], 2, 64, terms).fill_fast()
+    q = np.zeros((1, 2, 64), np.float32)
+    q[0, :, 0] = 1.0
+    for p in range(at // 128 * 128, 1025 if at == 1024 else at // 128 * 128 + 128):
+        c.k_pool[c.table[0, p // 16], :, p % 16, :, 0] = 0xFF80 if kind == "bf16" and terms == 1 else c.k_pool[c.table[0, p // 16], :, p % 16, :, 0]
+    c.k_pool[c.table[0, at // 16], :, at % 16] = 0x7FC0
+    k, v, table = cache_of(c)
+    dq, dout = Dev(encode(q, kind)), Dev(q)
+    cache, rs, kl = ee.PagedCache(k, v, table), Dev(c.row_start), Dev(c.kv_len)
+    n = ee.ee_attend_workspace(cache, rs, dq, max_kv=1025)
+    ee.ee_attend(cache, rs, kl, dq, dout, scale=0.125, max_kv=1025, workspace=workspace(n))
+    assert np.isnan(dout.numpy()).all()
+
+
+def test_attend_many_rows_infinite_scores():
+    """40 rows behind 560 positions: those that see the first 580 only have no softmax, the others have that of what is behind."""
+    c = ref.Case(15, [40], [600], 1, 64, 1).fill_fast()
+    q = np.zeros((40, 1, 64), np.float32)
+    q[:, 0, 0] = 1.0
+    for p in range(580):
+        c.k_pool[c.table[0, p // 16], 0, p % 16, 0, 0] = 0xFF80
+    k, v, table = cache_of(c)
+    dq, dout = Dev(encode(q, "bf16")), Dev(q)
+    cache, rs, kl = ee.PagedCache(k, v, table), Dev(c.row_start), Dev(c.kv_len)
+    n = ee.ee_attend_workspace(cache, rs, dq, max_kv=600)
+    ee.ee_attend(cache, rs, kl, dq, dout, scale=0.125, max_kv=600, workspace=workspace(n))
+    out = dout.numpy()
+    assert np.isnan(out[:20]).all()
+    K, V = c.keys(0)[0][580:, 0], c.values(0)[580:, 0]
+    for i in range(20, 40):
+        e = np.exp(K[: i - 19, 0] * 0.125)
+        assert np.abs(out[i, 0] - e @ V[: i - 19] / e.sum()).max() < 1e-4
+
+
+def test_attend_large_scores_of_many_rows():
+    c = ref.Case(16, [50], [200], 2, 64, 1).fill_fast(scale=30.0)
+    got, want, tol = run_attend(c, 2, "bf16", "fp32", scale=3.0)
+    assert np.isfinite(got).all()
+    close(got, want, tol, "large scores")
+
+
 def test_attend_large_scores():
     """Scores of thousands: the running maximum keeps exp in range."""
     c = ref.Case(13, [4], [200], 2, 64, 1).fill_fast(scale=30.0)
