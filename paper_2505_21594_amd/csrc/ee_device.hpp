@@ -274,7 +274,7 @@ struct SharedAtt {
         int n, pages, parts;             // members, pages in common, parts these are split into
     } group[ATT_MAX_GROUPS];
     struct Own {
-        short group, from, parts, first; // group or -1; pages that it reads for the session; parts of the others; items of the sessions before
+        int group, from, parts, first;   // group or -1; pages that it reads for the session; parts of the others; items of the sessions before
     } own[EE_MAX_BATCH];
 };
 void launch_shared_attention(const SharedAtt &a, int hd, int own_items, hipStream_t stream);

@@ -72,6 +72,7 @@ struct ee_model {
     const float *ad_bup[EE_MAX_EXITS];
 };
 
+constexpr size_t MARKS_MAX = 16;         // (every pass of a batch looks through them)
 struct ee_session {
     const ee_model *m;
     unsigned flags;
@@ -114,8 +115,8 @@ struct ee_session {
     int head_batch;                  // EE_OPT_HEAD_BATCH: exit heads per launch of the LM head
     bool scatter_pages;              // EE_OPT_SCATTER_PAGES
     int shared_att_opt;              // EE_OPT_SHARED_ATT
-    // What the session has in common with others: (id, n) for every fork its cache has gone through, n ascending.  Sessions that hold the same
-    // id hold the same keys and values at positions 0 .. n - 1 (nothing writes below kv_len; what takes kv_len below n takes the mark away).
+    // What the session has in common with others: (id, n) for every fork its cache has gone through, n ascending, the MARKS_MAX longest.  Sessions that
+    // hold the same id hold the same keys and values at positions 0 .. n - 1 (nothing writes below kv_len; what takes kv_len below n takes the mark away).
     std::vector<std::pair<unsigned long long, int>> marks;
     int pf_gemm_opt, pf_att_opt;     // EE_OPT_PREFILL_GEMM, EE_OPT_PREFILL_ATT_ROWS (0: chosen per launch)
     int flight_row0;                 // first row of this session in the pass in flight
@@ -1029,6 +1030,16 @@ static void attention_splits_by_session(const ee_session *lead, int items_cap, e
     }
 }
 
+static std::vector<std::pair<unsigned long long, int>>::iterator mark_at(ee_session *s, int n)
+{
+    return std::lower_bound(s->marks.begin(), s->marks.end(), n, [](const std::pair<unsigned long long, int> &x, int len) { return x.second < len; });
+}
+static bool has_mark(ee_session *s, const std::pair<unsigned long long, int> &mark)
+{
+    const auto at = mark_at(s, mark.second);
+    return at != s->marks.end() && *at == mark;
+}
+
 // Groups of a batch's sessions that have at least a page in common, most pages saved first; fills g's groups and own[].group / from.
 static void shared_groups(ee_session *const *sessions, int n_sess, SharedAtt &g)
 {
@@ -1038,34 +1049,32 @@ static void shared_groups(ee_session *const *sessions, int n_sess, SharedAtt &g)
     }
     g.n_groups = 0;
     while (g.n_groups < ATT_MAX_GROUPS) {
-        unsigned long long best = 0;
+        std::pair<unsigned long long, int> best = {0, 0};
         int best_pages = 0, best_n = 0;
         for (int i = 0; i < n_sess; ++i) {
             if (g.own[i].group >= 0) continue;
             for (const auto &mark : sessions[i]->marks) {
                 int n = 0;
-                for (int j = 0; j < n_sess; ++j)
-                    n += g.own[j].group < 0 && std::find(sessions[j]->marks.begin(), sessions[j]->marks.end(), mark) != sessions[j]->marks.end();
+                for (int j = 0; j < n_sess && !(j == i && n > 0); ++j)     // (counted already where an earlier session has it)
+                    n += g.own[j].group < 0 && has_mark(sessions[j], mark);
                 const int pages = mark.second / KV_PAGE;
                 if ((n - 1) * pages > (best_n - 1) * best_pages && n > 1) {
-                    best = mark.first;
+                    best = mark;
                     best_pages = pages;
                     best_n = n;
                 }
             }
         }
-        if (!best) break;
+        if (best_n == 0) break;
         SharedAtt::Group &grp = g.group[g.n_groups];
         grp.members = 0;
         grp.n = 0;
         grp.pages = best_pages;
         for (int i = 0; i < n_sess; ++i) {
-            bool has = false;
-            for (const auto &mark : sessions[i]->marks) has |= mark.first == best;
-            if (g.own[i].group >= 0 || !has) continue;
+            if (g.own[i].group >= 0 || !has_mark(sessions[i], best)) continue;
             grp.members |= (unsigned long long)i << (4 * grp.n++);
-            g.own[i].group = (short)g.n_groups;
-            g.own[i].from = (short)best_pages;
+            g.own[i].group = g.n_groups;
+            g.own[i].from = best_pages;
         }
         ++g.n_groups;
     }
@@ -1105,9 +1114,9 @@ static int plan_shared_attention(const ee_session *lead, int items_cap, ee_sessi
             g.group_items += (grp.n * M + 15) / 16 * grp.parts;
         }
         for (int i = 0; i < n_sess; ++i) {
-            g.own[i].first = (short)items;
-            g.own[i].parts = (short)((own_pages[i] + quota - 1) / quota);
-            g.most_own = std::max<int>(g.most_own, g.own[i].parts);
+            g.own[i].first = items;
+            g.own[i].parts = (own_pages[i] + quota - 1) / quota;
+            g.most_own = std::max(g.most_own, g.own[i].parts);
             items += g.own[i].parts;
         }
         const size_t need = (size_t)n_sess * M * H * (g.most_own + g.most_shared) * (hd + 2);
@@ -2332,12 +2341,13 @@ extern "C" int ee_session_fork(ee_session *from, int n, ee_session *to)
     to->kv_len = n;
     // a mark of this fork, unless the session has one at this length already (without memory for it the sessions only share nothing)
     try {
-        auto at = std::lower_bound(from->marks.begin(), from->marks.end(), n, [](const std::pair<unsigned long long, int> &x, int len) { return x.second < len; });
-        if (at == from->marks.end() || at->second != n) {
+        if (mark_at(from, n) == from->marks.end() || mark_at(from, n)->second != n) {
             static std::atomic<unsigned long long> forks{0};
-            at = from->marks.insert(at, {++forks, n});
+            from->marks.insert(mark_at(from, n), {++forks, n});
         }
-        to->marks.assign(from->marks.begin(), at + 1);
+        to->marks.assign(from->marks.begin(), mark_at(from, n) + 1);
+        if (from->marks.size() > MARKS_MAX) from->marks.erase(from->marks.begin());
+        if (to->marks.size() > MARKS_MAX) to->marks.erase(to->marks.begin());
     } catch (const std::bad_alloc &) {
         to->marks.clear();
     }

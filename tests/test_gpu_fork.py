@@ -157,6 +157,37 @@ def test_what_was_cut_off_is_not_shared(tiny):
             s.free()
 
 
+def test_more_forks_than_are_remembered(tiny):
+    """A source of many forks of different lengths still shares its longest ones, and its first ones stay right."""
+    g, o = tiny
+    base = tokens(o, 925, 340)
+    sess = [g.session(500, max_gamma=4, flags=ee.KEEP_LOGITS) for _ in range(4)]
+    osess = [o.session(500) for _ in range(4)]
+    cut = [340, 17, 300, 340]
+    try:
+        sess[0].ee_prefill(base)
+        sess[0].ee_session_fork(17, sess[1])
+        for n in range(34, 300, 11):
+            sess[0].ee_session_fork(n, sess[2])
+        sess[0].ee_session_fork(300, sess[2])
+        sess[2].ee_session_fork(200, sess[3])
+        sess[0].ee_session_fork(340, sess[3])
+        for b in range(4):
+            more = tokens(o, 926, 3 + b, session=b)
+            sess[b].ee_prefill(more, flags=ee.CONTINUE)
+            fo, _ = oracle_prefill(osess[b], base[:cut[b]] + more)
+            sess[b].ee_set_pending(fo)
+        sess[0].ee_session_option(ee.OPT_SHARED_ATT, 2)
+        drafts = [oracle_greedy(osess[b], 4) for b in range(4)]
+        ee.ee_verify_batch(sess, drafts, EXITS)
+        for b in range(4):
+            sess[b].ee_wait_final()
+            check_pass(osess[b].verify(drafts[b], EXITS, want_logits=True), sess[b].final_result(), gpu_logits(sess[b], 1), drafts[b], f"session {b}")
+    finally:
+        for s in sess:
+            s.free()
+
+
 def test_source_freed_first_and_sampled_batch(tiny):
     g, o = tiny
     a = g.session(300, max_gamma=4, flags=ee.SAMPLING)
