@@ -261,6 +261,7 @@ __device__ __forceinline__ double wave_scan_d(double x)
 
 constexpr int ACC_ROWS = 64;            // rows of a sequence whose stats are kept at hand
 
+// (six waves a SIMD cost 12 bytes of spill; four without any: 24 rounds on 100003 tokens 22.0 instead of 20.4 us, one on 32000 12.8 instead of 13.4)
 __global__ void __launch_bounds__(ACC_DRAW, 6) ee_accept_draw_kernel(AcceptDev a)
 {
     __shared__ double ws[ACC_WAVES];
