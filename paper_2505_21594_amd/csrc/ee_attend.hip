@@ -48,14 +48,16 @@ static size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
 
 // Pages of a part for the kernel for many lines: as many parts as give the least time by this estimate, the fewest of those within 5 %.  The largest
 // item's pages, at 0.22 us for each matrix product of a page, or all pages, at two items for a compute unit; parts are written and read again at 1.25
-// MB a microsecond, behind a launch.  us, 32 heads of 128, bf16, 1 / 2 / about 5 parts: 350 rows 16.4 / 20.8 / 23.5, 500 19.8 / 24.5 / 26.8, 350 behind 2000 cached
-// positions 61.5 / 41.6 / 41.4; 700 and 1000 rows behind 2000 69.7 and 76.6 / 58.2 and 67.2 (two parts).
+// MB a microsecond, behind a launch (at twice that where the new rows are all the positions: items then end one after the other).  us, heads of 128,
+// bf16, 32 heads, 1 / 2 / about 5 parts: 350 rows 16.4 / 20.8 / 23.5, 500 19.8 / 24.5 / 26.8, 350 behind 2000 cached positions 61.5 / 41.6 / 41.4; one and two
+// parts: 700 and 1000 rows behind 2000 69.7 / 58.2, 76.6 / 67.2, 1000 rows 31.8 / 31.9; 2041 rows of 16 heads 54.4 / 45.4.
 static int wide_quota(const ee_paged_cache &c, const ee_attend_args &p, int own_pages, long long chunks, int seqs)
 {
     const int step = c.terms == 1 ? 4 : 2;
     const int products = c.terms == 2 ? 10 : p.dtype == EE_BF16 ? 2 : 5;
     const double page = 0.22 * products * c.head_dim / 128, all = (double)chunks * c.n_kv_heads * own_pages * (seqs == 1 ? 1.0 : 0.5) / 512;
-    const double part = (double)p.n_rows * p.n_heads * c.head_dim * 4 / 1.25e6;
+    const double fresh = std::min(1.0, (double)p.n_rows / seqs / (16.0 * own_pages));
+    const double part = (double)p.n_rows * p.n_heads * c.head_dim * 4 / 1.25e6 * (1 - 0.5 * fresh);
     int best_quota = 0;
     double best = 0;
     for (int n = 1; n <= 64; ++n) {

@@ -297,73 +297,64 @@ __device__ __forceinline__ PairMask pair_mask(int pos0, int id0, int id1, int fi
     return m;
 }
 
-// Scores of a tile -> weights in s, with the running maximum and sum brought up to date.  Any number near the maximum serves as well: it is
+// Scores of a tile -> weights in z, with the running maximum and sum brought up to date.  Any number near the maximum serves as well: it is
 // moved (and the output rescaled) only where some line's scores exceed it by ATT_SLACK powers of two, after which weights are at most 2^ATT_SLACK.
+// The scores are therefore taken relative to the number in use right away, and the largest is found among those.
 constexpr float ATT_SLACK = 8.f;
-template <int NP>
-__device__ __forceinline__ float attend_largest(const float (&s)[NP][8], float scale2)
+__device__ __forceinline__ float attend_base(float mx) { return mx == -INFINITY ? 0.f : mx; }
+template <int NP, int RT, int NT>
+__device__ __forceinline__ void attend_raise(AttendState<RT, NT> &st, int t, float local, float (&z)[NP][8])
 {
-    float local = s[0][0];
-#pragma unroll
-    for (int p = 0; p < NP; ++p) local = max3(local, max3(max3(s[p][0], s[p][1], s[p][2]), s[p][3], s[p][4]), max3(s[p][5], s[p][6], s[p][7]));
-    return quads_max(local) * scale2;
-}
-template <int RT, int NT>
-__device__ __forceinline__ void attend_raise(AttendState<RT, NT> &st, int t, float local)
-{
-    const float m = fmaxf(st.mx[t], local), f = m == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(st.mx[t] - m);
+    const float base = attend_base(st.mx[t]), m = fmaxf(st.mx[t], base + local), up = m == -INFINITY ? 0.f : m - base;
+    const float f = m == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(st.mx[t] - m);
     st.mx[t] = m;
     st.sum[t] *= f;
+#pragma unroll
+    for (int p = 0; p < NP; ++p)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) z[p][e] -= up;
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
         for (int r = 0; r < 4; ++r) st.o[t][nt][r] *= f;
 }
 template <int PT, int NP, int RT, int NT>
-__device__ __forceinline__ void attend_exps(AttendState<RT, NT> &st, int t, float (&s)[NP][8], float scale2, bf16x8_t (&P)[NP][PT])
+__device__ __forceinline__ void attend_exps(AttendState<RT, NT> &st, int t, float (&z)[NP][8], bf16x8_t (&P)[NP][PT])
 {
-    const float base = st.mx[t] == -INFINITY ? 0.f : st.mx[t];
 #pragma unroll
     for (int p = 0; p < NP; ++p) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            s[p][e] = __builtin_amdgcn_exp2f(fmaf(s[p][e], scale2, -base));
-            st.sum[t] += s[p][e];
+            z[p][e] = __builtin_amdgcn_exp2f(z[p][e]);
+            st.sum[t] += z[p][e];
         }
-        split_terms<PT>(s[p], P[p]);
+        split_terms<PT>(z[p], P[p]);
     }
 }
 
-// max3 is not an instruction the compiler knows to keep away from a matrix product's results while they are on their way (NaN in a call of many rows
-// showed it): this waits for them.  A 16x16x32 product needs at most 12 wait states; where a select reads the scores first (MASKED) the compiler has seen to it.
-template <int NP>
-__device__ __forceinline__ void products_done(f32x4_t (&S)[NP][2])
-{
-    if constexpr (NP == 1)
-        asm("s_nop 15" : "+v"(S[0][0]), "+v"(S[0][1]));
-    else
-        asm("s_nop 15" : "+v"(S[0][0]), "+v"(S[0][1]), "+v"(S[1][0]), "+v"(S[1][1]));
-}
-
-// A tile's scores of NP pairs as the lane's eights.  MASKED: those that its line does not see are nothing; keep: of the lane's positions of a pair,
-// those that exist.  Returns the largest, scaled.
+// A tile's scores of NP pairs, times scale2 and relative to the running maximum, as the lane's eights.  MASKED: those that its line does not see are
+// nothing; keep: of the lane's positions of a pair, those that exist.  Returns the largest, and in `up` whether the maximum has to move.
 template <bool MASKED, int NP, int RT, int NT>
-__device__ __forceinline__ float attend_scores(AttendState<RT, NT> &st, int t, f32x4_t (&S)[NP][2], const int (&keep)[NP], int pos0, int last, int quad, float scale2,
-                                               float (&s)[NP][8])
+__device__ __forceinline__ float attend_scores(AttendState<RT, NT> &st, int t, const f32x4_t (&S)[NP][2], const int (&keep)[NP], int pos0, int last, int quad, float scale2,
+                                               float (&z)[NP][8], bool &up)
 {
     bool sees = false;
-    if constexpr (!MASKED) products_done<NP>(S);
+    const float base = attend_base(st.mx[t]);
+    float local = -INFINITY;
 #pragma unroll
     for (int p = 0; p < NP; ++p) {
         const int seen = min(keep[p], last - pos0 - p * 32 - quad * 8 + 1);
         sees |= seen > 0;
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            s[p][e] = S[p][e >> 2][e & 3];
-            if constexpr (MASKED) s[p][e] = e < seen ? s[p][e] : -INFINITY;
+            z[p][e] = fmaf(S[p][e >> 2][e & 3], scale2, -base);
+            if constexpr (MASKED) z[p][e] = e < seen ? z[p][e] : -INFINITY;
         }
+#pragma unroll
+        for (int e = 0; e < 8; e += 2) local = fmaxf(fmaxf(local, z[p][e]), z[p][e + 1]);
     }
-    const float local = attend_largest<NP>(s, scale2);
+    local = quads_max(local);
+    up |= local > (st.mx[t] == -INFINITY ? -INFINITY : ATT_SLACK);
     if (local == -INFINITY && (!MASKED || sees)) st.hollow |= 1u << t;     // (counts only where the maximum stays there)
     return local;
 }
@@ -614,17 +605,16 @@ __device__ __forceinline__ void attend_pages(const AttendDev &a, const AttendIte
 #pragma unroll
             for (int t = 0; t < RT; ++t) {
                 local[t] = -INFINITY;
-                if (t < tiles) local[t] = attend_scores<MASKED, 1>(st, t, S[t], keep, pos0, last[t], quad, a.scale2, s[t]);
-                up |= local[t] > st.mx[t] + ATT_SLACK;
+                if (t < tiles) local[t] = attend_scores<MASKED, 1>(st, t, S[t], keep, pos0, last[t], quad, a.scale2, s[t], up);
             }
             if (__any(up)) {
 #pragma unroll
                 for (int t = 0; t < RT; ++t)
-                    if (t < tiles) attend_raise(st, t, local[t]);
+                    if (t < tiles) attend_raise(st, t, local[t], s[t]);
             }
 #pragma unroll
             for (int t = 0; t < RT; ++t)
-                if (t < tiles) attend_exps<PT, 1>(st, t, s[t], a.scale2, P[t]);
+                if (t < tiles) attend_exps<PT, 1>(st, t, s[t], P[t]);
             if constexpr (MASKED)
                 if (mask.masked) attend_clean_v<TERMS>(st, vf, mask, keep[0], pos0, last, quad);
 #pragma unroll
@@ -868,16 +858,15 @@ __global__ void __launch_bounds__(256, QT == 1 ? 2 : 1) ee_attend_wide_kernel(At
             bool up = false;
 #pragma unroll
             for (int t = 0; t < RT; ++t) {
-                local[t] = attend_scores<MASKED, NP>(st, t, S[t], keep, pos0, last[t], quad, a.scale2, s[t]);
-                up |= local[t] > st.mx[t] + ATT_SLACK;
+                local[t] = attend_scores<MASKED, NP>(st, t, S[t], keep, pos0, last[t], quad, a.scale2, s[t], up);
             }
             if (__any(up)) {
 #pragma unroll
-                for (int t = 0; t < RT; ++t) attend_raise(st, t, local[t]);
+                for (int t = 0; t < RT; ++t) attend_raise(st, t, local[t], s[t]);
             }
             bf16x8_t P[RT][NP][PT];
 #pragma unroll
-            for (int t = 0; t < RT; ++t) attend_exps<PT, NP>(st, t, s[t], a.scale2, P[t]);
+            for (int t = 0; t < RT; ++t) attend_exps<PT, NP>(st, t, s[t], P[t]);
 #pragma unroll
             for (int n = 0; n < NP; ++n) {
                 uint4 v[NT][TERMS];

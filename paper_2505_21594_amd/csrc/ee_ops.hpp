@@ -45,14 +45,6 @@ __device__ __forceinline__ void pair32(unsigned x, unsigned &a, unsigned &b)
     a = r[0];
     b = r[1];
 }
-// (written out: of values it knows nothing about the compiler makes every one canonical first, an instruction each.  No operand may come straight
-// from a matrix product: the compiler adds the wait states that this needs only in front of instructions it chose itself)
-__device__ __forceinline__ float max3(float a, float b, float c)
-{
-    float r;
-    asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
-    return r;
-}
 // largest and sum over the lanes l, l ^ 16, l ^ 32, l ^ 48
 __device__ __forceinline__ float quads_max(float x)
 {
