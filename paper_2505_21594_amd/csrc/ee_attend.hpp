@@ -731,7 +731,8 @@ __global__ void __launch_bounds__(ATT_W * 64, 2) ee_attend_kernel(AttendDev a)
 //
 // Four waves have 32 lines each; K and V of a step of 64 positions (32 of a two-term cache) go through LDS for all of them, straight from the
 // records into operand order, the next step's on their way while this one is multiplied.  Two workgroups share a compute unit where the registers allow it:
-// one fills the matrix cores while the other has its exponentials.
+// one fills the matrix cores while the other has its exponentials.  (Heads of 128 spill 40 bytes for that: the results' places, stored before the loop
+// and loaded behind it.)
 
 constexpr int ATT_WIDE = 128;                  // lines of an item
 template <int TERMS>

@@ -1,4 +1,6 @@
 """Sessions forked from one prefix: the copies are exact, and a batch that reads common pages once matches the oracle."""
+import dataclasses
+
 import numpy as np
 import pytest
 
@@ -12,10 +14,11 @@ pytestmark = pytest.mark.gpu
 EXITS = [2]
 
 
-@pytest.fixture(scope="module")
-def tiny(model_dir):
-    p = f"{model_dir}/gpu_tiny_fork.bin"
-    eegen.write_model(p, eegen.TINY, 91, gains="uniform")
+@pytest.fixture(scope="module", params=[64, 128])
+def tiny(model_dir, request):
+    hd = request.param
+    p = f"{model_dir}/gpu_tiny_fork_{hd}.bin"
+    eegen.write_model(p, dataclasses.replace(eegen.TINY, n_heads=eegen.TINY.d_model // hd, head_dim=hd), 91, gains="uniform")
     g = ee.Model(p, max_rows=48)
     yield g, eo.Model(p)
     g.free()
