@@ -15,7 +15,34 @@ GUARD = 0x5A
 
 
 def cache_of(c):
-    return Dev(c.k_pool), Dev(c.v_pool), Dev(c.table)
+    return c.far if hasattr(c, "far") else (Dev(c.k_pool), Dev(c.v_pool), Dev(c.table))
+
+
+class Far:
+    """A pool of n pages in device memory of which the last ones are `pages`."""
+
+    def __init__(self, pages, n):
+        self.shape, self.dtype = (n,) + pages.shape[1:], "bfloat16"
+        self._last = Dev(pages[:1])                              # (its device)
+        self.device, self._count, self._page = self._last.device, len(pages), pages[0].nbytes
+        self._p = ctypes.c_void_p()
+        ok(hip().hipMalloc(ctypes.byref(self._p), n * self._page))
+        ok(hip().hipMemcpy(self._p.value + (n - self._count) * self._page, pages.ctypes.data, pages.nbytes, 1))
+
+    def data_ptr(self):
+        return self._p.value
+
+    def stride(self):
+        return tuple(int(np.prod(self.shape[i + 1:])) for i in range(5))
+
+    def pages(self):
+        out = np.empty((self._count,) + self.shape[1:], np.uint16)
+        ok(hip().hipDeviceSynchronize())
+        ok(hip().hipMemcpy(out.ctypes.data, self._p.value + (self.shape[0] - self._count) * self._page, out.nbytes, 2))
+        return out
+
+    def __del__(self):
+        hip().hipFree(self._p)
 
 
 def workspace(n):
@@ -122,6 +149,7 @@ MANY = [
     ([70, 70, 70], [2000, 71, 500], 2, 2, 128, 2, "fp32", "bf16", (), ()),
     ([66, 70, 1], [300, 290, 220], 4, 4, 128, 1, "bf16", "bf16", [(0, 3)], [13]),
     ([90, 66], [700, 90], 2, 2, 64, 2, "fp32", "fp32", [(0, 2)], [1]),
+    ([40] * 66, [40 + 7 * i for i in range(66)], 1, 1, 64, 1, "bf16", "fp32", (), ()),      # more sequences than lanes
 ]
 
 
@@ -145,6 +173,7 @@ GROUPS = [
     ([2, 2], [3000, 2050], [(0, 2)], [120], 4, 2, 128, 1, "bf16"),
     ([2, 2], [40, 40], [(0, 2)], [0], 4, 2, 128, 1, "bf16"),
     ([0, 0, 3], [32, 32, 50], [(0, 2), (2, 3)], [2, 3], 4, 2, 128, 2, "fp32"),                  # a group without rows, one of one
+    ([1] * 140, [50 + i % 30 for i in range(140)], [(2 * i, 2 * i + 2) for i in range(70)], [2] * 70, 2, 1, 64, 1, "bf16"),   # more groups than lanes
 ]
 
 
@@ -393,6 +422,30 @@ def test_append_bad_pages():
     c = ref.Case(321, [20, 3], [40, 19], 2, 64, 1, table_extra=0).fill()
     c.table[0, 1], c.table[1, 1] = -3, c.n_pages + 4
     run_append(c, 4, "fp32", "fp32", True, 64, False)
+
+
+@pytest.mark.parametrize("rows", [5, 70])
+def test_pools_beyond_32_bits(rows):
+    """Pools of 5.2 GB each, the pages in use behind 2^32 bytes and 2^31 elements."""
+    n = 20000
+    c = ref.Case(18, [rows, 2], [rows + 90, 40], 32, 128, 2, table_extra=0).fill_fast()
+    there = c.table.copy()
+    used = (there >= 0) & (there < c.n_pages)
+    far = Far(np.ascontiguousarray(c.k_pool), n), Far(np.ascontiguousarray(c.v_pool), n)
+    c.far = far + (Dev(np.where(used, there + n - c.n_pages, -1).astype(np.int32)),)
+    got, want, tol = run_attend(c, 32, "fp32", "fp32")
+    close(got, want, tol, "attention")
+    k, v = c.rng.standard_normal((2, rows + 2, 32, 128)).astype(np.float32)
+    rs, kl, dk, dv = Dev(c.row_start), Dev(c.kv_len), Dev(k), Dev(v)
+    ee.ee_kv_append(ee.PagedCache(*c.far), rs, kl, None, dk, dv, None)
+    kp, vp = c.k_pool.copy(), c.v_pool.copy()
+    for s in range(2):
+        for i in range(c.rows[s]):
+            p = c.lens[s] - c.rows[s] + i
+            page, slot, row = there[s, p // 16], p % 16, c.row_start[s] + i
+            kp[page, :, slot] = ref.split(k[row], 2).transpose(1, 0, 2)
+            vp[page, :, :, :, slot] = ref.split(v[row], 2).transpose(1, 0, 2)
+    assert (far[0].pages() == kp).all() and (far[1].pages() == vp).all()
 
 
 # ---------------------------------------------------------------- ee_accept_drafts
