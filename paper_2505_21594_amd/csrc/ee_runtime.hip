@@ -981,6 +981,7 @@ static int attention_splits(const ee_session *lead, int items_cap, int n_sess, i
 //   32 heads of 128   2 sessions, 512 in common (131072 saved) 14.0 / 15.7, 2048 (524288) 30.6 / 24.8
 //                     8 sessions, 128 (229376) 14.4 / 16.9, 256 (458752) 19.6 / 17.1, 1024 52.6 / 24.9, 4096 197 / 59
 //   20 heads of 64    4 sessions, 512 (122880) 11.1 / 12.7, 2048 (491520) 19.4 / 17.2;  8 sessions, 512 (286720) 13.0 / 14.4, 1024 18.5 / 15.2, 4096 65 / 30
+//   4 heads of 64     8 sessions, 4096 (458752) 16.7 / 20.3;  16 sessions of three rows, 2048 (491520) 16.8 / 15.5, 4096 26.5 / 21.2
 constexpr int SHARED_ATT_MIN = 64 * 32 * 128;
 
 // Splits of a batch by session: pages per split are the same for all, so that a session has as many splits as its own pages ask for,
