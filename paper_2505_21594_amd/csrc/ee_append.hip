@@ -2,11 +2,11 @@
 //
 // Bound by bytes (a row's queries, keys and values once in, once out) where there are many rows, by the chain of
 // dependent loads (row -> sequence -> page -> data) where there are few.
-// A block is up to 16 new rows of one sequence that lie on one page.  Its work is dealt to waves in units: a head of queries or keys of 64 / (HD / 16) rows, or a
-// head of values (two of 64).  Queries and keys: a row's head is HD / 16 lanes, each with eight neighbouring elements of either half, so that the partners of
-// a rotation (x_j and x_{j + HD/2}, or neighbours) are in one lane and every access is 16 bytes wide.  Values: the cache holds them transposed ([dim][position]), so a lane takes two dims of all 16 rows, and the
-// wave turns its 64-byte pieces into whole kilobytes through LDS; pages that the new rows cover only partly are written position by position,
-// so that the others stay as they are.
+// A block is up to 16 new rows of one sequence that lie on one page.  Its work is dealt to waves in units: a head of queries or keys of
+// 64 / (HD / 16) rows, or a head of values (two of 64).  Queries and keys: a row's head is HD / 16 lanes, each with eight neighbouring elements of either
+// half, so that the partners of a rotation (x_j and x_{j + HD/2}, or neighbours) are in one lane and every access is 16 bytes wide.  Values: the cache
+// holds them transposed ([dim][position]), so a lane takes two dims of all 16 rows, and the wave turns its 64-byte pieces into whole kilobytes through
+// LDS; pages that the new rows cover only partly are written position by position, so that the others stay as they are.
 // (Units of four heads, which fetch a row's cosines and sines once for all: eight rounds of five rows 7.7 -> 10.1 us, 2041 rows of 32 heads 26.2 -> 28.8.)
 #include "ee_ops.hpp"
 
