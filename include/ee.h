@@ -401,8 +401,8 @@ int ee_debug_div_small(int device, const int32_t *divisors, int n, long long *mi
    Calls that share an output or a workspace must not overlap in time; calls on one stream do not.
 
    A batch is n_seqs sequences whose new rows follow each other in arrays of n_rows rows: sequence s has the rows
-   row_start[s] .. row_start[s+1] - 1 (row_start: int32 [n_seqs + 1], not decreasing, within [0, n_rows]; a sequence may have none), and rows from
-   row_start[n_seqs] on are padding: never written, and what they hold does not matter.  kv_len[s] (int32) counts a sequence's positions, the
+   row_start[s] .. row_start[s+1] - 1 (row_start: int32 [n_seqs + 1], not decreasing, within [0, n_rows]; a sequence may have none).  Rows in front of
+   row_start[0] (of a call for some of a batch's sequences) and from row_start[n_seqs] on are never written, and what they hold does not matter.  kv_len[s] (int32) counts a sequence's positions, the
    new rows' included: the last row is position kv_len[s] - 1. */
 
 /* element types */

@@ -930,8 +930,8 @@ __global__ void __launch_bounds__(256) ee_attend_join_kernel(AttendDev a, int sp
         }
         if (base == sub) {
             const f32x2_t n = as_global(ml)[0];
-            const long long rows = a.b.start(a.b.n_seqs);
-            if (line < rows * a.n_heads) {
+            const long long from = a.b.start(0), rows = a.b.start(a.b.n_seqs);   // (no item has written counts of a row outside)
+            if (line >= from * a.n_heads && line < rows * a.n_heads) {
                 own = __float_as_int(n[0]);
                 shared = own ? __float_as_int(n[1]) : 0;                    // (own 0: written already)
             }
