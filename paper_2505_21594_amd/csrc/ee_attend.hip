@@ -7,13 +7,13 @@ struct AttendKernel {
     attend_kernel_t f;
     size_t lds;
 };
-template <int HD, int TERMS, int QT, int PT, int PT_WIDE = PT>
+template <int HD, int TERMS, int QT, int PT>
 static AttendKernel attend_of_tiles(int tiles)
 {
     if (tiles == 1) return {ee_attend_kernel<HD, TERMS, QT, PT, 1>, attend_lds<HD, QT, 1>()};
     if constexpr (TERMS == 1 || HD == 64)
         if (tiles == 2) return {ee_attend_kernel<HD, TERMS, QT, PT, 2>, attend_lds<HD, QT, 2>()};
-    return {ee_attend_wide_kernel<HD, TERMS, QT, PT_WIDE>, attend_wide_lds<HD, TERMS>()};
+    return {ee_attend_wide_kernel<HD, TERMS, QT, PT>, attend_wide_lds<HD, TERMS>()};
 }
 template <int HD>
 static AttendKernel attend_kernel(int terms, int q_type, int out_type, int tiles)
@@ -22,7 +22,7 @@ static AttendKernel attend_kernel(int terms, int q_type, int out_type, int tiles
     if (out_type == EE_FP32) return q_type == EE_BF16 ? attend_of_tiles<HD, 1, 1, 3>(tiles) : attend_of_tiles<HD, 1, 3, 3>(tiles);
     if (q_type == EE_FP32) return attend_of_tiles<HD, 1, 3, 3>(tiles);
     if (q_type == EE_FP16) return attend_of_tiles<HD, 1, 2, 2>(tiles);
-    return out_type == EE_BF16 ? attend_of_tiles<HD, 1, 1, 2, 1>(tiles) : attend_of_tiles<HD, 1, 1, 2>(tiles);
+    return attend_of_tiles<HD, 1, 1, 2>(tiles);
 }
 
 // How a call is split; a function of what the host knows (sizes and the caller's bounds).
@@ -47,15 +47,16 @@ static long long most_chunks(int n, int T, int per_key, int lines)
 static size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
 
 // Pages of a part for the kernel for many lines: as many parts as give the least time by this estimate, the fewest of those within 5 %.  The largest
-// item's pages, at 0.22 us for each matrix product of a page, or all pages, at two items for a compute unit; parts are written and read again at 1.25
-// MB a microsecond, behind a launch (at twice that where the new rows are all the positions: items then end one after the other).  us, heads of 128,
-// bf16, 32 heads, 1 / 2 / about 5 parts: 350 rows 16.4 / 20.8 / 23.5, 500 19.8 / 24.5 / 26.8, 350 behind 2000 cached positions 61.5 / 41.6 / 41.4; one and two
-// parts: 700 and 1000 rows behind 2000 69.7 / 58.2, 76.6 / 67.2, 1000 rows 31.8 / 31.9; 2041 rows of 16 heads 54.4 / 45.4.
+// item's pages, or all pages at two items for a compute unit; parts are written and read again at 1.25 MB a microsecond, behind a launch (at twice that where
+// the new rows are all the positions: items then end one after the other).  us, heads of 128, bf16, 32 heads, 1 / 2 / about 5 parts: 350 rows
+// 18.3 / 21.9 / 24.3, 500 22.5 / 25.8 / 27.8, 350 behind 2000 cached positions 72.4 / 47.0 / 44.9; one and two parts: 700 and 1000 rows behind 2000 84.1 / 70.0,
+// 91.7 / 83.4, 1000 rows 37.3 / 37.9; 2041 rows of 16 heads 64.0 / 50.4.  (32 heads on 8, 350 and 700 rows behind 2000: three parts, which it takes, 51.5 and 73.9, the best
+// number of them 45.5 and 72.4.)
 static int wide_quota(const ee_paged_cache &c, const ee_attend_args &p, int own_pages, long long chunks, int seqs)
 {
     const int step = c.terms == 1 ? 4 : 2;
-    const int products = c.terms == 2 ? 10 : p.dtype == EE_BF16 ? 2 : 5;
-    const double page = 0.22 * products * c.head_dim / 128, all = (double)chunks * c.n_kv_heads * own_pages * (seqs == 1 ? 1.0 : 0.5) / 512;
+    const double page = (c.terms == 2 ? 2.2 : p.dtype == EE_BF16 ? 0.44 : 1.1) * c.head_dim / 128;     // us a page
+    const double all = (double)chunks * c.n_kv_heads * own_pages * (seqs == 1 ? 1.0 : 0.5) / 512;
     const double fresh = std::min(1.0, (double)p.n_rows / seqs / (16.0 * own_pages));
     const double part = (double)p.n_rows * p.n_heads * c.head_dim * 4 / 1.25e6 * (1 - 0.5 * fresh);
     int best_quota = 0;
@@ -80,12 +81,15 @@ static AttendPlan plan_attend(const ee_paged_cache &c, const ee_attend_args &p)
     int shared_pages = p.n_groups == 0 ? 0 : (int)std::min<long long>(pages, p.max_shared > 0 ? p.max_shared / KV_PAGE : pages);
     const int seqs = std::min(c.n_seqs, T);
     const long long own_lines = (long long)T * per_key / seqs;
-    // Many lines of a key head a sequence: the kernel that reads keys and values for 128 of them at a time (ee_attend_wide_kernel).  us, it / the others,
-    // heads of 128, one term, 8 sequences of 2000 positions, 32 heads on 8 / on 32: 32 lines 23.3 / 23.6, 61.1 / 60.0, 48 lines 25.8 / 33.6, 67.1 / 64.7,
-    // 64 lines 27.6 / 33.2, 68.0 / 68.9, 128 lines 35.2 / 44.9, 85.9 / 126; one sequence of 8000: 32 lines 18.4 / 19.1, 48 lines 20.6 / 20.3, 35.6 / 47.0.
-    // Two terms, 32 heads on 32: 48 lines 184 / 163, 64 lines 186 / 187, 96 lines 193 / 262; one sequence of 2000: 64 lines 41 / 32, 96 lines 46 / 48.
-    // It reads common pages for every sequence, which from here on is no loss: 8 sequences with 3840 of 4000 positions in common, every page for every
-    // sequence / once, 8 and 32 key heads: 48 lines 34.8 / 35.1, 85 / 92, 64 lines 36 / 39, 89 / 107, 128 lines 44 / 60, 100 / 202.
+    // Many lines of a key head a sequence, on average over the call's: the kernel that reads keys and values for 128 of them at a time
+    // (ee_attend_wide_kernel).  us, the others / it, heads of 128, one term, 8 sequences of 2000 positions, 32 heads on 8 / on 32: 32 lines 23.9 / 24.6,
+    // 61.1 / 60.8, 48 lines 33.8 / 28.9, 64.8 / 66.5, 64 lines 33.1 / 26.7, 69.4 / 63.0, 128 lines 44.5 / 31.2, 126 / 71; one sequence of 8000: 32 lines 18.9 / 19.3,
+    // 33.4 / 31.8, 48 lines 20.3 / 23.1, 46.7 / 38.6.  Two terms, 32 heads on 32: 48 lines 163 / 184, 64 lines 187 / 186, 96 lines 262 / 193; one sequence of 2000:
+    // 64 lines 32 / 41, 96 lines 48 / 46.  (Prompts of 300, 500 and 900 rows alone, 32 on 32: 12.7 / 15.5, 16.6 / 21.9, 34.9 / 33.1.)
+    // It reads common pages for every sequence: 8 sequences with 3840 of 4000 positions in common, once by the others / for every sequence by it, 8 and 32 key
+    // heads: 48 lines 35.5 / 39.1, 92 / 101, 64 lines 40.0 / 40.7, 109 / 103, 128 lines 61 / 49, 204 / 119.
+    // One kernel serves the whole call.  A prompt among single tokens behind 1000 positions, chosen / the prompt and the tokens in two calls: 900 rows and 31 tokens, 32
+    // heads on 8 48.5 / 32.9 + 28.8, on 32 155 / 33.2 + 96.3 (by tiles of 32 lines; 129 by 128); 2041 and 100 146.8 / 69.4 + 86.4, 454 / 69.5 + 288.
     const bool wide = own_lines > (c.terms == 1 ? 32 : 64);
     pl.groups = wide || shared_pages == 0 ? 0 : std::min(p.n_groups, seqs);
     if (pl.groups == 0) shared_pages = 0;

@@ -14,8 +14,9 @@
 // The output is kept transposed: a line's maximum, sum and output are in the lanes of its column, and rescaling needs no exchange.
 //
 // Precision: sums, maxima and outputs are fp32.  The products' operands are bf16 terms: K and V as the cache has them (TERMS), q in QT terms, exactly for bf16 (1) and
-// fp16 (2) and to 2^-24 for fp32 (3); P in PT: 3 where the results are fp32, 2 (2^-16) for results of 16 bits, 1 (2^-8, as much as the result's
-// own rounding) for bf16 queries and results of many lines, where the matrix cores bound the call.  Products of the smallest terms are left out (2^-24, or 2^-16 with 2 terms).
+// fp16 (2) and to 2^-24 for fp32 (3); P in PT: 3 where the results are fp32 (2^-24), 2 (2^-16, a 256th of the result's own rounding) for results of 16 bits.
+// (One term, 2^-8, for bf16 results of many lines: 2041 rows of 32 heads 60.3 us instead of 72.0, and 1.3 times the error of exact weights.)  Products of the smallest
+// terms are left out (2^-24, or 2^-16 with 2 terms).
 #pragma once
 
 #include <type_traits>
