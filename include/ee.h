@@ -177,7 +177,8 @@ int ee_session_free(ee_session *s);
    kv_len = n.  With EE_HOLD_LAST (the paper's first round, where the drafts
    follow the prompt directly): kv_len = n-1, pending = tokens[n-1], no head is
    evaluated and *first_token is left alone.  Resets the session first; with EE_CONTINUE the rows follow the
-   kv_len positions that it has instead (all n of them: a pending token that is to stay is the first of the new ones).
+   kv_len positions that it has instead (all n of them: a pending token that is to stay is the first of the new ones),
+   and a pass in flight that failed is reported (EE_EDEVICE, nothing is cached) where a prompt of its own would give it up.
    tokens: n ids in [0, vocab). */
 int ee_prefill(ee_session *s, const int32_t *tokens, int n, unsigned flags, int32_t *first_token);
 /* Same, with n_emb rows of bf16[d_model] (raw uint16, row-major) placed before

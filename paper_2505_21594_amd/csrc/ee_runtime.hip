@@ -1701,11 +1701,11 @@ extern "C" int ee_prefill_embeds(ee_session *s, const uint16_t *emb_bf16, int n_
     if (!hold && total < 1) return fail(EE_EINVAL, "ee_prefill: empty prompt");
     if (total + 1 > s->max_ctx) return fail(EE_ECAPACITY, "ee_prefill: %d rows do not fit max_ctx %d", total, s->max_ctx);
     HIP_TRY(hipSetDevice(m->device));
+    const bool more = (flags & EE_CONTINUE) != 0;
     int rc = finish_flight(s);
-    if (rc != EE_OK && rc != EE_EDEVICE) return rc;
+    if (rc != EE_OK && (rc != EE_EDEVICE || more)) return rc;   // (with EE_CONTINUE the rows would stand behind positions that the failed pass has not committed)
     HIP_TRY(hipStreamSynchronize(s->stream));
     s->run_stream = s->stream;
-    const bool more = (flags & EE_CONTINUE) != 0;
     if (!more) reset_cache(s);
     const int base = s->kv_len;   // the first row's position
     if (base + total + 1 > s->max_ctx) return fail(EE_ECAPACITY, "ee_prefill: %d rows behind %d positions do not fit max_ctx %d", total, base, s->max_ctx);
