@@ -1101,7 +1101,7 @@ static int plan_shared_attention(const ee_session *lead, int items_cap, ee_sessi
         read += g.group[i].pages;
         longest = std::max(longest, g.group[i].pages);
     }
-    if (lead->shared_att_opt == 0 && (all - read) * H * hd < SHARED_ATT_MIN) return 0;
+    if (lead->shared_att_opt == 0 && (long long)(all - read) * H * hd < SHARED_ATT_MIN) return 0;
     // parts: the fewest pages each (multiples of 8: a pair for each wave) that leave at most two items for a compute unit, as the partials' room allows
     const size_t room = (size_t)items_cap * att_item(hd);
     for (int quota = 8;; quota += 8) {
