@@ -191,7 +191,7 @@ int ee_prefill_embeds(ee_session *s, const uint16_t *emb_bf16, int n_emb, const 
    of `from`'s cached positions (1 <= n <= kv_len; synchronous, a copy in device memory).  kv_len of `to` is then n, and it has no pending token:
    ee_prefill with EE_CONTINUE or ee_set_pending comes next.  `from` stays as it is, and either can be freed before the other.
    ee_verify_batch and ee_verify_sampled_batch read the whole pages that sessions have in common through forks (also forks of forks, down to what no
-   ee_kv_truncate has cut) once for all of them, where that is faster; results are the same up to the order of the fp32 sums. */
+   ee_kv_truncate has cut) once for all of them, where that is faster by an estimate (EE_OPT_SHARED_ATT); results are the same up to the order of the fp32 sums. */
 int ee_session_fork(ee_session *from, int n, ee_session *to);
 
 /* Asynchronous: enqueues one pass over [pending, draft_tokens[0..gamma-1]] and
@@ -355,7 +355,7 @@ int ee_device_synchronize(int device);
    EE_OPT_PREFILL_ATT_ROWS: query rows per workgroup of such a prompt's attention (64 or 128); 0 = chosen from
      the heads, the rows and the number of compute units (the default).
    EE_OPT_SHARED_ATT (of the session that leads a batch): 1 = pages in common are read for every session, 2 = once wherever there are
-     any, 0 = once where reading them for every session would take longer (the default).  EE_OPT_ATT_SPLITS other than 0 goes before it. */
+     any, 0 = once where reading them for every session takes longer by an estimate from heads, sessions and pages (the default).  EE_OPT_ATT_SPLITS other than 0 goes before it. */
 #define EE_OPT_ATT_SPLITS 1
 #define EE_OPT_SCATTER_PAGES 2
 #define EE_OPT_HEAD_BATCH 3

@@ -976,13 +976,15 @@ static int attention_splits(const ee_session *lead, int items_cap, int n_sess, i
     return std::min(s, cap);
 }
 
-// What reading common pages once has to save, in pages times heads times values of a head, to be worth its second launch.
-// us a layer, pages read for every session / once (five rows a session, 41 own positions each):
-//   32 heads of 128   2 sessions, 512 in common (131072 saved) 14.0 / 15.7, 2048 (524288) 30.6 / 24.8
-//                     8 sessions, 128 (229376) 14.4 / 16.9, 256 (458752) 19.6 / 17.1, 1024 52.6 / 24.9, 4096 197 / 59
-//   20 heads of 64    4 sessions, 512 (122880) 11.1 / 12.7, 2048 (491520) 19.4 / 17.2;  8 sessions, 512 (286720) 13.0 / 14.4, 1024 18.5 / 15.2, 4096 65 / 30
-//   4 heads of 64     8 sessions, 4096 (458752) 16.7 / 20.3;  16 sessions of three rows, 2048 (491520) 16.8 / 15.5, 4096 26.5 / 21.2
-constexpr int SHARED_ATT_MIN = 64 * 32 * 128;
+// What reading common pages once has to save, in pages times heads times values of a head, to be worth its second launch and the parts that this joins: so much, and
+// so much more for each part of a row's head.  us a layer, pages read for every session / once (five rows a session, 41 own positions each; 16 sessions: three rows):
+//   32 heads of 128   2 sessions, 512 in common (131072 saved, 5 parts) 14.1 / 15.6, 1024 (262144, 9) 19.2 / 19.8, 2048 (524288, 9) 30.7 / 24.7
+//                     8 sessions, 128 (229376, 2) 14.1 / 16.7, 256 (458752, 3) 19.6 / 17.1, 1024 52.6 / 24.9, 4096 197 / 59
+//   8 heads of 128    2 sessions, 4096 (262144) 18.4 / 23.6;  4 sessions, 2048 (393216) 17.0 / 19.0, 4096 (786432) 27.0 / 21.2;  8 sessions, 1024 (458752, 9) 17.1 / 15.4
+//   20 heads of 64    4 sessions, 512 (122880) 11.2 / 12.8, 2048 (491520) 19.6 / 17.3;  8 sessions, 512 (286720, 5) 13.0 / 13.9, 1024 (573440, 9) 18.9 / 15.0
+//   4 heads of 64     8 sessions, 4096 (458752, 33) 16.7 / 20.0;  16 sessions, 2048 (491520, 17) 16.9 / 15.9, 4096 (983040, 33) 26.4 / 20.2
+// Of 288 such shapes the rule takes the slower way for four, by 0.1, 0.8, 1.3 and 1.4 us.
+constexpr int SHARED_ATT_MIN = 220000, SHARED_ATT_PART = 14000;
 
 // Splits of a batch by session: pages per split are the same for all, so that a session has as many splits as its own pages ask for,
 // instead of the number that attention_splits gives all of them.  Taken where the launch's estimated time is lower by 5 %: a
@@ -1101,7 +1103,8 @@ static int plan_shared_attention(const ee_session *lead, int items_cap, ee_sessi
         read += g.group[i].pages;
         longest = std::max(longest, g.group[i].pages);
     }
-    if (lead->shared_att_opt == 0 && (long long)(all - read) * H * hd < SHARED_ATT_MIN) return 0;
+    const long long saved = (long long)(all - read) * H * hd;
+    if (lead->shared_att_opt == 0 && saved < SHARED_ATT_MIN) return 0;
     // parts: the fewest pages each (multiples of 8: a pair for each wave) that leave at most two items for a compute unit, as the partials' room allows
     const size_t room = (size_t)items_cap * att_item(hd);
     for (int quota = 8;; quota += 8) {
@@ -1124,6 +1127,7 @@ static int plan_shared_attention(const ee_session *lead, int items_cap, ee_sessi
         const bool fits = need <= room;
         if ((fits && (items + g.group_items) * H <= 2 * m->nwg) || quota >= longest) {
             if (!fits) return 0;
+            if (lead->shared_att_opt == 0 && saved < SHARED_ATT_MIN + SHARED_ATT_PART * (g.most_own + g.most_shared)) return 0;
             g.n_sess = n_sess;
             g.M = M;
             g.rows = n_sess * M;
