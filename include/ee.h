@@ -429,7 +429,7 @@ typedef struct {
                         rotated) for the pairs (a, b) = (x_j, x_{j + head_dim/2}), or (x_2j, x_2j+1) with rope_pairs = 1;
      queries  -> q_out (may be q where type and strides agree);  keys and values -> their positions' places in the cache.
    fp32 arithmetic, one rounding to the type stored.  q, k, v are of type `dtype`, q_out of q_out_dtype; strides count elements from row to
-   row and from head to head, a head's elements are contiguous; every row and head starts at a multiple of 16 bytes.  n_heads may be
+   row and from head to head, a head's elements are contiguous; every row and head starts at a multiple of 16 bytes (strides of a single row or head say nothing).  n_heads may be
    0 (keys and values only).  Rows whose position is negative, or beyond the page table or the rope table, get zeros in q_out and no
    place in the cache.  The places of two sequences' new rows must differ. */
 typedef struct {

@@ -501,6 +501,16 @@ def _vector(t, what: str, kind: str, device, n: int) -> int:
     return t.data_ptr()
 
 
+def _contiguous(t) -> bool:
+    """Whether an array's elements follow each other (the stride of a dimension of one says nothing)."""
+    at = 1
+    for size, stride in zip(reversed(t.shape), reversed(t.stride())):
+        if size > 1 and stride != at:
+            return False
+        at *= size
+    return True
+
+
 def _heads(t, what: str, rows, heads, dim: int, device):
     """(address, type, row stride, head stride, rows, heads) of [rows][heads][dim] with contiguous heads."""
     shape, s = t.shape, t.stride()
@@ -525,16 +535,12 @@ class PagedCache:
         device = _on(k_pool, "k_pool")
         self.device = k_pool.device
         for t, what in ((k_pool, "k_pool"), (v_pool, "v_pool")):
-            want, at = [], 1
-            for size in reversed(t.shape):
-                want.append(at)
-                at *= size
-            if _type(t) != "bfloat16" or tuple(t.stride()) != tuple(reversed(want)) or t.device != self.device:
+            if _type(t) != "bfloat16" or not _contiguous(t) or t.device != self.device:
                 raise ValueError(f"{what}: contiguous bf16 on {self.device} expected")
-        if len(page_table.shape) != 2 or _type(page_table) != "int32" or page_table.device != self.device or page_table.stride()[1] != 1:
+        if len(page_table.shape) != 2 or _type(page_table) != "int32" or page_table.device != self.device:
             raise ValueError("page_table: int32 [n_seqs][entries] expected")
         self.n_kv_heads, self.head_dim, self.n_seqs = heads, dim, page_table.shape[0]
-        if self.n_seqs > 1 and page_table.stride()[0] != page_table.shape[1]:
+        if not _contiguous(page_table):
             raise ValueError("page_table: contiguous expected")
         self.k_pool, self.v_pool, self.page_table = k_pool, v_pool, page_table
         self.c = PagedCacheC(device, heads, dim, terms, n, self.n_seqs, page_table.shape[1], 0, k_pool.data_ptr(), v_pool.data_ptr(), page_table.data_ptr())
@@ -558,7 +564,7 @@ def ee_kv_append(cache: PagedCache, row_start, kv_len, q, k, v, q_out, q_gain=No
     rp = positions = 0
     if rope is not None:
         shape = rope.shape
-        if len(shape) != 3 or shape[1] != dim // 2 or shape[2] != 2 or _type(rope) != "float32" or rope.device != dev or tuple(rope.stride()) != (dim, 2, 1):
+        if len(shape) != 3 or shape[1] != dim // 2 or shape[2] != 2 or _type(rope) != "float32" or rope.device != dev or not _contiguous(rope):
             raise ValueError(f"rope: contiguous fp32 [positions][{dim // 2}][2] on {dev} expected")
         rp, positions = rope.data_ptr(), shape[0]
     a = _APPEND_PACK(kind, kind_o, heads, rows, positions, 1 if rope_pairs else 0, eps, 0, _vector(row_start, "row_start", "int32", dev, n + 1),

@@ -306,18 +306,21 @@ extern "C" int ee_kv_append(const ee_paged_cache *c, const ee_append_args *p, vo
     if (!(p->eps >= 0.f) || !isfinite(p->eps)) return fail(EE_EINVAL, "%s: eps must not be negative", call);
     if (p->rope_pairs != 0 && p->rope_pairs != 1) return fail(EE_EINVAL, "%s: rope_pairs %d is neither 0 nor 1", call, p->rope_pairs);
     if (p->rope && p->rope_len < 1) return fail(EE_EINVAL, "%s: rope_len %d", call, p->rope_len);
-    for (int64_t s : {p->k_stride, p->k_head_stride, p->v_stride, p->v_head_stride})
-        if (!stride_ok(s, p->dtype)) return fail(EE_EINVAL, "%s: stride %lld keeps no 16-byte alignment", call, (long long)s);
-    if (p->n_heads)
-        for (int i = 0; i < 4; ++i) {
-            const int64_t s = i == 0 ? p->q_stride : i == 1 ? p->q_head_stride : i == 2 ? p->q_out_stride : p->q_out_head_stride;
-            if (!stride_ok(s, i < 2 ? p->dtype : p->q_out_dtype)) return fail(EE_EINVAL, "%s: stride %lld keeps no 16-byte alignment", call, (long long)s);
-        }
+    const struct {
+        int64_t stride;
+        int type, n;
+    } strides[8] = {{p->k_stride, p->dtype, p->n_rows},    {p->k_head_stride, p->dtype, c->n_kv_heads},    {p->v_stride, p->dtype, p->n_rows},
+                    {p->v_head_stride, p->dtype, c->n_kv_heads}, {p->q_stride, p->dtype, p->n_rows},        {p->q_head_stride, p->dtype, p->n_heads},
+                    {p->q_out_stride, p->q_out_dtype, p->n_rows}, {p->q_out_head_stride, p->q_out_dtype, p->n_heads}};
+    for (int i = 0; i < (p->n_heads ? 8 : 4); ++i)
+        if (!stride_ok(strides[i].stride, strides[i].type, strides[i].n))
+            return fail(EE_EINVAL, "%s: stride %lld keeps no 16-byte alignment", call, (long long)strides[i].stride);
     if (c->n_seqs == 0 || p->n_rows == 0) return EE_OK;
     if (!p->k || !p->v || (p->n_heads && (!p->q || !p->q_out))) return fail(EE_EINVAL, "%s: null q, k, v or q_out", call);
     for (const void *x : {p->q, p->k, p->v, (const void *)p->q_out, (const void *)p->q_gain, (const void *)p->k_gain, (const void *)p->rope})
         if (!aligned(x, 16)) return fail(EE_EINVAL, "%s: q, k, v, q_out, gains and rope must be 16-byte aligned", call);
-    if (p->n_heads && p->q == p->q_out && (p->dtype != p->q_out_dtype || p->q_stride != p->q_out_stride || p->q_head_stride != p->q_out_head_stride))
+    if (p->n_heads && p->q == p->q_out && (p->dtype != p->q_out_dtype || (p->n_rows > 1 && p->q_stride != p->q_out_stride) ||
+                                           (p->n_heads > 1 && p->q_head_stride != p->q_out_head_stride)))
         return fail(EE_EINVAL, "%s: q_out may be q only with the same type and strides", call);
 
     AppendDev a;

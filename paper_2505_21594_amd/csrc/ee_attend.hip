@@ -169,8 +169,8 @@ extern "C" int ee_attend(const ee_paged_cache *c, const ee_attend_args *p, void 
     static const char *const call = "ee_attend";
     int rc = check_attend(call, c, p);
     if (rc != EE_OK) return rc;
-    if (!stride_ok(p->q_stride, p->dtype) || !stride_ok(p->q_head_stride, p->dtype) || !stride_ok(p->out_stride, p->out_dtype) ||
-        !stride_ok(p->out_head_stride, p->out_dtype))
+    if (!stride_ok(p->q_stride, p->dtype, p->n_rows) || !stride_ok(p->q_head_stride, p->dtype, p->n_heads) || !stride_ok(p->out_stride, p->out_dtype, p->n_rows) ||
+        !stride_ok(p->out_head_stride, p->out_dtype, p->n_heads))
         return fail(EE_EINVAL, "%s: a stride keeps no 16-byte alignment", call);
     if (c->n_seqs == 0 || p->n_rows == 0) return EE_OK;
     if (!p->q || !p->out || (p->n_groups && (!p->group_start || !p->group_pages))) return fail(EE_EINVAL, "%s: null q, out, group_start or group_pages", call);

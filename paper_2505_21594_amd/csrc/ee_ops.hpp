@@ -187,8 +187,8 @@ __device__ __forceinline__ void store8(int type, void *base, size_t at, const fl
 
 inline size_t size_of_type(int type) { return type == EE_FP32 ? 4 : 2; }
 inline bool aligned(const void *p, size_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) == 0; }
-// a row or head stride: its multiples keep 16-byte alignment
-inline bool stride_ok(int64_t stride, int type) { return stride >= 0 && stride < (int64_t)1 << 40 && stride * (int64_t)size_of_type(type) % 16 == 0; }
+// a stride of n rows or heads: its multiples keep 16-byte alignment (of one row or head it says nothing)
+inline bool stride_ok(int64_t stride, int type, int n) { return n <= 1 || (stride >= 0 && stride < (int64_t)1 << 40 && stride * (int64_t)size_of_type(type) % 16 == 0); }
 
 // The GPU that a call works on is current inside it, the caller's again after it.
 struct DeviceScope {
