@@ -633,4 +633,4 @@ def ee_accept_drafts(logits, row_start, drafts, draft_probs, u, v, temperature, 
     """logits [rows][vocab], drafts int32 [rows], draft_probs fp32 [rows][vocab] or None, u and v fp32 [rows], temperature fp32 [sequences];
     results accept_len, next_token int32 [sequences]."""
     a = _accept_args(logits, row_start, drafts, draft_probs, u, v, temperature, accept_len, next_token)
-    _check((_lib or load_library()).ee_accept_drafts(a, _vector(workspace, "workspace", "uint8", logits.device, 0), workspace.shape[0], stream))
+    _check((_lib or load_library()).ee_accept_drafts(a, _vector(workspace, "workspace", "uint8", logits.device, 0), 0 if workspace is None else workspace.shape[0], stream))
