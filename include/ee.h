@@ -400,6 +400,8 @@ int ee_debug_div_small(int device, const int32_t *divisors, int n, long long *mi
    be captured into a graph, and what a call is given has to stay until its kernels are done.  Lengths, tables and tokens are read
    by the kernels: the host checks sizes, types, strides and alignment (EE_EINVAL before anything is enqueued), the kernels bounds.
    Calls that share an output or a workspace must not overlap in time; calls on one stream do not.
+   Sizes (EE_EINVAL beyond them): 2^20 sequences, 2^24 rows, 4096 key heads, and of ee_attend 65535 chunks of up to 128 lines (16 or 32 where lines are few) times parts;
+   65535 sequences, 65535 rows and a vocabulary of 2^24 of ee_accept_drafts.
 
    A batch is n_seqs sequences whose new rows follow each other in arrays of n_rows rows: sequence s has the rows
    row_start[s] .. row_start[s+1] - 1 (row_start: int32 [n_seqs + 1], not decreasing, within [0, n_rows]; a sequence may have none).  Rows in front of
