@@ -499,6 +499,126 @@ typedef struct {
 int ee_accept_workspace(const ee_accept_args *args, size_t *bytes);
 int ee_accept_drafts(const ee_accept_args *args, void *workspace, size_t workspace_bytes, void *stream);
 
+/* ------------------------------------------------------------------ operators around the LM head
+   What teaches an exit head (its adapters, norm and head matrix, or a draft model's) what the target says, and what reports the target's answer: linear layers and
+   norms with their gradients, scores of tokens, distillation.  As the operators above: DEVICE pointers, a caller's stream, nothing allocated, copied or
+   waited for, host checks before anything is enqueued.  A row stride counts elements (of a single row it says nothing); every result is written whole and depends on
+   nothing but its inputs (sums are taken in one order).  Outputs are arrays of their own unless said otherwise: one that overlaps an input in part gives
+   nothing meaningful. */
+#define EE_MAX_TOP 64            /* tokens of a row's list                               */
+
+/* ee_score_tokens: with  log p_i = logits_i / temperature - log sum_j exp(logits_j / temperature)  for every row
+     logprob   [n_rows]       log p of tokens[row] (int32; -infinity for one outside [0, vocab)); NULL: not wanted
+     entropy   [n_rows]       - sum_i p_i log p_i;                                                NULL: not wanted
+     top_ids, top_logprobs [n_rows][top]  the `top` (0 .. EE_MAX_TOP) largest logits, largest first, of equal ones the lower token, and their log p.
+   Tokens whose logit is -infinity (masked ones) have no part in a row; where fewer than `top` are left the list ends with -1 and -infinity.  A row
+   without a softmax (NaN, +infinity or nothing but -infinity among its logits) gets NaN, and -1 for its tokens.
+   logits [n_rows][vocab] of type `dtype` at any alignment of the type, sums in fp32 for each thread and 64 bits from there; results fp32, int32.  n_rows up to 2^20, vocab
+   up to 2^24 (EE_EINVAL where rows times parts of rows pass 2^24).
+   workspace: ee_score_workspace bytes (may be 0), 256-byte aligned; contents do not matter. */
+typedef struct {
+    int32_t device, dtype, n_rows, vocab, top;
+    float temperature;
+    const void *logits;
+    int64_t logits_stride;
+    const int32_t *tokens;
+    float *logprob, *entropy;
+    int32_t *top_ids;
+    float *top_logprobs;
+} ee_score_args;
+int ee_score_workspace(const ee_score_args *args, size_t *bytes);
+int ee_score_tokens(const ee_score_args *args, void *workspace, size_t workspace_bytes, void *stream);
+
+/* ee_distill: how far a student's distribution q = softmax(logits / temperature) is from a teacher's most likely tokens ids [n_rows][top] with
+   log-probabilities logprobs [n_rows][top] (what ee_score_tokens gives, at the same temperature), p = exp(logprobs), and the gradient of that:
+     rest = 1:  loss = sum_j p_j (log p_j - log q_j) + pi (log pi - log rho),  pi = max(1 - sum_j p_j, 0), rho = the sum of q over the tokens that the list
+                does not name (they are one class);
+                d loss / d logits_i = (q_i - p_i) / temperature for the list's, q_i (1 - pi / rho) / temperature for the others;
+     rest = 0:  p is divided by its sum;  loss = sum_j p_j (log p_j - log q_j),  d loss / d logits_i = (q_i - p_i) / temperature
+                (with top = 1 and logprobs = 0: the cross entropy of a label).
+   Entries whose id is not in [0, vocab) or whose log-probability is -infinity are not there (a list without any: loss 0, gradient 0); a token that is named
+   twice has the sum of both probabilities.
+   loss fp32 [n_rows], or NULL;  d_logits [n_rows][vocab] of type grad_dtype, or NULL: d_loss[row] (fp32 [n_rows]; NULL: 1) times the gradient; rows whose
+   d_loss is 0 get zeros, whatever their logits are.  d_logits may be logits (same type and stride).  A row without a softmax has loss and gradient NaN.  A student that
+   gives a named token, or all the others where pi > 0, no probability (-infinity) has an infinite loss; its gradient is finite (0 where q is).  Sums in fp32 for
+   each thread and 64 bits from there, everything that a row has once in 64 bits.  n_rows up to 2^20, vocab up to 2^24 (EE_EINVAL where rows times parts of rows pass 2^22).
+   workspace: ee_distill_workspace bytes (may be 0), 256-byte aligned; contents do not matter. */
+typedef struct {
+    int32_t device, dtype, grad_dtype, n_rows, vocab, top, rest;
+    float temperature;
+    const void *logits;
+    int64_t logits_stride;
+    const int32_t *ids;
+    const float *logprobs;
+    float *loss;
+    const float *d_loss;
+    void *d_logits;
+    int64_t d_logits_stride;
+} ee_distill_args;
+int ee_distill_workspace(const ee_distill_args *args, size_t *bytes);
+int ee_distill(const ee_distill_args *args, void *workspace, size_t workspace_bytes, void *stream);
+
+/* ee_norm: y = (x - mu) / sqrt(mean((x - mu)^2) + eps) * gain + bias  for every row of `dim` elements; mu = mean(x) with center = 1 (layer norm), 0 with
+   center = 0 (RMS norm, what the models here use).  gain, bias: fp32 [dim], or NULL (1, 0).  x of type dtype, y of out_dtype, at any alignment of their types; y may be
+   x (same type and stride).  fp32 arithmetic, one rounding.
+   ee_norm_grad: dx, and d_gain, d_bias (fp32 [dim], the sums over the rows; written, not added to), each NULL where it is not wanted, from x and dy; the row's statistics are formed
+   again.  dx may be x or dy (same type and stride).  workspace (for d_gain, d_bias): ee_norm_grad_workspace bytes, 256-byte aligned; contents do not matter. */
+#define EE_NORM_MAX_DIM 16384
+#define EE_NORM_MAX_ROWS (1 << 21)
+typedef struct {
+    int32_t device, dtype, out_dtype, n_rows, dim, center;
+    float eps;
+    int32_t reserved;
+    const void *x;
+    const float *gain, *bias;
+    void *y;
+    int64_t x_stride, y_stride;
+} ee_norm_args;
+typedef struct {
+    int32_t device, dtype, dy_dtype, dx_dtype, n_rows, dim, center;
+    float eps;
+    const void *x, *dy;
+    const float *gain;
+    void *dx;
+    float *d_gain, *d_bias;
+    int64_t x_stride, dy_stride, dx_stride;
+} ee_norm_grad_args;
+int ee_norm(const ee_norm_args *args, void *stream);
+int ee_norm_grad_workspace(const ee_norm_grad_args *args, size_t *bytes);
+int ee_norm_grad(const ee_norm_grad_args *args, void *workspace, size_t workspace_bytes, void *stream);
+
+/* ee_linear: z = x weight^T + bias,  y = act(z) + residual.  x [n_rows][n_in] and weight [n_out][n_in] of type dtype (EE_BF16, EE_FP16), bias fp32 [n_out] or NULL,
+   residual [n_rows][n_out] of residual_dtype or NULL (it may be y, with the same type and stride), y of out_dtype; pre: z rounded to dtype, what ee_linear_grad
+   needs where there is an activation, or NULL.  fp32 sums, one rounding of each result.  An exit's adapters are two such calls (the down matrices stacked, EE_ACT_SILU; the up
+   matrices side by side, residual h).
+   ee_linear_grad: dz = dy act'(pre);  dx = dz weight,  d_weight = dz^T x,  d_bias = sum over the rows of dz (fp32; written, not added to), each NULL where it is not wanted.  (The residual's
+   gradient is dy.)  dy and pre are of type dtype; dz is rounded to dtype where the result is of 16 bits, and is two (fp16) or three (bf16) terms of it where that is fp32.
+   Every row starts at a multiple of 16 bytes.  Any sizes up to EE_LINEAR_MAX, odd ones too.
+   workspace: bytes by the _workspace calls (may be 0), 256-byte aligned; contents do not matter. */
+#define EE_ACT_NONE 0
+#define EE_ACT_SILU 1            /* z / (1 + exp(-z))                                    */
+#define EE_ACT_GELU 2            /* z Phi(z), Phi the normal distribution function       */
+#define EE_LINEAR_MAX (1 << 22)
+typedef struct {
+    int32_t device, dtype, out_dtype, residual_dtype, act, n_rows, n_in, n_out;
+    const void *x, *weight;
+    const float *bias;
+    const void *residual;
+    void *y, *pre;
+    int64_t x_stride, weight_stride, residual_stride, y_stride, pre_stride;
+} ee_linear_args;
+typedef struct {
+    int32_t device, dtype, dx_dtype, dw_dtype, act, n_rows, n_in, n_out;
+    const void *x, *weight, *dy, *pre;
+    void *dx, *d_weight;
+    float *d_bias;
+    int64_t x_stride, weight_stride, dy_stride, pre_stride, dx_stride, dw_stride;
+} ee_linear_grad_args;
+int ee_linear_workspace(const ee_linear_args *args, size_t *bytes);
+int ee_linear(const ee_linear_args *args, void *workspace, size_t workspace_bytes, void *stream);
+int ee_linear_grad_workspace(const ee_linear_grad_args *args, size_t *bytes);
+int ee_linear_grad(const ee_linear_grad_args *args, void *workspace, size_t workspace_bytes, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

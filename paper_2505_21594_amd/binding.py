@@ -32,6 +32,8 @@ TIME_LAUNCHES = 16
 FORM_AUTO, FORM_PLAIN, FORM_PACKED = 0, 1, 2
 OPT_ATT_SPLITS, OPT_SCATTER_PAGES, OPT_HEAD_BATCH, OPT_PREFILL_GEMM, OPT_PREFILL_ATT_ROWS, OPT_SHARED_ATT = 1, 2, 3, 4, 5, 6
 BF16, FP16, FP32 = 0, 1, 2
+ACT_NONE, ACT_SILU, ACT_GELU = 0, 1, 2
+EE_MAX_TOP, EE_NORM_MAX_DIM, EE_NORM_MAX_ROWS, EE_LINEAR_MAX = 64, 16384, 1 << 21, 1 << 22
 LAUNCH_NAMES = ("qkv", "o", "gu", "dn", "head", "adapter_down", "adapter_up", "embed", "att", "sample")
 
 EXPORTS = [
@@ -42,6 +44,8 @@ EXPORTS = [
     "ee_verify_sampled_batch", "ee_debug_logits", "ee_debug_mfma_layout", "ee_debug_div_small", "ee_tune_k_split", "ee_device_synchronize", "ee_session_option",
     "ee_launch_times", "ee_debug_copy", "ee_exit_pop", "ee_exit_order", "ee_latency_model",
     "ee_kv_append", "ee_attend", "ee_attend_workspace", "ee_accept_drafts", "ee_accept_workspace",
+    "ee_score_tokens", "ee_score_workspace", "ee_distill", "ee_distill_workspace", "ee_norm", "ee_norm_grad", "ee_norm_grad_workspace",
+    "ee_linear", "ee_linear_workspace", "ee_linear_grad", "ee_linear_grad_workspace",
 ]
 
 
@@ -109,6 +113,38 @@ class AcceptArgsC(ctypes.Structure):
         ("probs_stride", ctypes.c_int64)] + [(k, ctypes.c_void_p) for k in ("u", "v", "temperature", "accept_len", "next_token")]
 
 
+class ScoreArgsC(ctypes.Structure):
+    _fields_ = [(k, ctypes.c_int32) for k in ("device", "dtype", "n_rows", "vocab", "top")] + [("temperature", ctypes.c_float), ("logits", ctypes.c_void_p),
+                ("logits_stride", ctypes.c_int64)] + [(k, ctypes.c_void_p) for k in ("tokens", "logprob", "entropy", "top_ids", "top_logprobs")]
+
+
+class DistillArgsC(ctypes.Structure):
+    _fields_ = [(k, ctypes.c_int32) for k in ("device", "dtype", "grad_dtype", "n_rows", "vocab", "top", "rest")] + [("temperature", ctypes.c_float), ("logits", ctypes.c_void_p),
+                ("logits_stride", ctypes.c_int64)] + [(k, ctypes.c_void_p) for k in ("ids", "logprobs", "loss", "d_loss", "d_logits")] + [("d_logits_stride", ctypes.c_int64)]
+
+
+class NormArgsC(ctypes.Structure):
+    _fields_ = [(k, ctypes.c_int32) for k in ("device", "dtype", "out_dtype", "n_rows", "dim", "center")] + [("eps", ctypes.c_float), ("reserved", ctypes.c_int32)] + [
+        (k, ctypes.c_void_p) for k in ("x", "gain", "bias", "y")] + [(k, ctypes.c_int64) for k in ("x_stride", "y_stride")]
+
+
+class NormGradArgsC(ctypes.Structure):
+    _fields_ = [(k, ctypes.c_int32) for k in ("device", "dtype", "dy_dtype", "dx_dtype", "n_rows", "dim", "center")] + [("eps", ctypes.c_float)] + [
+        (k, ctypes.c_void_p) for k in ("x", "dy", "gain", "dx", "d_gain", "d_bias")] + [(k, ctypes.c_int64) for k in ("x_stride", "dy_stride", "dx_stride")]
+
+
+class LinearArgsC(ctypes.Structure):
+    _fields_ = [(k, ctypes.c_int32) for k in ("device", "dtype", "out_dtype", "residual_dtype", "act", "n_rows", "n_in", "n_out")] + [
+        (k, ctypes.c_void_p) for k in ("x", "weight", "bias", "residual", "y", "pre")] + [
+        (k, ctypes.c_int64) for k in ("x_stride", "weight_stride", "residual_stride", "y_stride", "pre_stride")]
+
+
+class LinearGradArgsC(ctypes.Structure):
+    _fields_ = [(k, ctypes.c_int32) for k in ("device", "dtype", "dx_dtype", "dw_dtype", "act", "n_rows", "n_in", "n_out")] + [
+        (k, ctypes.c_void_p) for k in ("x", "weight", "dy", "pre", "dx", "d_weight", "d_bias")] + [
+        (k, ctypes.c_int64) for k in ("x_stride", "weight_stride", "dy_stride", "pre_stride", "dx_stride", "dw_stride")]
+
+
 _lib = None
 
 
@@ -171,6 +207,10 @@ def load_library():
     lib.ee_attend.argtypes = [vp, vp, vp, sz, vp]
     lib.ee_accept_workspace.argtypes = [vp, P(sz)]
     lib.ee_accept_drafts.argtypes = [vp, vp, sz, vp]
+    for name in ("score", "distill", "norm_grad", "linear", "linear_grad"):
+        getattr(lib, f"ee_{name}_workspace").argtypes = [vp, P(sz)]
+        getattr(lib, "ee_score_tokens" if name == "score" else f"ee_{name}").argtypes = [vp, vp, sz, vp]
+    lib.ee_norm.argtypes = [vp, vp]
     for name in EXPORTS:
         if name != "ee_last_error":
             getattr(lib, name).restype = ci
@@ -634,3 +674,163 @@ def ee_accept_drafts(logits, row_start, drafts, draft_probs, u, v, temperature, 
     results accept_len, next_token int32 [sequences]."""
     a = _accept_args(logits, row_start, drafts, draft_probs, u, v, temperature, accept_len, next_token)
     _check((_lib or load_library()).ee_accept_drafts(a, _vector(workspace, "workspace", "uint8", logits.device, 0), 0 if workspace is None else workspace.shape[0], stream))
+
+
+# ---------------------------------------------------------------- operators around the LM head
+
+_SCORE_PACK = struct.Struct("@5ifPq5P").pack
+_DISTILL_PACK = struct.Struct("@7ifPq5Pq").pack
+_NORM_PACK = struct.Struct("@6ifi4P2q").pack
+_NORM_GRAD_PACK = struct.Struct("@7if6P3q").pack
+_LINEAR_PACK = struct.Struct("@8i6P5q").pack
+_LINEAR_GRAD_PACK = struct.Struct("@8i7P6q").pack
+
+
+def _rows(t, what: str, rows, width, device):
+    """(address, type, row stride, rows, width) of [rows][width] with contiguous rows; None: nothing."""
+    if t is None:
+        return 0, FP32, 0, rows, width
+    shape, s = t.shape, t.stride()
+    kind = _FLOATS.get(_type(t))
+    if len(shape) != 2 or (rows is not None and shape[0] != rows) or (width is not None and shape[1] != width) or (shape[1] > 1 and s[1] != 1):
+        raise ValueError(f"{what}: [{rows if rows is not None else 'rows'}][{width if width is not None else 'width'}] with contiguous rows expected")
+    if kind is None or t.device != device:
+        raise ValueError(f"{what}: bf16, fp16 or fp32 on {device} expected")
+    return t.data_ptr(), kind, s[0], shape[0], shape[1]
+
+
+def _lists(t, what: str, kind: str, device, rows: int, top: int) -> int:
+    """Address of a contiguous array [rows][top] (None: 0)."""
+    if t is None:
+        return 0
+    if tuple(t.shape) != (rows, top) or _type(t) != kind or t.device != device or not _contiguous(t):
+        raise ValueError(f"{what}: contiguous {kind} [{rows}][{top}] on {device} expected")
+    return t.data_ptr()
+
+
+def _space(workspace, device):
+    return (0, 0) if workspace is None else (_vector(workspace, "workspace", "uint8", device, 0), workspace.shape[0])
+
+
+def _bytes_of(call, args) -> int:
+    n = ctypes.c_size_t()
+    _check(call(args, ctypes.byref(n)))
+    return int(n.value)
+
+
+def _score_args(logits, tokens, logprob, entropy, top_ids, top_logprobs, top, temperature) -> bytes:
+    dev = logits.device
+    zp, kind, zs, rows, V = _rows(logits, "logits", None, None, dev)
+    return _SCORE_PACK(_on(logits, "logits"), kind, rows, V, top, temperature, zp, zs, _vector(tokens, "tokens", "int32", dev, rows), _vector(logprob, "logprob", "float32", dev, rows),
+                       _vector(entropy, "entropy", "float32", dev, rows), _lists(top_ids, "top_ids", "int32", dev, rows, top),
+                       _lists(top_logprobs, "top_logprobs", "float32", dev, rows, top))
+
+
+def ee_score_workspace(logits, top: int = 0) -> int:
+    """Bytes of workspace for calls of ee_score_tokens with these sizes."""
+    return _bytes_of(load_library().ee_score_workspace, _score_args(logits, None, None, None, None, None, top, 1.0))
+
+
+def ee_score_tokens(logits, tokens=None, logprob=None, entropy=None, top_ids=None, top_logprobs=None, temperature: float = 1.0, workspace=None, stream: int = 0) -> None:
+    """logits [rows][vocab], tokens int32 [rows]; results logprob, entropy fp32 [rows], top_ids int32 and top_logprobs fp32 [rows][top], each None where it is
+    not wanted."""
+    top = 0 if top_ids is None else top_ids.shape[-1]
+    a = _score_args(logits, tokens, logprob, entropy, top_ids, top_logprobs, top, temperature)
+    _check((_lib or load_library()).ee_score_tokens(a, *_space(workspace, logits.device), stream))
+
+
+def _distill_args(logits, ids, logprobs, loss, d_loss, d_logits, top, rest, temperature) -> bytes:
+    dev = logits.device
+    zp, kind, zs, rows, V = _rows(logits, "logits", None, None, dev)
+    gp, kind_g, gs, _, _ = _rows(d_logits, "d_logits", rows, V, dev)
+    return _DISTILL_PACK(_on(logits, "logits"), kind, kind_g, rows, V, top, 1 if rest else 0, temperature, zp, zs, _lists(ids, "ids", "int32", dev, rows, top),
+                         _lists(logprobs, "logprobs", "float32", dev, rows, top), _vector(loss, "loss", "float32", dev, rows),
+                         _vector(d_loss, "d_loss", "float32", dev, rows), gp, gs)
+
+
+def ee_distill_workspace(logits, top: int) -> int:
+    """Bytes of workspace for calls of ee_distill with these sizes."""
+    return _bytes_of(load_library().ee_distill_workspace, _distill_args(logits, None, None, None, None, None, top, True, 1.0))
+
+
+def ee_distill(logits, ids, logprobs, loss=None, d_loss=None, d_logits=None, rest: bool = True, temperature: float = 1.0, workspace=None, stream: int = 0) -> None:
+    """logits [rows][vocab], ids int32 and logprobs fp32 [rows][top]; results loss fp32 [rows] and d_logits [rows][vocab] (times d_loss fp32 [rows]), each None
+    where it is not wanted."""
+    a = _distill_args(logits, ids, logprobs, loss, d_loss, d_logits, ids.shape[-1], rest, temperature)
+    _check((_lib or load_library()).ee_distill(a, *_space(workspace, logits.device), stream))
+
+
+def ee_norm(x, y, gain=None, bias=None, eps: float = 1e-5, center: bool = False, stream: int = 0) -> None:
+    """x, y [rows][dim]; gain, bias fp32 [dim]; center: layer norm instead of RMS norm."""
+    dev = x.device
+    xp, kind, xs, rows, dim = _rows(x, "x", None, None, dev)
+    yp, kind_y, ys, _, _ = _rows(y, "y", rows, dim, dev)
+    a = _NORM_PACK(_on(x, "x"), kind, kind_y, rows, dim, 1 if center else 0, eps, 0, xp, _vector(gain, "gain", "float32", dev, dim), _vector(bias, "bias", "float32", dev, dim), yp, xs, ys)
+    _check((_lib or load_library()).ee_norm(a, stream))
+
+
+def _norm_grad_args(x, dy, dx, gain, d_gain, d_bias, eps, center) -> bytes:
+    dev = x.device
+    xp, kind, xs, rows, dim = _rows(x, "x", None, None, dev)
+    up, kind_u, us, _, _ = _rows(dy, "dy", rows, dim, dev)
+    gp, kind_g, gs, _, _ = _rows(dx, "dx", rows, dim, dev)
+    return _NORM_GRAD_PACK(_on(x, "x"), kind, kind_u, kind_g, rows, dim, 1 if center else 0, eps, xp, up, _vector(gain, "gain", "float32", dev, dim), gp,
+                           _vector(d_gain, "d_gain", "float32", dev, dim), _vector(d_bias, "d_bias", "float32", dev, dim), xs, us, gs)
+
+
+def ee_norm_grad_workspace(x) -> int:
+    """Bytes of workspace for calls of ee_norm_grad with these sizes."""
+    return _bytes_of(load_library().ee_norm_grad_workspace, _norm_grad_args(x, None, None, None, None, None, 0.0, False))
+
+
+def ee_norm_grad(x, dy, dx=None, gain=None, d_gain=None, d_bias=None, eps: float = 1e-5, center: bool = False, workspace=None, stream: int = 0) -> None:
+    """x, dy [rows][dim] and ee_norm's gain, eps and center; results dx [rows][dim], d_gain and d_bias fp32 [dim], each None where it is not wanted."""
+    a = _norm_grad_args(x, dy, dx, gain, d_gain, d_bias, eps, center)
+    _check((_lib or load_library()).ee_norm_grad(a, *_space(workspace, x.device), stream))
+
+
+def _linear_args(x, weight, y, bias, act, residual, pre) -> bytes:
+    dev = x.device
+    xp, kind, xs, rows, n_in = _rows(x, "x", None, None, dev)
+    wp, kind_w, ws, n_out, _ = _rows(weight, "weight", None, n_in, dev)
+    yp, kind_y, ys, _, _ = _rows(y, "y", rows, n_out, dev)
+    rp, kind_r, rs, _, _ = _rows(residual, "residual", rows, n_out, dev)
+    pp, kind_p, ps, _, _ = _rows(pre, "pre", rows, n_out, dev)
+    if kind_w != kind or (pre is not None and kind_p != kind):
+        raise ValueError("x, weight and pre must be of one type")
+    return _LINEAR_PACK(_on(x, "x"), kind, kind_y, kind_r, act, rows, n_in, n_out, xp, wp, _vector(bias, "bias", "float32", dev, n_out), rp, yp, pp, xs, ws, rs, ys, ps)
+
+
+def ee_linear_workspace(x, weight) -> int:
+    """Bytes of workspace for calls of ee_linear with these sizes."""
+    return _bytes_of(load_library().ee_linear_workspace, _linear_args(x, weight, None, None, ACT_NONE, None, None))
+
+
+def ee_linear(x, weight, y, bias=None, act: int = ACT_NONE, residual=None, pre=None, workspace=None, stream: int = 0) -> None:
+    """x [rows][n_in], weight [n_out][n_in], bias fp32 [n_out], residual, y and pre [rows][n_out]."""
+    a = _linear_args(x, weight, y, bias, act, residual, pre)
+    _check((_lib or load_library()).ee_linear(a, *_space(workspace, x.device), stream))
+
+
+def _linear_grad_args(x, weight, dy, pre, act, dx, d_weight, d_bias) -> bytes:
+    dev = x.device
+    xp, kind, xs, rows, n_in = _rows(x, "x", None, None, dev)
+    wp, kind_w, ws, n_out, _ = _rows(weight, "weight", None, n_in, dev)
+    up, kind_u, us, _, _ = _rows(dy, "dy", rows, n_out, dev)
+    pp, kind_p, ps, _, _ = _rows(pre, "pre", rows, n_out, dev)
+    gp, kind_g, gs, _, _ = _rows(dx, "dx", rows, n_in, dev)
+    hp, kind_h, hs, _, _ = _rows(d_weight, "d_weight", n_out, n_in, dev)
+    if kind_w != kind or (dy is not None and kind_u != kind) or (pre is not None and kind_p != kind):
+        raise ValueError("x, weight, dy and pre must be of one type")
+    return _LINEAR_GRAD_PACK(_on(x, "x"), kind, kind_g, kind_h, act, rows, n_in, n_out, xp, wp, up, pp, gp, hp, _vector(d_bias, "d_bias", "float32", dev, n_out), xs, ws, us, ps, gs, hs)
+
+
+def ee_linear_grad_workspace(x, weight, act: int = ACT_NONE) -> int:
+    """Bytes of workspace for calls of ee_linear_grad with these sizes, whatever the results' types."""
+    return _bytes_of(load_library().ee_linear_grad_workspace, _linear_grad_args(x, weight, None, None, act, None, None, None))
+
+
+def ee_linear_grad(x, weight, dy, pre=None, act: int = ACT_NONE, dx=None, d_weight=None, d_bias=None, workspace=None, stream: int = 0) -> None:
+    """dy and pre [rows][n_out]; results dx [rows][n_in], d_weight [n_out][n_in], d_bias fp32 [n_out], each None where it is not wanted."""
+    a = _linear_grad_args(x, weight, dy, pre, act, dx, d_weight, d_bias)
+    _check((_lib or load_library()).ee_linear_grad(a, *_space(workspace, x.device), stream))

@@ -7,7 +7,7 @@
 //   2. draw: with a row's parts joined (Z), the keep tests; of the row that ends the round, every part's sum of max(q - p, 0); the
 //      sequence's workgroup that arrives last finds the part in which the sum over the parts passes v * sum, and in it the token.
 // All sums are taken in one order whatever the launch: results do not depend on timing.
-#include "ee_ops.hpp"
+#include "ee_vocab.hpp"
 
 namespace ee {
 
@@ -41,23 +41,6 @@ struct AcceptDev {
     __device__ __forceinline__ int start(int s) const { return min(max(as_global(row_start)[s], 0), n_rows); }
 };
 
-// Neighbouring elements at any alignment of the element type; past the end of the row: `fill`.
-template <int N, typename T>
-__device__ __forceinline__ void load_some(const T *p, int n, float fill, float (&x)[N])
-{
-    if (n >= N) {
-        typedef T some_t __attribute__((ext_vector_type(N), aligned(sizeof(T))));
-        const some_t e = *(const EE_GLOBAL some_t *)as_global(p);
-#pragma unroll
-        for (int i = 0; i < N; ++i) x[i] = (float)e[i];
-    } else {
-#pragma unroll
-        for (int i = 0; i < N; ++i) {
-            x[i] = fill;
-            if (i < n) x[i] = (float)as_global(p)[i];
-        }
-    }
-}
 template <int N>
 __device__ __forceinline__ void load_logits(const AcceptDev &a, int row, int first, float (&z)[N])
 {
@@ -108,38 +91,6 @@ __device__ __forceinline__ Scale scale_of(float t, float m)
 }
 __device__ __forceinline__ double term(const Scale &s, float z) { return exp2_down(((double)z - s.m) * s.c); }
 
-__device__ __forceinline__ double join_d(unsigned lo, unsigned hi) { return __longlong_as_double((long long)((unsigned long long)hi << 32 | lo)); }
-template <int CTRL, int ROWS = 0xF>
-__device__ __forceinline__ double dpp_d(double x)
-{
-    const unsigned long long b = (unsigned long long)__double_as_longlong(x);
-    return join_d((unsigned)dpp<CTRL, ROWS>(0, (int)(unsigned)b), (unsigned)dpp<CTRL, ROWS>(0, (int)(unsigned)(b >> 32)));
-}
-// sum over a wave, in every lane, always in the same order
-__device__ __forceinline__ double wave_sum_d(double x)
-{
-    x += dpp_d<DPP_XOR1>(x);
-    x += dpp_d<DPP_XOR2>(x);
-    x += dpp_d<DPP_HALF_MIRROR>(x);
-    x += dpp_d<DPP_MIRROR>(x);
-    unsigned la, lb, ha, hb;
-    unsigned long long b = (unsigned long long)__double_as_longlong(x);
-    pair16((unsigned)b, la, lb);
-    pair16((unsigned)(b >> 32), ha, hb);
-    x = join_d(la, ha) + join_d(lb, hb);
-    b = (unsigned long long)__double_as_longlong(x);
-    pair32((unsigned)b, la, lb);
-    pair32((unsigned)(b >> 32), ha, hb);
-    return join_d(la, ha) + join_d(lb, hb);
-}
-__device__ __forceinline__ float wave_max_f(float x)
-{
-    x = fmaxf(x, __int_as_float(dpp<DPP_XOR1>(0, __float_as_int(x))));
-    x = fmaxf(x, __int_as_float(dpp<DPP_XOR2>(0, __float_as_int(x))));
-    x = fmaxf(x, __int_as_float(dpp<DPP_HALF_MIRROR>(0, __float_as_int(x))));
-    x = fmaxf(x, __int_as_float(dpp<DPP_MIRROR>(0, __float_as_int(x))));
-    return quads_max(x);
-}
 // Rule by a sequence's temperature: 0: sampled, 1: greedy, 2: nothing is kept or drawn.
 __device__ __forceinline__ int rule_of(float t) { return t == 0.f ? 1 : t > 0.f && t < INFINITY ? 0 : 2; }
 
@@ -245,18 +196,6 @@ __device__ __forceinline__ void load_probs(const AcceptDev &a, int row, int firs
 #pragma unroll
         for (int i = 0; i < N; ++i) p[i] = first + i == draft ? 1.f : 0.f;
     }
-}
-
-// inclusive sums over the lanes of a wave
-__device__ __forceinline__ double wave_scan_d(double x)
-{
-    x += dpp_d<DPP_SHR + 1>(x);
-    x += dpp_d<DPP_SHR + 2>(x);
-    x += dpp_d<DPP_SHR + 4>(x);
-    x += dpp_d<DPP_SHR + 8>(x);
-    x += dpp_d<DPP_BCAST15, 0xA>(x);
-    x += dpp_d<DPP_BCAST31, 0xC>(x);
-    return x;
 }
 
 constexpr int ACC_ROWS = 64;            // rows of a sequence whose stats are kept at hand
@@ -425,8 +364,6 @@ __global__ void __launch_bounds__(ACC_DRAW, 6) ee_accept_draw_kernel(AcceptDev a
     __syncthreads();
     answer(i, found != 0x7FFFFFFF ? found : max(positive, 0));
 }
-
-static size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
 
 struct AcceptSpace {
     size_t weights, arrived, bytes;    // (rows come first)

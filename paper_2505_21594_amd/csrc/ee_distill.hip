@@ -1,0 +1,393 @@
+// ee_distill: the divergence of a student's distribution q = softmax(z / T) from a teacher's most likely tokens, and its gradient.
+//
+//   rest = 1:  L = sum_j p_j (log p_j - log q_j) + pi (log pi - log rho),  pi = 1 - sum p_j,  rho = the sum of q over the tokens that the list does not name;
+//              dL/dz_i = (q_i - p_i) / T for those it names, q_i (1 - pi / rho) / T for the others;
+//   rest = 0:  p divided by its sum;  L = sum_j p_j (log p_j - log q_j),  dL/dz_i = (q_i - p_i) / T.
+//
+// Bound by the logits' bytes, read once, and the gradient's, written once: a workgroup holds its row in registers (RowPart) from the sums to the gradient.
+// Rows that are too few to fill the chip, or too long for a workgroup, are taken in parts by two launches, of which the second reads the logits again.
+// The tokens that the list names are marked in LDS, one bit each, a thread's bits in one word, and left out of the sums: rho is a sum of its own, not
+// a difference.  With m' and S' the others' maximum and sum, M the row's maximum and A = exp((m' - M) / T) / S their share's scale, rho = A S' and
+// q_i (1 - pi / rho) = exp((z_i - m') / T) (A - pi / S').  Everything that a row has once is in 64 bits: the loss is a small difference of large terms.
+#include "ee_vocab.hpp"
+
+namespace ee {
+
+struct DistillPart {
+    double sum;                        // sum exp((z - m) / T) over the tokens that the list does not name
+    float m, unused;                   // their maximum
+};
+
+struct DistillDev {
+    const void *logits;
+    const int *ids;
+    const float *logprobs, *d_loss;
+    float *loss;
+    void *d_logits;
+    DistillPart *part;                 // [n_rows][parts]
+    float *z;                          // [n_rows][top]  logits of the list's tokens
+    long long stride, grad_stride;
+    int type, grad_type, V, top, rest, parts, length;
+    float c;                           // log2(e) / T
+    double inv_t;
+};
+
+// The teacher's list of a row: a lane of a wave for each entry.
+struct Entry {
+    int id;                            // -1: no entry
+    float z;
+    double lp;
+};
+__device__ __forceinline__ Entry entry_of(const DistillDev &a, int row, int lane)
+{
+    Entry e = {-1, 0.f, 0.0};
+    if (lane < a.top) {
+        const size_t at = (size_t)row * a.top + lane;
+        const int id = as_global(a.ids)[at];
+        const float lp = as_global(a.logprobs)[at];
+        if (id >= 0 && id < a.V && lp != -INFINITY) {
+            e.id = id;
+            e.lp = (double)lp;
+        }
+    }
+    return e;
+}
+
+__device__ __forceinline__ double readlane_d(double x, int l)
+{
+    const unsigned long long b = (unsigned long long)__double_as_longlong(x);
+    return join_d((unsigned)__builtin_amdgcn_readlane((int)(unsigned)b, l), (unsigned)__builtin_amdgcn_readlane((int)(unsigned)(b >> 32), l));
+}
+
+// A row's numbers from the others' maximum and sum and from its list; one wave calls it.
+struct RowTerms {
+    double loss;
+    float others;                      // gradient of a token that the list does not name: others * exp((z - m') / T)
+    float mine;                        // gradient of the lane's token
+    bool first;                        // the lane's token is named here for the first time
+};
+__device__ __forceinline__ RowTerms row_terms(const DistillDev &a, const Entry &e, float m_rest, double s_rest, double weight)
+{
+    RowTerms r;
+    const bool in = e.id >= 0;
+    const double p = in ? exp(e.lp) : 0.0;
+    // a token that is named twice has both probabilities
+    double both = 0.0;
+    r.first = in;
+    int distinct = 0;
+    const int lane = threadIdx.x & 63;
+    for (int i = 0; i < a.top; ++i) {
+        const int id = __builtin_amdgcn_readlane(e.id, i);
+        if (id >= 0 && id == e.id) {
+            both += readlane_d(p, i);
+            if (i < lane) r.first = false;
+        }
+    }
+    distinct = __popcll(__ballot(r.first));
+    const float M = fmaxf(m_rest, wave_max_f(in ? e.z : -INFINITY));
+    const double top = M == -INFINITY ? 0.0 : (double)M;
+    const double z = ((double)e.z - top) * a.inv_t, q1 = in ? exp(z) : 0.0;
+    const double down = m_rest == -INFINITY ? 0.0 : exp(((double)m_rest - top) * a.inv_t);
+    const double S = wave_sum_d(r.first ? q1 : 0.0) + (s_rest != 0.0 ? s_rest * down : 0.0);
+    const bool valid = S > 0.0 && S < INFINITY;
+    const double share = wave_sum_d(p), lse = log(S), A = down / S;
+    double others, scale = 1.0, shift = 0.0, tail = 0.0;
+    if (a.rest) {
+        const double pi = share < 1.0 ? 1.0 - share : share >= 1.0 ? 0.0 : share;        // (NaN stays)
+        others = A;
+        if (pi != 0.0 && distinct < a.V) {
+            others = s_rest > 0.0 ? A - pi / s_rest : 0.0;
+            tail = s_rest > 0.0 ? pi * (log(pi) - (((double)m_rest - top) * a.inv_t + log(s_rest) - lse)) : (double)INFINITY;
+            if (s_rest != s_rest || pi != pi) others = tail = (double)NAN;
+        }
+    } else {
+        scale = share > 0.0 ? 1.0 / share : share == 0.0 ? 0.0 : (double)NAN;
+        shift = share > 0.0 ? log(share) : 0.0;
+        others = share == 0.0 ? 0.0 : A;
+    }
+    const double term = in && p != 0.0 && scale != 0.0 ? p * scale * (e.lp - shift - (z - lse)) : 0.0;
+    r.loss = wave_sum_d(term) + tail;
+    double g = share == 0.0 && !a.rest ? 0.0 : q1 / S - both * scale;
+    if (!valid) r.loss = others = g = (double)NAN;
+    r.others = (float)(others * weight);
+    r.mine = (float)(g * weight);
+    return r;
+}
+
+enum DistillMode { WHOLE = 0, STATS = 1, GRAD = 2 };
+
+template <int TYPE, int E, int NT, int MODE>
+__global__ void __launch_bounds__(NT) ee_distill_kernel(DistillDev a)
+{
+    typedef RowPart<TYPE, E, NT> Part;
+    constexpr int N = Part::N, WAVES = NT / 64;
+    __shared__ uint32_t named[NT * E / 4];                   // a byte for each chunk, a bit for each of its elements
+    __shared__ float wm[WAVES];
+    __shared__ double ws[WAVES];
+    __shared__ float others_s, m_s;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int row = a.parts == 1 ? blockIdx.x : blockIdx.x / a.parts, part = a.parts == 1 ? 0 : blockIdx.x - row * a.parts;
+    const int first = part * a.length, len = min(a.length, a.V - first);
+    const void *logits = row_at(a.logits, TYPE, (size_t)row * a.stride);
+    Part z;
+    z.load(row_at(logits, TYPE, first), len, tid);
+    Entry e = {-1, 0.f, 0.0};
+    if (wave == 0) {
+        e = entry_of(a, row, lane);
+        if (e.id >= 0) e.z = MODE == GRAD ? as_global(a.z)[(size_t)row * a.top + lane] : logit_at(TYPE, logits, e.id);
+        if (MODE == STATS && part == 0 && lane < a.top) as_global_mut(a.z)[(size_t)row * a.top + lane] = e.z;
+    }
+#pragma unroll
+    for (int i = 0; i < E / 4; ++i) named[i * NT + tid] = 0;
+    __syncthreads();
+    const int at = e.id - first;
+    if (e.id >= 0 && at >= 0 && at < len) {
+        const int q = at / N, byte = (q % NT) * E + q / NT;
+        atomicOr(&named[byte / 4], 1u << (byte % 4 * 8 + at % N));
+    }
+    __syncthreads();
+    uint32_t marks[E / 4];
+#pragma unroll
+    for (int i = 0; i < E / 4; ++i) marks[i] = named[tid * (E / 4) + i];
+    auto marked = [&](int c) { return marks[c / 4] >> (c % 4 * 8) & 255u; };
+
+    float m_rest;
+    if constexpr (MODE != GRAD) {
+        float m = -INFINITY;
+#pragma unroll
+        for (int c = 0; c < E; ++c) {
+            float x[N];
+            z.chunk(c, x);
+            const uint32_t b = marked(c);
+            if (b) {
+#pragma unroll
+                for (int i = 0; i < N; ++i)
+                    if (!(b >> i & 1)) m = fmaxf(m, x[i]);
+            } else {
+#pragma unroll
+                for (int i = 0; i < N; ++i) m = fmaxf(m, x[i]);
+            }
+        }
+        const float ref = m == -INFINITY ? 0.f : m;
+        float s = 0.f;
+#pragma unroll
+        for (int c = 0; c < E; ++c) {
+            float x[N];
+            z.chunk(c, x);
+            const uint32_t b = marked(c);
+            if (b) {
+#pragma unroll
+                for (int i = 0; i < N; ++i)
+                    if (!(b >> i & 1)) s += __builtin_amdgcn_exp2f((x[i] - ref) * a.c);
+            } else {
+#pragma unroll
+                for (int i = 0; i < N; ++i) s += __builtin_amdgcn_exp2f((x[i] - ref) * a.c);
+            }
+        }
+        const float wave_m = wave_max_f(m);
+        if (lane == 0) wm[wave] = wave_m;
+        __syncthreads();
+        m_rest = wm[0];
+#pragma unroll
+        for (int w = 1; w < WAVES; ++w) m_rest = fmaxf(m_rest, wm[w]);
+        const double S1 = wave_sum_d((double)(s * __builtin_amdgcn_exp2f(m == -INFINITY ? 0.f : (m - m_rest) * a.c)));
+        if (lane == 0) ws[wave] = S1;
+        __syncthreads();
+        if constexpr (MODE == STATS) {
+            if (tid == 0) {
+                DistillPart p;
+                p.sum = ws[0];
+                for (int w = 1; w < WAVES; ++w) p.sum += ws[w];
+                p.m = m_rest;
+                p.unused = 0.f;
+                a.part[(size_t)row * a.parts + part] = p;
+            }
+            return;
+        }
+    }
+    const float weight = a.d_loss ? as_global(a.d_loss)[row] : 1.f;
+    if (wave == 0) {
+        double S;
+        if constexpr (MODE == GRAD) {
+            const DistillPart *parts = a.part + (size_t)row * a.parts;
+            float m = -INFINITY;
+            for (int p = lane; p < a.parts; p += 64) m = fmaxf(m, parts[p].m);
+            m_rest = wave_max_f(m);
+            S = 0.0;
+            for (int p = lane; p < a.parts; p += 64) {
+                const DistillPart x = parts[p];
+                if (x.sum != 0.0) S += x.sum * (x.m == -INFINITY ? 1.0 : exp(((double)x.m - (double)m_rest) * a.inv_t));
+            }
+            S = wave_sum_d(S);
+        } else {
+            S = ws[0];
+            for (int w = 1; w < WAVES; ++w) S += ws[w];
+        }
+        const RowTerms r = row_terms(a, e, m_rest, S, (double)weight * a.inv_t);
+        if (lane == 0) {
+            others_s = r.others;
+            m_s = m_rest;
+            if (a.loss && part == 0) as_global_mut(a.loss)[row] = (float)r.loss;
+        }
+        if (a.d_logits && r.first && at >= 0 && at < len) store_one(a.grad_type, a.d_logits, (size_t)row * a.grad_stride + e.id, weight == 0.f ? 0.f : r.mine);
+    }
+    if (!a.d_logits) return;
+    __syncthreads();
+    const float others = others_s, ref = m_s == -INFINITY ? 0.f : m_s;
+    const size_t out = (size_t)row * a.grad_stride + first;
+#pragma unroll
+    for (int c = 0; c < E; ++c) {
+        const int from = Part::offset(c, tid);
+        if (from >= len) continue;
+        float x[N];
+        z.chunk(c, x);
+#pragma unroll
+        for (int i = 0; i < N; ++i) x[i] = weight == 0.f ? 0.f : __builtin_amdgcn_exp2f((x[i] - ref) * a.c) * others;
+        const uint32_t b = marked(c);
+        if (b == 0 && from + N <= len) {
+            store_some<N>(a.grad_type, a.d_logits, out + from, x);
+        } else {
+#pragma unroll
+            for (int i = 0; i < N; ++i)
+                if (from + i < len && !(b >> i & 1)) store_one(a.grad_type, a.d_logits, out + from + i, x[i]);
+        }
+    }
+}
+
+// The loss of rows in parts, where no gradient is wanted: a wave for each row.
+__global__ void __launch_bounds__(256) ee_distill_loss_kernel(DistillDev a, int n_rows)
+{
+    const int lane = threadIdx.x & 63, row = blockIdx.x * 4 + (threadIdx.x >> 6);
+    if (row >= n_rows) return;
+    Entry e = entry_of(a, row, lane);
+    if (e.id >= 0) e.z = as_global(a.z)[(size_t)row * a.top + lane];
+    const DistillPart *parts = a.part + (size_t)row * a.parts;
+    float m = -INFINITY;
+    for (int p = lane; p < a.parts; p += 64) m = fmaxf(m, parts[p].m);
+    m = wave_max_f(m);
+    double S = 0.0;
+    for (int p = lane; p < a.parts; p += 64) {
+        const DistillPart x = parts[p];
+        if (x.sum != 0.0) S += x.sum * (x.m == -INFINITY ? 1.0 : exp(((double)x.m - (double)m) * a.inv_t));
+    }
+    const RowTerms r = row_terms(a, e, m, wave_sum_d(S), 1.0);
+    if (lane == 0) as_global_mut(a.loss)[row] = (float)r.loss;
+}
+
+struct DistillPlan {
+    int shape;                         // threads and chunks a thread: 256 x 4, 256 x 16, 1024 x 16
+    RowSplit split;
+    size_t part_bytes, bytes;
+};
+static DistillPlan plan_distill(const ee_distill_args &p)
+{
+    DistillPlan pl;
+    const int n = p.dtype == EE_FP32 ? 4 : 8, room[3] = {256 * 4 * n, 256 * 16 * n, 1024 * 16 * n};
+    pl.shape = p.vocab <= room[0] ? 0 : p.vocab <= room[1] ? 1 : 2;
+    if (p.n_rows >= 256 && p.vocab <= room[2]) {
+        pl.split.parts = 1;
+        pl.split.length = p.vocab;
+    } else {
+        pl.shape = p.n_rows >= 256 ? 1 : 0;
+        pl.split = split_rows(p.n_rows, p.vocab, room[pl.shape], 256 * n, pl.shape ? 1 : 512);
+    }
+    pl.part_bytes = pl.split.parts > 1 ? align256((size_t)p.n_rows * pl.split.parts * sizeof(DistillPart)) : 0;
+    pl.bytes = pl.part_bytes + (pl.split.parts > 1 ? align256((size_t)p.n_rows * p.top * sizeof(float)) : 0);
+    return pl;
+}
+
+static int check_distill(const char *call, const ee_distill_args *p)
+{
+    if (!p) return fail(EE_EINVAL, "%s: null argument", call);
+    if (p->device < 0) return fail(EE_EINVAL, "%s: device %d", call, p->device);
+    if (p->dtype < EE_BF16 || p->dtype > EE_FP32 || p->grad_dtype < EE_BF16 || p->grad_dtype > EE_FP32)
+        return fail(EE_EINVAL, "%s: unknown element type %d or %d", call, p->dtype, p->grad_dtype);
+    if (p->vocab < 1 || p->vocab > 1 << 24) return fail(EE_EINVAL, "%s: vocab %d out of range", call, p->vocab);
+    if (p->n_rows < 0 || p->n_rows > 1 << 20) return fail(EE_EINVAL, "%s: n_rows %d not in [0,2^20]", call, p->n_rows);
+    if (p->top < 1 || p->top > EE_MAX_TOP) return fail(EE_EINVAL, "%s: top %d not in [1,%d]", call, p->top, EE_MAX_TOP);
+    if (p->rest != 0 && p->rest != 1) return fail(EE_EINVAL, "%s: rest must be 0 or 1", call);
+    if (!(p->temperature > 0.f) || !isfinite(p->temperature) || !isfinite(1.5f / p->temperature)) return fail(EE_EINVAL, "%s: temperature must be positive and finite", call);
+    return EE_OK;
+}
+
+}  // namespace ee
+
+using namespace ee;
+
+extern "C" int ee_distill_workspace(const ee_distill_args *p, size_t *bytes)
+{
+    static const char *const call = "ee_distill_workspace";
+    if (!bytes) return fail(EE_EINVAL, "%s: null argument", call);
+    *bytes = 0;
+    int rc = check_distill(call, p);
+    if (rc == EE_OK && p->n_rows) *bytes = plan_distill(*p).bytes;
+    return rc;
+}
+
+typedef void (*distill_kernel_t)(DistillDev);
+template <int TYPE>
+static distill_kernel_t distill_kernel(int shape, int mode)
+{
+    if (mode == WHOLE)
+        return shape == 0 ? ee_distill_kernel<TYPE, 4, 256, WHOLE> : shape == 1 ? ee_distill_kernel<TYPE, 16, 256, WHOLE> : ee_distill_kernel<TYPE, 16, 1024, WHOLE>;
+    if (mode == STATS) return shape == 0 ? ee_distill_kernel<TYPE, 4, 256, STATS> : ee_distill_kernel<TYPE, 16, 256, STATS>;
+    return shape == 0 ? ee_distill_kernel<TYPE, 4, 256, GRAD> : ee_distill_kernel<TYPE, 16, 256, GRAD>;
+}
+
+extern "C" int ee_distill(const ee_distill_args *p, void *workspace, size_t workspace_bytes, void *stream)
+{
+    static const char *const call = "ee_distill";
+    int rc = check_distill(call, p);
+    if (rc != EE_OK) return rc;
+    if (p->n_rows == 0 || (!p->loss && !p->d_logits)) return EE_OK;
+    if (!p->logits || !p->ids || !p->logprobs) return fail(EE_EINVAL, "%s: null logits, ids or logprobs", call);
+    if (p->n_rows > 1 && (p->logits_stride < p->vocab || p->logits_stride >= (int64_t)1 << 40 || (p->d_logits && (p->d_logits_stride < p->vocab || p->d_logits_stride >= (int64_t)1 << 40))))
+        return fail(EE_EINVAL, "%s: a row stride is smaller than vocab", call);
+    if (p->d_logits == p->logits && (p->dtype != p->grad_dtype || (p->n_rows > 1 && p->logits_stride != p->d_logits_stride)))
+        return fail(EE_EINVAL, "%s: d_logits may be logits only with the same type and stride", call);
+    if (!aligned(p->logits, size_of_type(p->dtype)) || !aligned(p->d_logits, size_of_type(p->grad_dtype)))
+        return fail(EE_EINVAL, "%s: logits or d_logits are not aligned to their type", call);
+    for (const void *x : {(const void *)p->ids, (const void *)p->logprobs, (const void *)p->loss, (const void *)p->d_loss})
+        if (!aligned(x, 4)) return fail(EE_EINVAL, "%s: int32 and fp32 arrays must be 4-byte aligned", call);
+    const DistillPlan pl = plan_distill(*p);
+    if (pl.bytes > workspace_bytes || (pl.bytes && (!workspace || !aligned(workspace, 256))))
+        return fail(EE_EINVAL, "%s: the workspace has %zu bytes of %zu, or is not 256-byte aligned", call, workspace_bytes, pl.bytes);
+    if ((long long)p->n_rows * pl.split.parts >= 1 << 22) return fail(EE_EINVAL, "%s: too many rows of so many tokens", call);
+    DistillDev a;
+    a.logits = p->logits;
+    a.ids = p->ids;
+    a.logprobs = p->logprobs;
+    a.d_loss = p->d_loss;
+    a.loss = p->loss;
+    a.d_logits = p->d_logits;
+    a.part = static_cast<DistillPart *>(workspace);
+    a.z = reinterpret_cast<float *>(static_cast<unsigned char *>(workspace) + pl.part_bytes);
+    a.stride = p->n_rows > 1 ? p->logits_stride : 0;
+    a.grad_stride = p->n_rows > 1 ? p->d_logits_stride : 0;
+    a.type = p->dtype;
+    a.grad_type = p->grad_dtype;
+    a.V = p->vocab;
+    a.top = p->top;
+    a.rest = p->rest;
+    a.parts = pl.split.parts;
+    a.length = pl.split.length;
+    a.inv_t = 1.0 / (double)p->temperature;
+    a.c = (float)(1.4426950408889634 * a.inv_t);
+    DeviceScope scope(p->device);
+    HIP_TRY(scope.status);
+    const hipStream_t s = static_cast<hipStream_t>(stream);
+    const auto kernel = [&](int mode) {
+        return p->dtype == EE_BF16 ? distill_kernel<EE_BF16>(pl.shape, mode) : p->dtype == EE_FP16 ? distill_kernel<EE_FP16>(pl.shape, mode) : distill_kernel<EE_FP32>(pl.shape, mode);
+    };
+    const dim3 grid((unsigned)(p->n_rows * a.parts)), block(pl.shape == 2 ? 1024 : 256);
+    hipLaunchKernelGGL(kernel(a.parts == 1 ? WHOLE : STATS), grid, block, 0, s, a);
+    HIP_TRY(hipGetLastError());
+    if (a.parts > 1) {
+        if (a.d_logits)
+            hipLaunchKernelGGL(kernel(GRAD), grid, block, 0, s, a);
+        else
+            hipLaunchKernelGGL(ee_distill_loss_kernel, dim3((unsigned)((p->n_rows + 3) / 4)), dim3(256), 0, s, a, p->n_rows);
+        HIP_TRY(hipGetLastError());
+    }
+    return EE_OK;
+}

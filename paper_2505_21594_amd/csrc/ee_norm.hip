@@ -1,0 +1,395 @@
+// ee_norm, ee_norm_grad: layer norm (center = 1) and RMS norm (0) of rows, and their gradients.
+//
+//   x^ = (x - mu) r,  mu = mean x (0 without center),  r = 1 / sqrt(mean (x - mu)^2 + eps),   y = x^ g + b;
+//   u = dy g,   dx = r (u - mean u [center] - x^ mean(u x^)),   dg = sum over rows of dy x^,   db = sum over rows of dy.
+//
+// Bound by the rows' bytes: a wave, or a workgroup, holds a row in registers, so that mean, squares about the mean (no difference of large sums) and
+// result read memory once.  Backward, mean(u x^) is taken with u (x - mu), which needs no r: its sum travels with the squares'.  The
+// gradients of gains and biases stay in registers while a workgroup goes over its rows; the workgroups' sums are added up in order by a second launch.
+// Statistics and sums are fp32.
+#include "ee_vocab.hpp"
+
+namespace ee {
+
+struct NormDev {
+    const void *x, *dy;
+    const float *gain, *bias;
+    void *y;                           // dx in the backward pass
+    float *part_gain, *part_bias;      // [workgroups][dim]
+    long long x_stride, dy_stride, y_stride;
+    int x_type, dy_type, y_type, n_rows, dim, center, groups;
+    float eps, inv_dim;
+};
+
+// A row's elements as floats: chunk c of lane l holds 8 (c * LANES + l) .. + 7; 0 behind the row's end.
+template <int E, int LANES>
+__device__ __forceinline__ void load_row(int type, const void *base, size_t at, int n, int l, float (&x)[E][8])
+{
+    const void *p = row_at(base, type, at);
+#pragma unroll
+    for (int c = 0; c < E; ++c) {
+        const int from = (c * LANES + l) * 8;
+        if (type == EE_FP32)
+            load_some<8>(static_cast<const float *>(p) + from, n - from, 0.f, x[c]);
+        else if (type == EE_BF16)
+            load_some<8>(static_cast<const __bf16 *>(p) + from, n - from, 0.f, x[c]);
+        else
+            load_some<8>(static_cast<const _Float16 *>(p) + from, n - from, 0.f, x[c]);
+    }
+}
+template <int E, int LANES>
+__device__ __forceinline__ void store_row(int type, void *base, size_t at, int n, int l, const float (&x)[E][8])
+{
+#pragma unroll
+    for (int c = 0; c < E; ++c) {
+        const int from = (c * LANES + l) * 8;
+        if (from + 8 <= n) {
+            store_some<8>(type, base, at + from, x[c]);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (from + i < n) store_one(type, base, at + from + i, x[c][i]);
+        }
+    }
+}
+template <int E, int LANES>
+__device__ __forceinline__ void load_gain(const float *gain, int n, int l, float none, float (&g)[E][8])
+{
+#pragma unroll
+    for (int c = 0; c < E; ++c) {
+        const int from = (c * LANES + l) * 8;
+        if (gain) {
+            load_some<8>(gain + from, n - from, 0.f, g[c]);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) g[c][i] = none;
+        }
+    }
+}
+
+__device__ __forceinline__ float wave_sum_f(float x)
+{
+    x += __int_as_float(dpp<DPP_XOR1>(0, __float_as_int(x)));
+    x += __int_as_float(dpp<DPP_XOR2>(0, __float_as_int(x)));
+    x += __int_as_float(dpp<DPP_HALF_MIRROR>(0, __float_as_int(x)));
+    x += __int_as_float(dpp<DPP_MIRROR>(0, __float_as_int(x)));
+    return quads_sum(x);
+}
+// Sums over the LANES that hold a row, in every one of them.  `turn` alternates between two halves of the exchange, so that one barrier is enough.
+template <int LANES, int COUNT>
+__device__ __forceinline__ void row_sums(float (&v)[COUNT], float (*swap)[16][3], int &turn)
+{
+#pragma unroll
+    for (int i = 0; i < COUNT; ++i) v[i] = wave_sum_f(v[i]);
+    if constexpr (LANES > 64) {
+        const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+        if (lane == 0)
+#pragma unroll
+            for (int i = 0; i < COUNT; ++i) swap[turn][wave][i] = v[i];
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < COUNT; ++i) {
+            float s = 0.f;
+#pragma unroll
+            for (int w = 0; w < LANES / 64; ++w) s += swap[turn][w][i];
+            v[i] = s;
+        }
+        turn ^= 1;
+    }
+}
+
+template <int E, int LANES>
+__global__ void __launch_bounds__(LANES < 256 ? 256 : LANES) ee_norm_kernel(NormDev a)
+{
+    constexpr int ROWS = LANES < 256 ? 256 / LANES : 1;      // of a workgroup
+    __shared__ float swap[2][16][3];
+    const int l = threadIdx.x % LANES, row = blockIdx.x * ROWS + threadIdx.x / LANES;
+    if (LANES == 64 && row >= a.n_rows) return;
+    int turn = 0;
+    float x[E][8], g[E][8], b[E][8];
+    load_row<E, LANES>(a.x_type, a.x, (size_t)row * a.x_stride, a.dim, l, x);
+    load_gain<E, LANES>(a.gain, a.dim, l, 1.f, g);
+    load_gain<E, LANES>(a.bias, a.dim, l, 0.f, b);
+    float mu = 0.f;
+    if (a.center) {
+        float v[1] = {0.f};
+#pragma unroll
+        for (int c = 0; c < E; ++c)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[0] += x[c][i];
+        row_sums<LANES>(v, swap, turn);
+        mu = v[0] * a.inv_dim;
+    }
+    float v[1] = {0.f};
+#pragma unroll
+    for (int c = 0; c < E; ++c)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            x[c][i] = (c * LANES + l) * 8 + i < a.dim ? x[c][i] - mu : 0.f;
+            v[0] += x[c][i] * x[c][i];
+        }
+    row_sums<LANES>(v, swap, turn);
+    const float r = 1.f / sqrtf(v[0] * a.inv_dim + a.eps);
+#pragma unroll
+    for (int c = 0; c < E; ++c)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[c][i] = x[c][i] * r * g[c][i] + b[c][i];
+    store_row<E, LANES>(a.y_type, a.y, (size_t)row * a.y_stride, a.dim, l, x);
+}
+
+template <int E, int LANES>
+__global__ void __launch_bounds__(LANES < 256 ? 256 : LANES) ee_norm_grad_kernel(NormDev a)
+{
+    constexpr int ROWS = LANES < 256 ? 256 / LANES : 1;
+    __shared__ float swap[2][16][3];
+    __shared__ float sums[ROWS > 1 ? (ROWS - 1) * E * LANES * 8 : 1];
+    const int l = threadIdx.x % LANES, sub = threadIdx.x / LANES;
+    int turn = 0;
+    float dg[E][8], db[E][8], g[E][8];
+#pragma unroll
+    for (int c = 0; c < E; ++c)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) dg[c][i] = db[c][i] = 0.f;
+    load_gain<E, LANES>(a.gain, a.dim, l, 1.f, g);
+    for (int row = blockIdx.x * ROWS + sub; row < a.n_rows; row += gridDim.x * ROWS) {
+        float x[E][8], u[E][8];
+        load_row<E, LANES>(a.x_type, a.x, (size_t)row * a.x_stride, a.dim, l, x);
+        load_row<E, LANES>(a.dy_type, a.dy, (size_t)row * a.dy_stride, a.dim, l, u);
+        float mu = 0.f;
+        if (a.center) {
+            float v[1] = {0.f};
+#pragma unroll
+            for (int c = 0; c < E; ++c)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) v[0] += x[c][i];
+            row_sums<LANES>(v, swap, turn);
+            mu = v[0] * a.inv_dim;
+        }
+        float v[3] = {0.f, 0.f, 0.f};
+#pragma unroll
+        for (int c = 0; c < E; ++c)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                x[c][i] = (c * LANES + l) * 8 + i < a.dim ? x[c][i] - mu : 0.f;
+                const float t = u[c][i] * g[c][i];
+                v[0] += x[c][i] * x[c][i];
+                v[1] += t;
+                v[2] += t * x[c][i];
+            }
+        row_sums<LANES>(v, swap, turn);
+        const float r = 1.f / sqrtf(v[0] * a.inv_dim + a.eps), mean = a.center ? v[1] * a.inv_dim : 0.f, along = v[2] * a.inv_dim * r;
+#pragma unroll
+        for (int c = 0; c < E; ++c)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const float unit = x[c][i] * r, dy = u[c][i];
+                dg[c][i] += dy * unit;
+                db[c][i] += dy;
+                x[c][i] = r * (dy * g[c][i] - mean - unit * along);
+            }
+        if (a.y) store_row<E, LANES>(a.y_type, a.y, (size_t)row * a.y_stride, a.dim, l, x);
+    }
+    auto combine = [&](float (&v)[E][8], float *out) {
+        if constexpr (ROWS > 1) {
+            __syncthreads();
+            if (sub > 0)
+#pragma unroll
+                for (int c = 0; c < E; ++c)
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) sums[(((sub - 1) * E + c) * 8 + i) * LANES + l] = v[c][i];
+            __syncthreads();
+            if (sub > 0) return;
+#pragma unroll
+            for (int c = 0; c < E; ++c)
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    for (int w = 0; w < ROWS - 1; ++w) v[c][i] += sums[((w * E + c) * 8 + i) * LANES + l];
+        }
+        store_row<E, LANES>(EE_FP32, out, (size_t)blockIdx.x * a.dim, a.dim, l, v);
+    };
+    if (a.part_gain) combine(dg, a.part_gain);
+    if (a.part_bias) combine(db, a.part_bias);
+}
+
+constexpr int CS_COLS = 32, CS_ROWS = 16;
+__global__ void __launch_bounds__(CS_COLS *CS_ROWS) ee_column_sums_kernel(const float *part, int parts, int n, float *out, const float *part2, float *out2)
+{
+    __shared__ float sums[CS_ROWS][CS_COLS];
+    const int col = threadIdx.x % CS_COLS, r = threadIdx.x / CS_COLS, c = blockIdx.x * CS_COLS + col;
+    if (blockIdx.y == 1) {
+        part = part2;
+        out = out2;
+    }
+    const int per = (parts + CS_ROWS - 1) / CS_ROWS, to = min((r + 1) * per, parts);
+    float s = 0.f;
+    if (c < n) {
+#pragma unroll 8
+        for (int p = r * per; p < to; ++p) s += as_global(part)[(size_t)p * n + c];
+    }
+    sums[r][col] = s;
+    __syncthreads();
+    if (r == 0 && c < n) {
+        for (int i = 1; i < CS_ROWS; ++i) s += sums[i][col];
+        as_global_mut(out)[c] = s;
+    }
+}
+void launch_column_sums(const float *part, int parts, int n, float *out, const float *part2, float *out2, hipStream_t stream)
+{
+    if (!out) {
+        out = out2;
+        part = part2;
+        out2 = nullptr;
+    }
+    if (out) hipLaunchKernelGGL(ee_column_sums_kernel, dim3((unsigned)((n + CS_COLS - 1) / CS_COLS), out2 ? 2 : 1), dim3(CS_COLS * CS_ROWS), 0, stream, part, parts, n, out, part2, out2);
+}
+
+typedef void (*norm_kernel_t)(NormDev);
+struct NormShape {
+    int chunks, lanes;
+};
+static NormShape norm_shape(int dim)
+{
+    const int chunks = (dim + 7) / 8;
+    const int lanes = chunks <= 128 ? 64 : chunks <= 1024 ? 256 : 1024;
+    return {(chunks + lanes - 1) / lanes, lanes};
+}
+template <int E>
+static norm_kernel_t norm_kernel(int lanes, bool grad)
+{
+    if (lanes == 64) return grad ? ee_norm_grad_kernel<E, 64> : ee_norm_kernel<E, 64>;
+    if (lanes == 256) return grad ? ee_norm_grad_kernel<E, 256> : ee_norm_kernel<E, 256>;
+    if constexpr (E <= 2) return grad ? ee_norm_grad_kernel<E, 1024> : ee_norm_kernel<E, 1024>;
+    return nullptr;
+}
+static norm_kernel_t norm_kernel(const NormShape &s, bool grad)
+{
+    return s.chunks == 1 ? norm_kernel<1>(s.lanes, grad) : s.chunks == 2 ? norm_kernel<2>(s.lanes, grad) : s.chunks == 3 ? norm_kernel<3>(s.lanes, grad) : norm_kernel<4>(s.lanes, grad);
+}
+static int norm_groups(int n_rows, const NormShape &s)
+{
+    const int rows = s.lanes == 64 ? 4 : 1;
+    return std::min((n_rows + rows - 1) / rows, s.lanes == 1024 ? 256 : 512);
+}
+
+static int check_rows(const char *call, int device, int n_rows, int dim, int center, float eps)
+{
+    if (device < 0) return fail(EE_EINVAL, "%s: device %d", call, device);
+    if (n_rows < 0 || n_rows > EE_NORM_MAX_ROWS) return fail(EE_EINVAL, "%s: n_rows %d not in [0,2^21]", call, n_rows);
+    if (dim < 1 || dim > EE_NORM_MAX_DIM) return fail(EE_EINVAL, "%s: dim %d not in [1,%d]", call, dim, EE_NORM_MAX_DIM);
+    if (center != 0 && center != 1) return fail(EE_EINVAL, "%s: center must be 0 or 1", call);
+    if (!(eps >= 0.f) || !isfinite(eps)) return fail(EE_EINVAL, "%s: eps must be finite and not negative", call);
+    return EE_OK;
+}
+static int check_array(const char *call, const char *what, const void *p, int type, int64_t stride, int n_rows, int dim)
+{
+    if (type < EE_BF16 || type > EE_FP32) return fail(EE_EINVAL, "%s: unknown element type %d", call, type);
+    if (!p) return EE_OK;
+    if (!aligned(p, size_of_type(type))) return fail(EE_EINVAL, "%s: %s is not aligned to its type", call, what);
+    if (n_rows > 1 && (stride < dim || stride >= (int64_t)1 << 40)) return fail(EE_EINVAL, "%s: the row stride of %s is smaller than dim", call, what);
+    return EE_OK;
+}
+
+}  // namespace ee
+
+using namespace ee;
+
+extern "C" int ee_norm(const ee_norm_args *p, void *stream)
+{
+    static const char *const call = "ee_norm";
+    if (!p) return fail(EE_EINVAL, "%s: null argument", call);
+    int rc = check_rows(call, p->device, p->n_rows, p->dim, p->center, p->eps);
+    if (rc == EE_OK) rc = check_array(call, "x", p->x, p->dtype, p->x_stride, p->n_rows, p->dim);
+    if (rc == EE_OK) rc = check_array(call, "y", p->y, p->out_dtype, p->y_stride, p->n_rows, p->dim);
+    if (rc != EE_OK) return rc;
+    if (p->n_rows == 0) return EE_OK;
+    if (!p->x || !p->y) return fail(EE_EINVAL, "%s: null x or y", call);
+    if (p->x == p->y && (p->dtype != p->out_dtype || (p->n_rows > 1 && p->x_stride != p->y_stride))) return fail(EE_EINVAL, "%s: y may be x only with the same type and stride", call);
+    if (!aligned(p->gain, 4) || !aligned(p->bias, 4)) return fail(EE_EINVAL, "%s: fp32 arrays must be 4-byte aligned", call);
+    NormDev a = {};
+    a.x = p->x;
+    a.gain = p->gain;
+    a.bias = p->bias;
+    a.y = p->y;
+    a.x_stride = p->n_rows > 1 ? p->x_stride : 0;
+    a.y_stride = p->n_rows > 1 ? p->y_stride : 0;
+    a.x_type = p->dtype;
+    a.y_type = p->out_dtype;
+    a.n_rows = p->n_rows;
+    a.dim = p->dim;
+    a.center = p->center;
+    a.eps = p->eps;
+    a.inv_dim = 1.f / (float)p->dim;
+    DeviceScope scope(p->device);
+    HIP_TRY(scope.status);
+    const NormShape s = norm_shape(p->dim);
+    const int rows = s.lanes == 64 ? 4 : 1;
+    hipLaunchKernelGGL(norm_kernel(s, false), dim3((unsigned)((p->n_rows + rows - 1) / rows)), dim3(std::max(s.lanes, 256)), 0, static_cast<hipStream_t>(stream), a);
+    HIP_TRY(hipGetLastError());
+    return EE_OK;
+}
+
+static int check_norm_grad(const char *call, const ee_norm_grad_args *p)
+{
+    if (!p) return fail(EE_EINVAL, "%s: null argument", call);
+    return check_rows(call, p->device, p->n_rows, p->dim, p->center, p->eps);
+}
+static size_t norm_grad_bytes(const ee_norm_grad_args *p) { return 2 * align256((size_t)norm_groups(p->n_rows, norm_shape(p->dim)) * p->dim * sizeof(float)); }
+
+extern "C" int ee_norm_grad_workspace(const ee_norm_grad_args *p, size_t *bytes)
+{
+    static const char *const call = "ee_norm_grad_workspace";
+    if (!bytes) return fail(EE_EINVAL, "%s: null argument", call);
+    *bytes = 0;
+    int rc = check_norm_grad(call, p);
+    if (rc == EE_OK) *bytes = norm_grad_bytes(p);
+    return rc;
+}
+
+extern "C" int ee_norm_grad(const ee_norm_grad_args *p, void *workspace, size_t workspace_bytes, void *stream)
+{
+    static const char *const call = "ee_norm_grad";
+    int rc = check_norm_grad(call, p);
+    if (rc == EE_OK) rc = check_array(call, "x", p->x, p->dtype, p->x_stride, p->n_rows, p->dim);
+    if (rc == EE_OK) rc = check_array(call, "dy", p->dy, p->dy_dtype, p->dy_stride, p->n_rows, p->dim);
+    if (rc == EE_OK) rc = check_array(call, "dx", p->dx, p->dx_dtype, p->dx_stride, p->n_rows, p->dim);
+    if (rc != EE_OK) return rc;
+    if (!p->dx && !p->d_gain && !p->d_bias) return EE_OK;
+    if (p->n_rows && (!p->x || !p->dy)) return fail(EE_EINVAL, "%s: null x or dy", call);
+    if (p->dx && ((p->dx == p->x && (p->dtype != p->dx_dtype || (p->n_rows > 1 && p->x_stride != p->dx_stride))) ||
+                  (p->dx == p->dy && (p->dy_dtype != p->dx_dtype || (p->n_rows > 1 && p->dy_stride != p->dx_stride)))))
+        return fail(EE_EINVAL, "%s: dx may be x or dy only with the same type and stride", call);
+    for (const void *x : {(const void *)p->gain, (const void *)p->d_gain, (const void *)p->d_bias})
+        if (!aligned(x, 4)) return fail(EE_EINVAL, "%s: fp32 arrays must be 4-byte aligned", call);
+    const size_t need = norm_grad_bytes(p);
+    if (p->d_gain || p->d_bias)
+        if (need > workspace_bytes || (need && (!workspace || !aligned(workspace, 256))))
+            return fail(EE_EINVAL, "%s: the workspace has %zu bytes of %zu, or is not 256-byte aligned", call, workspace_bytes, need);
+    const NormShape s = norm_shape(p->dim);
+    NormDev a = {};
+    a.x = p->x;
+    a.dy = p->dy;
+    a.gain = p->gain;
+    a.y = p->dx;
+    a.part_gain = p->d_gain ? static_cast<float *>(workspace) : nullptr;
+    a.part_bias = p->d_bias ? reinterpret_cast<float *>(static_cast<unsigned char *>(workspace) + need / 2) : nullptr;
+    a.x_stride = p->n_rows > 1 ? p->x_stride : 0;
+    a.dy_stride = p->n_rows > 1 ? p->dy_stride : 0;
+    a.y_stride = p->n_rows > 1 ? p->dx_stride : 0;
+    a.x_type = p->dtype;
+    a.dy_type = p->dy_dtype;
+    a.y_type = p->dx_dtype;
+    a.n_rows = p->n_rows;
+    a.dim = p->dim;
+    a.center = p->center;
+    a.eps = p->eps;
+    a.inv_dim = 1.f / (float)p->dim;
+    const int groups = norm_groups(p->n_rows, s);
+    DeviceScope scope(p->device);
+    HIP_TRY(scope.status);
+    const hipStream_t st = static_cast<hipStream_t>(stream);
+    if (groups) hipLaunchKernelGGL(norm_kernel(s, true), dim3((unsigned)groups), dim3(std::max(s.lanes, 256)), 0, st, a);
+    HIP_TRY(hipGetLastError());
+    launch_column_sums(a.part_gain, groups, p->dim, p->d_gain, a.part_bias, p->d_bias, st);
+    HIP_TRY(hipGetLastError());
+    return EE_OK;
+}

@@ -212,4 +212,7 @@ struct DeviceScope {
 int check_cache(const char *call, const ee_paged_cache *c, int n_rows, int n_heads, const void *row_start, const void *kv_len);
 BatchDev batch_of(const ee_paged_cache &c, int n_rows, const int32_t *row_start, const int32_t *kv_len);
 
+// out[c] = sum of part[p][c] over the parts in their order, of n columns; two arrays that follow each other at once (ee_norm.hip).
+void launch_column_sums(const float *part, int parts, int n, float *out, const float *part2, float *out2, hipStream_t stream);
+
 }  // namespace ee
