@@ -1,5 +1,7 @@
 #include "ee_linear.hpp"
 
+#include <atomic>
+
 namespace ee {
 
 // Eight neighbouring elements of row r at column c of an array of R rows and C columns; 0 outside it.  Rows start at multiples of 16 bytes.
@@ -15,58 +17,196 @@ __device__ __forceinline__ u32x4_t load_piece(const uint16_t *p, long long ld, i
     return v;
 }
 
-constexpr int GT = 128, GK = 32, GLD = GK + 8;     // tile of 128 x 128, 32 of the sum at a time
+// A tile of TI x TJ results by four waves, each a quarter of it.  32 of the sum at a time go from memory straight to LDS (NS stages, NS - 1 of them on their
+// way), without a register, in the order in which the waves read them:
+//   sum's index contiguous in memory: kilobytes of 16 rows x 32, lane l's piece the operand's of lane l (row l & 15, elements 8 (l >> 4) .. + 7);
+//   result's index contiguous: rows of the stage, pieces of 32 bytes swapped by the row's number, so that the transposing reads (ds_read_b64_tr_b16: four rows x 16
+//   columns for 16 lanes) of a wave meet no bank twice.
+// The weights' side is the first operand: a lane has four neighbouring results of a row.
+template <int TI, int TJ>
+constexpr int gemm_stages() { return TI * TJ >= 256 * 128 ? 3 : 6; }
+template <int TI, int TJ>
+constexpr size_t gemm_lds() { return (size_t)gemm_stages<TI, TJ>() * (TI + TJ) * 64; }
 
-template <bool ALONG>
-__device__ __forceinline__ void stage(const uint16_t *p, long long ld, int rows, int K, int r0, int k0, uint16_t (*to)[GLD], int tid)
-{
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-        const int piece = tid + h * 256;
+// Operand of T rows (of results): its units of a kilobyte in a stage.
+template <bool ALONG, int T>
+struct Operand {
+    static constexpr int UNITS = T / 16, EACH = UNITS / 4;           // ... and of a wave
+    static constexpr int PIECES = T / 8;                             // pieces of a row of the stage, where the result's index is contiguous
+
+    // which of the pieces (pairs of them) of row k of the stage are swapped
+    static __device__ __forceinline__ int swap(int k) { return T >= 128 ? (k & 3) | (k >> 3 & 1) << 2 : k & 3; }
+    // what lane l of unit u holds: results r .. of the tile, sum's index k .. of the stage
+    static __device__ __forceinline__ void place(int u, int l, int &r, int &k)
+    {
         if (ALONG) {
-            const int r = piece / 4, k = piece % 4 * 8;
-            *reinterpret_cast<u32x4_t *>(&to[r][k]) = load_piece(p, ld, rows, K, r0 + r, k0 + k);
+            r = u * 16 + (l & 15);
+            k = (l >> 4) * 8;
         } else {
-            const int k = piece / 16, r = piece % 16 * 8;
-            const u32x4_t v = load_piece(p, ld, K, rows, k0 + k, r0 + r);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) to[r + i][k] = (uint16_t)(v[i / 2] >> (i % 2 * 16));
+            k = u * (512 / T) + l / PIECES;
+            const int c = l % PIECES;
+            r = ((((c >> 1) ^ swap(k)) << 1) | (c & 1)) * 8;
         }
+    }
+    // byte offset of a lane's piece from the stage's first element of the tile; results beyond the array's `n` are read from its first
+    static __device__ __forceinline__ int offset(int u, int l, int n, long long ld)
+    {
+        int r, k;
+        place(u, l, r, k);
+        if (ALONG) return (int)(min(r, n - 1) * ld + k) * 2;
+        return (int)(k * ld + (r < n ? r : 0)) * 2;
+    }
+    // lane's part of the operand for results 16 f .. 16 f + 15 of the tile
+    static __device__ __forceinline__ u32x4_t read(const char *at, int f, int lane)
+    {
+        if (ALONG) return *reinterpret_cast<const u32x4_t *>(at + f * 1024 + lane * 16);
+        typedef __attribute__((ext_vector_type(4))) short s16x4_v;
+        const int s = lane & 15, quad = lane >> 4, k = quad * 8 + (s >> 2);
+        const char *p = at + k * (T * 2) + ((f ^ swap(k)) * 32 + (s & 3) * 8);
+        EE_LDS s16x4_v *q = (EE_LDS s16x4_v *)(p);
+        const s16x4_v a = __builtin_amdgcn_ds_read_tr16_b64_v4i16(q), b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((EE_LDS s16x4_v *)(p + 4 * T * 2));
+        const u32x2_t x = __builtin_bit_cast(u32x2_t, a), y = __builtin_bit_cast(u32x2_t, b);
+        return (u32x4_t){x[0], x[1], y[0], y[1]};
+    }
+};
+
+template <int TYPE, bool A_ALONG, bool B_ALONG, int TI, int TJ>
+__global__ void __launch_bounds__(256, 2) ee_gemm16_kernel(GemmDev g)
+{
+    typedef Operand<A_ALONG, TI> OpA;
+    typedef Operand<B_ALONG, TJ> OpB;
+    constexpr int NS = gemm_stages<TI, TJ>(), PER = OpA::EACH + OpB::EACH, FI = TI / 32, FJ = TJ / 32;
+    constexpr unsigned STAGE = (TI + TJ) * 64;
+    extern __shared__ __align__(16) char lds[];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int wi = wave & 1, wj = wave >> 1;
+    // Workgroups go to the XCDs in turn; each XCD has a contiguous run of the tiles, which walk groups of eight blocks of rows over all blocks of columns: what
+    // runs together on an XCD shares operands in its L2.
+    const int T = g.ni * g.nj * g.splits;
+    int t, part, i0, j0;
+    {
+        const int x = blockIdx.x % NUM_XCD, n = blockIdx.x / NUM_XCD, base = T / NUM_XCD, extra = T % NUM_XCD;
+        t = x * base + min(x, extra) + n;
+        part = t / (g.ni * g.nj);
+        t -= part * g.ni * g.nj;
+        const int group = t / (8 * g.nj), rem = t - group * 8 * g.nj, width = min(8, g.ni - group * 8);
+        j0 = rem / width;
+        i0 = (group * 8 + rem - j0 * width) * TI;
+        j0 *= TJ;
+    }
+    const int lo = part * g.per, hi = min(lo + g.per, g.K);
+    // The last step is loaded with a look at every piece where it is not whole, or where a piece at the end of its rows is not.
+    const bool ragged = !A_ALONG && (g.I & 7), ragged_b = !B_ALONG && (g.J & 7);
+    // (Rows too far apart for 32-bit offsets: all steps are.)
+    const int full = g.far ? 0 : max((hi - lo) / 32 - (hi == g.K && (hi - lo) % 32 == 0 && (ragged || ragged_b)), 0);
+    const unsigned lds0 = lds_offset(lds);
+    int off_a[OpA::EACH], off_b[OpB::EACH];
+#pragma unroll
+    for (int i = 0; i < OpA::EACH; ++i) off_a[i] = OpA::offset(wave * OpA::EACH + i, lane, g.I - i0, g.lda);
+#pragma unroll
+    for (int i = 0; i < OpB::EACH; ++i) off_b[i] = OpB::offset(wave * OpB::EACH + i, lane, g.J - j0, g.ldb);
+    const char *const b0 = reinterpret_cast<const char *>(g.B + (B_ALONG ? (size_t)j0 * g.ldb + lo : (size_t)lo * g.ldb + j0));
+    const size_t step_a = A_ALONG ? 64 : (size_t)g.lda * 64, step_b = B_ALONG ? 64 : (size_t)g.ldb * 64;
+
+    f32x4_t acc[FJ][FI];
+#pragma unroll
+    for (int j = 0; j < FJ; ++j)
+#pragma unroll
+        for (int i = 0; i < FI; ++i) acc[j][i] = (f32x4_t){0.f, 0.f, 0.f, 0.f};
+    auto compute = [&](const char *st) __attribute__((always_inline)) {
+        u32x4_t a[FI], b[FJ];
+#pragma unroll
+        for (int j = 0; j < FJ; ++j) b[j] = OpB::read(st + TI * 64, wj * FJ + j, lane);
+#pragma unroll
+        for (int i = 0; i < FI; ++i) a[i] = OpA::read(st, wi * FI + i, lane);
+#pragma unroll
+        for (int i = 0; i < FI; ++i)
+#pragma unroll
+            for (int j = 0; j < FJ; ++j) acc[j][i] = mfma16<TYPE>(b[j], a[i], acc[j][i]);
+    };
+    for (int term = 0; term < g.terms; ++term) {
+        const uint16_t *const A = g.A + term * g.plane;
+        const char *const a0 = reinterpret_cast<const char *>(A + (A_ALONG ? (size_t)i0 * g.lda + lo : (size_t)lo * g.lda + i0));
+        auto request = [&](int s, int buf) __attribute__((always_inline)) {
+            const unsigned dst = lds0 + buf * STAGE;
+            const void *pa = uniform_ptr(a0 + s * step_a), *pb = uniform_ptr(b0 + s * step_b);
+#pragma unroll
+            for (int i = 0; i < OpA::EACH; ++i) load_lds_kb(pa, off_a[i], dst + (wave * OpA::EACH + i) * 1024);
+#pragma unroll
+            for (int i = 0; i < OpB::EACH; ++i) load_lds_kb(pb, off_b[i], dst + TI * 64 + (wave * OpB::EACH + i) * 1024);
+        };
+#pragma unroll
+        for (int s = 0; s < NS - 1; ++s)
+            if (s < full) request(s, s);
+        int buf = 0;
+        for (int s = 0; s < full; ++s) {
+            // this wave's loads of stage s have landed; after the barrier everybody's have, and nobody reads the buffer of stage s - 1 any more
+            if (s + NS - 2 < full)
+                wait_pending<PER *(NS - 2)>();
+            else
+                wait_pending<0>();
+            lds_barrier();
+            if (s + NS - 1 < full) request(s + NS - 1, buf == 0 ? NS - 1 : buf - 1);
+            compute(lds + buf * STAGE);
+            buf = buf + 1 == NS ? 0 : buf + 1;
+        }
+        for (int k0 = lo + full * 32; k0 < hi; k0 += 32) {
+            lds_barrier();
+#pragma unroll
+            for (int i = 0; i < OpA::EACH; ++i) {
+                int r, k;
+                OpA::place(wave * OpA::EACH + i, lane, r, k);
+                *reinterpret_cast<u32x4_t *>(lds + (wave * OpA::EACH + i) * 1024 + lane * 16) = A_ALONG ? load_piece(A, g.lda, g.I, hi, i0 + r, k0 + k) : load_piece(A, g.lda, hi, g.I, k0 + k, i0 + r);
+            }
+#pragma unroll
+            for (int i = 0; i < OpB::EACH; ++i) {
+                int r, k;
+                OpB::place(wave * OpB::EACH + i, lane, r, k);
+                *reinterpret_cast<u32x4_t *>(lds + TI * 64 + (wave * OpB::EACH + i) * 1024 + lane * 16) = B_ALONG ? load_piece(g.B, g.ldb, g.J, hi, j0 + r, k0 + k) : load_piece(g.B, g.ldb, hi, g.J, k0 + k, j0 + r);
+            }
+            lds_barrier();
+            compute(lds);
+        }
+        if (term + 1 < g.terms) lds_barrier();
+    }
+    // Results turn in LDS (64 rows of a wave at a time), so that stores are whole lines and the code behind the sums is there once, not for every register.
+    constexpr int HALF = FI < 4 ? FI : 4, COLS = FJ * 16, LD = COLS + 4, LANES = COLS / 4;
+    static_assert(4 * HALF * 16 * LD * 4 <= gemm_lds<TI, TJ>(), "a turn fits the stages' room");
+    float *const turn = reinterpret_cast<float *>(lds) + wave * (HALF * 16 * LD);
+    const int col = j0 + wj * COLS + lane % LANES * 4;
+#pragma unroll
+    for (int h = 0; h < FI; h += HALF) {
+        if (h == 0) lds_barrier();                           // (every wave has read the last stage)
+#pragma unroll
+        for (int i = 0; i < HALF; ++i)
+#pragma unroll
+            for (int j = 0; j < FJ; ++j) *reinterpret_cast<f32x4_t *>(turn + (i * 16 + (lane & 15)) * LD + j * 16 + (lane >> 4) * 4) = acc[j][h + i];
+        wave_lds_order();
+#pragma unroll 1
+        for (int r = lane / LANES; r < HALF * 16; r += 64 / LANES) {
+            const f32x4_t v = *reinterpret_cast<const f32x4_t *>(turn + r * LD + lane % LANES * 4);
+            const int row = i0 + (wi * FI + h) * 16 + r;
+            if (g.splits == 1)
+                finish4(g, row, col, v);
+            else if (row < g.I && col < g.J)
+                *as_global_mut(reinterpret_cast<f32x4_t *>(g.part + ((size_t)part * g.I + row) * g.part_ld + col)) = v;
+        }
+        wave_lds_order();
     }
 }
 
-template <int TYPE, bool A_ALONG, bool B_ALONG>
-__global__ void __launch_bounds__(256) ee_gemm16_kernel(GemmDev g)
+// The parts of a sum, in their order.
+__global__ void __launch_bounds__(256) ee_gemm16_join_kernel(GemmDev g)
 {
-    __shared__ __attribute__((aligned(16))) uint16_t as[GT][GLD], bs[GT][GLD];
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, i0 = blockIdx.y * GT, j0 = blockIdx.x * GT;
-    const int wi = (wave & 1) * 64, wj = (wave >> 1) * 64, r = lane & 15, quad = lane >> 4;
-    f32x4_t acc[4][4];
-#pragma unroll
-    for (int j = 0; j < 4; ++j)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) acc[j][i] = (f32x4_t){0.f, 0.f, 0.f, 0.f};
-    for (int t = 0; t < g.terms; ++t)
-        for (int k = 0; k < g.K; k += GK) {
-            __syncthreads();
-            stage<A_ALONG>(g.A + t * g.plane, g.lda, g.I, g.K, i0, k, as, tid);
-            stage<B_ALONG>(g.B, g.ldb, g.J, g.K, j0, k, bs, tid);
-            __syncthreads();
-            u32x4_t a[4], b[4];
-#pragma unroll
-            for (int x = 0; x < 4; ++x) {
-                a[x] = *reinterpret_cast<const u32x4_t *>(&as[wi + x * 16 + r][quad * 8]);
-                b[x] = *reinterpret_cast<const u32x4_t *>(&bs[wj + x * 16 + r][quad * 8]);
-            }
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) acc[j][i] = mfma16<TYPE>(b[j], a[i], acc[j][i]);
-        }
-#pragma unroll
-    for (int j = 0; j < 4; ++j)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) finish4(g, i0 + wi + i * 16 + r, j0 + wj + j * 16 + quad * 4, acc[j][i]);
+    const int per_row = (int)(g.part_ld / 4);
+    const size_t at = (size_t)blockIdx.x * 256 + threadIdx.x;
+    const int row = (int)(at / per_row), col = (int)(at - (size_t)row * per_row) * 4;
+    if (row >= g.I) return;
+    const float *p = g.part + (size_t)row * g.part_ld + col;
+    f32x4_t v = *as_global(reinterpret_cast<const f32x4_t *>(p));
+#pragma unroll 4
+    for (int s = 1; s < g.splits; ++s) v += *as_global(reinterpret_cast<const f32x4_t *>(p + (size_t)s * g.I * g.part_ld));
+    finish4(g, row, col, v);
 }
 
 // dz = dy act'(z) as 16-bit terms, and sums of its columns over a part of the rows: a thread has eight columns.
@@ -127,12 +267,67 @@ __global__ void __launch_bounds__(SL_COLS *SL_SUBS) ee_slope_kernel(SlopeDev a)
 }
 
 typedef void (*gemm16_kernel_t)(GemmDev);
-static int launch_gemm16(const GemmDev &g, bool a_along, bool b_along, hipStream_t s)
+template <int TYPE, int TI, int TJ>
+static gemm16_kernel_t gemm16_kernel(bool a_along, bool b_along)
 {
-    const gemm16_kernel_t k = g.type == EE_BF16 ? (a_along ? (b_along ? ee_gemm16_kernel<EE_BF16, true, true> : ee_gemm16_kernel<EE_BF16, true, false>) : ee_gemm16_kernel<EE_BF16, false, false>)
-                                                : (a_along ? (b_along ? ee_gemm16_kernel<EE_FP16, true, true> : ee_gemm16_kernel<EE_FP16, true, false>) : ee_gemm16_kernel<EE_FP16, false, false>);
-    hipLaunchKernelGGL(k, dim3((unsigned)((g.J + GT - 1) / GT), (unsigned)((g.I + GT - 1) / GT)), dim3(256), 0, s, g);
+    return a_along ? (b_along ? ee_gemm16_kernel<TYPE, true, true, TI, TJ> : ee_gemm16_kernel<TYPE, true, false, TI, TJ>) : ee_gemm16_kernel<TYPE, false, false, TI, TJ>;
+}
+
+// How a product is split: tiles of 256 x 128 or 64 x 64, and parts of the sum.
+struct GemmPlan16 {
+    bool large;
+    int ni, nj, splits, per;
+    long long part_ld;
+    size_t bytes;
+};
+static GemmPlan16 plan_gemm16(int I, int J, int K)
+{
+    GemmPlan16 pl = {};
+    const auto tiles = [&](int ti, int tj) { return std::max(1ll, (long long)((I + ti - 1) / ti) * ((J + tj - 1) / tj)); };
+    pl.large = tiles(256, 128) >= 128;
+    const long long n = pl.large ? tiles(256, 128) : tiles(64, 64);
+    pl.ni = (I + (pl.large ? 255 : 63)) / (pl.large ? 256 : 64);
+    pl.nj = (J + (pl.large ? 127 : 63)) / (pl.large ? 128 : 64);
+    const int most = std::max(1, K / 512);
+    pl.splits = (int)std::min<long long>(most, std::max<long long>(1, (pl.large ? 256 : 768) / n));
+    pl.per = std::max(((K + pl.splits - 1) / pl.splits + 31) / 32 * 32, 32);
+    pl.splits = std::max(1, (K + pl.per - 1) / pl.per);
+    pl.part_ld = ((long long)J + 3) / 4 * 4;
+    pl.bytes = pl.splits > 1 ? align256((size_t)pl.splits * I * pl.part_ld * sizeof(float)) : 0;
+    return pl;
+}
+constexpr long long GEMM_FAR = 1 << 21;            // elements from row to row that 32-bit offsets within a tile allow
+static int launch_gemm16(GemmDev g, bool a_along, bool b_along, void *space, hipStream_t s)
+{
+    const GemmPlan16 pl = plan_gemm16(g.I, g.J, g.K);
+    g.ni = pl.ni;
+    g.nj = pl.nj;
+    g.splits = pl.splits;
+    g.per = pl.per;
+    g.part = static_cast<float *>(space);
+    g.part_ld = pl.part_ld;
+    g.far = g.lda > GEMM_FAR || g.ldb > GEMM_FAR;
+    const gemm16_kernel_t k = pl.large ? (g.type == EE_BF16 ? gemm16_kernel<EE_BF16, 256, 128>(a_along, b_along) : gemm16_kernel<EE_FP16, 256, 128>(a_along, b_along))
+                                       : (g.type == EE_BF16 ? gemm16_kernel<EE_BF16, 64, 64>(a_along, b_along) : gemm16_kernel<EE_FP16, 64, 64>(a_along, b_along));
+    const size_t lds = pl.large ? gemm_lds<256, 128>() : gemm_lds<64, 64>();
+    if (lds > 64 << 10) {                              // said once for a kernel on a device
+        static std::atomic<uint64_t> said[2][2][2];
+        std::atomic<uint64_t> &mine = said[g.type == EE_BF16][a_along][b_along];
+        int device = 0;
+        HIP_TRY(hipGetDevice(&device));
+        const uint64_t bit = 1ull << (device & 63);
+        if (!(mine.load(std::memory_order_relaxed) & bit)) {
+            HIP_TRY(hipFuncSetAttribute(reinterpret_cast<const void *>(k), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds));
+            if (device < 64) mine.fetch_or(bit, std::memory_order_relaxed);
+        }
+    }
+    hipLaunchKernelGGL(k, dim3((unsigned)(pl.ni * pl.nj * pl.splits)), dim3(256), lds, s, g);
     HIP_TRY(hipGetLastError());
+    if (pl.splits > 1) {
+        const size_t n = (size_t)g.I * (pl.part_ld / 4);
+        hipLaunchKernelGGL(ee_gemm16_join_kernel, dim3((unsigned)((n + 255) / 256)), dim3(256), 0, s, g);
+        HIP_TRY(hipGetLastError());
+    }
     return EE_OK;
 }
 
@@ -143,6 +338,8 @@ static int check_sizes(const char *call, int device, int dtype, int act, int n_r
     if (act < EE_ACT_NONE || act > EE_ACT_GELU) return fail(EE_EINVAL, "%s: unknown activation %d", call, act);
     if (n_rows < 0 || n_rows > EE_LINEAR_MAX) return fail(EE_EINVAL, "%s: n_rows %d not in [0,2^22]", call, n_rows);
     if (n_in < 1 || n_in > EE_LINEAR_MAX || n_out < 1 || n_out > EE_LINEAR_MAX) return fail(EE_EINVAL, "%s: n_in %d or n_out %d not in [1,2^22]", call, n_in, n_out);
+    const auto tiles = [](int a, int b) { return (((long long)a + 63) / 64) * (((long long)b + 63) / 64); };
+    if (std::max(tiles(n_rows, n_in), std::max(tiles(n_rows, n_out), tiles(n_in, n_out))) >= 1 << 23) return fail(EE_EINVAL, "%s: n_rows %d, n_in %d, n_out %d are too many at once", call, n_rows, n_in, n_out);
     return EE_OK;
 }
 // rows of an array: 16-byte aligned, `width` elements at least from one to the next
@@ -166,8 +363,8 @@ struct GradPlan {
     int terms_dx, terms_dw, terms;     // of dz, where it is formed
     int parts, per;                    // of the rows, for the bias's gradient and dz
     long long ldz;
-    size_t dz_bytes, part_bytes;
-    size_t bytes() const { return dz_bytes + part_bytes; }
+    size_t dz_bytes, part_bytes, gemm_bytes;
+    size_t bytes() const { return dz_bytes + part_bytes + gemm_bytes; }
 };
 static GradPlan plan_grad(const ee_linear_grad_args &p)
 {
@@ -183,6 +380,7 @@ static GradPlan plan_grad(const ee_linear_grad_args &p)
     pl.parts = (p.n_rows + pl.per - 1) / pl.per;
     pl.dz_bytes = align256((size_t)pl.terms * p.n_rows * pl.ldz * 2);
     pl.part_bytes = align256((size_t)pl.parts * p.n_out * sizeof(float));
+    pl.gemm_bytes = std::max(plan_gemm16(p.n_rows, p.n_in, p.n_out).bytes, plan_gemm16(p.n_out, p.n_in, p.n_rows).bytes);
     return pl;
 }
 static int check_linear_grad(const char *call, const ee_linear_grad_args *p)
@@ -202,7 +400,9 @@ extern "C" int ee_linear_workspace(const ee_linear_args *p, size_t *bytes)
     static const char *const call = "ee_linear_workspace";
     if (!bytes) return fail(EE_EINVAL, "%s: null argument", call);
     *bytes = 0;
-    return check_linear(call, p);
+    int rc = check_linear(call, p);
+    if (rc == EE_OK) *bytes = plan_gemm16(p->n_rows, p->n_out, p->n_in).bytes;
+    return rc;
 }
 
 extern "C" int ee_linear(const ee_linear_args *p, void *workspace, size_t workspace_bytes, void *stream)
@@ -221,6 +421,9 @@ extern "C" int ee_linear(const ee_linear_args *p, void *workspace, size_t worksp
     if (p->residual == p->y && (p->residual_dtype != p->out_dtype || (p->n_rows > 1 && p->residual_stride != p->y_stride)))
         return fail(EE_EINVAL, "%s: y may be residual only with the same type and stride", call);
     if (!aligned(p->bias, 4)) return fail(EE_EINVAL, "%s: fp32 arrays must be 4-byte aligned", call);
+    const size_t need = plan_gemm16(p->n_rows, p->n_out, p->n_in).bytes;
+    if (need > workspace_bytes || (need && (!workspace || !aligned(workspace, 256))))
+        return fail(EE_EINVAL, "%s: the workspace has %zu bytes of %zu, or is not 256-byte aligned", call, workspace_bytes, need);
     GemmDev g = {};
     g.A = static_cast<const uint16_t *>(p->x);
     g.B = static_cast<const uint16_t *>(p->weight);
@@ -243,7 +446,7 @@ extern "C" int ee_linear(const ee_linear_args *p, void *workspace, size_t worksp
     g.act = p->act;
     DeviceScope scope(p->device);
     HIP_TRY(scope.status);
-    return launch_gemm16(g, true, true, static_cast<hipStream_t>(stream));
+    return launch_gemm16(g, true, true, workspace, static_cast<hipStream_t>(stream));
 }
 
 extern "C" int ee_linear_grad_workspace(const ee_linear_grad_args *p, size_t *bytes)
@@ -285,6 +488,7 @@ extern "C" int ee_linear_grad(const ee_linear_grad_args *p, void *workspace, siz
     const hipStream_t s = static_cast<hipStream_t>(stream);
     uint16_t *const dz = static_cast<uint16_t *>(workspace);
     float *const part = reinterpret_cast<float *>(static_cast<unsigned char *>(workspace) + pl.dz_bytes);
+    void *const space = static_cast<unsigned char *>(workspace) + pl.dz_bytes + pl.part_bytes;
     const long long plane = (long long)p->n_rows * pl.ldz;
     if (pl.parts && (p->d_bias || p->act != EE_ACT_NONE)) {
         SlopeDev a = {};
@@ -323,7 +527,7 @@ extern "C" int ee_linear_grad(const ee_linear_grad_args *p, void *workspace, siz
         g.y = p->dx;
         g.y_type = p->dx_dtype;
         g.y_stride = p->n_rows > 1 ? p->dx_stride : 0;
-        if ((rc = launch_gemm16(g, true, false, s)) != EE_OK) return rc;
+        if ((rc = launch_gemm16(g, true, false, space, s)) != EE_OK) return rc;
     }
     if (p->d_weight) {
         g.B = static_cast<const uint16_t *>(p->x);
@@ -335,7 +539,7 @@ extern "C" int ee_linear_grad(const ee_linear_grad_args *p, void *workspace, siz
         g.y = p->d_weight;
         g.y_type = p->dw_dtype;
         g.y_stride = p->n_out > 1 ? p->dw_stride : 0;
-        if ((rc = launch_gemm16(g, false, false, s)) != EE_OK) return rc;
+        if ((rc = launch_gemm16(g, false, false, space, s)) != EE_OK) return rc;
     }
     return EE_OK;
 }

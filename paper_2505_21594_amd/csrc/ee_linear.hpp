@@ -20,6 +20,10 @@ struct GemmDev {
     void *y, *pre;
     long long res_stride, y_stride, pre_stride;
     int res_type, y_type, type, act;
+    int ni, nj, splits, per;           // tiles, parts of the sum, and a part's length
+    int far;                           // rows are too far apart for 32-bit offsets
+    float *part;                       // [splits][I][part_ld]
+    long long part_ld;
 };
 
 template <int TYPE>

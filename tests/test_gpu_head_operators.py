@@ -407,6 +407,56 @@ def test_linear_grad(rows, n_in, n_out, kind):
         assert got[n_out] == FILL
 
 
+class Large:
+    """Matrices for products that fill the chip, made of few different rows so that the 64-bit form is quick: row i is row i % 37 of a small one."""
+
+    def __init__(self, rng, rows, width, kind, scale=1.0):
+        self.small = Rows(scale * rng.standard_normal((37, width)), kind, up8(width))
+        self.index = np.arange(rows) % 37
+        self.all = Rows(np.zeros((1, 1)), kind)
+        host = np.ascontiguousarray(self.small.inside())[self.index]
+        wide = np.full((rows, up8(width) + 8), encode(np.full(1, np.nan, np.float32), kind)[0])
+        wide[:, :width] = host
+        self.dev = Dev(wide)
+        self.view = self.dev.view((rows, width), (up8(width) + 8, 1))
+
+    def values(self):
+        return self.small.values()
+
+
+@pytest.mark.parametrize("kind", ["bf16", "fp16"])
+@pytest.mark.parametrize("rows,n_in,n_out", [(2600, 96, 2100), (2050, 133, 2433), (4100, 64, 1025), (40000, 40, 72), (72, 8200, 40)])
+def test_linear_that_fills_the_chip(rows, n_in, n_out, kind):
+    """Every result, by the large tiles or in parts of the sum."""
+    rng = np.random.default_rng(rows)
+    x, w = Large(rng, rows, n_in, kind), Large(rng, n_out, n_in, kind, 0.2)
+    bias = np.float32(rng.standard_normal(n_out))
+    y, pre = empty(rows, n_out, "fp32", up8(n_out)), empty(rows, n_out, kind, up8(n_out))
+    ws = Space(ee.ee_linear_workspace(x.view, w.view))
+    ee.ee_linear(x.view, w.view, y.view, bias=Dev(bias), act=ee.ACT_SILU, pre=pre.view, workspace=ws.view)
+    ws.check()
+    z = (x.values() @ w.values().T)[x.index][:, w.index] + bias
+    size = (np.abs(x.values()) @ np.abs(w.values()).T)[x.index][:, w.index]
+    tol_z = (n_in + 2) * ref.U * size + 2 * ref.U * np.abs(z)
+    value = ref.act(z, 1)
+    close(y.result(), (value, 1.13 * tol_z + ref.ACT * (np.abs(z) + np.abs(value)) + ref.U * np.abs(value)), "y")
+    close(pre.result(), (z, tol_z + HALF_STEP[kind] * np.abs(z) * (1 + 2.0 ** -8) + SUBNORMAL[kind]), "pre")
+    # backward: dy of 37 kinds of rows as well, by columns of 37 kinds
+    d = rng.standard_normal((37, 37))
+    dy = Rows(d[x.index][:, w.index], kind, up8(n_out) + 8)
+    dv = decode(encode(d.astype(np.float32), kind))
+    dx, dw, db = empty(rows, n_in, "fp32", up8(n_in)), empty(n_out, n_in, "fp32", up8(n_in)), Dev(np.zeros(n_out, np.float32))
+    ws = Space(ee.ee_linear_grad_workspace(x.view, w.view))
+    ee.ee_linear_grad(x.view, w.view, dy.view, dx=dx.view, d_weight=dw.view, d_bias=db, workspace=ws.view)
+    ws.check()
+    nx, nw = np.bincount(x.index, minlength=37).astype(float), np.bincount(w.index, minlength=37).astype(float)
+    want = (dv * nw) @ w.values()
+    close(dx.result(), (want[x.index], ((n_out + 2) * ref.U * ((np.abs(dv) * nw) @ np.abs(w.values())))[x.index]), "dx")
+    want = (dv.T * nx) @ x.values()
+    close(dw.result(), (want[w.index], ((rows + 2) * ref.U * ((np.abs(dv).T * nx) @ np.abs(x.values())))[w.index]), "d_weight")
+    close(db.numpy().astype(np.float64), ((dv.T @ nx)[w.index], (rows * ref.U * (np.abs(dv).T @ nx))[w.index]), "d_bias")
+
+
 def test_linear_one_result_at_a_time_and_no_rows():
     rng = np.random.default_rng(9)
     x, w, dy = matrix(rng, 70, 96, "bf16"), matrix(rng, 40, 96, "bf16"), matrix(rng, 70, 40, "bf16")

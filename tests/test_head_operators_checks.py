@@ -118,6 +118,13 @@ def test_workspaces_are_checked():
     refused(lib.ee_linear_workspace(ctypes.byref(linear_args(dtype=ee.FP32)), ctypes.byref(n)), "bf16")
 
 
+def test_workspaces_of_no_rows():
+    lib, n = ee.load_library(), ctypes.c_size_t()
+    for name, args in (("score", score_args(n_rows=0)), ("distill", distill_args(n_rows=0)), ("norm_grad", norm_grad_args(n_rows=0)), ("linear", linear_args(n_rows=0)),
+                       ("linear_grad", linear_grad_args(n_rows=0))):
+        assert getattr(lib, f"ee_{name}_workspace")(ctypes.byref(args), ctypes.byref(n)) == ee.EE_OK
+
+
 def test_nothing_to_do_is_fine():
     lib = ee.load_library()
     assert lib.ee_score_tokens(ctypes.byref(score_args(n_rows=0)), None, 0, None) == ee.EE_OK
