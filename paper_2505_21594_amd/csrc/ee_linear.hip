@@ -19,7 +19,8 @@ __device__ __forceinline__ u32x4_t load_piece(const uint16_t *p, long long ld, i
 
 // A tile of TI x TJ results by four waves, each a quarter of it.  32 of the sum at a time go from memory straight to LDS (NS stages, NS - 1 of them on their
 // way), without a register, in the order in which the waves read them:
-//   sum's index contiguous in memory: kilobytes of 16 rows x 32, lane l's piece the operand's of lane l (row l & 15, elements 8 (l >> 4) .. + 7);
+//   sum's index contiguous in memory: kilobytes of 16 rows x 32, four lanes a row (neighbouring lanes that read neighbouring lines cost four times the
+//                               look-ups), a row's four pieces swapped by its number, so that eight lanes of a read meet every bank once;
 //   result's index contiguous: rows of the stage, pieces of 32 bytes swapped by the row's number, so that the transposing reads (ds_read_b64_tr_b16: four rows x 16
 //   columns for 16 lanes) of a wave meet no bank twice.
 // The weights' side is the first operand: a lane has four neighbouring results of a row.
@@ -40,8 +41,8 @@ struct Operand {
     static __device__ __forceinline__ void place(int u, int l, int &r, int &k)
     {
         if (ALONG) {
-            r = u * 16 + (l & 15);
-            k = (l >> 4) * 8;
+            r = u * 16 + (l >> 2);
+            k = ((l & 3) ^ (l >> 3 & 3)) * 8;
         } else {
             k = u * (512 / T) + l / PIECES;
             const int c = l % PIECES;
@@ -59,9 +60,10 @@ struct Operand {
     // lane's part of the operand for results 16 f .. 16 f + 15 of the tile
     static __device__ __forceinline__ u32x4_t read(const char *at, int f, int lane)
     {
-        if (ALONG) return *reinterpret_cast<const u32x4_t *>(at + f * 1024 + lane * 16);
+        const int s = lane & 15, quad = lane >> 4;
+        if (ALONG) return *reinterpret_cast<const u32x4_t *>(at + f * 1024 + s * 64 + (quad ^ (s >> 1 & 3)) * 16);
         typedef __attribute__((ext_vector_type(4))) short s16x4_v;
-        const int s = lane & 15, quad = lane >> 4, k = quad * 8 + (s >> 2);
+        const int k = quad * 8 + (s >> 2);
         const char *p = at + k * (T * 2) + ((f ^ swap(k)) * 32 + (s & 3) * 8);
         EE_LDS s16x4_v *q = (EE_LDS s16x4_v *)(p);
         const s16x4_v a = __builtin_amdgcn_ds_read_tr16_b64_v4i16(q), b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((EE_LDS s16x4_v *)(p + 4 * T * 2));
@@ -174,6 +176,7 @@ __global__ void __launch_bounds__(256, 2) ee_gemm16_kernel(GemmDev g)
     static_assert(4 * HALF * 16 * LD * 4 <= gemm_lds<TI, TJ>(), "a turn fits the stages' room");
     float *const turn = reinterpret_cast<float *>(lds) + wave * (HALF * 16 * LD);
     const int col = j0 + wj * COLS + lane % LANES * 4;
+    const f32x4_t bias = bias_at(g, col);
 #pragma unroll
     for (int h = 0; h < FI; h += HALF) {
         if (h == 0) lds_barrier();                           // (every wave has read the last stage)
@@ -182,15 +185,22 @@ __global__ void __launch_bounds__(256, 2) ee_gemm16_kernel(GemmDev g)
 #pragma unroll
             for (int j = 0; j < FJ; ++j) *reinterpret_cast<f32x4_t *>(turn + (i * 16 + (lane & 15)) * LD + j * 16 + (lane >> 4) * 4) = acc[j][h + i];
         wave_lds_order();
+        constexpr int STEP = 64 / LANES, AT_ONCE = 4;
+        if (col < g.J)
 #pragma unroll 1
-        for (int r = lane / LANES; r < HALF * 16; r += 64 / LANES) {
-            const f32x4_t v = *reinterpret_cast<const f32x4_t *>(turn + r * LD + lane % LANES * 4);
-            const int row = i0 + (wi * FI + h) * 16 + r;
-            if (g.splits == 1)
-                finish4(g, row, col, v);
-            else if (row < g.I && col < g.J)
-                *as_global_mut(reinterpret_cast<f32x4_t *>(g.part + ((size_t)part * g.I + row) * g.part_ld + col)) = v;
-        }
+            for (int r = lane / LANES; r < HALF * 16; r += STEP * AT_ONCE) {
+                const int row = i0 + (wi * FI + h) * 16 + r;
+                f32x4_t v[AT_ONCE];
+#pragma unroll
+                for (int e = 0; e < AT_ONCE; ++e) v[e] = *reinterpret_cast<const f32x4_t *>(turn + (r + e * STEP) * LD + lane % LANES * 4);
+                if (g.splits == 1) {
+                    finish<AT_ONCE>(g, row, STEP, col, bias, v);
+                } else {
+#pragma unroll
+                    for (int e = 0; e < AT_ONCE; ++e)
+                        if (row + e * STEP < g.I) *as_global_mut(reinterpret_cast<f32x4_t *>(g.part + ((size_t)part * g.I + row + e * STEP) * g.part_ld + col)) = v[e];
+                }
+            }
         wave_lds_order();
     }
 }
@@ -201,12 +211,13 @@ __global__ void __launch_bounds__(256) ee_gemm16_join_kernel(GemmDev g)
     const int per_row = (int)(g.part_ld / 4);
     const size_t at = (size_t)blockIdx.x * 256 + threadIdx.x;
     const int row = (int)(at / per_row), col = (int)(at - (size_t)row * per_row) * 4;
-    if (row >= g.I) return;
+    if (row >= g.I || col >= g.J) return;
     const float *p = g.part + (size_t)row * g.part_ld + col;
     f32x4_t v = *as_global(reinterpret_cast<const f32x4_t *>(p));
 #pragma unroll 4
     for (int s = 1; s < g.splits; ++s) v += *as_global(reinterpret_cast<const f32x4_t *>(p + (size_t)s * g.I * g.part_ld));
-    finish4(g, row, col, v);
+    f32x4_t one[1] = {v};
+    finish<1>(g, row, 1, col, bias_at(g, col), one);
 }
 
 // dz = dy act'(z) as 16-bit terms, and sums of its columns over a part of the rows: a thread has eight columns.
