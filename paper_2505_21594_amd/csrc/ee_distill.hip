@@ -117,7 +117,7 @@ __device__ __forceinline__ RowTerms row_terms(const DistillDev &a, const Entry &
 enum DistillMode { WHOLE = 0, STATS = 1, GRAD = 2 };
 
 template <int TYPE, int E, int NT, int MODE>
-__global__ void __launch_bounds__(NT) ee_distill_kernel(DistillDev a)
+__global__ void __launch_bounds__(NT, 4) ee_distill_kernel(DistillDev a)
 {
     typedef RowPart<TYPE, E, NT> Part;
     constexpr int N = Part::N, WAVES = NT / 64;
@@ -170,6 +170,7 @@ __global__ void __launch_bounds__(NT) ee_distill_kernel(DistillDev a)
         }
         const float ref = m == -INFINITY ? 0.f : m;
         float s = 0.f;
+        z.again();
 #pragma unroll
         for (int c = 0; c < E; ++c) {
             float x[N];
@@ -235,6 +236,7 @@ __global__ void __launch_bounds__(NT) ee_distill_kernel(DistillDev a)
     __syncthreads();
     const float others = others_s, ref = m_s == -INFINITY ? 0.f : m_s;
     const size_t out = (size_t)row * a.grad_stride + first;
+    z.again();
 #pragma unroll
     for (int c = 0; c < E; ++c) {
         const int from = Part::offset(c, tid);

@@ -11,7 +11,7 @@
 
 namespace ee {
 
-constexpr int SC_THREADS = 256, SC_WAVES = SC_THREADS / 64;
+constexpr int SC_THREADS = 256, SC_WAVES = SC_THREADS / 64;   // of the second launch
 constexpr int SC_CHUNKS = 512;         // chunks with a candidate that LDS has room for
 constexpr int SC_CAND = 256;           // candidates, four for each lane of a wave
 
@@ -122,12 +122,15 @@ __device__ __forceinline__ void write_row(const ScoreDev &a, int row, int lane, 
 }
 
 // Sums of a part from its threads' (relative to the maximum m of each), in every thread.
+template <int WAVES>
 __device__ __forceinline__ void join_sums(float &m, double &S, double &D, float s, float d, float c, int lane, int wave, float *wm, double *ws, double *wd)
 {
     const float wave_m = wave_max_f(m);
     if (lane == 0) wm[wave] = wave_m;
     __syncthreads();
-    const float all = fmaxf(fmaxf(wm[0], wm[1]), fmaxf(wm[2], wm[3]));
+    float all = wm[0];
+#pragma unroll
+    for (int w = 1; w < WAVES; ++w) all = fmaxf(all, wm[w]);
     const float down = m == -INFINITY ? 0.f : m - all;        // (a thread without a finite maximum has sums of 0, or of NaN)
     const float scale = __builtin_amdgcn_exp2f(down * c);
     const double S1 = (double)(s * scale), D1 = (double)(d * scale) + (s != 0.f ? (double)down * S1 : 0.0);
@@ -138,18 +141,23 @@ __device__ __forceinline__ void join_sums(float &m, double &S, double &D, float 
     }
     __syncthreads();
     m = all;
-    S = (ws[0] + ws[1]) + (ws[2] + ws[3]);
-    D = (wd[0] + wd[1]) + (wd[2] + wd[3]);
+    S = ws[0];
+    D = wd[0];
+#pragma unroll
+    for (int w = 1; w < WAVES; ++w) {
+        S += ws[w];
+        D += wd[w];
+    }
 }
 
-template <int TYPE, int E>
-__global__ void __launch_bounds__(SC_THREADS) ee_score_kernel(ScoreDev a)
+template <int TYPE, int E, int NT>
+__global__ void __launch_bounds__(NT, 4) ee_score_kernel(ScoreDev a)
 {
-    typedef RowPart<TYPE, E, SC_THREADS> Part;
-    constexpr int N = Part::N;
-    __shared__ float wm[SC_WAVES];
-    __shared__ double ws[SC_WAVES], wd[SC_WAVES];
-    __shared__ unsigned bound[SC_WAVES];
+    typedef RowPart<TYPE, E, NT> Part;
+    constexpr int N = Part::N, WAVES = NT / 64;
+    __shared__ float wm[WAVES];
+    __shared__ double ws[WAVES], wd[WAVES];
+    __shared__ unsigned bound[WAVES];
     __shared__ u32x4_t chunks[SC_CHUNKS];
     __shared__ int chunk_at[SC_CHUNKS];
     __shared__ Cand cands[SC_CAND], best[64];
@@ -172,6 +180,7 @@ __global__ void __launch_bounds__(SC_THREADS) ee_score_kernel(ScoreDev a)
     }
     const float ref = m == -INFINITY ? 0.f : m;
     float s = 0.f, d = 0.f;
+    z.again();
 #pragma unroll
     for (int c = 0; c < E; ++c) {
         float x[N];
@@ -183,6 +192,7 @@ __global__ void __launch_bounds__(SC_THREADS) ee_score_kernel(ScoreDev a)
             d += fmaxf(y, -3e38f) * e;                       // (-infinity times 0 is nothing)
         }
     }
+    z.again();
     const int k = min(a.top, len);
     if (k > 0) {                                             // a bound that k elements of this wave reach, if it has so many
         unsigned u[4];
@@ -197,11 +207,14 @@ __global__ void __launch_bounds__(SC_THREADS) ee_score_kernel(ScoreDev a)
         if (lane == 0) bound[wave] = t;
     }
     double S, D;
-    join_sums(m, S, D, s, d, a.c, lane, wave, wm, ws, wd);
+    join_sums<WAVES>(m, S, D, s, d, a.c, lane, wave, wm, ws, wd);
     D *= a.inv_td;
     int count = 0;
     if (k > 0) {
-        const float t = of_key(max(max(max(bound[0], bound[1]), max(bound[2], bound[3])), KEY_LEAST));
+        unsigned most = KEY_LEAST;
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) most = max(most, bound[w]);
+        const float t = of_key(most);
         int mine = 0;
 #pragma unroll
         for (int c = 0; c < E; ++c) mine += __popcll(__ballot(cm[c] >= t));
@@ -223,7 +236,7 @@ __global__ void __launch_bounds__(SC_THREADS) ee_score_kernel(ScoreDev a)
         }
         __syncthreads();
         const int n = min(n_chunks, SC_CHUNKS);
-        for (int i = tid; i < n * N; i += SC_THREADS) {
+        for (int i = tid; i < n * N; i += NT) {
             float x;
             if constexpr (TYPE == EE_FP32)
                 x = reinterpret_cast<const float *>(chunks)[i];
@@ -251,18 +264,22 @@ __global__ void __launch_bounds__(SC_THREADS) ee_score_kernel(ScoreDev a)
                 count = wave_best(u, token, k, lane, best);
             }
         } else {
-            // many equal ones: a round for each token, the best behind the last one in order.  (One of finite logits; -infinity is none.)
-            __shared__ unsigned long long round_best[SC_WAVES];
+            // many equal ones: a round for each token, the best behind the last one in order, by reading the part again (registers that live through this cost
+            // every row of a call).  (Of finite logits; -infinity is none.)
+            __shared__ unsigned long long round_best[WAVES];
             unsigned long long last = ~0ull;
+            const void *part_at = row_at(a.logits, TYPE, (size_t)row * a.stride + first);
             for (int r = 0; r < k; ++r) {
                 unsigned long long mine_best = 0;
-#pragma unroll
-                for (int c = 0; c < E; ++c) {
+#pragma unroll 1
+                for (int at = 0; at < len; at += Part::ROOM / E) {
+                    RowPart<TYPE, 1, NT> some;
+                    some.load(row_at(part_at, TYPE, at), len - at, tid);
                     float x[N];
-                    z.chunk(c, x);
+                    some.chunk(0, x);
 #pragma unroll
                     for (int i = 0; i < N; ++i) {
-                        const unsigned long long o = (unsigned long long)key_of(x[i]) << 32 | (0x7FFFFFFFu - (unsigned)(first + Part::offset(c, tid) + i));
+                        const unsigned long long o = (unsigned long long)key_of(x[i]) << 32 | (0x7FFFFFFFu - (unsigned)(first + at + tid * N + i));
                         if (x[i] >= -3.4028235e38f && o < last && o > mine_best) mine_best = o;
                     }
                 }
@@ -272,7 +289,9 @@ __global__ void __launch_bounds__(SC_THREADS) ee_score_kernel(ScoreDev a)
                 }
                 if (lane == 0) round_best[wave] = mine_best;
                 __syncthreads();
-                last = max(max(round_best[0], round_best[1]), max(round_best[2], round_best[3]));
+                last = 0;
+#pragma unroll
+                for (int w = 0; w < WAVES; ++w) last = max(last, round_best[w]);
                 __syncthreads();
                 if (last == 0) break;
                 if (tid == 0) best[r] = Cand{(unsigned)(last >> 32), (int)(0x7FFFFFFFu - (unsigned)last)};
@@ -367,16 +386,16 @@ __global__ void __launch_bounds__(SC_THREADS) ee_score_join_kernel(ScoreDev a)
 
 typedef void (*score_kernel_t)(ScoreDev);
 struct ScorePlan {
-    bool wide;                         // parts of 16 chunks a thread
+    bool wide;                         // 512 threads of eight chunks for a part; 256 of four
     RowSplit split;
     size_t part_bytes, bytes;
 };
 static ScorePlan plan_score(const ee_score_args &p)
 {
     ScorePlan pl;
-    const int n = p.dtype == EE_FP32 ? 4 : 8, wide = 16 * SC_THREADS * n;
+    const int n = p.dtype == EE_FP32 ? 4 : 8, wide = 8 * 512 * n;
     pl.wide = (long long)p.n_rows * ((p.vocab + wide - 1) / wide) >= 512;
-    pl.split = split_rows(p.n_rows, p.vocab, pl.wide ? wide : 4 * SC_THREADS * n, SC_THREADS * n, pl.wide ? 1 : 512);
+    pl.split = split_rows(p.n_rows, p.vocab, pl.wide ? wide : 4 * 256 * n, 256 * n, pl.wide ? 1 : 512);
     pl.part_bytes = pl.split.parts > 1 ? align256((size_t)p.n_rows * pl.split.parts * sizeof(ScorePart)) : 0;
     pl.bytes = pl.part_bytes + (pl.split.parts > 1 ? align256((size_t)p.n_rows * pl.split.parts * p.top * sizeof(Cand)) : 0);
     return pl;
@@ -424,7 +443,7 @@ extern "C" int ee_score_tokens(const ee_score_args *p, void *workspace, size_t w
     const ScorePlan pl = plan_score(*p);
     if (pl.bytes > workspace_bytes || (pl.bytes && (!workspace || !aligned(workspace, 256))))
         return fail(EE_EINVAL, "%s: the workspace has %zu bytes of %zu, or is not 256-byte aligned", call, workspace_bytes, pl.bytes);
-    if ((long long)p->n_rows * pl.split.parts >= 1 << 24) return fail(EE_EINVAL, "%s: too many rows of so many tokens", call);
+    if ((long long)p->n_rows * pl.split.parts >= 1 << 23) return fail(EE_EINVAL, "%s: too many rows of so many tokens", call);
     ScoreDev a;
     a.logits = p->logits;
     a.tokens = p->tokens;
@@ -446,11 +465,11 @@ extern "C" int ee_score_tokens(const ee_score_args *p, void *workspace, size_t w
     a.c = (float)(1.4426950408889634 / (double)p->temperature);
     DeviceScope scope(p->device);
     HIP_TRY(scope.status);
-    static const score_kernel_t kernels[3][2] = {{ee_score_kernel<EE_BF16, 4>, ee_score_kernel<EE_BF16, 16>},
-                                                 {ee_score_kernel<EE_FP16, 4>, ee_score_kernel<EE_FP16, 16>},
-                                                 {ee_score_kernel<EE_FP32, 4>, ee_score_kernel<EE_FP32, 16>}};
+    static const score_kernel_t kernels[3][2] = {{ee_score_kernel<EE_BF16, 4, 256>, ee_score_kernel<EE_BF16, 8, 512>},
+                                                 {ee_score_kernel<EE_FP16, 4, 256>, ee_score_kernel<EE_FP16, 8, 512>},
+                                                 {ee_score_kernel<EE_FP32, 4, 256>, ee_score_kernel<EE_FP32, 8, 512>}};
     const hipStream_t s = static_cast<hipStream_t>(stream);
-    hipLaunchKernelGGL(kernels[p->dtype][pl.wide], dim3((unsigned)(p->n_rows * pl.split.parts)), dim3(SC_THREADS), 0, s, a);
+    hipLaunchKernelGGL(kernels[p->dtype][pl.wide], dim3((unsigned)(p->n_rows * pl.split.parts)), dim3(pl.wide ? 512 : 256), 0, s, a);
     HIP_TRY(hipGetLastError());
     if (a.parts > 1) {
         hipLaunchKernelGGL(ee_score_join_kernel, dim3((unsigned)p->n_rows), dim3(SC_THREADS), 0, s, a);

@@ -2,6 +2,8 @@
 // over a wave in 64 bits, a row's logits in registers.
 #pragma once
 
+#include <type_traits>
+
 #include "ee_ops.hpp"
 
 namespace ee {
@@ -67,6 +69,9 @@ __device__ __forceinline__ double wave_scan_d(double x)
     return x;
 }
 
+typedef uint32_t u32x4_at4_t __attribute__((ext_vector_type(4), aligned(4)));
+typedef uint32_t u32x4_at2_t __attribute__((ext_vector_type(4), aligned(2)));
+
 // Part of a row in a workgroup's registers, as it lies in memory: chunk c of thread t holds the elements (c * NT + t) * N .. + N - 1 behind the
 // part's first, N of them in 16 bytes; -infinity behind the part's end.
 template <int TYPE, int E, int NT>
@@ -76,44 +81,34 @@ struct RowPart {
     u32x4_t raw[E];
 
     static __device__ __forceinline__ int offset(int c, int tid) { return (c * NT + tid) * N; }
-    // the part of `n` elements at `p`, which is aligned to the element type
+    // the part of `n` elements at `p` (the same in every lane), which is aligned to the element type
     __device__ __forceinline__ void load(const void *p, int n, int tid)
     {
-        if constexpr (TYPE == EE_FP32) {
-            typedef uint32_t some_t __attribute__((ext_vector_type(4), aligned(4)));
-            const uint32_t *q = static_cast<const uint32_t *>(p);
+        constexpr uint32_t NOTHING = TYPE == EE_FP32 ? 0xFF800000u : TYPE == EE_BF16 ? 0xFF80FF80u : 0xFC00FC00u;
+        typedef std::conditional_t<TYPE == EE_FP32, u32x4_at4_t, u32x4_at2_t> some_t;
+        const EE_GLOBAL char *const base = (const EE_GLOBAL char *)as_global(static_cast<const char *>(p));
+        const int mine = n - tid * N;
 #pragma unroll
-            for (int c = 0; c < E; ++c) {
-                const int at = offset(c, tid);
-                if (at + N <= n) {
-                    raw[c] = *(const EE_GLOBAL some_t *)as_global(q + at);
-                } else {
+        for (int c = 0; c < E; ++c) {
+            raw[c] = (u32x4_t){NOTHING, NOTHING, NOTHING, NOTHING};
+            if (mine >= c * NT * N + N) raw[c] = *(const EE_GLOBAL some_t *)(base + c * NT * 16 + (unsigned)tid * 16u);
+        }
+        // the chunk that the part's end is in
+        const int last = n / N;
+        if (n % N != 0 && tid == last % NT) {
+            uint32_t w[4] = {NOTHING, NOTHING, NOTHING, NOTHING};
+            const EE_GLOBAL char *const q = base + (size_t)last * 16;
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        raw[c][i] = 0xFF800000u;
-                        if (at + i < n) raw[c][i] = as_global(q)[at + i];
-                    }
+            for (int i = 0; i < N - 1; ++i)
+                if (last * N + i < n) {
+                    if constexpr (TYPE == EE_FP32)
+                        w[i] = *(const EE_GLOBAL uint32_t *)(q + i * 4);
+                    else
+                        w[i / 2] = i % 2 ? (w[i / 2] & 0xFFFFu) | (uint32_t) * (const EE_GLOBAL uint16_t *)(q + i * 2) << 16 : (w[i / 2] & 0xFFFF0000u) | *(const EE_GLOBAL uint16_t *)(q + i * 2);
                 }
-            }
-        } else {
-            typedef uint32_t some_t __attribute__((ext_vector_type(4), aligned(2)));
-            const uint16_t *q = static_cast<const uint16_t *>(p);
-            constexpr uint32_t NOTHING = TYPE == EE_BF16 ? 0xFF80u : 0xFC00u;
 #pragma unroll
-            for (int c = 0; c < E; ++c) {
-                const int at = offset(c, tid);
-                if (at + N <= n) {
-                    raw[c] = *(const EE_GLOBAL some_t *)as_global(q + at);
-                } else {
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        uint32_t a = NOTHING, b = NOTHING;
-                        if (at + 2 * i < n) a = as_global(q)[at + 2 * i];
-                        if (at + 2 * i + 1 < n) b = as_global(q)[at + 2 * i + 1];
-                        raw[c][i] = a | b << 16;
-                    }
-                }
-            }
+            for (int c = 0; c < E; ++c)
+                if (c == last / NT) raw[c] = (u32x4_t){w[0], w[1], w[2], w[3]};
         }
     }
     static __device__ __forceinline__ void values(const u32x4_t &r, float (&x)[N])
@@ -135,6 +130,18 @@ struct RowPart {
         }
     }
     __device__ __forceinline__ void chunk(int c, float (&x)[N]) const { values(raw[c], x); }
+    // Between two walks over the part: the compiler takes the elements as others than before, and does not keep them all as floats in the meantime (twice the registers).
+    __device__ __forceinline__ void again()
+    {
+#pragma unroll
+        for (int c = 0; c < E; ++c)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                uint32_t w = raw[c][i];
+                asm volatile("" : "+v"(w));
+                raw[c][i] = w;
+            }
+    }
 };
 
 // One element of a row.
