@@ -7,15 +7,16 @@
 // Bound by the logits' bytes, read once, and the gradient's, written once: a workgroup holds its row in registers (RowPart) from the sums to the gradient.
 // Rows that are too few to fill the chip, or too long for a workgroup, are taken in parts by two launches, of which the second reads the logits again.
 // The tokens that the list names are marked in LDS, one bit each, a thread's bits in one word, and left out of the sums: rho is a sum of its own, not
-// a difference.  With m' and S' the others' maximum and sum, M the row's maximum and A = exp((m' - M) / T) / S their share's scale, rho = A S' and
-// q_i (1 - pi / rho) = exp((z_i - m') / T) (A - pi / S').  Everything that a row has once is in 64 bits: the loss is a small difference of large terms.
+// a difference.  In powers of two, c = log2(e) / T rounded to fp32 (another temperature by 2^-24 of it): with r and S' = sum 2^(z c - r) the others' largest exponent
+// and sum, R the row's largest and A = 2^(r - R) / S their share's scale, rho = A S' and q_i (1 - pi / rho) = 2^(z_i c - r) (A - pi / S').
+// Everything that a row has once is in 64 bits: the loss is a small difference of large terms.
 #include "ee_vocab.hpp"
 
 namespace ee {
 
 struct DistillPart {
-    double sum;                        // sum exp((z - m) / T) over the tokens that the list does not name
-    float m, unused;                   // their maximum
+    double sum;                        // sum 2^(z c - r) over the tokens that the list does not name
+    float r, unused;                   // the largest z c of them
 };
 
 struct DistillDev {
@@ -29,7 +30,6 @@ struct DistillDev {
     long long stride, grad_stride;
     int type, grad_type, V, top, rest, parts, length;
     float c;                           // log2(e) / T
-    double inv_t;
 };
 
 // The teacher's list of a row: a lane of a wave for each entry.
@@ -62,42 +62,43 @@ __device__ __forceinline__ double readlane_d(double x, int l)
 // A row's numbers from the others' maximum and sum and from its list; one wave calls it.
 struct RowTerms {
     double loss;
-    float others;                      // gradient of a token that the list does not name: others * exp((z - m') / T)
+    float others;                      // gradient of a token that the list does not name: others * 2^(z c - r)
     float mine;                        // gradient of the lane's token
     bool first;                        // the lane's token is named here for the first time
 };
-__device__ __forceinline__ RowTerms row_terms(const DistillDev &a, const Entry &e, float m_rest, double s_rest, double weight)
+__device__ __forceinline__ RowTerms row_terms(const DistillDev &a, const Entry &e, float r_rest, double s_rest, float d_loss)
 {
+    constexpr double LN2 = 0.6931471805599453;
     RowTerms r;
     const bool in = e.id >= 0;
-    const double p = in ? exp(e.lp) : 0.0;
+    const double c = (double)a.c, p = in ? exp(e.lp) : 0.0;
     // a token that is named twice has both probabilities
     double both = 0.0;
     r.first = in;
-    int distinct = 0;
     const int lane = threadIdx.x & 63;
     for (int i = 0; i < a.top; ++i) {
         const int id = __builtin_amdgcn_readlane(e.id, i);
+        const double other = readlane_d(p, i);
         if (id >= 0 && id == e.id) {
-            both += readlane_d(p, i);
+            both += other;
             if (i < lane) r.first = false;
         }
     }
-    distinct = __popcll(__ballot(r.first));
-    const float M = fmaxf(m_rest, wave_max_f(in ? e.z : -INFINITY));
-    const double top = M == -INFINITY ? 0.0 : (double)M;
-    const double z = ((double)e.z - top) * a.inv_t, q1 = in ? exp(z) : 0.0;
-    const double down = m_rest == -INFINITY ? 0.0 : exp(((double)m_rest - top) * a.inv_t);
-    const double S = wave_sum_d(r.first ? q1 : 0.0) + (s_rest != 0.0 ? s_rest * down : 0.0);
+    const int distinct = __popcll(__ballot(r.first));
+    const float largest = fmaxf(r_rest, wave_max_f(in ? e.z * a.c : -INFINITY));
+    const double R = largest == -INFINITY ? 0.0 : (double)largest;
+    const double z = (double)e.z * c - R, q1 = in ? exp2(z) : 0.0;
+    const double down = r_rest == -INFINITY ? 0.0 : (double)r_rest - R, scale_rest = r_rest == -INFINITY ? 0.0 : exp2(down);
+    const double S = wave_sum_d(r.first ? q1 : 0.0) + (s_rest != 0.0 ? s_rest * scale_rest : 0.0);
     const bool valid = S > 0.0 && S < INFINITY;
-    const double share = wave_sum_d(p), lse = log(S), A = down / S;
+    const double share = wave_sum_d(p), log_S = log2(S), A = scale_rest / S;
     double others, scale = 1.0, shift = 0.0, tail = 0.0;
     if (a.rest) {
         const double pi = share < 1.0 ? 1.0 - share : share >= 1.0 ? 0.0 : share;        // (NaN stays)
         others = A;
         if (pi != 0.0 && distinct < a.V) {
             others = s_rest > 0.0 ? A - pi / s_rest : 0.0;
-            tail = s_rest > 0.0 ? pi * (log(pi) - (((double)m_rest - top) * a.inv_t + log(s_rest) - lse)) : (double)INFINITY;
+            tail = s_rest > 0.0 ? pi * (log2(pi) - (down + log2(s_rest) - log_S)) * LN2 : (double)INFINITY;
             if (s_rest != s_rest || pi != pi) others = tail = (double)NAN;
         }
     } else {
@@ -105,26 +106,42 @@ __device__ __forceinline__ RowTerms row_terms(const DistillDev &a, const Entry &
         shift = share > 0.0 ? log(share) : 0.0;
         others = share == 0.0 ? 0.0 : A;
     }
-    const double term = in && p != 0.0 && scale != 0.0 ? p * scale * (e.lp - shift - (z - lse)) : 0.0;
+    const double term = in && p != 0.0 && scale != 0.0 ? p * scale * (e.lp - shift - (z - log_S) * LN2) : 0.0;
     r.loss = wave_sum_d(term) + tail;
     double g = share == 0.0 && !a.rest ? 0.0 : q1 / S - both * scale;
     if (!valid) r.loss = others = g = (double)NAN;
+    const double weight = (double)d_loss * (c * LN2);
     r.others = (float)(others * weight);
     r.mine = (float)(g * weight);
     return r;
 }
 
+// The others' largest exponent and sum from the parts of a row; one wave calls it.
+__device__ __forceinline__ double join_parts(const DistillDev &a, int row, int lane, float &r)
+{
+    const DistillPart *parts = a.part + (size_t)row * a.parts;
+    r = -INFINITY;
+    for (int p = lane; p < a.parts; p += 64) r = fmaxf(r, parts[p].r);
+    r = wave_max_f(r);
+    double S = 0.0;
+    for (int p = lane; p < a.parts; p += 64) {
+        const DistillPart x = parts[p];
+        if (x.sum != 0.0) S += x.sum * (x.r == -INFINITY ? 1.0 : exp2((double)x.r - (double)r));
+    }
+    return wave_sum_d(S);
+}
+
 enum DistillMode { WHOLE = 0, STATS = 1, GRAD = 2 };
 
 template <int TYPE, int E, int NT, int MODE>
-__global__ void __launch_bounds__(NT, 4) ee_distill_kernel(DistillDev a)
+__global__ void __launch_bounds__(NT, NT == 512 ? 6 : 4) ee_distill_kernel(DistillDev a)
 {
     typedef RowPart<TYPE, E, NT> Part;
     constexpr int N = Part::N, WAVES = NT / 64;
     __shared__ uint32_t named[NT * E / 4];                   // a byte for each chunk, a bit for each of its elements
-    __shared__ float wm[WAVES];
+    __shared__ float wr[WAVES];
     __shared__ double ws[WAVES];
-    __shared__ float others_s, m_s;
+    __shared__ float others_s, r_s;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int row = a.parts == 1 ? blockIdx.x : blockIdx.x / a.parts, part = a.parts == 1 ? 0 : blockIdx.x - row * a.parts;
     const int first = part * a.length, len = min(a.length, a.V - first);
@@ -151,7 +168,7 @@ __global__ void __launch_bounds__(NT, 4) ee_distill_kernel(DistillDev a)
     for (int i = 0; i < E / 4; ++i) marks[i] = named[tid * (E / 4) + i];
     auto marked = [&](int c) { return marks[c / 4] >> (c % 4 * 8) & 255u; };
 
-    float m_rest;
+    float r_rest;
     if constexpr (MODE != GRAD) {
         float m = -INFINITY;
 #pragma unroll
@@ -168,7 +185,7 @@ __global__ void __launch_bounds__(NT, 4) ee_distill_kernel(DistillDev a)
                 for (int i = 0; i < N; ++i) m = fmaxf(m, x[i]);
             }
         }
-        const float ref = m == -INFINITY ? 0.f : m;
+        const float r = m * a.c, ref = m == -INFINITY ? 0.f : r;
         float s = 0.f;
         z.again();
 #pragma unroll
@@ -179,19 +196,19 @@ __global__ void __launch_bounds__(NT, 4) ee_distill_kernel(DistillDev a)
             if (b) {
 #pragma unroll
                 for (int i = 0; i < N; ++i)
-                    if (!(b >> i & 1)) s += __builtin_amdgcn_exp2f((x[i] - ref) * a.c);
+                    if (!(b >> i & 1)) s += __builtin_amdgcn_exp2f(fmaf(x[i], a.c, -ref));
             } else {
 #pragma unroll
-                for (int i = 0; i < N; ++i) s += __builtin_amdgcn_exp2f((x[i] - ref) * a.c);
+                for (int i = 0; i < N; ++i) s += __builtin_amdgcn_exp2f(fmaf(x[i], a.c, -ref));
             }
         }
-        const float wave_m = wave_max_f(m);
-        if (lane == 0) wm[wave] = wave_m;
+        const float wave_r = wave_max_f(r);
+        if (lane == 0) wr[wave] = wave_r;
         __syncthreads();
-        m_rest = wm[0];
+        r_rest = wr[0];
 #pragma unroll
-        for (int w = 1; w < WAVES; ++w) m_rest = fmaxf(m_rest, wm[w]);
-        const double S1 = wave_sum_d((double)(s * __builtin_amdgcn_exp2f(m == -INFINITY ? 0.f : (m - m_rest) * a.c)));
+        for (int w = 1; w < WAVES; ++w) r_rest = fmaxf(r_rest, wr[w]);
+        const double S1 = wave_sum_d((double)(s * __builtin_amdgcn_exp2f(m == -INFINITY ? 0.f : r - r_rest)));
         if (lane == 0) ws[wave] = S1;
         __syncthreads();
         if constexpr (MODE == STATS) {
@@ -199,7 +216,7 @@ __global__ void __launch_bounds__(NT, 4) ee_distill_kernel(DistillDev a)
                 DistillPart p;
                 p.sum = ws[0];
                 for (int w = 1; w < WAVES; ++w) p.sum += ws[w];
-                p.m = m_rest;
+                p.r = r_rest;
                 p.unused = 0.f;
                 a.part[(size_t)row * a.parts + part] = p;
             }
@@ -210,31 +227,22 @@ __global__ void __launch_bounds__(NT, 4) ee_distill_kernel(DistillDev a)
     if (wave == 0) {
         double S;
         if constexpr (MODE == GRAD) {
-            const DistillPart *parts = a.part + (size_t)row * a.parts;
-            float m = -INFINITY;
-            for (int p = lane; p < a.parts; p += 64) m = fmaxf(m, parts[p].m);
-            m_rest = wave_max_f(m);
-            S = 0.0;
-            for (int p = lane; p < a.parts; p += 64) {
-                const DistillPart x = parts[p];
-                if (x.sum != 0.0) S += x.sum * (x.m == -INFINITY ? 1.0 : exp(((double)x.m - (double)m_rest) * a.inv_t));
-            }
-            S = wave_sum_d(S);
+            S = join_parts(a, row, lane, r_rest);
         } else {
             S = ws[0];
             for (int w = 1; w < WAVES; ++w) S += ws[w];
         }
-        const RowTerms r = row_terms(a, e, m_rest, S, (double)weight * a.inv_t);
+        const RowTerms r = row_terms(a, e, r_rest, S, weight);
         if (lane == 0) {
             others_s = r.others;
-            m_s = m_rest;
+            r_s = r_rest;
             if (a.loss && part == 0) as_global_mut(a.loss)[row] = (float)r.loss;
         }
         if (a.d_logits && r.first && at >= 0 && at < len) store_one(a.grad_type, a.d_logits, (size_t)row * a.grad_stride + e.id, weight == 0.f ? 0.f : r.mine);
     }
     if (!a.d_logits) return;
     __syncthreads();
-    const float others = others_s, ref = m_s == -INFINITY ? 0.f : m_s;
+    const float others = others_s, ref = r_s == -INFINITY ? 0.f : r_s;
     const size_t out = (size_t)row * a.grad_stride + first;
     z.again();
 #pragma unroll
@@ -244,7 +252,7 @@ __global__ void __launch_bounds__(NT, 4) ee_distill_kernel(DistillDev a)
         float x[N];
         z.chunk(c, x);
 #pragma unroll
-        for (int i = 0; i < N; ++i) x[i] = weight == 0.f ? 0.f : __builtin_amdgcn_exp2f((x[i] - ref) * a.c) * others;
+        for (int i = 0; i < N; ++i) x[i] = weight == 0.f ? 0.f : __builtin_amdgcn_exp2f(fmaf(x[i], a.c, -ref)) * others;
         const uint32_t b = marked(c);
         if (b == 0 && from + N <= len) {
             store_some<N>(a.grad_type, a.d_logits, out + from, x);
@@ -263,30 +271,23 @@ __global__ void __launch_bounds__(256) ee_distill_loss_kernel(DistillDev a, int 
     if (row >= n_rows) return;
     Entry e = entry_of(a, row, lane);
     if (e.id >= 0) e.z = as_global(a.z)[(size_t)row * a.top + lane];
-    const DistillPart *parts = a.part + (size_t)row * a.parts;
-    float m = -INFINITY;
-    for (int p = lane; p < a.parts; p += 64) m = fmaxf(m, parts[p].m);
-    m = wave_max_f(m);
-    double S = 0.0;
-    for (int p = lane; p < a.parts; p += 64) {
-        const DistillPart x = parts[p];
-        if (x.sum != 0.0) S += x.sum * (x.m == -INFINITY ? 1.0 : exp(((double)x.m - (double)m) * a.inv_t));
-    }
-    const RowTerms r = row_terms(a, e, m, wave_sum_d(S), 1.0);
+    float r_rest;
+    const double S = join_parts(a, row, lane, r_rest);
+    const RowTerms r = row_terms(a, e, r_rest, S, 1.f);
     if (lane == 0) as_global_mut(a.loss)[row] = (float)r.loss;
 }
 
 struct DistillPlan {
-    int shape;                         // threads and chunks a thread: 256 x 4, 256 x 16, 1024 x 16
+    int shape;                         // threads and chunks a thread: 256 x 4, 512 x 8, 1024 x 16
     RowSplit split;
     size_t part_bytes, bytes;
 };
-static DistillPlan plan_distill(const ee_distill_args &p)
+static DistillPlan plan_distill(const ee_distill_args &p, bool grad)
 {
     DistillPlan pl;
-    const int n = p.dtype == EE_FP32 ? 4 : 8, room[3] = {256 * 4 * n, 256 * 16 * n, 1024 * 16 * n};
+    const int n = p.dtype == EE_FP32 ? 4 : 8, room[3] = {256 * 4 * n, 512 * 8 * n, 1024 * 16 * n};
     pl.shape = p.vocab <= room[0] ? 0 : p.vocab <= room[1] ? 1 : 2;
-    if (p.n_rows >= 256 && p.vocab <= room[2]) {
+    if (p.n_rows >= 256 && p.vocab <= room[grad ? 2 : 1]) {
         pl.split.parts = 1;
         pl.split.length = p.vocab;
     } else {
@@ -322,7 +323,7 @@ extern "C" int ee_distill_workspace(const ee_distill_args *p, size_t *bytes)
     if (!bytes) return fail(EE_EINVAL, "%s: null argument", call);
     *bytes = 0;
     int rc = check_distill(call, p);
-    if (rc == EE_OK && p->n_rows) *bytes = plan_distill(*p).bytes;
+    if (rc == EE_OK && p->n_rows) *bytes = std::max(plan_distill(*p, false).bytes, plan_distill(*p, true).bytes);   // (whichever results are wanted)
     return rc;
 }
 
@@ -331,9 +332,9 @@ template <int TYPE>
 static distill_kernel_t distill_kernel(int shape, int mode)
 {
     if (mode == WHOLE)
-        return shape == 0 ? ee_distill_kernel<TYPE, 4, 256, WHOLE> : shape == 1 ? ee_distill_kernel<TYPE, 16, 256, WHOLE> : ee_distill_kernel<TYPE, 16, 1024, WHOLE>;
-    if (mode == STATS) return shape == 0 ? ee_distill_kernel<TYPE, 4, 256, STATS> : ee_distill_kernel<TYPE, 16, 256, STATS>;
-    return shape == 0 ? ee_distill_kernel<TYPE, 4, 256, GRAD> : ee_distill_kernel<TYPE, 16, 256, GRAD>;
+        return shape == 0 ? ee_distill_kernel<TYPE, 4, 256, WHOLE> : shape == 1 ? ee_distill_kernel<TYPE, 8, 512, WHOLE> : ee_distill_kernel<TYPE, 16, 1024, WHOLE>;
+    if (mode == STATS) return shape == 0 ? ee_distill_kernel<TYPE, 4, 256, STATS> : ee_distill_kernel<TYPE, 8, 512, STATS>;
+    return shape == 0 ? ee_distill_kernel<TYPE, 4, 256, GRAD> : ee_distill_kernel<TYPE, 8, 512, GRAD>;
 }
 
 extern "C" int ee_distill(const ee_distill_args *p, void *workspace, size_t workspace_bytes, void *stream)
@@ -351,7 +352,7 @@ extern "C" int ee_distill(const ee_distill_args *p, void *workspace, size_t work
         return fail(EE_EINVAL, "%s: logits or d_logits are not aligned to their type", call);
     for (const void *x : {(const void *)p->ids, (const void *)p->logprobs, (const void *)p->loss, (const void *)p->d_loss})
         if (!aligned(x, 4)) return fail(EE_EINVAL, "%s: int32 and fp32 arrays must be 4-byte aligned", call);
-    const DistillPlan pl = plan_distill(*p);
+    const DistillPlan pl = plan_distill(*p, p->d_logits != nullptr);
     if (pl.bytes > workspace_bytes || (pl.bytes && (!workspace || !aligned(workspace, 256))))
         return fail(EE_EINVAL, "%s: the workspace has %zu bytes of %zu, or is not 256-byte aligned", call, workspace_bytes, pl.bytes);
     if ((long long)p->n_rows * pl.split.parts >= 1 << 22) return fail(EE_EINVAL, "%s: too many rows of so many tokens", call);
@@ -373,15 +374,14 @@ extern "C" int ee_distill(const ee_distill_args *p, void *workspace, size_t work
     a.rest = p->rest;
     a.parts = pl.split.parts;
     a.length = pl.split.length;
-    a.inv_t = 1.0 / (double)p->temperature;
-    a.c = (float)(1.4426950408889634 * a.inv_t);
+    a.c = (float)(1.4426950408889634 / (double)p->temperature);
     DeviceScope scope(p->device);
     HIP_TRY(scope.status);
     const hipStream_t s = static_cast<hipStream_t>(stream);
     const auto kernel = [&](int mode) {
         return p->dtype == EE_BF16 ? distill_kernel<EE_BF16>(pl.shape, mode) : p->dtype == EE_FP16 ? distill_kernel<EE_FP16>(pl.shape, mode) : distill_kernel<EE_FP32>(pl.shape, mode);
     };
-    const dim3 grid((unsigned)(p->n_rows * a.parts)), block(pl.shape == 2 ? 1024 : 256);
+    const dim3 grid((unsigned)(p->n_rows * a.parts)), block(pl.shape == 0 ? 256 : pl.shape == 1 ? 512 : 1024);
     hipLaunchKernelGGL(kernel(a.parts == 1 ? WHOLE : STATS), grid, block, 0, s, a);
     HIP_TRY(hipGetLastError());
     if (a.parts > 1) {

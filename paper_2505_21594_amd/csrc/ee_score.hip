@@ -3,7 +3,9 @@
 //   log p_i = z_i / T - L,  L = log sum exp(z / T);   H = L - sum p z / T;   the `top` largest logits, of equal ones the lower token first.
 //
 // Bound by the logits' bytes.  A workgroup holds a row, or a part of it, in registers (RowPart): the sums and the search for the largest read memory
-// once.  Sums: every thread takes exponentials relative to its own maximum, so that nothing waits for the row's; they meet in 64 bits.
+// once.  Sums: every thread takes exponentials relative to its own maximum, so that nothing waits for the row's; they meet in 64 bits.  All of it in powers of two:
+// with c = log2(e) / T rounded to fp32 (another temperature by 2^-24 of it) an exponential is 2^(z c - r), one multiply-add and one instruction, r a number
+// of fp32 itself, so that nothing is lost where the sums are put together.
 // The largest: the `top`-th largest among the maxima of a wave's 256 groups of chunks is a bound that at least `top` elements reach; the chunks with an element
 // above the workgroup's best bound go to LDS (a few more than `top`), then their elements above it, and of those one wave keeps exactly `top`.  Rows
 // with so many equal elements that this overflows take as many rounds as tokens are wanted.
@@ -16,8 +18,8 @@ constexpr int SC_CHUNKS = 512;         // chunks with a candidate that LDS has r
 constexpr int SC_CAND = 256;           // candidates, four for each lane of a wave
 
 struct ScorePart {
-    double sum, dot;                   // sum exp((z - m) / T),  sum (z - m) / T * exp((z - m) / T)
-    float m;
+    double sum, dot;                   // sum 2^(z c - r),  sum (z c - r) 2^(z c - r)
+    float r;
     int count;                         // candidates that it has
 };
 // A token in the order of the results: the larger key first, of equal ones the lower token.
@@ -35,8 +37,7 @@ struct ScoreDev {
     ScorePart *part;                   // [n_rows][parts]
     Cand *cand;                        // [n_rows][parts][top]
     int type, n_rows, V, top, parts, length;
-    float inv_t, c;                    // 1 / T, log2(e) / T
-    double inv_td;
+    float c;                           // log2(e) / T
 };
 
 // floats in the order of unsigned numbers (-0 as +0)
@@ -92,18 +93,19 @@ __device__ __forceinline__ int wave_best(const unsigned (&u)[4], const int (&tok
 }
 
 // What one wave writes for a row: its n (at most 64) best in order, and the row's numbers.
-__device__ __forceinline__ void write_row(const ScoreDev &a, int row, int lane, double S, double D, float m, const Cand *list, int n)
+__device__ __forceinline__ void write_row(const ScoreDev &a, int row, int lane, double S, double D, float r, const Cand *list, int n)
 {
+    constexpr double LN2 = 0.6931471805599453;
     const bool valid = S > 0.0 && S < INFINITY;               // (NaN, +infinity or nothing but -infinity: no softmax)
-    const double lse = valid ? log(S) : (double)NAN, m_t = (double)m * a.inv_td;
+    const double c = (double)a.c, log_S = valid ? log2(S) : (double)NAN, l = log_S + (double)r;
     if (lane == 0) {
         if (a.logprob) {
             const int t = as_global(a.tokens)[row];
             float lp = valid ? -INFINITY : NAN;
-            if (valid && t >= 0 && t < a.V) lp = (float)((double)logit_at(a.type, row_at(a.logits, a.type, (size_t)row * a.stride), t) * a.inv_td - m_t - lse);
+            if (valid && t >= 0 && t < a.V) lp = (float)(((double)logit_at(a.type, row_at(a.logits, a.type, (size_t)row * a.stride), t) * c - l) * LN2);
             as_global_mut(a.logprob)[row] = lp;
         }
-        if (a.entropy) as_global_mut(a.entropy)[row] = (float)fmax(lse - D / S, valid ? 0.0 : (double)NAN);
+        if (a.entropy) as_global_mut(a.entropy)[row] = (float)fmax((log_S - D / S) * LN2, valid ? 0.0 : (double)NAN);
     }
     if (a.top == 0) return;
     if (!valid) n = 0;
@@ -117,22 +119,22 @@ __device__ __forceinline__ void write_row(const ScoreDev &a, int row, int lane, 
     if (lane < a.top) {
         const size_t at = (size_t)row * a.top + (lane < n ? rank : lane);
         as_global_mut(a.top_ids)[at] = mine.token;
-        as_global_mut(a.top_logprobs)[at] = lane < n ? (float)((double)of_key(mine.key) * a.inv_td - m_t - lse) : valid ? -INFINITY : NAN;
+        as_global_mut(a.top_logprobs)[at] = lane < n ? (float)(((double)of_key(mine.key) * c - l) * LN2) : valid ? -INFINITY : NAN;
     }
 }
 
-// Sums of a part from its threads' (relative to the maximum m of each), in every thread.
+// Sums of a part from its threads' (relative to the r of each, -infinity where it has no finite logit), in every thread.
 template <int WAVES>
-__device__ __forceinline__ void join_sums(float &m, double &S, double &D, float s, float d, float c, int lane, int wave, float *wm, double *ws, double *wd)
+__device__ __forceinline__ void join_sums(float &r, double &S, double &D, float s, float d, int lane, int wave, float *wr, double *ws, double *wd)
 {
-    const float wave_m = wave_max_f(m);
-    if (lane == 0) wm[wave] = wave_m;
+    const float wave_r = wave_max_f(r);
+    if (lane == 0) wr[wave] = wave_r;
     __syncthreads();
-    float all = wm[0];
+    float all = wr[0];
 #pragma unroll
-    for (int w = 1; w < WAVES; ++w) all = fmaxf(all, wm[w]);
-    const float down = m == -INFINITY ? 0.f : m - all;        // (a thread without a finite maximum has sums of 0, or of NaN)
-    const float scale = __builtin_amdgcn_exp2f(down * c);
+    for (int w = 1; w < WAVES; ++w) all = fmaxf(all, wr[w]);
+    const float down = r == -INFINITY ? 0.f : r - all;        // (a thread without a finite maximum has sums of 0, or of NaN)
+    const float scale = __builtin_amdgcn_exp2f(down);
     const double S1 = (double)(s * scale), D1 = (double)(d * scale) + (s != 0.f ? (double)down * S1 : 0.0);
     const double S2 = wave_sum_d(S1), D2 = wave_sum_d(D1);
     if (lane == 0) {
@@ -140,7 +142,7 @@ __device__ __forceinline__ void join_sums(float &m, double &S, double &D, float 
         wd[wave] = D2;
     }
     __syncthreads();
-    m = all;
+    r = all;
     S = ws[0];
     D = wd[0];
 #pragma unroll
@@ -151,11 +153,11 @@ __device__ __forceinline__ void join_sums(float &m, double &S, double &D, float 
 }
 
 template <int TYPE, int E, int NT>
-__global__ void __launch_bounds__(NT, 4) ee_score_kernel(ScoreDev a)
+__global__ void __launch_bounds__(NT, NT == 512 ? 6 : 4) ee_score_kernel(ScoreDev a)
 {
     typedef RowPart<TYPE, E, NT> Part;
     constexpr int N = Part::N, WAVES = NT / 64;
-    __shared__ float wm[WAVES];
+    __shared__ float wr[WAVES];
     __shared__ double ws[WAVES], wd[WAVES];
     __shared__ unsigned bound[WAVES];
     __shared__ u32x4_t chunks[SC_CHUNKS];
@@ -178,7 +180,8 @@ __global__ void __launch_bounds__(NT, 4) ee_score_kernel(ScoreDev a)
         for (int i = 1; i < N; ++i) cm[c] = fmaxf(cm[c], x[i]);
         m = fmaxf(m, cm[c]);
     }
-    const float ref = m == -INFINITY ? 0.f : m;
+    float r = m * a.c;
+    const float ref = m == -INFINITY ? 0.f : r;
     float s = 0.f, d = 0.f;
     z.again();
 #pragma unroll
@@ -187,7 +190,7 @@ __global__ void __launch_bounds__(NT, 4) ee_score_kernel(ScoreDev a)
         z.chunk(c, x);
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-            const float y = x[i] - ref, e = __builtin_amdgcn_exp2f(y * a.c);
+            const float y = fmaf(x[i], a.c, -ref), e = __builtin_amdgcn_exp2f(y);
             s += e;
             d += fmaxf(y, -3e38f) * e;                       // (-infinity times 0 is nothing)
         }
@@ -207,8 +210,7 @@ __global__ void __launch_bounds__(NT, 4) ee_score_kernel(ScoreDev a)
         if (lane == 0) bound[wave] = t;
     }
     double S, D;
-    join_sums<WAVES>(m, S, D, s, d, a.c, lane, wave, wm, ws, wd);
-    D *= a.inv_td;
+    join_sums<WAVES>(r, S, D, s, d, lane, wave, wr, ws, wd);
     int count = 0;
     if (k > 0) {
         unsigned most = KEY_LEAST;
@@ -303,7 +305,7 @@ __global__ void __launch_bounds__(NT, 4) ee_score_kernel(ScoreDev a)
     if (wave != 0) return;
     wave_lds_order();
     if (a.parts == 1) {
-        write_row(a, row, lane, S, D, m, best, count);
+        write_row(a, row, lane, S, D, r, best, count);
         return;
     }
     const size_t at = (size_t)row * a.parts + part;
@@ -311,7 +313,7 @@ __global__ void __launch_bounds__(NT, 4) ee_score_kernel(ScoreDev a)
         ScorePart p;
         p.sum = S;
         p.dot = D;
-        p.m = m;
+        p.r = r;
         p.count = count;
         a.part[at] = p;
     }
@@ -369,19 +371,19 @@ __global__ void __launch_bounds__(SC_THREADS) ee_score_join_kernel(ScoreDev a)
         n = wave_best(u, token, a.top, lane, best);
         wave_lds_order();
     }
-    float m = -INFINITY;
-    for (int p = lane; p < a.parts; p += 64) m = fmaxf(m, parts[p].m);
-    m = wave_max_f(m);
+    float r = -INFINITY;
+    for (int p = lane; p < a.parts; p += 64) r = fmaxf(r, parts[p].r);
+    r = wave_max_f(r);
     double S = 0.0, D = 0.0;
     for (int p = lane; p < a.parts; p += 64) {
         const ScorePart x = parts[p];
-        const double down = x.m == -INFINITY ? 0.0 : ((double)x.m - (double)m) * a.inv_td, e = exp(down);
+        const double down = x.r == -INFINITY ? 0.0 : (double)x.r - (double)r, e = exp2(down);
         S += x.sum * e;
         if (x.sum != 0.0) D += (x.dot + down * x.sum) * e;
     }
     S = wave_sum_d(S);
     D = wave_sum_d(D);
-    write_row(a, row, lane, S, D, m, best, n);
+    write_row(a, row, lane, S, D, r, best, n);
 }
 
 typedef void (*score_kernel_t)(ScoreDev);
@@ -460,8 +462,6 @@ extern "C" int ee_score_tokens(const ee_score_args *p, void *workspace, size_t w
     a.top = p->top;
     a.parts = pl.split.parts;
     a.length = pl.split.length;
-    a.inv_td = 1.0 / (double)p->temperature;
-    a.inv_t = (float)a.inv_td;
     a.c = (float)(1.4426950408889634 / (double)p->temperature);
     DeviceScope scope(p->device);
     HIP_TRY(scope.status);
