@@ -703,7 +703,8 @@ def _lists(t, what: str, kind: str, device, rows: int, top: int) -> int:
     """Address of a contiguous array [rows][top] (None: 0)."""
     if t is None:
         return 0
-    if tuple(t.shape) != (rows, top) or _type(t) != kind or t.device != device or not _contiguous(t):
+    shape = t.shape
+    if len(shape) != 2 or shape[0] != rows or shape[1] != top or _type(t) != kind or t.device != device or (tuple(t.stride()) != (top, 1) and not _contiguous(t)):
         raise ValueError(f"{what}: contiguous {kind} [{rows}][{top}] on {device} expected")
     return t.data_ptr()
 

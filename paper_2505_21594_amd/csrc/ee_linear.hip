@@ -205,6 +205,97 @@ __global__ void __launch_bounds__(256, 2) ee_gemm16_kernel(GemmDev g)
     }
 }
 
+// Few rows: bound by the weights' bytes.  A workgroup has 16 TN columns of results, its four waves take steps of 32 of the sum in turn, each through
+// a ring of its own in LDS (no barrier but the last): 10 KB on their way for a wave, 80 for a compute unit.  The rows are MT tiles of 16; the waves' sums meet in LDS.
+constexpr int THIN_STAGES = 3;
+template <int TN, int MT>
+constexpr size_t thin_lds() { return (size_t)4 * THIN_STAGES * (TN + MT) * 1024; }
+
+template <int TYPE, int TN, int MT>
+__global__ void __launch_bounds__(256, 2) ee_gemm16_thin_kernel(GemmDev g)
+{
+    typedef Operand<true, 16 * TN * 4> Op;      // (only its placing of rows: kilobytes of 16 rows x 32)
+    constexpr int NS = THIN_STAGES, PER = TN + MT, STAGE = PER * 1024;
+    static_assert(4 * TN * MT * 1024 <= thin_lds<TN, MT>(), "the sums fit the rings' room");
+    extern __shared__ __align__(16) char lds[];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int n0 = blockIdx.x * 16 * TN, part = blockIdx.y, lo = part * g.per, hi = min(lo + g.per, g.K);
+    const int full = g.far ? 0 : (hi - lo) / 32, steps = (hi - lo + 31) / 32;
+    char *const ring = lds + wave * NS * STAGE;
+    const unsigned lds0 = lds_offset(ring);
+    const char *const w0 = reinterpret_cast<const char *>(g.B + (size_t)n0 * g.ldb + lo), *const x0 = reinterpret_cast<const char *>(g.A + lo);
+    int off[PER];
+#pragma unroll
+    for (int i = 0; i < PER; ++i) off[i] = i < TN ? Op::offset(i, lane, g.J - n0, g.ldb) : Op::offset(i - TN, lane, g.I, g.lda);
+    auto request = [&](int s, int buf) __attribute__((always_inline)) {
+        const void *pw = uniform_ptr(w0 + (size_t)s * 64), *px = uniform_ptr(x0 + (size_t)s * 64);
+#pragma unroll
+        for (int i = 0; i < PER; ++i) load_lds_kb(i < TN ? pw : px, off[i], lds0 + buf * STAGE + i * 1024);
+    };
+    f32x4_t acc[TN][MT];
+#pragma unroll
+    for (int n = 0; n < TN; ++n)
+#pragma unroll
+        for (int m = 0; m < MT; ++m) acc[n][m] = (f32x4_t){0.f, 0.f, 0.f, 0.f};
+    auto compute = [&](const char *st) __attribute__((always_inline)) {
+        u32x4_t w[TN], x[MT];
+#pragma unroll
+        for (int i = 0; i < TN; ++i) w[i] = Op::read(st, i, lane);
+#pragma unroll
+        for (int i = 0; i < MT; ++i) x[i] = Op::read(st, TN + i, lane);
+#pragma unroll
+        for (int n = 0; n < TN; ++n)
+#pragma unroll
+            for (int m = 0; m < MT; ++m) acc[n][m] = mfma16<TYPE>(w[n], x[m], acc[n][m]);
+    };
+#pragma unroll
+    for (int i = 0; i < NS - 1; ++i)
+        if (wave + 4 * i < full) request(wave + 4 * i, i);
+    int buf = 0;
+    for (int s = wave; s < full; s += 4) {
+        if (s + 4 * (NS - 2) < full)
+            wait_pending<PER *(NS - 2)>();
+        else
+            wait_pending<0>();
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // (the last step's reads are done before its place is written again)
+        if (s + 4 * (NS - 1) < full) request(s + 4 * (NS - 1), buf == 0 ? NS - 1 : buf - 1);
+        compute(ring + buf * STAGE);
+        buf = buf + 1 == NS ? 0 : buf + 1;
+    }
+    // steps that are not whole
+    for (int s = full + (wave - full % 4 + 4) % 4; s < steps; s += 4) {
+        wave_lds_order();
+        int r, k;
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            Op::place(i < TN ? i : i - TN, lane, r, k);
+            k += lo + s * 32;
+            *reinterpret_cast<u32x4_t *>(ring + i * 1024 + lane * 16) = i < TN ? load_piece(g.B, g.ldb, g.J, hi, n0 + r, k) : load_piece(g.A, g.lda, g.I, hi, r, k);
+        }
+        wave_lds_order();
+        compute(ring);
+    }
+    lds_barrier();
+#pragma unroll
+    for (int n = 0; n < TN; ++n)
+#pragma unroll
+        for (int m = 0; m < MT; ++m) *reinterpret_cast<f32x4_t *>(lds + (((wave * TN + n) * MT + m) * 64 + lane) * 16) = acc[n][m];
+    lds_barrier();
+    for (int i = wave; i < TN * MT; i += 4) {
+        f32x4_t v = *reinterpret_cast<const f32x4_t *>(lds + (i * 64 + lane) * 16);
+#pragma unroll
+        for (int w = 1; w < 4; ++w) v += *reinterpret_cast<const f32x4_t *>(lds + ((w * TN * MT + i) * 64 + lane) * 16);
+        const int row = i % MT * 16 + (lane & 15), col = n0 + i / MT * 16 + (lane >> 4) * 4;
+        if (row >= g.I || col >= g.J) continue;
+        if (g.splits == 1) {
+            f32x4_t one[1] = {v};
+            finish<1>(g, row, 1, col, bias_at(g, col), one);
+        } else {
+            *as_global_mut(reinterpret_cast<f32x4_t *>(g.part + ((size_t)part * g.I + row) * g.part_ld + col)) = v;
+        }
+    }
+}
+
 // The parts of a sum, in their order.
 __global__ void __launch_bounds__(256) ee_gemm16_join_kernel(GemmDev g)
 {
@@ -284,23 +375,37 @@ static gemm16_kernel_t gemm16_kernel(bool a_along, bool b_along)
     return a_along ? (b_along ? ee_gemm16_kernel<TYPE, true, true, TI, TJ> : ee_gemm16_kernel<TYPE, true, false, TI, TJ>) : ee_gemm16_kernel<TYPE, false, false, TI, TJ>;
 }
 
-// How a product is split: tiles of 256 x 128 or 64 x 64, and parts of the sum.
+template <int TYPE, int MT>
+static gemm16_kernel_t thin_kernel(int tn)
+{
+    static_assert(thin_lds<4, 1>() <= 64 << 10 && thin_lds<2, 2>() <= 64 << 10, "what a launch gets unasked");
+    if constexpr (MT == 1)
+        if (tn == 4) return ee_gemm16_thin_kernel<TYPE, 4, 1>;
+    return tn == 1 ? ee_gemm16_thin_kernel<TYPE, 1, MT> : ee_gemm16_thin_kernel<TYPE, 2, MT>;
+}
+
+// How a product is split: tiles of 256 x 128 or 64 x 64 or few rows at a time, and parts of the sum.
+enum GemmForm { LARGE, SMALL, THIN };
 struct GemmPlan16 {
-    bool large;
+    int form, tn;                     // tn: of few rows, tiles of 16 columns for a workgroup
     int ni, nj, splits, per;
     long long part_ld;
     size_t bytes;
 };
-static GemmPlan16 plan_gemm16(int I, int J, int K)
+static GemmPlan16 plan_gemm16(int I, int J, int K, bool along)
 {
     GemmPlan16 pl = {};
     const auto tiles = [&](int ti, int tj) { return std::max(1ll, (long long)((I + ti - 1) / ti) * ((J + tj - 1) / tj)); };
-    pl.large = tiles(256, 128) >= 128;
-    const long long n = pl.large ? tiles(256, 128) : tiles(64, 64);
-    pl.ni = (I + (pl.large ? 255 : 63)) / (pl.large ? 256 : 64);
-    pl.nj = (J + (pl.large ? 127 : 63)) / (pl.large ? 128 : 64);
+    pl.form = along && I <= 32 ? THIN : tiles(256, 128) >= 128 ? LARGE : SMALL;
+    pl.tn = 1;
+    if (pl.form == THIN)
+        while (pl.tn < (I > 16 ? 2 : 4) && J >= 16 * 2 * pl.tn * 400) pl.tn *= 2;
+    const int ti = pl.form == LARGE ? 256 : pl.form == SMALL ? 64 : 32, tj = pl.form == LARGE ? 128 : pl.form == SMALL ? 64 : 16 * pl.tn;
+    const long long n = tiles(ti, tj);
+    pl.ni = (I + ti - 1) / ti;
+    pl.nj = (J + tj - 1) / tj;
     const int most = std::max(1, K / 512);
-    pl.splits = (int)std::min<long long>(most, std::max<long long>(1, (pl.large ? 256 : 768) / n));
+    pl.splits = (int)std::min<long long>(most, std::max<long long>(1, (pl.form == LARGE ? 256 : pl.form == SMALL ? 768 : 512) / n));
     pl.per = std::max(((K + pl.splits - 1) / pl.splits + 31) / 32 * 32, 32);
     pl.splits = std::max(1, (K + pl.per - 1) / pl.per);
     pl.part_ld = ((long long)J + 3) / 4 * 4;
@@ -310,7 +415,7 @@ static GemmPlan16 plan_gemm16(int I, int J, int K)
 constexpr long long GEMM_FAR = 1 << 21;            // elements from row to row that 32-bit offsets within a tile allow
 static int launch_gemm16(GemmDev g, bool a_along, bool b_along, void *space, hipStream_t s)
 {
-    const GemmPlan16 pl = plan_gemm16(g.I, g.J, g.K);
+    const GemmPlan16 pl = plan_gemm16(g.I, g.J, g.K, a_along && b_along);
     g.ni = pl.ni;
     g.nj = pl.nj;
     g.splits = pl.splits;
@@ -318,21 +423,29 @@ static int launch_gemm16(GemmDev g, bool a_along, bool b_along, void *space, hip
     g.part = static_cast<float *>(space);
     g.part_ld = pl.part_ld;
     g.far = g.lda > GEMM_FAR || g.ldb > GEMM_FAR;
-    const gemm16_kernel_t k = pl.large ? (g.type == EE_BF16 ? gemm16_kernel<EE_BF16, 256, 128>(a_along, b_along) : gemm16_kernel<EE_FP16, 256, 128>(a_along, b_along))
-                                       : (g.type == EE_BF16 ? gemm16_kernel<EE_BF16, 64, 64>(a_along, b_along) : gemm16_kernel<EE_FP16, 64, 64>(a_along, b_along));
-    const size_t lds = pl.large ? gemm_lds<256, 128>() : gemm_lds<64, 64>();
-    if (lds > 64 << 10) {                              // said once for a kernel on a device
+    const bool bf16 = g.type == EE_BF16;
+    if (pl.form == THIN) {
+        const bool two = g.I > 16;
+        const gemm16_kernel_t k = bf16 ? (two ? thin_kernel<EE_BF16, 2>(pl.tn) : thin_kernel<EE_BF16, 1>(pl.tn)) : (two ? thin_kernel<EE_FP16, 2>(pl.tn) : thin_kernel<EE_FP16, 1>(pl.tn));
+        hipLaunchKernelGGL(k, dim3((unsigned)pl.nj, (unsigned)pl.splits), dim3(256), (size_t)4 * THIN_STAGES * (pl.tn + (two ? 2 : 1)) * 1024, s, g);
+    } else if (pl.form == SMALL) {
+        const gemm16_kernel_t k = bf16 ? gemm16_kernel<EE_BF16, 64, 64>(a_along, b_along) : gemm16_kernel<EE_FP16, 64, 64>(a_along, b_along);
+        hipLaunchKernelGGL(k, dim3((unsigned)(pl.ni * pl.nj * pl.splits)), dim3(256), (gemm_lds<64, 64>()), s, g);
+    } else {
+        const gemm16_kernel_t k = bf16 ? gemm16_kernel<EE_BF16, 256, 128>(a_along, b_along) : gemm16_kernel<EE_FP16, 256, 128>(a_along, b_along);
+        constexpr size_t lds = gemm_lds<256, 128>();
+        static_assert(lds > 64 << 10, "more than a launch gets unasked: said once for a kernel on a device");
         static std::atomic<uint64_t> said[2][2][2];
-        std::atomic<uint64_t> &mine = said[g.type == EE_BF16][a_along][b_along];
+        std::atomic<uint64_t> &mine = said[bf16][a_along][b_along];
         int device = 0;
         HIP_TRY(hipGetDevice(&device));
         const uint64_t bit = 1ull << (device & 63);
-        if (!(mine.load(std::memory_order_relaxed) & bit)) {
+        if (device >= 64 || !(mine.load(std::memory_order_relaxed) & bit)) {
             HIP_TRY(hipFuncSetAttribute(reinterpret_cast<const void *>(k), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds));
             if (device < 64) mine.fetch_or(bit, std::memory_order_relaxed);
         }
+        hipLaunchKernelGGL(k, dim3((unsigned)(pl.ni * pl.nj * pl.splits)), dim3(256), lds, s, g);
     }
-    hipLaunchKernelGGL(k, dim3((unsigned)(pl.ni * pl.nj * pl.splits)), dim3(256), lds, s, g);
     HIP_TRY(hipGetLastError());
     if (pl.splits > 1) {
         const size_t n = (size_t)g.I * (pl.part_ld / 4);
@@ -391,7 +504,7 @@ static GradPlan plan_grad(const ee_linear_grad_args &p)
     pl.parts = (p.n_rows + pl.per - 1) / pl.per;
     pl.dz_bytes = align256((size_t)pl.terms * p.n_rows * pl.ldz * 2);
     pl.part_bytes = align256((size_t)pl.parts * p.n_out * sizeof(float));
-    pl.gemm_bytes = std::max(plan_gemm16(p.n_rows, p.n_in, p.n_out).bytes, plan_gemm16(p.n_out, p.n_in, p.n_rows).bytes);
+    pl.gemm_bytes = std::max(plan_gemm16(p.n_rows, p.n_in, p.n_out, false).bytes, plan_gemm16(p.n_out, p.n_in, p.n_rows, false).bytes);
     return pl;
 }
 static int check_linear_grad(const char *call, const ee_linear_grad_args *p)
@@ -412,7 +525,7 @@ extern "C" int ee_linear_workspace(const ee_linear_args *p, size_t *bytes)
     if (!bytes) return fail(EE_EINVAL, "%s: null argument", call);
     *bytes = 0;
     int rc = check_linear(call, p);
-    if (rc == EE_OK) *bytes = plan_gemm16(p->n_rows, p->n_out, p->n_in).bytes;
+    if (rc == EE_OK) *bytes = plan_gemm16(p->n_rows, p->n_out, p->n_in, true).bytes;
     return rc;
 }
 
@@ -432,7 +545,7 @@ extern "C" int ee_linear(const ee_linear_args *p, void *workspace, size_t worksp
     if (p->residual == p->y && (p->residual_dtype != p->out_dtype || (p->n_rows > 1 && p->residual_stride != p->y_stride)))
         return fail(EE_EINVAL, "%s: y may be residual only with the same type and stride", call);
     if (!aligned(p->bias, 4)) return fail(EE_EINVAL, "%s: fp32 arrays must be 4-byte aligned", call);
-    const size_t need = plan_gemm16(p->n_rows, p->n_out, p->n_in).bytes;
+    const size_t need = plan_gemm16(p->n_rows, p->n_out, p->n_in, true).bytes;
     if (need > workspace_bytes || (need && (!workspace || !aligned(workspace, 256))))
         return fail(EE_EINVAL, "%s: the workspace has %zu bytes of %zu, or is not 256-byte aligned", call, workspace_bytes, need);
     GemmDev g = {};

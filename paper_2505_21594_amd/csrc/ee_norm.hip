@@ -21,28 +21,80 @@ struct NormDev {
     float eps, inv_dim;
 };
 
-// A row's elements as floats: chunk c of lane l holds 8 (c * LANES + l) .. + 7; 0 behind the row's end.
-template <int E, int LANES>
-__device__ __forceinline__ void load_row(int type, const void *base, size_t at, int n, int l, float (&x)[E][8])
+// A row's elements as they lie in memory (eight of 16 bits in four words, of fp32 in eight): chunk c of lane l (of `lanes` that hold the row) holds elements
+// 8 (c * lanes + l) .. + 7; 0 behind the row's end.  Loading converts nothing, so that nothing waits for it before the values are used.
+template <int E, bool WIDE>
+struct RawRow {
+    u32x4_t w[E][WIDE ? 2 : 1];        // WIDE: fp32 too
+};
+template <int E, bool WIDE>
+__device__ __forceinline__ void load_raw(int type, const void *base, size_t at, int n, int l, int lanes, RawRow<E, WIDE> &x)
 {
-    const void *p = row_at(base, type, at);
+    const EE_GLOBAL char *const p = (const EE_GLOBAL char *)as_global(static_cast<const char *>(row_at(base, type, at)));
 #pragma unroll
     for (int c = 0; c < E; ++c) {
-        const int from = (c * LANES + l) * 8;
-        if (type == EE_FP32)
-            load_some<8>(static_cast<const float *>(p) + from, n - from, 0.f, x[c]);
-        else if (type == EE_BF16)
-            load_some<8>(static_cast<const __bf16 *>(p) + from, n - from, 0.f, x[c]);
-        else
-            load_some<8>(static_cast<const _Float16 *>(p) + from, n - from, 0.f, x[c]);
+        const int from = (c * lanes + l) * 8, left = n - from;
+#pragma unroll
+        for (int h = 0; h < (WIDE ? 2 : 1); ++h) x.w[c][h] = (u32x4_t){0, 0, 0, 0};
+        if (left >= 8) {
+            if (WIDE && type == EE_FP32) {
+#pragma unroll
+                for (int h = 0; h < (WIDE ? 2 : 1); ++h) x.w[c][h] = *(const EE_GLOBAL u32x4_at4_t *)(p + (size_t)from * 4 + h * 16);
+            } else {
+                x.w[c][0] = *(const EE_GLOBAL u32x4_at2_t *)(p + (size_t)from * 2);
+            }
+        } else if (left > 0) {
+            if (WIDE && type == EE_FP32) {
+                const EE_GLOBAL uint32_t *const q = (const EE_GLOBAL uint32_t *)p + from;
+                x.w[c][0][0] = q[0];
+                if (left > 1) x.w[c][0][1] = q[1];
+                if (left > 2) x.w[c][0][2] = q[2];
+                if (left > 3) x.w[c][0][3] = q[3];
+                if (left > 4) x.w[c][WIDE][0] = q[4];
+                if (left > 5) x.w[c][WIDE][1] = q[5];
+                if (left > 6) x.w[c][WIDE][2] = q[6];
+            } else {
+                const EE_GLOBAL uint16_t *const q = (const EE_GLOBAL uint16_t *)p + from;
+                uint32_t a = q[0], b = 0, d = 0, e = 0;
+                if (left > 1) a |= (uint32_t)q[1] << 16;
+                if (left > 2) b = q[2];
+                if (left > 3) b |= (uint32_t)q[3] << 16;
+                if (left > 4) d = q[4];
+                if (left > 5) d |= (uint32_t)q[5] << 16;
+                if (left > 6) e = q[6];
+                x.w[c][0] = (u32x4_t){a, b, d, e};
+            }
+        }
     }
 }
-template <int E, int LANES>
-__device__ __forceinline__ void store_row(int type, void *base, size_t at, int n, int l, const float (&x)[E][8])
+template <int E, bool WIDE>
+__device__ __forceinline__ void values_of(int type, const RawRow<E, WIDE> &r, float (&x)[E][8])
 {
 #pragma unroll
     for (int c = 0; c < E; ++c) {
-        const int from = (c * LANES + l) * 8;
+        if (WIDE && type == EE_FP32) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[c][i] = __uint_as_float(r.w[c][WIDE ? i / 4 : 0][i % 4]);
+        } else if (type == EE_BF16) {
+            RowPart<EE_BF16, 1, 64>::values(r.w[c][0], x[c]);
+        } else {
+            RowPart<EE_FP16, 1, 64>::values(r.w[c][0], x[c]);
+        }
+    }
+}
+template <int E>
+__device__ __forceinline__ void load_row(int type, const void *base, size_t at, int n, int l, int lanes, float (&x)[E][8])
+{
+    RawRow<E, true> r;
+    load_raw<E, true>(type, base, at, n, l, lanes, r);
+    values_of<E, true>(type, r, x);
+}
+template <int E>
+__device__ __forceinline__ void store_row(int type, void *base, size_t at, int n, int l, int lanes, const float (&x)[E][8])
+{
+#pragma unroll
+    for (int c = 0; c < E; ++c) {
+        const int from = (c * lanes + l) * 8;
         if (from + 8 <= n) {
             store_some<8>(type, base, at + from, x[c]);
         } else {
@@ -52,12 +104,12 @@ __device__ __forceinline__ void store_row(int type, void *base, size_t at, int n
         }
     }
 }
-template <int E, int LANES>
-__device__ __forceinline__ void load_gain(const float *gain, int n, int l, float none, float (&g)[E][8])
+template <int E>
+__device__ __forceinline__ void load_gain(const float *gain, int n, int l, int lanes, float none, float (&g)[E][8])
 {
 #pragma unroll
     for (int c = 0; c < E; ++c) {
-        const int from = (c * LANES + l) * 8;
+        const int from = (c * lanes + l) * 8;
         if (gain) {
             load_some<8>(gain + from, n - from, 0.f, g[c]);
         } else {
@@ -75,41 +127,45 @@ __device__ __forceinline__ float wave_sum_f(float x)
     x += __int_as_float(dpp<DPP_MIRROR>(0, __float_as_int(x)));
     return quads_sum(x);
 }
-// Sums over the LANES that hold a row, in every one of them.  `turn` alternates between two halves of the exchange, so that one barrier is enough.
-template <int LANES, int COUNT>
-__device__ __forceinline__ void row_sums(float (&v)[COUNT], float (*swap)[16][3], int &turn)
+// Sums over the lanes that hold a row, a wave's or the workgroup's, in every one of them.  `turn` alternates between two halves of the exchange, so that one
+// barrier is enough.
+template <bool ONE, int COUNT>
+__device__ __forceinline__ void row_sums(float (&v)[COUNT], float (*swap)[3][16], int &turn)
 {
 #pragma unroll
     for (int i = 0; i < COUNT; ++i) v[i] = wave_sum_f(v[i]);
-    if constexpr (LANES > 64) {
-        const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    if constexpr (!ONE) {
+        const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
         if (lane == 0)
 #pragma unroll
-            for (int i = 0; i < COUNT; ++i) swap[turn][wave][i] = v[i];
+            for (int i = 0; i < COUNT; ++i) swap[turn][i][wave] = v[i];
         __syncthreads();
 #pragma unroll
         for (int i = 0; i < COUNT; ++i) {
-            float s = 0.f;
-#pragma unroll
-            for (int w = 0; w < LANES / 64; ++w) s += swap[turn][w][i];
+            // (the waves' sums by 16 lanes of each wave, added up in one order by every one)
+            float s = (lane & 15) < waves ? swap[turn][i][lane & 15] : 0.f;
+            s += __int_as_float(dpp<DPP_XOR1>(0, __float_as_int(s)));
+            s += __int_as_float(dpp<DPP_XOR2>(0, __float_as_int(s)));
+            s += __int_as_float(dpp<DPP_HALF_MIRROR>(0, __float_as_int(s)));
+            s += __int_as_float(dpp<DPP_MIRROR>(0, __float_as_int(s)));
             v[i] = s;
         }
         turn ^= 1;
     }
 }
 
-template <int E, int LANES>
-__global__ void __launch_bounds__(LANES < 256 ? 256 : LANES) ee_norm_kernel(NormDev a)
+// ONE: a wave holds a row, a workgroup of 256 threads four of them; otherwise the workgroup, of as many waves as it takes.
+template <int E, bool ONE>
+__global__ void __launch_bounds__(ONE ? 256 : 1024) ee_norm_kernel(NormDev a)
 {
-    constexpr int ROWS = LANES < 256 ? 256 / LANES : 1;      // of a workgroup
-    __shared__ float swap[2][16][3];
-    const int l = threadIdx.x % LANES, row = blockIdx.x * ROWS + threadIdx.x / LANES;
-    if (LANES == 64 && row >= a.n_rows) return;
+    __shared__ float swap[2][3][16];
+    const int lanes = ONE ? 64 : blockDim.x, l = ONE ? threadIdx.x & 63 : threadIdx.x, row = ONE ? blockIdx.x * 4 + (threadIdx.x >> 6) : blockIdx.x;
+    if (ONE && row >= a.n_rows) return;
     int turn = 0;
     float x[E][8], g[E][8], b[E][8];
-    load_row<E, LANES>(a.x_type, a.x, (size_t)row * a.x_stride, a.dim, l, x);
-    load_gain<E, LANES>(a.gain, a.dim, l, 1.f, g);
-    load_gain<E, LANES>(a.bias, a.dim, l, 0.f, b);
+    load_row<E>(a.x_type, a.x, (size_t)row * a.x_stride, a.dim, l, lanes, x);
+    load_gain<E>(a.gain, a.dim, l, lanes, 1.f, g);
+    load_gain<E>(a.bias, a.dim, l, lanes, 0.f, b);
     float mu = 0.f;
     if (a.center) {
         float v[1] = {0.f};
@@ -117,7 +173,7 @@ __global__ void __launch_bounds__(LANES < 256 ? 256 : LANES) ee_norm_kernel(Norm
         for (int c = 0; c < E; ++c)
 #pragma unroll
             for (int i = 0; i < 8; ++i) v[0] += x[c][i];
-        row_sums<LANES>(v, swap, turn);
+        row_sums<ONE>(v, swap, turn);
         mu = v[0] * a.inv_dim;
     }
     float v[1] = {0.f};
@@ -125,36 +181,48 @@ __global__ void __launch_bounds__(LANES < 256 ? 256 : LANES) ee_norm_kernel(Norm
     for (int c = 0; c < E; ++c)
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            x[c][i] = (c * LANES + l) * 8 + i < a.dim ? x[c][i] - mu : 0.f;
+            x[c][i] = (c * lanes + l) * 8 + i < a.dim ? x[c][i] - mu : 0.f;
             v[0] += x[c][i] * x[c][i];
         }
-    row_sums<LANES>(v, swap, turn);
+    row_sums<ONE>(v, swap, turn);
     const float r = 1.f / sqrtf(v[0] * a.inv_dim + a.eps);
 #pragma unroll
     for (int c = 0; c < E; ++c)
 #pragma unroll
         for (int i = 0; i < 8; ++i) x[c][i] = x[c][i] * r * g[c][i] + b[c][i];
-    store_row<E, LANES>(a.y_type, a.y, (size_t)row * a.y_stride, a.dim, l, x);
+    store_row<E>(a.y_type, a.y, (size_t)row * a.y_stride, a.dim, l, lanes, x);
 }
 
-template <int E, int LANES>
-__global__ void __launch_bounds__(LANES < 256 ? 256 : LANES) ee_norm_grad_kernel(NormDev a)
+// The next row's loads are on their way while a row is worked on: a compute unit has two workgroups, whose sums of gains' and biases' gradients are written once for all
+// their rows (more workgroups write more of them).
+template <int E, bool ONE, bool WIDE>
+__global__ void __launch_bounds__(ONE ? 256 : 1024, !ONE && E == 1 && !WIDE ? 5 : 1) ee_norm_grad_kernel(NormDev a)
 {
-    constexpr int ROWS = LANES < 256 ? 256 / LANES : 1;
-    __shared__ float swap[2][16][3];
-    __shared__ float sums[ROWS > 1 ? (ROWS - 1) * E * LANES * 8 : 1];
-    const int l = threadIdx.x % LANES, sub = threadIdx.x / LANES;
+    constexpr int ROWS = ONE ? 4 : 1;
+    __shared__ float swap[2][3][16];
+    __shared__ float sums[ONE ? 3 * E * 64 * 8 : 1];
+    const int lanes = ONE ? 64 : blockDim.x, l = ONE ? threadIdx.x & 63 : threadIdx.x, sub = ONE ? threadIdx.x >> 6 : 0, step = gridDim.x * ROWS;
     int turn = 0;
     float dg[E][8], db[E][8], g[E][8];
+    RawRow<E, WIDE> next_x, next_u;
 #pragma unroll
     for (int c = 0; c < E; ++c)
 #pragma unroll
         for (int i = 0; i < 8; ++i) dg[c][i] = db[c][i] = 0.f;
-    load_gain<E, LANES>(a.gain, a.dim, l, 1.f, g);
-    for (int row = blockIdx.x * ROWS + sub; row < a.n_rows; row += gridDim.x * ROWS) {
+    int row = blockIdx.x * ROWS + sub;
+    if (row < a.n_rows) {
+        load_raw<E, WIDE>(a.x_type, a.x, (size_t)row * a.x_stride, a.dim, l, lanes, next_x);
+        load_raw<E, WIDE>(a.dy_type, a.dy, (size_t)row * a.dy_stride, a.dim, l, lanes, next_u);
+    }
+    load_gain<E>(a.gain, a.dim, l, lanes, 1.f, g);
+    for (; row < a.n_rows; row += step) {
         float x[E][8], u[E][8];
-        load_row<E, LANES>(a.x_type, a.x, (size_t)row * a.x_stride, a.dim, l, x);
-        load_row<E, LANES>(a.dy_type, a.dy, (size_t)row * a.dy_stride, a.dim, l, u);
+        values_of<E, WIDE>(a.x_type, next_x, x);
+        values_of<E, WIDE>(a.dy_type, next_u, u);
+        if (row + step < a.n_rows) {
+            load_raw<E, WIDE>(a.x_type, a.x, (size_t)(row + step) * a.x_stride, a.dim, l, lanes, next_x);
+            load_raw<E, WIDE>(a.dy_type, a.dy, (size_t)(row + step) * a.dy_stride, a.dim, l, lanes, next_u);
+        }
         float mu = 0.f;
         if (a.center) {
             float v[1] = {0.f};
@@ -162,7 +230,7 @@ __global__ void __launch_bounds__(LANES < 256 ? 256 : LANES) ee_norm_grad_kernel
             for (int c = 0; c < E; ++c)
 #pragma unroll
                 for (int i = 0; i < 8; ++i) v[0] += x[c][i];
-            row_sums<LANES>(v, swap, turn);
+            row_sums<ONE>(v, swap, turn);
             mu = v[0] * a.inv_dim;
         }
         float v[3] = {0.f, 0.f, 0.f};
@@ -170,13 +238,13 @@ __global__ void __launch_bounds__(LANES < 256 ? 256 : LANES) ee_norm_grad_kernel
         for (int c = 0; c < E; ++c)
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                x[c][i] = (c * LANES + l) * 8 + i < a.dim ? x[c][i] - mu : 0.f;
+                x[c][i] = (c * lanes + l) * 8 + i < a.dim ? x[c][i] - mu : 0.f;
                 const float t = u[c][i] * g[c][i];
                 v[0] += x[c][i] * x[c][i];
                 v[1] += t;
                 v[2] += t * x[c][i];
             }
-        row_sums<LANES>(v, swap, turn);
+        row_sums<ONE>(v, swap, turn);
         const float r = 1.f / sqrtf(v[0] * a.inv_dim + a.eps), mean = a.center ? v[1] * a.inv_dim : 0.f, along = v[2] * a.inv_dim * r;
 #pragma unroll
         for (int c = 0; c < E; ++c)
@@ -187,25 +255,25 @@ __global__ void __launch_bounds__(LANES < 256 ? 256 : LANES) ee_norm_grad_kernel
                 db[c][i] += dy;
                 x[c][i] = r * (dy * g[c][i] - mean - unit * along);
             }
-        if (a.y) store_row<E, LANES>(a.y_type, a.y, (size_t)row * a.y_stride, a.dim, l, x);
+        if (a.y) store_row<E>(a.y_type, a.y, (size_t)row * a.y_stride, a.dim, l, lanes, x);
     }
     auto combine = [&](float (&v)[E][8], float *out) {
-        if constexpr (ROWS > 1) {
+        if constexpr (ONE) {
             __syncthreads();
             if (sub > 0)
 #pragma unroll
                 for (int c = 0; c < E; ++c)
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) sums[(((sub - 1) * E + c) * 8 + i) * LANES + l] = v[c][i];
+                    for (int i = 0; i < 8; ++i) sums[(((sub - 1) * E + c) * 8 + i) * 64 + l] = v[c][i];
             __syncthreads();
             if (sub > 0) return;
 #pragma unroll
             for (int c = 0; c < E; ++c)
 #pragma unroll
                 for (int i = 0; i < 8; ++i)
-                    for (int w = 0; w < ROWS - 1; ++w) v[c][i] += sums[((w * E + c) * 8 + i) * LANES + l];
+                    for (int w = 0; w < 3; ++w) v[c][i] += sums[((w * E + c) * 8 + i) * 64 + l];
         }
-        store_row<E, LANES>(EE_FP32, out, (size_t)blockIdx.x * a.dim, a.dim, l, v);
+        store_row<E>(EE_FP32, out, (size_t)blockIdx.x * a.dim, a.dim, l, lanes, v);
     };
     if (a.part_gain) combine(dg, a.part_gain);
     if (a.part_bias) combine(db, a.part_bias);
@@ -245,31 +313,29 @@ void launch_column_sums(const float *part, int parts, int n, float *out, const f
 
 typedef void (*norm_kernel_t)(NormDev);
 struct NormShape {
-    int chunks, lanes;
+    int chunks, threads;
+    bool one;
+    int rows() const { return one ? 4 : 1; }
 };
 static NormShape norm_shape(int dim)
 {
-    const int chunks = (dim + 7) / 8;
-    const int lanes = chunks <= 128 ? 64 : chunks <= 1024 ? 256 : 1024;
-    return {(chunks + lanes - 1) / lanes, lanes};
+    const int pieces = (dim + 7) / 8;
+    if (pieces <= 128) return {(pieces + 63) / 64, 256, true};
+    const int chunks = pieces <= 1024 ? 1 : 2;
+    return {chunks, ((pieces + chunks - 1) / chunks + 63) / 64 * 64, false};
 }
-template <int E>
-static norm_kernel_t norm_kernel(int lanes, bool grad)
+static norm_kernel_t norm_kernel(const NormShape &s)
 {
-    if (lanes == 64) return grad ? ee_norm_grad_kernel<E, 64> : ee_norm_kernel<E, 64>;
-    if (lanes == 256) return grad ? ee_norm_grad_kernel<E, 256> : ee_norm_kernel<E, 256>;
-    if constexpr (E <= 2) return grad ? ee_norm_grad_kernel<E, 1024> : ee_norm_kernel<E, 1024>;
-    return nullptr;
+    if (s.one) return s.chunks == 1 ? ee_norm_kernel<1, true> : ee_norm_kernel<2, true>;
+    return s.chunks == 1 ? ee_norm_kernel<1, false> : ee_norm_kernel<2, false>;
 }
-static norm_kernel_t norm_kernel(const NormShape &s, bool grad)
+template <bool WIDE>
+static norm_kernel_t norm_grad_kernel(const NormShape &s)
 {
-    return s.chunks == 1 ? norm_kernel<1>(s.lanes, grad) : s.chunks == 2 ? norm_kernel<2>(s.lanes, grad) : s.chunks == 3 ? norm_kernel<3>(s.lanes, grad) : norm_kernel<4>(s.lanes, grad);
+    if (s.one) return s.chunks == 1 ? ee_norm_grad_kernel<1, true, WIDE> : ee_norm_grad_kernel<2, true, WIDE>;
+    return s.chunks == 1 ? ee_norm_grad_kernel<1, false, WIDE> : ee_norm_grad_kernel<2, false, WIDE>;
 }
-static int norm_groups(int n_rows, const NormShape &s)
-{
-    const int rows = s.lanes == 64 ? 4 : 1;
-    return std::min((n_rows + rows - 1) / rows, s.lanes == 1024 ? 256 : 512);
-}
+static int norm_groups(int n_rows, const NormShape &s) { return std::min((n_rows + s.rows() - 1) / s.rows(), 512); }
 
 static int check_rows(const char *call, int device, int n_rows, int dim, int center, float eps)
 {
@@ -322,8 +388,7 @@ extern "C" int ee_norm(const ee_norm_args *p, void *stream)
     DeviceScope scope(p->device);
     HIP_TRY(scope.status);
     const NormShape s = norm_shape(p->dim);
-    const int rows = s.lanes == 64 ? 4 : 1;
-    hipLaunchKernelGGL(norm_kernel(s, false), dim3((unsigned)((p->n_rows + rows - 1) / rows)), dim3(std::max(s.lanes, 256)), 0, static_cast<hipStream_t>(stream), a);
+    hipLaunchKernelGGL(norm_kernel(s), dim3((unsigned)((p->n_rows + s.rows() - 1) / s.rows())), dim3(s.threads), 0, static_cast<hipStream_t>(stream), a);
     HIP_TRY(hipGetLastError());
     return EE_OK;
 }
@@ -387,7 +452,7 @@ extern "C" int ee_norm_grad(const ee_norm_grad_args *p, void *workspace, size_t 
     DeviceScope scope(p->device);
     HIP_TRY(scope.status);
     const hipStream_t st = static_cast<hipStream_t>(stream);
-    if (groups) hipLaunchKernelGGL(norm_kernel(s, true), dim3((unsigned)groups), dim3(std::max(s.lanes, 256)), 0, st, a);
+    if (groups) hipLaunchKernelGGL(p->dtype == EE_FP32 || p->dy_dtype == EE_FP32 ? norm_grad_kernel<true>(s) : norm_grad_kernel<false>(s), dim3((unsigned)groups), dim3(s.threads), 0, st, a);
     HIP_TRY(hipGetLastError());
     launch_column_sums(a.part_gain, groups, p->dim, p->d_gain, a.part_bias, p->d_bias, st);
     HIP_TRY(hipGetLastError());

@@ -425,7 +425,7 @@ class Large:
 
 
 @pytest.mark.parametrize("kind", ["bf16", "fp16"])
-@pytest.mark.parametrize("rows,n_in,n_out", [(2600, 96, 2100), (2050, 133, 2433), (4100, 64, 1025), (40000, 40, 72), (72, 8200, 40)])
+@pytest.mark.parametrize("rows,n_in,n_out", [(2600, 96, 2100), (2050, 133, 2433), (4100, 64, 1025), (40000, 40, 72), (72, 8200, 40), (5, 72, 26000), (20, 40, 26003), (16, 2100, 13000)])
 def test_linear_that_fills_the_chip(rows, n_in, n_out, kind):
     """Every result, by the large tiles or in parts of the sum."""
     rng = np.random.default_rng(rows)
