@@ -170,20 +170,15 @@ __global__ void __launch_bounds__(NT, NT == 512 ? 6 : 4) ee_distill_kernel(Disti
 
     float r_rest;
     if constexpr (MODE != GRAD) {
+        // (the named ones become -infinity, which no sum notices)
         float m = -INFINITY;
 #pragma unroll
         for (int c = 0; c < E; ++c) {
+            if (const uint32_t b = marked(c)) z.drop(c, b);
             float x[N];
             z.chunk(c, x);
-            const uint32_t b = marked(c);
-            if (b) {
 #pragma unroll
-                for (int i = 0; i < N; ++i)
-                    if (!(b >> i & 1)) m = fmaxf(m, x[i]);
-            } else {
-#pragma unroll
-                for (int i = 0; i < N; ++i) m = fmaxf(m, x[i]);
-            }
+            for (int i = 0; i < N; ++i) m = larger(m, x[i]);
         }
         const float r = m * a.c, ref = m == -INFINITY ? 0.f : r;
         float s = 0.f;
@@ -192,15 +187,8 @@ __global__ void __launch_bounds__(NT, NT == 512 ? 6 : 4) ee_distill_kernel(Disti
         for (int c = 0; c < E; ++c) {
             float x[N];
             z.chunk(c, x);
-            const uint32_t b = marked(c);
-            if (b) {
 #pragma unroll
-                for (int i = 0; i < N; ++i)
-                    if (!(b >> i & 1)) s += __builtin_amdgcn_exp2f(fmaf(x[i], a.c, -ref));
-            } else {
-#pragma unroll
-                for (int i = 0; i < N; ++i) s += __builtin_amdgcn_exp2f(fmaf(x[i], a.c, -ref));
-            }
+            for (int i = 0; i < N; ++i) s += __builtin_amdgcn_exp2f(fmaf(x[i], a.c, -ref));
         }
         const float wave_r = wave_max_f(r);
         if (lane == 0) wr[wave] = wave_r;
@@ -244,6 +232,7 @@ __global__ void __launch_bounds__(NT, NT == 512 ? 6 : 4) ee_distill_kernel(Disti
     __syncthreads();
     const float others = others_s, ref = r_s == -INFINITY ? 0.f : r_s;
     const size_t out = (size_t)row * a.grad_stride + first;
+    const bool nothing = __builtin_amdgcn_readfirstlane(__float_as_int(weight) << 1) == 0;       // (a weight of 0, whatever the logits are)
     z.again();
 #pragma unroll
     for (int c = 0; c < E; ++c) {
@@ -252,7 +241,10 @@ __global__ void __launch_bounds__(NT, NT == 512 ? 6 : 4) ee_distill_kernel(Disti
         float x[N];
         z.chunk(c, x);
 #pragma unroll
-        for (int i = 0; i < N; ++i) x[i] = weight == 0.f ? 0.f : __builtin_amdgcn_exp2f(fmaf(x[i], a.c, -ref)) * others;
+        for (int i = 0; i < N; ++i) x[i] = __builtin_amdgcn_exp2f(fmaf(x[i], a.c, -ref)) * others;
+        if (nothing)
+#pragma unroll
+            for (int i = 0; i < N; ++i) x[i] = 0.f;
         const uint32_t b = marked(c);
         if (b == 0 && from + N <= len) {
             store_some<N>(a.grad_type, a.d_logits, out + from, x);

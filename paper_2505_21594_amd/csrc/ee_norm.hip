@@ -193,7 +193,7 @@ __global__ void __launch_bounds__(ONE ? 256 : 1024) ee_norm_kernel(NormDev a)
     store_row<E>(a.y_type, a.y, (size_t)row * a.y_stride, a.dim, l, lanes, x);
 }
 
-// The next row's loads are on their way while a row is worked on: a compute unit has two workgroups, whose sums of gains' and biases' gradients are written once for all
+// The next two rows' loads are on their way while a row is worked on: a compute unit has two workgroups, whose sums of gains' and biases' gradients are written once for all
 // their rows (more workgroups write more of them).
 template <int E, bool ONE, bool WIDE>
 __global__ void __launch_bounds__(ONE ? 256 : 1024, !ONE && E == 1 && !WIDE ? 5 : 1) ee_norm_grad_kernel(NormDev a)
@@ -204,25 +204,28 @@ __global__ void __launch_bounds__(ONE ? 256 : 1024, !ONE && E == 1 && !WIDE ? 5 
     const int lanes = ONE ? 64 : blockDim.x, l = ONE ? threadIdx.x & 63 : threadIdx.x, sub = ONE ? threadIdx.x >> 6 : 0, step = gridDim.x * ROWS;
     int turn = 0;
     float dg[E][8], db[E][8], g[E][8];
-    RawRow<E, WIDE> next_x, next_u;
+    RawRow<E, WIDE> next_x[2], next_u[2];
 #pragma unroll
     for (int c = 0; c < E; ++c)
 #pragma unroll
         for (int i = 0; i < 8; ++i) dg[c][i] = db[c][i] = 0.f;
+    auto request = [&](int row, RawRow<E, WIDE> &x, RawRow<E, WIDE> &u) __attribute__((always_inline)) {
+        if (row < a.n_rows) {
+            load_raw<E, WIDE>(a.x_type, a.x, (size_t)row * a.x_stride, a.dim, l, lanes, x);
+            load_raw<E, WIDE>(a.dy_type, a.dy, (size_t)row * a.dy_stride, a.dim, l, lanes, u);
+        }
+    };
     int row = blockIdx.x * ROWS + sub;
-    if (row < a.n_rows) {
-        load_raw<E, WIDE>(a.x_type, a.x, (size_t)row * a.x_stride, a.dim, l, lanes, next_x);
-        load_raw<E, WIDE>(a.dy_type, a.dy, (size_t)row * a.dy_stride, a.dim, l, lanes, next_u);
-    }
+    request(row, next_x[0], next_u[0]);
+    request(row + step, next_x[1], next_u[1]);
     load_gain<E>(a.gain, a.dim, l, lanes, 1.f, g);
     for (; row < a.n_rows; row += step) {
         float x[E][8], u[E][8];
-        values_of<E, WIDE>(a.x_type, next_x, x);
-        values_of<E, WIDE>(a.dy_type, next_u, u);
-        if (row + step < a.n_rows) {
-            load_raw<E, WIDE>(a.x_type, a.x, (size_t)(row + step) * a.x_stride, a.dim, l, lanes, next_x);
-            load_raw<E, WIDE>(a.dy_type, a.dy, (size_t)(row + step) * a.dy_stride, a.dim, l, lanes, next_u);
-        }
+        values_of<E, WIDE>(a.x_type, next_x[0], x);
+        values_of<E, WIDE>(a.dy_type, next_u[0], u);
+        next_x[0] = next_x[1];
+        next_u[0] = next_u[1];
+        request(row + 2 * step, next_x[1], next_u[1]);
         float mu = 0.f;
         if (a.center) {
             float v[1] = {0.f};

@@ -177,8 +177,8 @@ __global__ void __launch_bounds__(NT, NT == 512 ? 6 : 4) ee_score_kernel(ScoreDe
         z.chunk(c, x);
         cm[c] = x[0];
 #pragma unroll
-        for (int i = 1; i < N; ++i) cm[c] = fmaxf(cm[c], x[i]);
-        m = fmaxf(m, cm[c]);
+        for (int i = 1; i < N; ++i) cm[c] = larger(cm[c], x[i]);
+        m = larger(m, cm[c]);
     }
     float r = m * a.c;
     const float ref = m == -INFINITY ? 0.f : r;
@@ -203,7 +203,7 @@ __global__ void __launch_bounds__(NT, NT == 512 ? 6 : 4) ee_score_kernel(ScoreDe
         for (int g = 0; g < 4; ++g) {
             float x = -INFINITY;
 #pragma unroll
-            for (int c = g; c < E; c += 4) x = fmaxf(x, cm[c]);
+            for (int c = g; c < E; c += 4) x = larger(x, cm[c]);
             u[g] = key_of(x);
         }
         const unsigned t = wave_bound(u, k, 16);

@@ -130,6 +130,22 @@ struct RowPart {
         }
     }
     __device__ __forceinline__ void chunk(int c, float (&x)[N]) const { values(raw[c], x); }
+    // the elements of chunk c whose bits are set become -infinity
+    __device__ __forceinline__ void drop(int c, uint32_t bits)
+    {
+        constexpr uint32_t NOTHING = TYPE == EE_FP32 ? 0xFF800000u : TYPE == EE_BF16 ? 0xFF80u : 0xFC00u;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            uint32_t w = raw[c][i];
+            if constexpr (TYPE == EE_FP32) {
+                w = bits >> i & 1 ? NOTHING : w;
+            } else {
+                w = bits >> (2 * i) & 1 ? (w & 0xFFFF0000u) | NOTHING : w;
+                w = bits >> (2 * i + 1) & 1 ? (w & 0xFFFFu) | NOTHING << 16 : w;
+            }
+            raw[c][i] = w;
+        }
+    }
     // Between two walks over the part: the compiler takes the elements as others than before, and does not keep them all as floats in the meantime (twice the registers).
     __device__ __forceinline__ void again()
     {
@@ -143,6 +159,9 @@ struct RowPart {
             }
     }
 };
+
+// The larger one; NaN where one is (what fmaxf does for NaN costs an instruction more for every value that comes from memory).
+__device__ __forceinline__ float larger(float a, float b) { return __builtin_elementwise_maximum(a, b); }
 
 // One element of a row.
 __device__ __forceinline__ float logit_at(int type, const void *row, size_t i)
