@@ -182,7 +182,7 @@ __global__ void __launch_bounds__(NT, NT == 512 ? 6 : 4) ee_distill_kernel(Disti
         }
         const float r = m * a.c, ref = m == -INFINITY ? 0.f : r;
         float s = 0.f;
-        z.again();
+        z.again(m);
 #pragma unroll
         for (int c = 0; c < E; ++c) {
             float x[N];
@@ -233,7 +233,7 @@ __global__ void __launch_bounds__(NT, NT == 512 ? 6 : 4) ee_distill_kernel(Disti
     const float others = others_s, ref = r_s == -INFINITY ? 0.f : r_s;
     const size_t out = (size_t)row * a.grad_stride + first;
     const bool nothing = __builtin_amdgcn_readfirstlane(__float_as_int(weight) << 1) == 0;       // (a weight of 0, whatever the logits are)
-    z.again();
+    z.again(others);
 #pragma unroll
     for (int c = 0; c < E; ++c) {
         const int from = Part::offset(c, tid);

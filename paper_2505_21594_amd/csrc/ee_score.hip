@@ -183,7 +183,7 @@ __global__ void __launch_bounds__(NT, NT == 512 ? 6 : 4) ee_score_kernel(ScoreDe
     float r = m * a.c;
     const float ref = m == -INFINITY ? 0.f : r;
     float s = 0.f, d = 0.f;
-    z.again();
+    z.again(m);
 #pragma unroll
     for (int c = 0; c < E; ++c) {
         float x[N];
@@ -195,7 +195,7 @@ __global__ void __launch_bounds__(NT, NT == 512 ? 6 : 4) ee_score_kernel(ScoreDe
             d += fmaxf(y, -3e38f) * e;                       // (-infinity times 0 is nothing)
         }
     }
-    z.again();
+    z.again(s, d);
     const int k = min(a.top, len);
     if (k > 0) {                                             // a bound that k elements of this wave reach, if it has so many
         unsigned u[4];

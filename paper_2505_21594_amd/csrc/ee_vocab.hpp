@@ -90,8 +90,12 @@ struct RowPart {
         const int mine = n - tid * N;
 #pragma unroll
         for (int c = 0; c < E; ++c) {
-            raw[c] = (u32x4_t){NOTHING, NOTHING, NOTHING, NOTHING};
-            if (mine >= c * NT * N + N) raw[c] = *(const EE_GLOBAL some_t *)(base + c * NT * 16 + (unsigned)tid * 16u);
+            if (n >= (c + 1) * NT * N) {
+                raw[c] = *(const EE_GLOBAL some_t *)(base + c * NT * 16 + (unsigned)tid * 16u);
+            } else {
+                raw[c] = (u32x4_t){NOTHING, NOTHING, NOTHING, NOTHING};
+                if (mine >= c * NT * N + N) raw[c] = *(const EE_GLOBAL some_t *)(base + c * NT * 16 + (unsigned)tid * 16u);
+            }
         }
         // the chunk that the part's end is in
         const int last = n / N;
@@ -146,15 +150,16 @@ struct RowPart {
             raw[c][i] = w;
         }
     }
-    // Between two walks over the part: the compiler takes the elements as others than before, and does not keep them all as floats in the meantime (twice the registers).
-    __device__ __forceinline__ void again()
+    // Between two walks over the part, the first of which gave `done` and `too`: the compiler takes the elements as others than before, and does not keep them all as floats
+    // in the meantime (twice the registers).
+    __device__ __forceinline__ void again(float done, float too = 0.f)
     {
 #pragma unroll
         for (int c = 0; c < E; ++c)
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 uint32_t w = raw[c][i];
-                asm volatile("" : "+v"(w));
+                asm volatile("" : "+v"(w) : "v"(done), "v"(too));
                 raw[c][i] = w;
             }
     }
