@@ -138,7 +138,7 @@ __global__ void __launch_bounds__(NT, NT == 512 ? 6 : 4) ee_distill_kernel(Disti
 {
     typedef RowPart<TYPE, E, NT> Part;
     constexpr int N = Part::N, WAVES = NT / 64;
-    __shared__ uint32_t named[NT * E / 4];                   // a byte for each chunk, a bit for each of its elements
+    __shared__ uint32_t named[MODE == GRAD ? 1 : NT * E / 4];       // a byte for each chunk, a bit for each of its elements
     __shared__ float wr[WAVES];
     __shared__ double ws[WAVES];
     __shared__ float others_s, r_s;
@@ -154,27 +154,24 @@ __global__ void __launch_bounds__(NT, NT == 512 ? 6 : 4) ee_distill_kernel(Disti
         if (e.id >= 0) e.z = MODE == GRAD ? as_global(a.z)[(size_t)row * a.top + lane] : logit_at(TYPE, logits, e.id);
         if (MODE == STATS && part == 0 && lane < a.top) as_global_mut(a.z)[(size_t)row * a.top + lane] = e.z;
     }
-#pragma unroll
-    for (int i = 0; i < E / 4; ++i) named[i * NT + tid] = 0;
-    __syncthreads();
     const int at = e.id - first;
-    if (e.id >= 0 && at >= 0 && at < len) {
-        const int q = at / N, byte = (q % NT) * E + q / NT;
-        atomicOr(&named[byte / 4], 1u << (byte % 4 * 8 + at % N));
-    }
-    __syncthreads();
-    uint32_t marks[E / 4];
-#pragma unroll
-    for (int i = 0; i < E / 4; ++i) marks[i] = named[tid * (E / 4) + i];
-    auto marked = [&](int c) { return marks[c / 4] >> (c % 4 * 8) & 255u; };
-
-    float r_rest;
+    const bool here = e.id >= 0 && at >= 0 && at < len;
+    float r_rest = 0.f;
     if constexpr (MODE != GRAD) {
+#pragma unroll
+        for (int i = 0; i < E / 4; ++i) named[i * NT + tid] = 0;
+        __syncthreads();
+        if (here) {
+            const int q = at / N, byte = (q % NT) * E + q / NT;
+            atomicOr(&named[byte / 4], 1u << (byte % 4 * 8 + at % N));
+        }
+        __syncthreads();
         // (the named ones become -infinity, which no sum notices)
         float m = -INFINITY;
 #pragma unroll
         for (int c = 0; c < E; ++c) {
-            if (const uint32_t b = marked(c)) z.drop(c, b);
+            const uint32_t marks = named[tid * (E / 4) + c / 4] >> (c % 4 * 8) & 255u;
+            if (marks) z.drop(c, marks);
             float x[N];
             z.chunk(c, x);
 #pragma unroll
@@ -212,6 +209,9 @@ __global__ void __launch_bounds__(NT, NT == 512 ? 6 : 4) ee_distill_kernel(Disti
         }
     }
     const float weight = a.d_loss ? as_global(a.d_loss)[row] : 1.f;
+    const bool nothing = __builtin_amdgcn_readfirstlane(__float_as_int(weight) << 1) == 0;       // (a weight of 0, whatever the logits are)
+    float mine = 0.f;
+    bool store_mine = false;
     if (wave == 0) {
         double S;
         if constexpr (MODE == GRAD) {
@@ -226,34 +226,41 @@ __global__ void __launch_bounds__(NT, NT == 512 ? 6 : 4) ee_distill_kernel(Disti
             r_s = r_rest;
             if (a.loss && part == 0) as_global_mut(a.loss)[row] = (float)r.loss;
         }
-        if (a.d_logits && r.first && at >= 0 && at < len) store_one(a.grad_type, a.d_logits, (size_t)row * a.grad_stride + e.id, weight == 0.f ? 0.f : r.mine);
+        mine = nothing ? 0.f : r.mine;
+        store_mine = r.first && here;
     }
     if (!a.d_logits) return;
     __syncthreads();
     const float others = others_s, ref = r_s == -INFINITY ? 0.f : r_s;
     const size_t out = (size_t)row * a.grad_stride + first;
-    const bool nothing = __builtin_amdgcn_readfirstlane(__float_as_int(weight) << 1) == 0;       // (a weight of 0, whatever the logits are)
-    z.again(others);
-#pragma unroll
-    for (int c = 0; c < E; ++c) {
-        const int from = Part::offset(c, tid);
-        if (from >= len) continue;
-        float x[N];
-        z.chunk(c, x);
+    auto gradient = [&](const u32x4_t &raw, float (&x)[N]) __attribute__((always_inline)) {
+        Part::values(raw, x);
 #pragma unroll
         for (int i = 0; i < N; ++i) x[i] = __builtin_amdgcn_exp2f(fmaf(x[i], a.c, -ref)) * others;
         if (nothing)
 #pragma unroll
             for (int i = 0; i < N; ++i) x[i] = 0.f;
-        const uint32_t b = marked(c);
-        if (b == 0 && from + N <= len) {
-            store_some<N>(a.grad_type, a.d_logits, out + from, x);
-        } else {
+    };
+    z.again(others);
 #pragma unroll
-            for (int i = 0; i < N; ++i)
-                if (from + i < len && !(b >> i & 1)) store_one(a.grad_type, a.d_logits, out + from + i, x[i]);
-        }
+    for (int c = 0; c < E; ++c) {
+        const int from = Part::offset(c, tid);
+        if (from + N > len) continue;
+        float x[N];
+        gradient(z.raw[c], x);
+        store_some<N>(a.grad_type, a.d_logits, out + from, x);
     }
+    const int last = len / N;                                // the chunk that the part's end is in
+    if (len % N != 0 && tid == last % NT) {
+        float x[N];
+        gradient(z.end, x);
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            if (last * N + i < len) store_one(a.grad_type, a.d_logits, out + last * N + i, x[i]);
+    }
+    wait_vmem();                                             // the workgroup's stores are there: the named tokens' go on top of them
+    __syncthreads();
+    if (store_mine) store_one(a.grad_type, a.d_logits, out + at, mine);
 }
 
 // The loss of rows in parts, where no gradient is wanted: a wave for each row.

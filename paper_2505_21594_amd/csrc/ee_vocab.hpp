@@ -79,6 +79,7 @@ struct RowPart {
     static constexpr int N = TYPE == EE_FP32 ? 4 : 8;      // elements of a chunk
     static constexpr int ROOM = E * NT * N;                // of a part at most
     u32x4_t raw[E];
+    u32x4_t end;                                           // the chunk that the part's end is in, of the thread that has it
 
     static __device__ __forceinline__ int offset(int c, int tid) { return (c * NT + tid) * N; }
     // the part of `n` elements at `p` (the same in every lane), which is aligned to the element type
@@ -99,6 +100,7 @@ struct RowPart {
         }
         // the chunk that the part's end is in
         const int last = n / N;
+        end = (u32x4_t){NOTHING, NOTHING, NOTHING, NOTHING};
         if (n % N != 0 && tid == last % NT) {
             uint32_t w[4] = {NOTHING, NOTHING, NOTHING, NOTHING};
             const EE_GLOBAL char *const q = base + (size_t)last * 16;
@@ -110,9 +112,10 @@ struct RowPart {
                     else
                         w[i / 2] = i % 2 ? (w[i / 2] & 0xFFFFu) | (uint32_t) * (const EE_GLOBAL uint16_t *)(q + i * 2) << 16 : (w[i / 2] & 0xFFFF0000u) | *(const EE_GLOBAL uint16_t *)(q + i * 2);
                 }
+            end = (u32x4_t){w[0], w[1], w[2], w[3]};
 #pragma unroll
             for (int c = 0; c < E; ++c)
-                if (c == last / NT) raw[c] = (u32x4_t){w[0], w[1], w[2], w[3]};
+                if (c == last / NT) raw[c] = end;
         }
     }
     static __device__ __forceinline__ void values(const u32x4_t &r, float (&x)[N])
