@@ -17,39 +17,47 @@ __device__ __forceinline__ u32x4_t load_piece(const uint16_t *p, long long ld, i
     return v;
 }
 
-// A tile of TI x TJ results by four waves, each a quarter of it.  32 of the sum at a time go from memory straight to LDS (NS stages, NS - 1 of them on their
-// way), without a register, in the order in which the waves read them:
-//   sum's index contiguous in memory: kilobytes of 16 rows x 32, four lanes a row (neighbouring lanes that read neighbouring lines cost four times the
-//                               look-ups), a row's four pieces swapped by its number, so that eight lanes of a read meet every bank once;
-//   result's index contiguous: rows of the stage, pieces of 32 bytes swapped by the row's number, so that the transposing reads (ds_read_b64_tr_b16: four rows x 16
+// A tile of TI x TJ results by four waves, each a quarter of it.  32 KS of the sum at a time (a step) go from memory straight to LDS (NS steps, NS - 1 of them on their
+// way), without a register, in an order that suits the waves' reads:
+//   sum's index contiguous in memory: rows of 64 KS bytes, by four (KS = 2: eight) neighbouring lanes each (neighbouring lanes that read neighbouring lines cost four times the
+//                               look-ups); a row's pieces are swapped by its number, so that eight lanes of a read meet every bank once;
+//   result's index contiguous: rows of the step, pieces of 32 bytes swapped by the row's number, so that the transposing reads (ds_read_b64_tr_b16: four rows x 16
 //   columns for 16 lanes) of a wave meet no bank twice.
 // The weights' side is the first operand: a lane has four neighbouring results of a row.
-template <int TI, int TJ>
-constexpr int gemm_stages() { return TI * TJ >= 256 * 128 ? 3 : 6; }
-template <int TI, int TJ>
-constexpr size_t gemm_lds() { return (size_t)gemm_stages<TI, TJ>() * (TI + TJ) * 64; }
+template <int TI_, int TJ_, int KS_, int NS_>
+struct Tile {
+    static constexpr int TI = TI_, TJ = TJ_, KS = KS_, NS = NS_;
+    static constexpr size_t LDS = (size_t)NS * (TI + TJ) * KS * 64;
+};
+typedef Tile<256, 128, 1, 3> LargeTile;      // where the result's index is contiguous on both sides
+typedef Tile<192, 128, 2, 2> WideTile;       // ... and where it is not: whole lines of 128 bytes
+typedef Tile<128, 128, 2, 2> MediumTile;
+typedef Tile<64, 64, 2, 3> SmallTile;
 
-// Operand of T rows (of results): its units of a kilobyte in a stage.
-template <bool ALONG, int T>
+// Operand of T rows (of results): its units of a kilobyte in a step.
+template <bool ALONG, int T, int KS>
 struct Operand {
-    static constexpr int UNITS = T / 16, EACH = UNITS / 4;           // ... and of a wave
-    static constexpr int PIECES = T / 8;                             // pieces of a row of the stage, where the result's index is contiguous
+    static constexpr int UNITS = T * KS / 16, EACH = UNITS / 4;      // ... and of a wave
+    static constexpr int PIECES = T / 8;                             // pieces of a row of the step, where the result's index is contiguous
 
-    // which of the pieces (pairs of them) of row k of the stage are swapped
+    // which of the pieces (pairs of them) of row k of the step are swapped
     static __device__ __forceinline__ int swap(int k) { return T >= 128 ? (k & 3) | (k >> 3 & 1) << 2 : k & 3; }
-    // what lane l of unit u holds: results r .. of the tile, sum's index k .. of the stage
+    // what lane l of unit u holds: results r .. of the tile, sum's index k .. of the step
     static __device__ __forceinline__ void place(int u, int l, int &r, int &k)
     {
-        if (ALONG) {
+        if (ALONG && KS == 1) {
             r = u * 16 + (l >> 2);
             k = ((l & 3) ^ (l >> 3 & 3)) * 8;
+        } else if (ALONG) {
+            r = u * 8 + (l >> 3);
+            k = ((l & 7) ^ (l >> 3)) * 8;
         } else {
             k = u * (512 / T) + l / PIECES;
             const int c = l % PIECES;
             r = ((((c >> 1) ^ swap(k)) << 1) | (c & 1)) * 8;
         }
     }
-    // byte offset of a lane's piece from the stage's first element of the tile; results beyond the array's `n` are read from its first
+    // byte offset of a lane's piece from the step's first element of the tile; results beyond the array's `n` are read from its first
     static __device__ __forceinline__ int offset(int u, int l, int n, long long ld)
     {
         int r, k;
@@ -57,13 +65,14 @@ struct Operand {
         if (ALONG) return (int)(min(r, n - 1) * ld + k) * 2;
         return (int)(k * ld + (r < n ? r : 0)) * 2;
     }
-    // lane's part of the operand for results 16 f .. 16 f + 15 of the tile
-    static __device__ __forceinline__ u32x4_t read(const char *at, int f, int lane)
+    // lane's part of the operand for results 16 f .. 16 f + 15 of the tile and the h-th 32 of the step
+    static __device__ __forceinline__ u32x4_t read(const char *at, int f, int h, int lane)
     {
         const int s = lane & 15, quad = lane >> 4;
-        if (ALONG) return *reinterpret_cast<const u32x4_t *>(at + f * 1024 + s * 64 + (quad ^ (s >> 1 & 3)) * 16);
+        if (ALONG && KS == 1) return *reinterpret_cast<const u32x4_t *>(at + f * 1024 + s * 64 + (quad ^ (s >> 1 & 3)) * 16);
+        if (ALONG) return *reinterpret_cast<const u32x4_t *>(at + f * 2048 + s * 128 + ((h * 4 + quad) ^ (s & 7)) * 16);
         typedef __attribute__((ext_vector_type(4))) short s16x4_v;
-        const int k = quad * 8 + (s >> 2);
+        const int k = h * 32 + quad * 8 + (s >> 2);
         const char *p = at + k * (T * 2) + ((f ^ swap(k)) * 32 + (s & 3) * 8);
         EE_LDS s16x4_v *q = (EE_LDS s16x4_v *)(p);
         const s16x4_v a = __builtin_amdgcn_ds_read_tr16_b64_v4i16(q), b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((EE_LDS s16x4_v *)(p + 4 * T * 2));
@@ -72,13 +81,14 @@ struct Operand {
     }
 };
 
-template <int TYPE, bool A_ALONG, bool B_ALONG, int TI, int TJ>
+template <int TYPE, bool A_ALONG, bool B_ALONG, typename TILE>
 __global__ void __launch_bounds__(256, 2) ee_gemm16_kernel(GemmDev g)
 {
-    typedef Operand<A_ALONG, TI> OpA;
-    typedef Operand<B_ALONG, TJ> OpB;
-    constexpr int NS = gemm_stages<TI, TJ>(), PER = OpA::EACH + OpB::EACH, FI = TI / 32, FJ = TJ / 32;
-    constexpr unsigned STAGE = (TI + TJ) * 64;
+    constexpr int TI = TILE::TI, TJ = TILE::TJ, KS = TILE::KS, NS = TILE::NS, STEP = 32 * KS;
+    typedef Operand<A_ALONG, TI, KS> OpA;
+    typedef Operand<B_ALONG, TJ, KS> OpB;
+    constexpr int PER = OpA::EACH + OpB::EACH, FI = TI / 32, FJ = TJ / 32;
+    constexpr unsigned STAGE = (TI + TJ) * KS * 64, B_AT = TI * KS * 64;
     extern __shared__ __align__(16) char lds[];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wi = wave & 1, wj = wave >> 1;
@@ -100,7 +110,7 @@ __global__ void __launch_bounds__(256, 2) ee_gemm16_kernel(GemmDev g)
     // The last step is loaded with a look at every piece where it is not whole, or where a piece at the end of its rows is not.
     const bool ragged = !A_ALONG && (g.I & 7), ragged_b = !B_ALONG && (g.J & 7);
     // (Rows too far apart for 32-bit offsets: all steps are.)
-    const int full = g.far ? 0 : max((hi - lo) / 32 - (hi == g.K && (hi - lo) % 32 == 0 && (ragged || ragged_b)), 0);
+    const int full = g.far ? 0 : max((hi - lo) / STEP - (hi == g.K && (hi - lo) % STEP == 0 && (ragged || ragged_b)), 0);
     const unsigned lds0 = lds_offset(lds);
     int off_a[OpA::EACH], off_b[OpB::EACH];
 #pragma unroll
@@ -108,7 +118,7 @@ __global__ void __launch_bounds__(256, 2) ee_gemm16_kernel(GemmDev g)
 #pragma unroll
     for (int i = 0; i < OpB::EACH; ++i) off_b[i] = OpB::offset(wave * OpB::EACH + i, lane, g.J - j0, g.ldb);
     const char *const b0 = reinterpret_cast<const char *>(g.B + (B_ALONG ? (size_t)j0 * g.ldb + lo : (size_t)lo * g.ldb + j0));
-    const size_t step_a = A_ALONG ? 64 : (size_t)g.lda * 64, step_b = B_ALONG ? 64 : (size_t)g.ldb * 64;
+    const size_t step_a = A_ALONG ? STEP * 2 : (size_t)g.lda * (STEP * 2), step_b = B_ALONG ? STEP * 2 : (size_t)g.ldb * (STEP * 2);
 
     f32x4_t acc[FJ][FI];
 #pragma unroll
@@ -116,15 +126,18 @@ __global__ void __launch_bounds__(256, 2) ee_gemm16_kernel(GemmDev g)
 #pragma unroll
         for (int i = 0; i < FI; ++i) acc[j][i] = (f32x4_t){0.f, 0.f, 0.f, 0.f};
     auto compute = [&](const char *st) __attribute__((always_inline)) {
-        u32x4_t a[FI], b[FJ];
 #pragma unroll
-        for (int j = 0; j < FJ; ++j) b[j] = OpB::read(st + TI * 64, wj * FJ + j, lane);
+        for (int h = 0; h < KS; ++h) {
+            u32x4_t a[FI], b[FJ];
 #pragma unroll
-        for (int i = 0; i < FI; ++i) a[i] = OpA::read(st, wi * FI + i, lane);
+            for (int j = 0; j < FJ; ++j) b[j] = OpB::read(st + B_AT, wj * FJ + j, h, lane);
 #pragma unroll
-        for (int i = 0; i < FI; ++i)
+            for (int i = 0; i < FI; ++i) a[i] = OpA::read(st, wi * FI + i, h, lane);
 #pragma unroll
-            for (int j = 0; j < FJ; ++j) acc[j][i] = mfma16<TYPE>(b[j], a[i], acc[j][i]);
+            for (int i = 0; i < FI; ++i)
+#pragma unroll
+                for (int j = 0; j < FJ; ++j) acc[j][i] = mfma16<TYPE>(b[j], a[i], acc[j][i]);
+        }
     };
     for (int term = 0; term < g.terms; ++term) {
         const uint16_t *const A = g.A + term * g.plane;
@@ -135,7 +148,7 @@ __global__ void __launch_bounds__(256, 2) ee_gemm16_kernel(GemmDev g)
 #pragma unroll
             for (int i = 0; i < OpA::EACH; ++i) load_lds_kb(pa, off_a[i], dst + (wave * OpA::EACH + i) * 1024);
 #pragma unroll
-            for (int i = 0; i < OpB::EACH; ++i) load_lds_kb(pb, off_b[i], dst + TI * 64 + (wave * OpB::EACH + i) * 1024);
+            for (int i = 0; i < OpB::EACH; ++i) load_lds_kb(pb, off_b[i], dst + B_AT + (wave * OpB::EACH + i) * 1024);
         };
 #pragma unroll
         for (int s = 0; s < NS - 1; ++s)
@@ -152,7 +165,7 @@ __global__ void __launch_bounds__(256, 2) ee_gemm16_kernel(GemmDev g)
             compute(lds + buf * STAGE);
             buf = buf + 1 == NS ? 0 : buf + 1;
         }
-        for (int k0 = lo + full * 32; k0 < hi; k0 += 32) {
+        for (int k0 = lo + full * STEP; k0 < hi; k0 += STEP) {
             lds_barrier();
 #pragma unroll
             for (int i = 0; i < OpA::EACH; ++i) {
@@ -164,16 +177,16 @@ __global__ void __launch_bounds__(256, 2) ee_gemm16_kernel(GemmDev g)
             for (int i = 0; i < OpB::EACH; ++i) {
                 int r, k;
                 OpB::place(wave * OpB::EACH + i, lane, r, k);
-                *reinterpret_cast<u32x4_t *>(lds + TI * 64 + (wave * OpB::EACH + i) * 1024 + lane * 16) = B_ALONG ? load_piece(g.B, g.ldb, g.J, hi, j0 + r, k0 + k) : load_piece(g.B, g.ldb, hi, g.J, k0 + k, j0 + r);
+                *reinterpret_cast<u32x4_t *>(lds + B_AT + (wave * OpB::EACH + i) * 1024 + lane * 16) = B_ALONG ? load_piece(g.B, g.ldb, g.J, hi, j0 + r, k0 + k) : load_piece(g.B, g.ldb, hi, g.J, k0 + k, j0 + r);
             }
             lds_barrier();
             compute(lds);
         }
         if (term + 1 < g.terms) lds_barrier();
     }
-    // Results turn in LDS (64 rows of a wave at a time), so that stores are whole lines and the code behind the sums is there once, not for every register.
-    constexpr int HALF = FI < 4 ? FI : 4, COLS = FJ * 16, LD = COLS + 4, LANES = COLS / 4;
-    static_assert(4 * HALF * 16 * LD * 4 <= gemm_lds<TI, TJ>(), "a turn fits the stages' room");
+    // Results turn in LDS (some rows of a wave at a time), so that stores are whole lines and the code behind the sums is there once, not for every register.
+    constexpr int COLS = FJ * 16, LD = COLS + 4, LANES = COLS / 4, ROOM = (int)(TILE::LDS / (4 * 16 * LD * 4)), HALF = FI % 4 == 0 && ROOM >= 4 ? 4 : FI % 3 == 0 && ROOM >= 3 ? 3 : 2;
+    static_assert(FI % HALF == 0 && HALF <= ROOM, "a turn fits the steps' room");
     float *const turn = reinterpret_cast<float *>(lds) + wave * (HALF * 16 * LD);
     const int col = j0 + wj * COLS + lane % LANES * 4;
     const f32x4_t bias = bias_at(g, col);
@@ -185,20 +198,20 @@ __global__ void __launch_bounds__(256, 2) ee_gemm16_kernel(GemmDev g)
 #pragma unroll
             for (int j = 0; j < FJ; ++j) *reinterpret_cast<f32x4_t *>(turn + (i * 16 + (lane & 15)) * LD + j * 16 + (lane >> 4) * 4) = acc[j][h + i];
         wave_lds_order();
-        constexpr int STEP = 64 / LANES, AT_ONCE = 4;
+        constexpr int APART = 64 / LANES, AT_ONCE = HALF * 16 / APART < 4 ? HALF * 16 / APART : 4;
         if (col < g.J)
 #pragma unroll 1
-            for (int r = lane / LANES; r < HALF * 16; r += STEP * AT_ONCE) {
+            for (int r = lane / LANES; r < HALF * 16; r += APART * AT_ONCE) {
                 const int row = i0 + (wi * FI + h) * 16 + r;
                 f32x4_t v[AT_ONCE];
 #pragma unroll
-                for (int e = 0; e < AT_ONCE; ++e) v[e] = *reinterpret_cast<const f32x4_t *>(turn + (r + e * STEP) * LD + lane % LANES * 4);
+                for (int e = 0; e < AT_ONCE; ++e) v[e] = *reinterpret_cast<const f32x4_t *>(turn + (r + e * APART) * LD + lane % LANES * 4);
                 if (g.splits == 1) {
-                    finish<AT_ONCE>(g, row, STEP, col, bias, v);
+                    finish<AT_ONCE>(g, row, APART, col, bias, v);
                 } else {
 #pragma unroll
                     for (int e = 0; e < AT_ONCE; ++e)
-                        if (row + e * STEP < g.I) *as_global_mut(reinterpret_cast<f32x4_t *>(g.part + ((size_t)part * g.I + row + e * STEP) * g.part_ld + col)) = v[e];
+                        if (row + e * APART < g.I) *as_global_mut(reinterpret_cast<f32x4_t *>(g.part + ((size_t)part * g.I + row + e * APART) * g.part_ld + col)) = v[e];
                 }
             }
         wave_lds_order();
@@ -214,7 +227,7 @@ constexpr size_t thin_lds() { return (size_t)4 * THIN_STAGES * (TN + MT) * 1024;
 template <int TYPE, int TN, int MT>
 __global__ void __launch_bounds__(256, 2) ee_gemm16_thin_kernel(GemmDev g)
 {
-    typedef Operand<true, 16 * TN * 4> Op;      // (only its placing of rows: kilobytes of 16 rows x 32)
+    typedef Operand<true, 16 * TN * 4, 1> Op;      // (only its placing of rows: kilobytes of 16 rows x 32)
     constexpr int NS = THIN_STAGES, PER = TN + MT, STAGE = PER * 1024;
     static_assert(4 * TN * MT * 1024 <= thin_lds<TN, MT>(), "the sums fit the rings' room");
     extern __shared__ __align__(16) char lds[];
@@ -240,9 +253,9 @@ __global__ void __launch_bounds__(256, 2) ee_gemm16_thin_kernel(GemmDev g)
     auto compute = [&](const char *st) __attribute__((always_inline)) {
         u32x4_t w[TN], x[MT];
 #pragma unroll
-        for (int i = 0; i < TN; ++i) w[i] = Op::read(st, i, lane);
+        for (int i = 0; i < TN; ++i) w[i] = Op::read(st, i, 0, lane);
 #pragma unroll
-        for (int i = 0; i < MT; ++i) x[i] = Op::read(st, TN + i, lane);
+        for (int i = 0; i < MT; ++i) x[i] = Op::read(st, TN + i, 0, lane);
 #pragma unroll
         for (int n = 0; n < TN; ++n)
 #pragma unroll
@@ -369,10 +382,15 @@ __global__ void __launch_bounds__(SL_COLS *SL_SUBS) ee_slope_kernel(SlopeDev a)
 }
 
 typedef void (*gemm16_kernel_t)(GemmDev);
-template <int TYPE, int TI, int TJ>
-static gemm16_kernel_t gemm16_kernel(bool a_along, bool b_along)
+template <typename TILE>
+static gemm16_kernel_t gemm16_kernel(bool bf16, bool a_along, bool b_along)
 {
-    return a_along ? (b_along ? ee_gemm16_kernel<TYPE, true, true, TI, TJ> : ee_gemm16_kernel<TYPE, true, false, TI, TJ>) : ee_gemm16_kernel<TYPE, false, false, TI, TJ>;
+    if constexpr (TILE::TI == 256)
+        return bf16 ? ee_gemm16_kernel<EE_BF16, false, false, TILE> : ee_gemm16_kernel<EE_FP16, false, false, TILE>;
+    if constexpr (TILE::TI == 192)
+        return bf16 ? (b_along ? ee_gemm16_kernel<EE_BF16, true, true, TILE> : ee_gemm16_kernel<EE_BF16, true, false, TILE>) : (b_along ? ee_gemm16_kernel<EE_FP16, true, true, TILE> : ee_gemm16_kernel<EE_FP16, true, false, TILE>);
+    if (bf16) return a_along ? (b_along ? ee_gemm16_kernel<EE_BF16, true, true, TILE> : ee_gemm16_kernel<EE_BF16, true, false, TILE>) : ee_gemm16_kernel<EE_BF16, false, false, TILE>;
+    return a_along ? (b_along ? ee_gemm16_kernel<EE_FP16, true, true, TILE> : ee_gemm16_kernel<EE_FP16, true, false, TILE>) : ee_gemm16_kernel<EE_FP16, false, false, TILE>;
 }
 
 template <int TYPE, int MT>
@@ -384,29 +402,54 @@ static gemm16_kernel_t thin_kernel(int tn)
     return tn == 1 ? ee_gemm16_thin_kernel<TYPE, 1, MT> : ee_gemm16_thin_kernel<TYPE, 2, MT>;
 }
 
-// How a product is split: tiles of 256 x 128 or 64 x 64 or few rows at a time, and parts of the sum.
-enum GemmForm { LARGE, SMALL, THIN };
+enum GemmForm { LARGE, MEDIUM, SMALL, THIN };
+// How a product is split: in tiles (or few rows at a time), and parts of the sum, by an estimate of its time in us: the tiles of the busiest compute unit at 4.7e-7 us for each
+// element of a tile and of the sum (times what a tile's shape costs, and what workgroups with few beside them on their compute unit do), a start and an end, and the
+// parts' way through memory.  Measured, us, the chosen way first, then the best of the others (L, M, S: the tile, parts behind it): 2041 x 4096 x 11008 forward L1 181,
+// M1 186; dx M1 176, L2 205; dW L1 184, M1 205; 4096 columns M1 69, L1 82; 384 columns S1 19.6, S2 18.4, M6 20.8; 128 rows of 4096 x 4096 S4 13.7, S2 15.2; 300 x 1000 x
+// 1000 S1 8.0, M4 11.5; dW of 512 x 512 from 8000 rows S4 16.3, S6 15.8, M12 20.1.
+static double gemm_time(int form, bool a_along, double tiles, int area, int K, int splits, double results)
+{
+    const double shape = form == LARGE ? (a_along ? 1.04 : 1.15) : form == MEDIUM ? 1.0 : 0.68;
+    const double each = tiles * splits / 256, busiest = each <= 1 ? 1 : (ceil(each) + each) / 2;
+    const double alone = 0.45 + 0.55 * std::min(1.0, each / (form == SMALL ? 3 : 2));
+    return busiest * area * (double)K / splits * 4.7e-7 / (shape * alone) + 4 + (splits > 1 ? 5 + splits * results * 8 / 4e6 : 0);
+}
 struct GemmPlan16 {
     int form, tn;                     // tn: of few rows, tiles of 16 columns for a workgroup
     int ni, nj, splits, per;
     long long part_ld;
     size_t bytes;
 };
-static GemmPlan16 plan_gemm16(int I, int J, int K, bool along)
+static GemmPlan16 plan_gemm16(int I, int J, int K, bool a_along, bool b_along)
 {
     GemmPlan16 pl = {};
-    const auto tiles = [&](int ti, int tj) { return std::max(1ll, (long long)((I + ti - 1) / ti) * ((J + tj - 1) / tj)); };
-    pl.form = along && I <= 32 ? THIN : tiles(256, 128) >= 128 ? LARGE : SMALL;
+    const auto count = [](int n, int t) { return std::max((n + t - 1) / t, 1); };
     pl.tn = 1;
-    if (pl.form == THIN)
+    if (a_along && b_along && I <= 32) {
+        pl.form = THIN;
         while (pl.tn < (I > 16 ? 2 : 4) && J >= 16 * 2 * pl.tn * 400) pl.tn *= 2;
-    const int ti = pl.form == LARGE ? 256 : pl.form == SMALL ? 64 : 32, tj = pl.form == LARGE ? 128 : pl.form == SMALL ? 64 : 16 * pl.tn;
-    const long long n = tiles(ti, tj);
-    pl.ni = (I + ti - 1) / ti;
-    pl.nj = (J + tj - 1) / tj;
-    const int most = std::max(1, K / 512);
-    pl.splits = (int)std::min<long long>(most, std::max<long long>(1, (pl.form == LARGE ? 256 : pl.form == SMALL ? 768 : 512) / n));
-    pl.per = std::max(((K + pl.splits - 1) / pl.splits + 31) / 32 * 32, 32);
+        pl.ni = 1;
+        pl.nj = count(J, 16 * pl.tn);
+        pl.splits = std::min(std::max(1, K / 512), std::max(1, 512 / pl.nj));
+    } else {
+        double best = 0;
+        for (int form = LARGE; form <= SMALL; ++form) {
+            const int ti = form == LARGE ? (a_along ? 192 : 256) : form == MEDIUM ? 128 : 64, tj = form == SMALL ? 64 : 128;
+            const long long n = (long long)count(I, ti) * count(J, tj);
+            for (int splits = 1; splits <= 16 && (splits == 1 || (K / splits >= 256 && n * splits <= 1024)); ++splits) {
+                const double t = gemm_time(form, a_along, (double)n, ti * tj, K, splits, (double)I * J);
+                if (best == 0 || t < best) {
+                    best = t;
+                    pl.form = form;
+                    pl.ni = count(I, ti);
+                    pl.nj = count(J, tj);
+                    pl.splits = splits;
+                }
+            }
+        }
+    }
+    pl.per = std::max(((K + pl.splits - 1) / pl.splits + 63) / 64 * 64, 64);
     pl.splits = std::max(1, (K + pl.per - 1) / pl.per);
     pl.part_ld = ((long long)J + 3) / 4 * 4;
     pl.bytes = pl.splits > 1 ? align256((size_t)pl.splits * I * pl.part_ld * sizeof(float)) : 0;
@@ -415,7 +458,7 @@ static GemmPlan16 plan_gemm16(int I, int J, int K, bool along)
 constexpr long long GEMM_FAR = 1 << 21;            // elements from row to row that 32-bit offsets within a tile allow
 static int launch_gemm16(GemmDev g, bool a_along, bool b_along, void *space, hipStream_t s)
 {
-    const GemmPlan16 pl = plan_gemm16(g.I, g.J, g.K, a_along && b_along);
+    const GemmPlan16 pl = plan_gemm16(g.I, g.J, g.K, a_along, b_along);
     g.ni = pl.ni;
     g.nj = pl.nj;
     g.splits = pl.splits;
@@ -428,13 +471,14 @@ static int launch_gemm16(GemmDev g, bool a_along, bool b_along, void *space, hip
         const bool two = g.I > 16;
         const gemm16_kernel_t k = bf16 ? (two ? thin_kernel<EE_BF16, 2>(pl.tn) : thin_kernel<EE_BF16, 1>(pl.tn)) : (two ? thin_kernel<EE_FP16, 2>(pl.tn) : thin_kernel<EE_FP16, 1>(pl.tn));
         hipLaunchKernelGGL(k, dim3((unsigned)pl.nj, (unsigned)pl.splits), dim3(256), (size_t)4 * THIN_STAGES * (pl.tn + (two ? 2 : 1)) * 1024, s, g);
-    } else if (pl.form == SMALL) {
-        const gemm16_kernel_t k = bf16 ? gemm16_kernel<EE_BF16, 64, 64>(a_along, b_along) : gemm16_kernel<EE_FP16, 64, 64>(a_along, b_along);
-        hipLaunchKernelGGL(k, dim3((unsigned)(pl.ni * pl.nj * pl.splits)), dim3(256), (gemm_lds<64, 64>()), s, g);
+    } else if (pl.form != LARGE) {
+        const bool small = pl.form == SMALL;
+        static_assert(SmallTile::LDS <= 64 << 10 && MediumTile::LDS <= 64 << 10, "what a launch gets unasked");
+        hipLaunchKernelGGL(small ? gemm16_kernel<SmallTile>(bf16, a_along, b_along) : gemm16_kernel<MediumTile>(bf16, a_along, b_along), dim3((unsigned)(pl.ni * pl.nj * pl.splits)), dim3(256),
+                           small ? SmallTile::LDS : MediumTile::LDS, s, g);
     } else {
-        const gemm16_kernel_t k = bf16 ? gemm16_kernel<EE_BF16, 256, 128>(a_along, b_along) : gemm16_kernel<EE_FP16, 256, 128>(a_along, b_along);
-        constexpr size_t lds = gemm_lds<256, 128>();
-        static_assert(lds > 64 << 10, "more than a launch gets unasked: said once for a kernel on a device");
+        const gemm16_kernel_t k = a_along ? gemm16_kernel<WideTile>(bf16, true, b_along) : gemm16_kernel<LargeTile>(bf16, false, false);
+        const size_t lds = a_along ? WideTile::LDS : LargeTile::LDS;      // (more than a launch gets unasked: said once for a kernel on a device)
         static std::atomic<uint64_t> said[2][2][2];
         std::atomic<uint64_t> &mine = said[bf16][a_along][b_along];
         int device = 0;
@@ -504,7 +548,7 @@ static GradPlan plan_grad(const ee_linear_grad_args &p)
     pl.parts = (p.n_rows + pl.per - 1) / pl.per;
     pl.dz_bytes = align256((size_t)pl.terms * p.n_rows * pl.ldz * 2);
     pl.part_bytes = align256((size_t)pl.parts * p.n_out * sizeof(float));
-    pl.gemm_bytes = std::max(plan_gemm16(p.n_rows, p.n_in, p.n_out, false).bytes, plan_gemm16(p.n_out, p.n_in, p.n_rows, false).bytes);
+    pl.gemm_bytes = std::max(plan_gemm16(p.n_rows, p.n_in, p.n_out, true, false).bytes, plan_gemm16(p.n_out, p.n_in, p.n_rows, false, false).bytes);
     return pl;
 }
 static int check_linear_grad(const char *call, const ee_linear_grad_args *p)
@@ -525,7 +569,7 @@ extern "C" int ee_linear_workspace(const ee_linear_args *p, size_t *bytes)
     if (!bytes) return fail(EE_EINVAL, "%s: null argument", call);
     *bytes = 0;
     int rc = check_linear(call, p);
-    if (rc == EE_OK) *bytes = plan_gemm16(p->n_rows, p->n_out, p->n_in, true).bytes;
+    if (rc == EE_OK) *bytes = plan_gemm16(p->n_rows, p->n_out, p->n_in, true, true).bytes;
     return rc;
 }
 
@@ -545,7 +589,7 @@ extern "C" int ee_linear(const ee_linear_args *p, void *workspace, size_t worksp
     if (p->residual == p->y && (p->residual_dtype != p->out_dtype || (p->n_rows > 1 && p->residual_stride != p->y_stride)))
         return fail(EE_EINVAL, "%s: y may be residual only with the same type and stride", call);
     if (!aligned(p->bias, 4)) return fail(EE_EINVAL, "%s: fp32 arrays must be 4-byte aligned", call);
-    const size_t need = plan_gemm16(p->n_rows, p->n_out, p->n_in, true).bytes;
+    const size_t need = plan_gemm16(p->n_rows, p->n_out, p->n_in, true, true).bytes;
     if (need > workspace_bytes || (need && (!workspace || !aligned(workspace, 256))))
         return fail(EE_EINVAL, "%s: the workspace has %zu bytes of %zu, or is not 256-byte aligned", call, workspace_bytes, need);
     GemmDev g = {};
