@@ -514,7 +514,7 @@ int ee_accept_drafts(const ee_accept_args *args, void *workspace, size_t workspa
    Tokens whose logit is -infinity (masked ones) have no part in a row; where fewer than `top` are left the list ends with -1 and -infinity.  A row
    without a softmax (NaN, +infinity or nothing but -infinity among its logits) gets NaN, and -1 for its tokens.
    logits [n_rows][vocab] of type `dtype` at any alignment of the type, sums in fp32 for each thread and 64 bits from there; results fp32, int32.  n_rows up to 2^20, vocab
-   up to 2^24 (EE_EINVAL where rows times parts of rows pass 2^23).
+   up to 2^24 (EE_EINVAL where rows times parts of rows pass 2^22).
    workspace: ee_score_workspace bytes (may be 0), 256-byte aligned; contents do not matter. */
 typedef struct {
     int32_t device, dtype, n_rows, vocab, top;

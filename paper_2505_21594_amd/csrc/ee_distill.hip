@@ -285,13 +285,16 @@ static DistillPlan plan_distill(const ee_distill_args &p, bool grad)
 {
     DistillPlan pl;
     const int n = p.dtype == EE_FP32 ? 4 : 8, room[3] = {256 * 4 * n, 512 * 8 * n, 1024 * 16 * n};
-    pl.shape = p.vocab <= room[0] ? 0 : p.vocab <= room[1] ? 1 : 2;
-    if (p.n_rows >= 256 && p.vocab <= room[grad ? 2 : 1]) {
+    // A row that a workgroup can hold is one part, in the smallest workgroup that can where rows fill the chip; the loss alone of longer rows is better off in parts (600 rows
+    // of 100003: 149 us by workgroups of 1024 threads, 43 in four parts).
+    const bool many = p.n_rows >= 256;
+    if (p.vocab <= room[grad || !many ? 2 : 1]) {
+        pl.shape = p.vocab <= room[0] ? 0 : p.vocab <= room[1] && many ? 1 : 2;
         pl.split.parts = 1;
         pl.split.length = p.vocab;
     } else {
-        pl.shape = p.n_rows >= 256 ? 1 : 0;
-        pl.split = split_rows(p.n_rows, p.vocab, room[pl.shape], 256 * n, pl.shape ? 1 : 512);
+        pl.shape = many ? 1 : 0;
+        pl.split = split_rows(p.n_rows, p.vocab, room[pl.shape], 256 * n, many ? 1 : 512);
     }
     pl.part_bytes = pl.split.parts > 1 ? align256((size_t)p.n_rows * pl.split.parts * sizeof(DistillPart)) : 0;
     pl.bytes = pl.part_bytes + (pl.split.parts > 1 ? align256((size_t)p.n_rows * p.top * sizeof(float)) : 0);

@@ -388,16 +388,18 @@ __global__ void __launch_bounds__(SC_THREADS) ee_score_join_kernel(ScoreDev a)
 
 typedef void (*score_kernel_t)(ScoreDev);
 struct ScorePlan {
-    bool wide;                         // 512 threads of eight chunks for a part; 256 of four
+    int shape;                         // threads and chunks a thread: 256 x 4, 512 x 8, 1024 x 8
     RowSplit split;
     size_t part_bytes, bytes;
 };
+// A row that a workgroup can hold is one part: a second launch costs more than what more workgroups save (five rows of 32000 in 32 parts each 13.7 us).
 static ScorePlan plan_score(const ee_score_args &p)
 {
     ScorePlan pl;
-    const int n = p.dtype == EE_FP32 ? 4 : 8, wide = 8 * 512 * n;
-    pl.wide = (long long)p.n_rows * ((p.vocab + wide - 1) / wide) >= 512;
-    pl.split = split_rows(p.n_rows, p.vocab, pl.wide ? wide : 4 * 256 * n, 256 * n, pl.wide ? 1 : 512);
+    const int n = p.dtype == EE_FP32 ? 4 : 8, room[3] = {256 * 4 * n, 512 * 8 * n, 1024 * 8 * n};
+    const bool many = (long long)p.n_rows * ((p.vocab + room[1] - 1) / room[1]) >= 512;
+    pl.shape = p.vocab <= room[0] ? 0 : p.vocab <= room[1] && p.n_rows >= 256 ? 1 : p.vocab <= room[2] && !many ? 2 : many ? 1 : 0;
+    pl.split = split_rows(p.n_rows, p.vocab, room[pl.shape], 256 * n, p.vocab <= room[pl.shape] || many ? 1 : 512);
     pl.part_bytes = pl.split.parts > 1 ? align256((size_t)p.n_rows * pl.split.parts * sizeof(ScorePart)) : 0;
     pl.bytes = pl.part_bytes + (pl.split.parts > 1 ? align256((size_t)p.n_rows * pl.split.parts * p.top * sizeof(Cand)) : 0);
     return pl;
@@ -445,7 +447,7 @@ extern "C" int ee_score_tokens(const ee_score_args *p, void *workspace, size_t w
     const ScorePlan pl = plan_score(*p);
     if (pl.bytes > workspace_bytes || (pl.bytes && (!workspace || !aligned(workspace, 256))))
         return fail(EE_EINVAL, "%s: the workspace has %zu bytes of %zu, or is not 256-byte aligned", call, workspace_bytes, pl.bytes);
-    if ((long long)p->n_rows * pl.split.parts >= 1 << 23) return fail(EE_EINVAL, "%s: too many rows of so many tokens", call);
+    if ((long long)p->n_rows * pl.split.parts >= 1 << 22) return fail(EE_EINVAL, "%s: too many rows of so many tokens", call);
     ScoreDev a;
     a.logits = p->logits;
     a.tokens = p->tokens;
@@ -465,11 +467,11 @@ extern "C" int ee_score_tokens(const ee_score_args *p, void *workspace, size_t w
     a.c = (float)(1.4426950408889634 / (double)p->temperature);
     DeviceScope scope(p->device);
     HIP_TRY(scope.status);
-    static const score_kernel_t kernels[3][2] = {{ee_score_kernel<EE_BF16, 4, 256>, ee_score_kernel<EE_BF16, 8, 512>},
-                                                 {ee_score_kernel<EE_FP16, 4, 256>, ee_score_kernel<EE_FP16, 8, 512>},
-                                                 {ee_score_kernel<EE_FP32, 4, 256>, ee_score_kernel<EE_FP32, 8, 512>}};
+    static const score_kernel_t kernels[3][3] = {{ee_score_kernel<EE_BF16, 4, 256>, ee_score_kernel<EE_BF16, 8, 512>, ee_score_kernel<EE_BF16, 8, 1024>},
+                                                 {ee_score_kernel<EE_FP16, 4, 256>, ee_score_kernel<EE_FP16, 8, 512>, ee_score_kernel<EE_FP16, 8, 1024>},
+                                                 {ee_score_kernel<EE_FP32, 4, 256>, ee_score_kernel<EE_FP32, 8, 512>, ee_score_kernel<EE_FP32, 8, 1024>}};
     const hipStream_t s = static_cast<hipStream_t>(stream);
-    hipLaunchKernelGGL(kernels[p->dtype][pl.wide], dim3((unsigned)(p->n_rows * pl.split.parts)), dim3(pl.wide ? 512 : 256), 0, s, a);
+    hipLaunchKernelGGL(kernels[p->dtype][pl.shape], dim3((unsigned)(p->n_rows * pl.split.parts)), dim3(256 << pl.shape), 0, s, a);
     HIP_TRY(hipGetLastError());
     if (a.parts > 1) {
         hipLaunchKernelGGL(ee_score_join_kernel, dim3((unsigned)p->n_rows), dim3(SC_THREADS), 0, s, a);
