@@ -156,7 +156,7 @@ __device__ __forceinline__ void row_sums(float (&v)[COUNT], float (*swap)[3][16]
 
 // ONE: a wave holds a row, a workgroup of 256 threads four of them; otherwise the workgroup, of as many waves as it takes.
 template <int E, bool ONE>
-__global__ void __launch_bounds__(ONE ? 256 : 1024) ee_norm_kernel(NormDev a)
+__global__ void __launch_bounds__(ONE ? 256 : 512) ee_norm_kernel(NormDev a)
 {
     __shared__ float swap[2][3][16];
     const int lanes = ONE ? 64 : blockDim.x, l = ONE ? threadIdx.x & 63 : threadIdx.x, row = ONE ? blockIdx.x * 4 + (threadIdx.x >> 6) : blockIdx.x;
@@ -195,8 +195,8 @@ __global__ void __launch_bounds__(ONE ? 256 : 1024) ee_norm_kernel(NormDev a)
 
 // The next two rows' loads are on their way while a row is worked on: a compute unit has two workgroups, whose sums of gains' and biases' gradients are written once for all
 // their rows (more workgroups write more of them).
-template <int E, bool ONE, bool WIDE>
-__global__ void __launch_bounds__(ONE ? 256 : 1024, !ONE && E == 1 && !WIDE ? 5 : 1) ee_norm_grad_kernel(NormDev a)
+template <int E, bool ONE, bool WIDE, int DEPTH>
+__global__ void __launch_bounds__(ONE ? 256 : 1024, !ONE && E == 1 && !WIDE ? (DEPTH == 1 ? 6 : 5) : 1) ee_norm_grad_kernel(NormDev a)
 {
     constexpr int ROWS = ONE ? 4 : 1;
     __shared__ float swap[2][3][16];
@@ -204,7 +204,7 @@ __global__ void __launch_bounds__(ONE ? 256 : 1024, !ONE && E == 1 && !WIDE ? 5 
     const int lanes = ONE ? 64 : blockDim.x, l = ONE ? threadIdx.x & 63 : threadIdx.x, sub = ONE ? threadIdx.x >> 6 : 0, step = gridDim.x * ROWS;
     int turn = 0;
     float dg[E][8], db[E][8], g[E][8];
-    RawRow<E, WIDE> next_x[2], next_u[2];
+    RawRow<E, WIDE> next_x[DEPTH], next_u[DEPTH];
 #pragma unroll
     for (int c = 0; c < E; ++c)
 #pragma unroll
@@ -216,16 +216,18 @@ __global__ void __launch_bounds__(ONE ? 256 : 1024, !ONE && E == 1 && !WIDE ? 5 
         }
     };
     int row = blockIdx.x * ROWS + sub;
-    request(row, next_x[0], next_u[0]);
-    request(row + step, next_x[1], next_u[1]);
+#pragma unroll
+    for (int d = 0; d < DEPTH; ++d) request(row + d * step, next_x[d], next_u[d]);
     load_gain<E>(a.gain, a.dim, l, lanes, 1.f, g);
     for (; row < a.n_rows; row += step) {
         float x[E][8], u[E][8];
         values_of<E, WIDE>(a.x_type, next_x[0], x);
         values_of<E, WIDE>(a.dy_type, next_u[0], u);
-        next_x[0] = next_x[1];
-        next_u[0] = next_u[1];
-        request(row + 2 * step, next_x[1], next_u[1]);
+        if constexpr (DEPTH == 2) {
+            next_x[0] = next_x[1];
+            next_u[0] = next_u[1];
+        }
+        request(row + DEPTH * step, next_x[DEPTH - 1], next_u[DEPTH - 1]);
         float mu = 0.f;
         if (a.center) {
             float v[1] = {0.f};
@@ -320,25 +322,39 @@ struct NormShape {
     bool one;
     int rows() const { return one ? 4 : 1; }
 };
+// Forward, four waves for a row as long as four chunks a lane are enough: more of it on its way for every wave (rows of 5120: ten waves of one chunk 45 us, FWD5120).
 static NormShape norm_shape(int dim)
 {
     const int pieces = (dim + 7) / 8;
     if (pieces <= 128) return {(pieces + 63) / 64, 256, true};
+    const int threads = pieces <= 1024 ? 256 : 512;
+    return {(pieces + threads - 1) / threads, threads, false};
+}
+// Backward, a chunk a lane, whose registers hold its part of the gains' and biases' gradients too; waves in fours, so that a compute unit's SIMDs have room for a second workgroup.
+static NormShape norm_grad_shape(int dim)
+{
+    const int pieces = (dim + 7) / 8;
+    if (pieces <= 128) return {(pieces + 63) / 64, 256, true};
     const int chunks = pieces <= 1024 ? 1 : 2;
-    return {chunks, ((pieces + chunks - 1) / chunks + 63) / 64 * 64, false};
+    return {chunks, ((pieces + chunks - 1) / chunks + 255) / 256 * 256, false};
 }
 static norm_kernel_t norm_kernel(const NormShape &s)
 {
     if (s.one) return s.chunks == 1 ? ee_norm_kernel<1, true> : ee_norm_kernel<2, true>;
-    return s.chunks == 1 ? ee_norm_kernel<1, false> : ee_norm_kernel<2, false>;
+    return s.chunks == 1 ? ee_norm_kernel<1, false> : s.chunks == 2 ? ee_norm_kernel<2, false> : s.chunks == 3 ? ee_norm_kernel<3, false> : ee_norm_kernel<4, false>;
 }
 template <bool WIDE>
 static norm_kernel_t norm_grad_kernel(const NormShape &s)
 {
-    if (s.one) return s.chunks == 1 ? ee_norm_grad_kernel<1, true, WIDE> : ee_norm_grad_kernel<2, true, WIDE>;
-    return s.chunks == 1 ? ee_norm_grad_kernel<1, false, WIDE> : ee_norm_grad_kernel<2, false, WIDE>;
+    if (s.one) return s.chunks == 1 ? ee_norm_grad_kernel<1, true, WIDE, 2> : ee_norm_grad_kernel<2, true, WIDE, 2>;
+    return s.chunks == 1 ? (s.threads <= 512 ? ee_norm_grad_kernel<1, false, WIDE, 2> : ee_norm_grad_kernel<1, false, WIDE, 1>) : ee_norm_grad_kernel<2, false, WIDE, 1>;
 }
-static int norm_groups(int n_rows, const NormShape &s) { return std::min((n_rows + s.rows() - 1) / s.rows(), 512); }
+// Workgroups of the backward pass: four rows for each at least where there are as many (each one's sums are written and read again), two for a compute unit at most.
+static int norm_groups(int n_rows, const NormShape &s)
+{
+    const int n = (n_rows + s.rows() - 1) / s.rows();
+    return std::min(std::max((n + 3) / 4, std::min(n, 128)), 512);
+}
 
 static int check_rows(const char *call, int device, int n_rows, int dim, int center, float eps)
 {
@@ -401,7 +417,7 @@ static int check_norm_grad(const char *call, const ee_norm_grad_args *p)
     if (!p) return fail(EE_EINVAL, "%s: null argument", call);
     return check_rows(call, p->device, p->n_rows, p->dim, p->center, p->eps);
 }
-static size_t norm_grad_bytes(const ee_norm_grad_args *p) { return 2 * align256((size_t)norm_groups(p->n_rows, norm_shape(p->dim)) * p->dim * sizeof(float)); }
+static size_t norm_grad_bytes(const ee_norm_grad_args *p) { return 2 * align256((size_t)norm_groups(p->n_rows, norm_grad_shape(p->dim)) * p->dim * sizeof(float)); }
 
 extern "C" int ee_norm_grad_workspace(const ee_norm_grad_args *p, size_t *bytes)
 {
@@ -432,7 +448,7 @@ extern "C" int ee_norm_grad(const ee_norm_grad_args *p, void *workspace, size_t 
     if (p->d_gain || p->d_bias)
         if (need > workspace_bytes || (need && (!workspace || !aligned(workspace, 256))))
             return fail(EE_EINVAL, "%s: the workspace has %zu bytes of %zu, or is not 256-byte aligned", call, workspace_bytes, need);
-    const NormShape s = norm_shape(p->dim);
+    const NormShape s = norm_grad_shape(p->dim);
     NormDev a = {};
     a.x = p->x;
     a.dy = p->dy;

@@ -6,16 +6,16 @@
 // once.  Sums: every thread takes exponentials relative to its own maximum, so that nothing waits for the row's; they meet in 64 bits.  All of it in powers of two:
 // with c = log2(e) / T rounded to fp32 (another temperature by 2^-24 of it) an exponential is 2^(z c - r), one multiply-add and one instruction, r a number
 // of fp32 itself, so that nothing is lost where the sums are put together.
-// The largest: the `top`-th largest among the maxima of a wave's 256 groups of chunks is a bound that at least `top` elements reach; the chunks with an element
-// above the workgroup's best bound go to LDS (a few more than `top`), then their elements above it, and of those one wave keeps exactly `top`.  Rows
-// with so many equal elements that this overflows take as many rounds as tokens are wanted.
+// The largest: a wave's bound for n is the n-th largest among the maxima of its 256 groups of chunks, which n of its elements reach.  The least of w waves' bounds
+// for top / w is one that `top` elements reach; the chunks with an element above it go to LDS, then their elements above it (a few more than `top`), and of those one
+// wave keeps exactly `top`.  Rows with so many equal elements, or one wave's so far below the others', that this overflows take as many rounds as tokens are wanted.
 #include "ee_vocab.hpp"
 
 namespace ee {
 
 constexpr int SC_THREADS = 256, SC_WAVES = SC_THREADS / 64;   // of the second launch
 constexpr int SC_CHUNKS = 512;         // chunks with a candidate that LDS has room for
-constexpr int SC_CAND = 256;           // candidates, four for each lane of a wave
+constexpr int SC_CAND = 1024;          // candidates
 
 struct ScorePart {
     double sum, dot;                   // sum 2^(z c - r),  sum (z c - r) 2^(z c - r)
@@ -49,11 +49,11 @@ __device__ __forceinline__ unsigned key_of(float x)
 __device__ __forceinline__ float of_key(unsigned k) { return __int_as_float((int)k < 0 ? (int)(k & 0x7FFFFFFFu) : (int)~k); }
 constexpr unsigned KEY_LEAST = 0x00800000u;      // of the lowest finite number
 
-// Largest t whose bits below `low` are zero and that at least k of the wave's 4 x 64 keys reach; 0 if there are fewer than k.
-__device__ __forceinline__ unsigned wave_bound(const unsigned (&u)[4], int k, int low)
+// Largest t whose bits below `low` are zero and that at least k of the wave's 4 x 64 keys (of bits below `bits`) reach; 0 if there are fewer than k.
+__device__ __forceinline__ unsigned wave_bound(const unsigned (&u)[4], int k, int bits, int low)
 {
     unsigned t = 0;
-    for (int b = 31; b >= low; --b) {
+    for (int b = bits - 1; b >= low; --b) {
         const unsigned x = t | 1u << b;
         int n = 0;
 #pragma unroll
@@ -63,10 +63,18 @@ __device__ __forceinline__ unsigned wave_bound(const unsigned (&u)[4], int k, in
     return t;
 }
 
+// Bits of a key that say nothing: of logits of 16 bits.
+__host__ __device__ constexpr int idle_bits(int type) { return type == EE_FP32 ? 0 : type == EE_BF16 ? 16 : 13; }
+
+__device__ __forceinline__ int lanes_before(unsigned long long who) { return __builtin_amdgcn_mbcnt_hi((unsigned)(who >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)who, 0)); }
+
 // Of the wave's 4 x 64 candidates (key 0: none) the k best to list[0 ..], in no order; their number.
-__device__ __forceinline__ int wave_best(const unsigned (&u)[4], const int (&token)[4], int k, int lane, Cand *list)
+__device__ __forceinline__ int wave_best(const unsigned (&key)[4], const int (&token)[4], int k, int idle, Cand *list)
 {
-    const unsigned t = max(wave_bound(u, k, 0), 1u);
+    unsigned u[4];
+#pragma unroll
+    for (int g = 0; g < 4; ++g) u[g] = key[g] >> idle;
+    const unsigned t = max(wave_bound(u, k, 32 - idle, 0), 1u);
     int above = 0, equal = 0;
 #pragma unroll
     for (int g = 0; g < 4; ++g) {
@@ -78,18 +86,38 @@ __device__ __forceinline__ int wave_best(const unsigned (&u)[4], const int (&tok
     if (above + equal > k) {
         unsigned w[4];
 #pragma unroll
-        for (int g = 0; g < 4; ++g) w[g] = u[g] == t ? 0x7FFFFFFFu - (unsigned)token[g] : 0u;
-        v = wave_bound(w, k - above, 0);
+        for (int g = 0; g < 4; ++g) w[g] = u[g] == t ? 0x1FFFFFFu - (unsigned)token[g] : 0u;
+        v = wave_bound(w, k - above, 25, 0);
     }
     int n = 0;
 #pragma unroll
     for (int g = 0; g < 4; ++g) {
-        const bool in = u[g] > t || (u[g] == t && 0x7FFFFFFFu - (unsigned)token[g] >= v);
+        const bool in = u[g] > t || (u[g] == t && 0x1FFFFFFu - (unsigned)token[g] >= v);
         const unsigned long long who = __ballot(in);
-        if (in) list[n + __builtin_amdgcn_mbcnt_hi((unsigned)(who >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)who, 0))] = Cand{u[g], token[g]};
+        if (in) list[n + lanes_before(who)] = Cand{key[g], token[g]};
         n += __popcll(who);
     }
     return n;
+}
+// ... of n candidates in LDS; list has room for 64.
+__device__ __forceinline__ int wave_best_of(const Cand *cands, int n, int k, int idle, int lane, Cand *list)
+{
+    unsigned key[4];
+    int token[4], kept = 0;
+    for (int base = 0; base < n; base += base ? 192 : 256) {
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            const int i = base + g * 64 + lane;
+            const bool old = g == 3 && base, in = old ? lane < kept : i < n;
+            const Cand x = in ? (old ? list[lane] : cands[i]) : Cand{0, 0};
+            key[g] = x.key;
+            token[g] = x.token;
+        }
+        wave_lds_order();
+        kept = wave_best(key, token, k, idle, list);
+        wave_lds_order();
+    }
+    return kept;
 }
 
 // What one wave writes for a row: its n (at most 64) best in order, and the row's numbers.
@@ -196,8 +224,8 @@ __global__ void __launch_bounds__(NT, NT == 512 ? 6 : 4) ee_score_kernel(ScoreDe
         }
     }
     z.again(s, d);
-    const int k = min(a.top, len);
-    if (k > 0) {                                             // a bound that k elements of this wave reach, if it has so many
+    const int k = min(a.top, len), holding = min((len + 64 * N - 1) / (64 * N), WAVES);      // (waves that have elements at all)
+    if (k > 0) {
         unsigned u[4];
 #pragma unroll
         for (int g = 0; g < 4; ++g) {
@@ -206,65 +234,58 @@ __global__ void __launch_bounds__(NT, NT == 512 ? 6 : 4) ee_score_kernel(ScoreDe
             for (int c = g; c < E; c += 4) x = larger(x, cm[c]);
             u[g] = key_of(x);
         }
-        const unsigned t = wave_bound(u, k, 16);
+        const unsigned t = wave < holding ? wave_bound(u, (k + holding - 1) / holding, 32, 16) : ~0u;
         if (lane == 0) bound[wave] = t;
     }
     double S, D;
     join_sums<WAVES>(r, S, D, s, d, lane, wave, wr, ws, wd);
     int count = 0;
     if (k > 0) {
-        unsigned most = KEY_LEAST;
+        unsigned least = bound[0];
 #pragma unroll
-        for (int w = 0; w < WAVES; ++w) most = max(most, bound[w]);
-        const float t = of_key(most);
+        for (int w = 1; w < WAVES; ++w) least = min(least, bound[w]);
+        const float t = of_key(max(least, KEY_LEAST));
         int mine = 0;
 #pragma unroll
         for (int c = 0; c < E; ++c) mine += __popcll(__ballot(cm[c] >= t));
         int at = 0;
-        if (lane == 0) at = atomicAdd(&n_chunks, mine);
+        if (lane == 0 && mine) at = atomicAdd(&n_chunks, mine);
         at = __builtin_amdgcn_readfirstlane(at);
+        if (mine)
 #pragma unroll
-        for (int c = 0; c < E; ++c) {
-            const bool in = cm[c] >= t;
-            const unsigned long long who = __ballot(in);
-            if (who) {
-                const int place = at + __builtin_amdgcn_mbcnt_hi((unsigned)(who >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)who, 0));
+            for (int c = 0; c < E; ++c) {
+                const bool in = cm[c] >= t;
+                const unsigned long long who = __ballot(in);
+                const int place = at + lanes_before(who);
                 if (in && place < SC_CHUNKS) {
                     chunks[place] = z.raw[c];
                     chunk_at[place] = Part::offset(c, tid);
                 }
                 at += __popcll(who);
             }
-        }
         __syncthreads();
         const int n = min(n_chunks, SC_CHUNKS);
-        for (int i = tid; i < n * N; i += NT) {
-            float x;
-            if constexpr (TYPE == EE_FP32)
-                x = reinterpret_cast<const float *>(chunks)[i];
-            else if constexpr (TYPE == EE_BF16)
-                x = bf16_to_f32(reinterpret_cast<const uint16_t *>(chunks)[i]);
-            else
-                x = (float)reinterpret_cast<const _Float16 *>(chunks)[i];
-            if (x >= t) {
-                const int place = atomicAdd(&n_cands, 1);
-                if (place < SC_CAND) cands[place] = Cand{key_of(x), first + chunk_at[i / N] + i % N};
+        for (int base = wave * 64; base < n * N; base += NT) {
+            const int i = base + lane;
+            float x = -INFINITY;
+            if (i < n * N) {
+                if constexpr (TYPE == EE_FP32)
+                    x = reinterpret_cast<const float *>(chunks)[i];
+                else if constexpr (TYPE == EE_BF16)
+                    x = bf16_to_f32(reinterpret_cast<const uint16_t *>(chunks)[i]);
+                else
+                    x = (float)reinterpret_cast<const _Float16 *>(chunks)[i];
             }
+            const bool in = x >= t;
+            const unsigned long long who = __ballot(in);
+            int place = 0;
+            if (lane == 0 && who) place = atomicAdd(&n_cands, __popcll(who));
+            place = __builtin_amdgcn_readfirstlane(place) + lanes_before(who);
+            if (in && place < SC_CAND) cands[place] = Cand{key_of(x), first + chunk_at[i / N] + i % N};
         }
         __syncthreads();
         if (n_chunks <= SC_CHUNKS && n_cands <= SC_CAND) {
-            if (wave == 0) {
-                unsigned u[4];
-                int token[4];
-#pragma unroll
-                for (int g = 0; g < 4; ++g) {
-                    const bool in = g * 64 + lane < n_cands;
-                    const Cand x = cands[in ? g * 64 + lane : 0];
-                    u[g] = in ? x.key : 0u;
-                    token[g] = in ? x.token : 0;
-                }
-                count = wave_best(u, token, k, lane, best);
-            }
+            if (wave == 0) count = wave_best_of(cands, n_cands, k, idle_bits(TYPE), lane, best);
         } else {
             // many equal ones: a round for each token, the best behind the last one in order, by reading the part again (registers that live through this cost
             // every row of a call).  (Of finite logits; -infinity is none.)
@@ -331,6 +352,7 @@ __global__ void __launch_bounds__(SC_THREADS) ee_score_join_kernel(ScoreDev a)
     if (a.top > 0) {
         // a quarter of the parts' lists for each wave, 192 candidates at a time beside the best so far
         const int per = (a.parts + SC_WAVES - 1) / SC_WAVES, from = min(wave * per, a.parts) * a.top, to = min((wave + 1) * per, a.parts) * a.top;
+        const int idle = idle_bits(a.type);
         int n = 0;
         for (int base = from; base < to; base += 192) {
             unsigned u[4];
@@ -351,7 +373,7 @@ __global__ void __launch_bounds__(SC_THREADS) ee_score_join_kernel(ScoreDev a)
             u[3] = x.key;
             token[3] = x.token;
             wave_lds_order();
-            n = wave_best(u, token, a.top, lane, lists[wave]);
+            n = wave_best(u, token, a.top, idle, lists[wave]);
             wave_lds_order();
         }
         if (lane == 0) counts[wave] = n;
@@ -368,7 +390,7 @@ __global__ void __launch_bounds__(SC_THREADS) ee_score_join_kernel(ScoreDev a)
             u[g] = x.key;
             token[g] = x.token;
         }
-        n = wave_best(u, token, a.top, lane, best);
+        n = wave_best(u, token, a.top, idle_bits(a.type), best);
         wave_lds_order();
     }
     float r = -INFINITY;
