@@ -151,9 +151,9 @@ __device__ __forceinline__ void write_row(const ScoreDev &a, int row, int lane, 
     }
 }
 
-// Sums of a part from its threads' (relative to the r of each, -infinity where it has no finite logit), in every thread.
+// The waves' sums from their threads' (relative to the r of each, -infinity where it has no finite logit), relative to the part's r, which comes back.
 template <int WAVES>
-__device__ __forceinline__ void join_sums(float &r, double &S, double &D, float s, float d, int lane, int wave, float *wr, double *ws, double *wd)
+__device__ __forceinline__ float wave_sums(float r, float s, float d, int lane, int wave, float *wr, double *ws, double *wd)
 {
     const float wave_r = wave_max_f(r);
     if (lane == 0) wr[wave] = wave_r;
@@ -169,15 +169,7 @@ __device__ __forceinline__ void join_sums(float &r, double &S, double &D, float 
         ws[wave] = S2;
         wd[wave] = D2;
     }
-    __syncthreads();
-    r = all;
-    S = ws[0];
-    D = wd[0];
-#pragma unroll
-    for (int w = 1; w < WAVES; ++w) {
-        S += ws[w];
-        D += wd[w];
-    }
+    return all;
 }
 
 template <int TYPE, int E, int NT>
@@ -237,8 +229,8 @@ __global__ void __launch_bounds__(NT, NT == 512 ? 6 : 4) ee_score_kernel(ScoreDe
         const unsigned t = wave < holding ? wave_bound(u, (k + holding - 1) / holding, 32, 16) : ~0u;
         if (lane == 0) bound[wave] = t;
     }
-    double S, D;
-    join_sums<WAVES>(r, S, D, s, d, lane, wave, wr, ws, wd);
+    r = wave_sums<WAVES>(r, s, d, lane, wave, wr, ws, wd);
+    __syncthreads();
     int count = 0;
     if (k > 0) {
         unsigned least = bound[0];
@@ -325,6 +317,11 @@ __global__ void __launch_bounds__(NT, NT == 512 ? 6 : 4) ee_score_kernel(ScoreDe
     }
     if (wave != 0) return;
     wave_lds_order();
+    double S = ws[0], D = wd[0];
+    for (int w = 1; w < WAVES; ++w) {
+        S += ws[w];
+        D += wd[w];
+    }
     if (a.parts == 1) {
         write_row(a, row, lane, S, D, r, best, count);
         return;
