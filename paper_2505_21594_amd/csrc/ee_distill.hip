@@ -59,44 +59,62 @@ __device__ __forceinline__ double readlane_d(double x, int l)
     return join_d((unsigned)__builtin_amdgcn_readlane((int)(unsigned)b, l), (unsigned)__builtin_amdgcn_readlane((int)(unsigned)(b >> 32), l));
 }
 
+// What the list alone says; one wave calls it (while its row is on the way).
+struct ListTerms {
+    double p, both, share;             // the lane's probability, that of all entries that name its token, all entries' sum
+    int distinct;                      // tokens that are named
+    bool first;                        // the lane's token is named here for the first time
+};
+__device__ __forceinline__ ListTerms list_terms(const DistillDev &a, const Entry &e)
+{
+    ListTerms t;
+    const int lane = threadIdx.x & 63;
+    t.p = e.id >= 0 ? exp(e.lp) : 0.0;
+    // a token that is named twice has both probabilities (few lists do that: the sums only where one does)
+    t.first = e.id >= 0;
+    bool twice = false;
+    for (int i = 0; i < a.top; ++i) {
+        const bool same = __builtin_amdgcn_readlane(e.id, i) == e.id;
+        t.first = t.first && !(same && i < lane);
+        twice = twice || (same && i != lane);
+    }
+    t.both = t.p;
+    if (__ballot(twice && e.id >= 0)) {
+        t.both = 0.0;
+        for (int i = 0; i < a.top; ++i) {
+            const double other = readlane_d(t.p, i);
+            if (__builtin_amdgcn_readlane(e.id, i) == e.id) t.both += other;
+        }
+    }
+    t.distinct = __popcll(__ballot(t.first));
+    t.share = wave_sum_d(t.p);
+    return t;
+}
+
 // A row's numbers from the others' maximum and sum and from its list; one wave calls it.
 struct RowTerms {
     double loss;
     float others;                      // gradient of a token that the list does not name: others * 2^(z c - r)
     float mine;                        // gradient of the lane's token
-    bool first;                        // the lane's token is named here for the first time
 };
-__device__ __forceinline__ RowTerms row_terms(const DistillDev &a, const Entry &e, float r_rest, double s_rest, float d_loss)
+__device__ __forceinline__ RowTerms row_terms(const DistillDev &a, const Entry &e, const ListTerms &t, float r_rest, double s_rest, float d_loss)
 {
     constexpr double LN2 = 0.6931471805599453;
     RowTerms r;
     const bool in = e.id >= 0;
-    const double c = (double)a.c, p = in ? exp(e.lp) : 0.0;
-    // a token that is named twice has both probabilities
-    double both = 0.0;
-    r.first = in;
-    const int lane = threadIdx.x & 63;
-    for (int i = 0; i < a.top; ++i) {
-        const int id = __builtin_amdgcn_readlane(e.id, i);
-        const double other = readlane_d(p, i);
-        if (id >= 0 && id == e.id) {
-            both += other;
-            if (i < lane) r.first = false;
-        }
-    }
-    const int distinct = __popcll(__ballot(r.first));
+    const double c = (double)a.c, p = t.p, share = t.share;
     const float largest = fmaxf(r_rest, wave_max_f(in ? e.z * a.c : -INFINITY));
     const double R = largest == -INFINITY ? 0.0 : (double)largest;
     const double z = (double)e.z * c - R, q1 = in ? exp2(z) : 0.0;
     const double down = r_rest == -INFINITY ? 0.0 : (double)r_rest - R, scale_rest = r_rest == -INFINITY ? 0.0 : exp2(down);
-    const double S = wave_sum_d(r.first ? q1 : 0.0) + (s_rest != 0.0 ? s_rest * scale_rest : 0.0);
+    const double S = wave_sum_d(t.first ? q1 : 0.0) + (s_rest != 0.0 ? s_rest * scale_rest : 0.0);
     const bool valid = S > 0.0 && S < INFINITY;
-    const double share = wave_sum_d(p), log_S = log2(S), A = scale_rest / S;
+    const double log_S = log2(S), A = scale_rest / S;
     double others, scale = 1.0, shift = 0.0, tail = 0.0;
     if (a.rest) {
         const double pi = share < 1.0 ? 1.0 - share : share >= 1.0 ? 0.0 : share;        // (NaN stays)
         others = A;
-        if (pi != 0.0 && distinct < a.V) {
+        if (pi != 0.0 && t.distinct < a.V) {
             others = s_rest > 0.0 ? A - pi / s_rest : 0.0;
             tail = s_rest > 0.0 ? pi * (log2(pi) - (down + log2(s_rest) - log_S)) * LN2 : (double)INFINITY;
             if (s_rest != s_rest || pi != pi) others = tail = (double)NAN;
@@ -108,7 +126,7 @@ __device__ __forceinline__ RowTerms row_terms(const DistillDev &a, const Entry &
     }
     const double term = in && p != 0.0 && scale != 0.0 ? p * scale * (e.lp - shift - (z - log_S) * LN2) : 0.0;
     r.loss = wave_sum_d(term) + tail;
-    double g = share == 0.0 && !a.rest ? 0.0 : q1 / S - both * scale;
+    double g = share == 0.0 && !a.rest ? 0.0 : q1 / S - t.both * scale;
     if (!valid) r.loss = others = g = (double)NAN;
     const double weight = (double)d_loss * (c * LN2);
     r.others = (float)(others * weight);
@@ -146,11 +164,12 @@ __global__ void __launch_bounds__(NT, NT == 512 ? 6 : 4) ee_distill_kernel(Disti
     const int row = a.parts == 1 ? blockIdx.x : blockIdx.x / a.parts, part = a.parts == 1 ? 0 : blockIdx.x - row * a.parts;
     const int first = part * a.length, len = min(a.length, a.V - first);
     const void *logits = row_at(a.logits, TYPE, (size_t)row * a.stride);
+    Entry e = {-1, 0.f, 0.0};
+    ListTerms list = {0.0, 0.0, 0.0, 0, false};
+    if (wave == 0) e = entry_of(a, row, lane);
     Part z;
     z.load(row_at(logits, TYPE, first), len, tid);
-    Entry e = {-1, 0.f, 0.0};
     if (wave == 0) {
-        e = entry_of(a, row, lane);
         if (e.id >= 0) e.z = MODE == GRAD ? as_global(a.z)[(size_t)row * a.top + lane] : logit_at(TYPE, logits, e.id);
         if (MODE == STATS && part == 0 && lane < a.top) as_global_mut(a.z)[(size_t)row * a.top + lane] = e.z;
     }
@@ -165,6 +184,7 @@ __global__ void __launch_bounds__(NT, NT == 512 ? 6 : 4) ee_distill_kernel(Disti
             const int q = at / N, byte = (q % NT) * E + q / NT;
             atomicOr(&named[byte / 4], 1u << (byte % 4 * 8 + at % N));
         }
+        if (MODE == WHOLE && wave == 0) list = list_terms(a, e);
         __syncthreads();
         // (the named ones become -infinity, which no sum notices)
         float m = -INFINITY;
@@ -215,19 +235,20 @@ __global__ void __launch_bounds__(NT, NT == 512 ? 6 : 4) ee_distill_kernel(Disti
     if (wave == 0) {
         double S;
         if constexpr (MODE == GRAD) {
+            list = list_terms(a, e);
             S = join_parts(a, row, lane, r_rest);
         } else {
             S = ws[0];
             for (int w = 1; w < WAVES; ++w) S += ws[w];
         }
-        const RowTerms r = row_terms(a, e, r_rest, S, weight);
+        const RowTerms r = row_terms(a, e, list, r_rest, S, weight);
         if (lane == 0) {
             others_s = r.others;
             r_s = r_rest;
             if (a.loss && part == 0) as_global_mut(a.loss)[row] = (float)r.loss;
         }
         mine = nothing ? 0.f : r.mine;
-        store_mine = r.first && here;
+        store_mine = list.first && here;
     }
     if (!a.d_logits) return;
     __syncthreads();
@@ -272,32 +293,34 @@ __global__ void __launch_bounds__(256) ee_distill_loss_kernel(DistillDev a, int 
     if (e.id >= 0) e.z = as_global(a.z)[(size_t)row * a.top + lane];
     float r_rest;
     const double S = join_parts(a, row, lane, r_rest);
-    const RowTerms r = row_terms(a, e, r_rest, S, 1.f);
+    const RowTerms r = row_terms(a, e, list_terms(a, e), r_rest, S, 1.f);
     if (lane == 0) as_global_mut(a.loss)[row] = (float)r.loss;
 }
 
 struct DistillPlan {
-    int shape;                         // threads and chunks a thread: 256 x 4, 512 x 8, 1024 x 16
+    int shape;                         // threads and chunks a thread: 256 x 4, 512 x 8, 1024 x 8, 1024 x 16
+    bool whole;                        // one launch does all of a row; otherwise the sums have one of their own
     RowSplit split;
     size_t part_bytes, bytes;
 };
 static DistillPlan plan_distill(const ee_distill_args &p, bool grad)
 {
     DistillPlan pl;
-    const int n = p.dtype == EE_FP32 ? 4 : 8, room[3] = {256 * 4 * n, 512 * 8 * n, 1024 * 16 * n};
-    // A row that a workgroup can hold is one part, in the smallest workgroup that can where rows fill the chip; the loss alone of longer rows is better off in parts (600 rows
-    // of 100003: 149 us by workgroups of 1024 threads, 43 in four parts).
+    const int n = p.dtype == EE_FP32 ? 4 : 8, room[4] = {256 * 4 * n, 512 * 8 * n, 1024 * 8 * n, 1024 * 16 * n};
+    // A row that a workgroup can hold is one part, in the smallest workgroup that can where rows fill the chip.  The loss alone is better off with two launches, whose first has half the
+    // registers (4096 rows of 32000 71 us in one, LOSS2 in two).
     const bool many = p.n_rows >= 256;
-    if (p.vocab <= room[grad || !many ? 2 : 1]) {
-        pl.shape = p.vocab <= room[0] ? 0 : p.vocab <= room[1] && many ? 1 : 2;
+    pl.whole = grad && p.vocab <= room[3];
+    if (pl.whole) {
+        pl.shape = p.vocab <= room[0] ? 0 : p.vocab <= room[1] && many ? 1 : p.vocab <= room[2] ? 2 : 3;
         pl.split.parts = 1;
         pl.split.length = p.vocab;
     } else {
-        pl.shape = many ? 1 : 0;
+        pl.shape = many && p.vocab > room[0] ? 1 : 0;
         pl.split = split_rows(p.n_rows, p.vocab, room[pl.shape], 256 * n, many ? 1 : 512);
     }
-    pl.part_bytes = pl.split.parts > 1 ? align256((size_t)p.n_rows * pl.split.parts * sizeof(DistillPart)) : 0;
-    pl.bytes = pl.part_bytes + (pl.split.parts > 1 ? align256((size_t)p.n_rows * p.top * sizeof(float)) : 0);
+    pl.part_bytes = pl.whole ? 0 : align256((size_t)p.n_rows * pl.split.parts * sizeof(DistillPart));
+    pl.bytes = pl.part_bytes + (pl.whole ? 0 : align256((size_t)p.n_rows * p.top * sizeof(float)));
     return pl;
 }
 
@@ -334,7 +357,7 @@ template <int TYPE>
 static distill_kernel_t distill_kernel(int shape, int mode)
 {
     if (mode == WHOLE)
-        return shape == 0 ? ee_distill_kernel<TYPE, 4, 256, WHOLE> : shape == 1 ? ee_distill_kernel<TYPE, 8, 512, WHOLE> : ee_distill_kernel<TYPE, 16, 1024, WHOLE>;
+        return shape == 0 ? ee_distill_kernel<TYPE, 4, 256, WHOLE> : shape == 1 ? ee_distill_kernel<TYPE, 8, 512, WHOLE> : shape == 2 ? ee_distill_kernel<TYPE, 8, 1024, WHOLE> : ee_distill_kernel<TYPE, 16, 1024, WHOLE>;
     if (mode == STATS) return shape == 0 ? ee_distill_kernel<TYPE, 4, 256, STATS> : ee_distill_kernel<TYPE, 8, 512, STATS>;
     return shape == 0 ? ee_distill_kernel<TYPE, 4, 256, GRAD> : ee_distill_kernel<TYPE, 8, 512, GRAD>;
 }
@@ -384,9 +407,9 @@ extern "C" int ee_distill(const ee_distill_args *p, void *workspace, size_t work
         return p->dtype == EE_BF16 ? distill_kernel<EE_BF16>(pl.shape, mode) : p->dtype == EE_FP16 ? distill_kernel<EE_FP16>(pl.shape, mode) : distill_kernel<EE_FP32>(pl.shape, mode);
     };
     const dim3 grid((unsigned)(p->n_rows * a.parts)), block(pl.shape == 0 ? 256 : pl.shape == 1 ? 512 : 1024);
-    hipLaunchKernelGGL(kernel(a.parts == 1 ? WHOLE : STATS), grid, block, 0, s, a);
+    hipLaunchKernelGGL(kernel(pl.whole ? WHOLE : STATS), grid, block, 0, s, a);
     HIP_TRY(hipGetLastError());
-    if (a.parts > 1) {
+    if (!pl.whole) {
         if (a.d_logits)
             hipLaunchKernelGGL(kernel(GRAD), grid, block, 0, s, a);
         else
