@@ -307,8 +307,9 @@ static DistillPlan plan_distill(const ee_distill_args &p, bool grad)
 {
     DistillPlan pl;
     const int n = p.dtype == EE_FP32 ? 4 : 8, room[4] = {256 * 4 * n, 512 * 8 * n, 1024 * 8 * n, 1024 * 16 * n};
-    // A row that a workgroup can hold is one part, in the smallest workgroup that can where rows fill the chip.  The loss alone is better off with two launches, whose first has half the
-    // registers (4096 rows of 32000 71 us in one, LOSS2 in two).
+    // us, bf16 and fp16, one launch for all of a row / two, of which the second reads the logits again.  With a gradient: 600 rows of 100003 87 / 108, 1500 of 70000 138 / 145, so that a row
+    // that a workgroup can hold is one part, in the smallest workgroup that can where rows fill the chip and of 1024 threads where they do not (five rows of 32000, fp32, by sixteen
+    // chunks a thread 19.4, by eight 8.9).  The loss alone: 4096 rows of 32000 72 / 61, 600 of 100003 149 / 44, five of 32000 17.3 / 7.4: the first launch alone has half the registers.
     const bool many = p.n_rows >= 256;
     pl.whole = grad && p.vocab <= room[3];
     if (pl.whole) {

@@ -193,8 +193,8 @@ __global__ void __launch_bounds__(ONE ? 256 : 512) ee_norm_kernel(NormDev a)
     store_row<E>(a.y_type, a.y, (size_t)row * a.y_stride, a.dim, l, lanes, x);
 }
 
-// The next two rows' loads are on their way while a row is worked on: a compute unit has two workgroups, whose sums of gains' and biases' gradients are written once for all
-// their rows (more workgroups write more of them).
+// The next rows' loads (DEPTH of them) are on their way while a row is worked on: a compute unit has two workgroups, whose sums of gains' and biases' gradients are written once for
+// all their rows (more workgroups write more of them).
 template <int E, bool ONE, bool WIDE, int DEPTH>
 __global__ void __launch_bounds__(ONE ? 256 : 1024, !ONE && E == 1 && !WIDE ? (DEPTH == 1 ? 6 : 5) : 1) ee_norm_grad_kernel(NormDev a)
 {
@@ -322,7 +322,7 @@ struct NormShape {
     bool one;
     int rows() const { return one ? 4 : 1; }
 };
-// Forward, four waves for a row as long as four chunks a lane are enough: more of it on its way for every wave (rows of 5120: ten waves of one chunk 45 us, FWD5120).
+// Forward, four waves for a row as long as four chunks a lane are enough: more of it on its way for every wave (8191 rows of 5120, bf16: ten waves of one chunk 45.1 us, four of three 41.8; 8192 of 4096: eight of one 29.1, four of two 28.2).
 static NormShape norm_shape(int dim)
 {
     const int pieces = (dim + 7) / 8;
@@ -330,7 +330,8 @@ static NormShape norm_shape(int dim)
     const int threads = pieces <= 1024 ? 256 : 512;
     return {(pieces + threads - 1) / threads, threads, false};
 }
-// Backward, a chunk a lane, whose registers hold its part of the gains' and biases' gradients too; waves in fours, so that a compute unit's SIMDs have room for a second workgroup.
+// Backward, a chunk a lane, whose registers hold its part of the gains' and biases' gradients too; waves in fours, and few enough registers, so that a compute unit's SIMDs have room
+// for a second workgroup (8191 rows of 5120: ten waves of 92 registers 83 us, twelve of 80 67.5; 8192 of 4096 by eight 48.7; 2000 of 16384 85).
 static NormShape norm_grad_shape(int dim)
 {
     const int pieces = (dim + 7) / 8;

@@ -507,6 +507,79 @@ def test_linear_does_not_read_behind_rows():
         close(dw.result(), want[1], "d_weight")
 
 
+# ---------------------------------------------------------------- far apart
+
+class far_rows:
+    """Rows so far apart that offsets pass 32 bits."""
+
+    def __init__(self, x, kind, stride):
+        self.host = np.ascontiguousarray(encode(np.asarray(x, np.float32), kind))
+        self._stride, item = stride, self.host.itemsize
+        self._p = ctypes.c_void_p()
+        ok(hip().hipMalloc(ctypes.byref(self._p), ((len(x) - 1) * stride + x.shape[1]) * item + 256))
+        for r in range(len(x)):
+            ok(hip().hipMemcpy(self._p.value + r * stride * item, self.host[r].ctypes.data, x.shape[1] * item, 1))
+        like = Dev(self.host[:1])
+        self.shape, self.dtype, self.device = x.shape, like.dtype, like.device
+
+    def data_ptr(self):
+        return self._p.value
+
+    def stride(self):
+        return (self._stride, 1)
+
+    def result(self):
+        out = np.empty_like(self.host)
+        ok(hip().hipDeviceSynchronize())
+        for r in range(len(out)):
+            ok(hip().hipMemcpy(out[r].ctypes.data, self._p.value + r * self._stride * out.itemsize, out.shape[1] * out.itemsize, 2))
+        return decode(out)
+
+    def __del__(self):
+        hip().hipFree(self._p)
+
+
+def test_rows_beyond_32_bits():
+    rng = np.random.default_rng(0)
+    far = (1 << 31) + 8                                            # elements from row to row
+    z = logits(rng, 3, 700, "bf16")
+    d, g = far_rows(z, "bf16", far), far_rows(z, "bf16", far)
+    ids, tl = Dev(np.zeros((3, 5), np.int32)), Dev(np.zeros((3, 5), np.float32))
+    ee.ee_score_tokens(d, top_ids=ids, top_logprobs=tl, workspace=Space(ee.ee_score_workspace(d, top=5)).view)
+    want = ref.score(z, None, 5, 1.0)
+    assert (ids.numpy() == want["top_ids"]).all()
+    ee.ee_distill(d, ids, tl, d_logits=g, workspace=Space(ee.ee_distill_workspace(d, top=5)).view)
+    close(g.result(), ref.distill(z, want["top_ids"], tl.numpy(), 1.0, True, None, HALF_STEP["bf16"])[1], "gradient")
+    x = decode(encode(rng.standard_normal((3, 64)).astype(np.float32), "bf16"))
+    d, y, dy = far_rows(x, "bf16", far), far_rows(0 * x, "bf16", far), far_rows(x[::-1], "bf16", far)
+    ee.ee_norm(d, y)
+    close(y.result(), ref.norm(x, None, None, 1e-5, 0, HALF_STEP["bf16"]), "norm")
+    ee.ee_norm_grad(d, dy, dx=y)
+    close(y.result(), ref.norm_grad(x, x[::-1], None, 1e-5, 0, HALF_STEP["bf16"])[0], "norm's gradient")
+    w = matrix(rng, 40, 64, "bf16")
+    y, dx, dw = far_rows(np.zeros((3, 40)), "bf16", far), far_rows(0 * x, "bf16", far), empty(40, 64, "fp32")
+    v = decode(encode(rng.standard_normal((3, 40)).astype(np.float32), "bf16"))
+    dy = far_rows(v, "bf16", far)
+    ws = Space(max(ee.ee_linear_workspace(d, w.view), ee.ee_linear_grad_workspace(d, w.view)))
+    ee.ee_linear(d, w.view, y, workspace=ws.view)
+    close(y.result(), ref.linear(x, w.values(), None, None, 0, HALF_STEP["bf16"], 0)[0], "linear")
+    ee.ee_linear_grad(d, w.view, dy, dx=dx, d_weight=dw.view, workspace=ws.view)
+    want = ref.linear_grad(x, w.values(), v, None, 0, HALF_STEP["bf16"], 2.0 ** -24, 0, 0)
+    close(dx.result(), want[0], "dx")
+    close(dw.result(), want[1], "d_weight")
+
+
+def test_linear_rows_beyond_offsets_of_a_tile():
+    """Rows of operands farther apart than 32-bit offsets within a tile allow."""
+    rng = np.random.default_rng(1)
+    for rows in (5, 70):
+        x = decode(encode(rng.standard_normal((rows, 96)).astype(np.float32), "bf16"))
+        d, w, y = far_rows(x, "bf16", (1 << 22) + 8), matrix(rng, 72, 96, "bf16"), empty(rows, 72, "fp32")
+        ws = Space(ee.ee_linear_workspace(d, w.view))
+        ee.ee_linear(d, w.view, y.view, workspace=ws.view)
+        close(y.result(), ref.linear(x, w.values(), None, None, 0, 2.0 ** -24, 0)[0], "y")
+
+
 # ---------------------------------------------------------------- a run of them together
 
 class Step:
