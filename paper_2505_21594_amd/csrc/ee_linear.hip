@@ -1,3 +1,10 @@
+// Products by tiles through LDS: bound by the matrix cores and by how they are fed where rows are many, by the weights' bytes where they are few (ee_gemm16_thin_kernel).
+// One MI355X, bf16, us and TFLOP/s (a library's product of the same matrices in the same run): 2041 x 4096 x 11008 forward 179, 1030 (159, 1158), dx 163, 1127, dW 174, 1055;
+// 8192 x 8192 x 8192 930, 1183 (661, 1664), 960, 880 (dW 1250 TFLOP/s); 4096 x 4096 x 4096 128 (87), 126, 116.  Five rows of 4096 through 32000 columns 52.8 us, 5.0 TB/s.
+//
+// What the tile's loads cost decides: with the sum's index contiguous and lane l at row l & 15 (the operands' own order) 2041 x 4096 x 11008 forward took 267 us, with four lanes a
+// row 206, and 179 with whole lines of 128 bytes (KS = 2; half lines are fetched twice, as the cache of a compute unit does not hold them from one step to the next).
+// 256 x 128 tiles of 64 of the sum leave a compute unit one workgroup: 244 us.
 #include "ee_linear.hpp"
 
 #include <atomic>
@@ -220,6 +227,7 @@ __global__ void __launch_bounds__(256, 2) ee_gemm16_kernel(GemmDev g)
 
 // Few rows: bound by the weights' bytes.  A workgroup has 16 TN columns of results, its four waves take steps of 32 of the sum in turn, each through
 // a ring of its own in LDS (no barrier but the last): 10 KB on their way for a wave, 80 for a compute unit.  The rows are MT tiles of 16; the waves' sums meet in LDS.
+// (Five rows of 4096 through 32000 columns: 52.8 us, 5.0 TB/s; by tiles whose waves share a ring 73.7.)
 constexpr int THIN_STAGES = 3;
 template <int TN, int MT>
 constexpr size_t thin_lds() { return (size_t)4 * THIN_STAGES * (TN + MT) * 1024; }
@@ -324,7 +332,7 @@ __global__ void __launch_bounds__(256) ee_gemm16_join_kernel(GemmDev g)
     finish<1>(g, row, 1, col, bias_at(g, col), one);
 }
 
-// dz = dy act'(z) as 16-bit terms, and sums of its columns over a part of the rows: a thread has eight columns.
+// dz = dy act'(z) as 16-bit terms, and sums of its columns over a part of the rows: a thread has eight columns.  Bound by bytes (2041 x 11008 bf16, the sums alone: 16.3 us, 45 MB, 2.8 TB/s).
 struct SlopeDev {
     const uint16_t *dy, *pre;
     long long dy_stride, pre_stride, ldz, plane;
@@ -357,13 +365,10 @@ __global__ void __launch_bounds__(SL_COLS *SL_SUBS) ee_slope_kernel(SlopeDev a)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     w[i] = a.type == EE_BF16 ? pack_bf16(x[2 * i], x[2 * i + 1]) : pack_fp16(x[2 * i], x[2 * i + 1]);
-                    if (a.type == EE_BF16) {
-                        x[2 * i] -= __uint_as_float(w[i] << 16);
-                        x[2 * i + 1] -= __uint_as_float(w[i] & 0xFFFF0000u);
-                    } else {
-                        x[2 * i] -= (float)__builtin_bit_cast(_Float16, (uint16_t)w[i]);
-                        x[2 * i + 1] -= (float)__builtin_bit_cast(_Float16, (uint16_t)(w[i] >> 16));
-                    }
+                    const float lo = a.type == EE_BF16 ? __uint_as_float(w[i] << 16) : (float)__builtin_bit_cast(_Float16, (uint16_t)w[i]);
+                    const float hi = a.type == EE_BF16 ? __uint_as_float(w[i] & 0xFFFF0000u) : (float)__builtin_bit_cast(_Float16, (uint16_t)(w[i] >> 16));
+                    x[2 * i] = fabsf(lo) == INFINITY ? 0.f : x[2 * i] - lo;              // (an infinity is one term, not one and its negative)
+                    x[2 * i + 1] = fabsf(hi) == INFINITY ? 0.f : x[2 * i + 1] - hi;
                 }
                 *as_global_mut(reinterpret_cast<u32x4_t *>(a.dz + t * a.plane + (size_t)row * a.ldz + col)) = w;
             }

@@ -46,6 +46,7 @@ __device__ __forceinline__ float act_of(int act, float z)
 }
 __device__ __forceinline__ float act_slope(int act, float z)
 {
+    if (fabsf(z) > 100.f) z = copysignf(100.f, z);                                       // (where the slope is 0 or 1: no infinity times 0; NaN stays)
     if (act == EE_ACT_SILU) {
         const float s = logistic(z);
         return s * (1.f + z * (1.f - s));

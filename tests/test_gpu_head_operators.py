@@ -735,3 +735,33 @@ def test_results_do_not_depend_on_timing():
         s.run()
         again = s.results()
         assert all(np.array_equal(first[k], again[k]) for k in first)
+
+
+def test_infinities_and_far_arguments_of_activations():
+    """The slope of an activation far out is 0 or 1, of pre = +-infinity (z beyond the type) too; an infinite dy stays infinite in every number of terms."""
+    rng = np.random.default_rng(21)
+    x, w = matrix(rng, 40, 16, "fp16"), matrix(rng, 24, 16, "fp16")
+    dyv = rng.standard_normal((40, 24))
+    prev = rng.standard_normal((40, 24))
+    prev[3, 5], prev[4, 6], prev[5, 7], prev[6, 8] = np.inf, -np.inf, 6e4, -6e4
+    for out in ("fp16", "fp32"):
+        for act in (ee.ACT_SILU, ee.ACT_GELU):
+            dy, pre, dx, dw = Rows(dyv, "fp16"), Rows(prev, "fp16"), empty(40, 16, out), empty(24, 16, out)
+            ws = Space(ee.ee_linear_grad_workspace(x.view, w.view, act=act))
+            ee.ee_linear_grad(x.view, w.view, dy.view, pre=pre.view, act=act, dx=dx.view, d_weight=dw.view, workspace=ws.view)
+            limit = np.where(np.abs(prev) > 1e3, np.copysign(100, prev), pre.values())
+            step = 2.0 ** -22 if out == "fp32" else HALF_STEP["fp16"]
+            want = ref.linear_grad(x.values(), w.values(), dy.values(), limit, act, HALF_STEP[out], HALF_STEP[out], step, step)
+            small = 2.0 ** -25
+            close(dx.result(), (want[0][0], want[0][1] + SUBNORMAL[out] + small * np.abs(w.values()).sum(0)), "dx")
+            close(dw.result(), (want[1][0], want[1][1] + SUBNORMAL[out] + small * np.abs(x.values()).sum(0)), "d_weight")
+    for kind in ("bf16", "fp16"):
+        x, w = matrix(rng, 4, 8, kind), matrix(rng, 8, 8, kind)
+        w = Rows(np.eye(8) * 2, kind)
+        dyv = rng.standard_normal((4, 8))
+        dyv[1, 3] = np.inf
+        dx = empty(4, 8, "fp32")
+        ws = Space(ee.ee_linear_grad_workspace(x.view, w.view, act=ee.ACT_SILU))
+        ee.ee_linear_grad(x.view, w.view, Rows(dyv, kind).view, pre=Rows(np.full((4, 8), 2.0), kind).view, act=ee.ACT_SILU, dx=dx.view, workspace=ws.view)
+        got = dx.result()
+        assert got[1, 3] == np.inf and np.isfinite(got[[0, 2, 3]]).all()
