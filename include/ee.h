@@ -514,7 +514,7 @@ int ee_accept_drafts(const ee_accept_args *args, void *workspace, size_t workspa
    Tokens whose logit is -infinity (masked ones) have no part in a row; where fewer than `top` are left the list ends with -1 and -infinity.  A row
    without a softmax (NaN, +infinity or nothing but -infinity among its logits) gets NaN, and -1 for its tokens.
    logits [n_rows][vocab] of type `dtype` at any alignment of the type, sums in fp32 for each thread and 64 bits from there; results fp32, int32.  n_rows up to 2^20, vocab
-   up to 2^24 (EE_EINVAL where rows times parts of rows pass 2^22).
+   up to 2^24 (EE_EINVAL where rows times parts of rows pass 2^22).  A row whose largest |logit| / temperature is above 2^126 may get NaN.
    workspace: ee_score_workspace bytes (may be 0), 256-byte aligned; contents do not matter. */
 typedef struct {
     int32_t device, dtype, n_rows, vocab, top;
@@ -542,6 +542,7 @@ int ee_score_tokens(const ee_score_args *args, void *workspace, size_t workspace
    d_loss is 0 get zeros, whatever their logits are.  d_logits may be logits (same type and stride).  A row without a softmax has loss and gradient NaN.  A student that
    gives a named token, or all the others where pi > 0, no probability (-infinity) has an infinite loss; its gradient is finite (0 where q is).  Sums in fp32 for
    each thread and 64 bits from there, everything that a row has once in 64 bits.  n_rows up to 2^20, vocab up to 2^24 (EE_EINVAL where rows times parts of rows pass 2^22).
+   A row whose largest |logit| / temperature is above 2^126 may get NaN.
    workspace: ee_distill_workspace bytes (may be 0), 256-byte aligned; contents do not matter. */
 typedef struct {
     int32_t device, dtype, grad_dtype, n_rows, vocab, top, rest;
@@ -592,7 +593,8 @@ int ee_norm_grad(const ee_norm_grad_args *args, void *workspace, size_t workspac
    needs where there is an activation, or NULL.  fp32 sums, one rounding of each result.  An exit's adapters are two such calls (the down matrices stacked, EE_ACT_SILU; the up
    matrices side by side, residual h).
    ee_linear_grad: dz = dy act'(pre);  dx = dz weight,  d_weight = dz^T x,  d_bias = sum over the rows of dz (fp32; written, not added to), each NULL where it is not wanted.  (The residual's
-   gradient is dy.)  dy and pre are of type dtype; dz is rounded to dtype where the result is of 16 bits, and is two (fp16) or three (bf16) terms of it where that is fp32.
+   gradient is dy.)  dy and pre are of type dtype; dz is rounded to dtype where the result is of 16 bits, and is two (fp16) or three (bf16) terms of it where that is fp32 (past the
+   largest fp16 it is infinite).
    Every row starts at a multiple of 16 bytes.  Any sizes up to EE_LINEAR_MAX, odd ones too (EE_EINVAL where two of them make 2^23 tiles of 64 x 64).
    workspace: bytes by the _workspace calls (may be 0), 256-byte aligned; contents do not matter. */
 #define EE_ACT_NONE 0

@@ -12,6 +12,7 @@ SUM = 190 * U
 
 def score(z, tokens, top, T, half=U):
     """z: float64 logits as the call reads them.  {name: (values, tolerance)}; tokens of the lists exactly."""
+    T = float(np.float32(T))                                     # (what the call receives)
     rows, V = z.shape
     out = {k: (np.zeros(rows), np.zeros(rows)) for k in ("logprob", "entropy")}
     ids, lps, tols = np.full((rows, top), -1, np.int64), np.full((rows, top), -np.inf), np.zeros((rows, top))
@@ -45,6 +46,7 @@ def score(z, tokens, top, T, half=U):
 
 def distill(z, ids, logprobs, T, rest, weight=None, half=U, subnormal=0.0):
     """(loss, tolerance), (gradient, tolerance); `half`: half a step of the gradient's type, `subnormal`: of its smallest numbers."""
+    T = float(np.float32(T))                                     # (what the call receives)
     rows, V = z.shape
     loss, loss_tol, grad, grad_tol = np.zeros(rows), np.zeros(rows), np.zeros((rows, V)), np.zeros((rows, V))
     for r in range(rows):

@@ -226,6 +226,33 @@ def test_distill_one_result_and_in_place(rows, V):
         check_distill(z, "bf16", ids, lp, 1.0, True, "bf16", **kw)
 
 
+@pytest.mark.parametrize("T", [2.5, 0.7, 1.0])
+def test_log_probabilities_of_far_tokens(T):
+    """A far token's log-probability is rounded once, at 2^-24 of it: the factor log2(e) / T in fp32 (0.82 of that off for T = 2.5) has no part in it."""
+    rng = np.random.default_rng(31)
+    rows, V = 64, 300
+    z = 2 * rng.standard_normal((rows, V))
+    z[:, 7] = -np.exp(rng.uniform(np.log(1e2), np.log(6e4), rows))
+    z = decode(encode(z.astype(np.float32), "fp32"))
+    check_score(z, "fp32", np.full(rows, 7), 8, T)
+    ids, lp = np.full((rows, 1), 7, np.int32), np.zeros((rows, 1), np.float32)
+    check_distill(z, "fp32", ids, lp, T, False, "fp32")
+    far = decode(encode((z[:, 7:8] + np.arange(9)[None] / 4).astype(np.float32), "fp32"))
+    far[:, 4] = 3.0                                              # the one token that the teacher names, with half its probability; the others are far
+    check_distill(far, "fp32", np.full((rows, 1), 4, np.int32), np.full((rows, 1), np.log(0.5), np.float32), T, True, "fp32")
+
+
+@pytest.mark.parametrize("rows,V,kind", [(2, 140001, "bf16"), (2, 70001, "fp32"), (260, 140001, "bf16")])
+def test_distill_in_place_in_parts(rows, V, kind):
+    """Rows too long for a workgroup: the second launch reads logits where the first parts of the same row hold gradients already."""
+    rng = np.random.default_rng(V + rows)
+    z = logits(rng, rows, V, kind, special=True)
+    ids, lp = teacher(rng, z, 64, 0.7, "near")
+    ids[:, 0], ids[:, 1] = 0, V - 1
+    weight = np.where(np.arange(rows) % 2, 0, 1.5).astype(np.float32)
+    check_distill(z, kind, ids, lp, 0.7, True, kind, weight, in_place=True)
+
+
 def test_distill_label_is_cross_entropy():
     rng = np.random.default_rng(2)
     z = logits(rng, 5, 900, "fp32")

@@ -233,3 +233,11 @@ def test_planted_mistakes_are_outside_the_tolerances():
     (y, tol), _ = ref.linear(x, w, None, None, 1, 2.0 ** -8, 2.0 ** -8)
     x[:, 299] = 0                                                                       # the last element of the sums left out
     assert (np.abs(ref.linear(x, w, None, None, 1, 0, 0)[0][0] - y) > tol).any()
+
+
+def test_more_parts_than_a_grid_are_refused():
+    """2^20 rows of 2^24 tokens: refused before anything is launched (a workspace of any size is claimed, none is touched)."""
+    lib = ee.load_library()
+    size = dict(n_rows=1 << 20, vocab=1 << 24, logits_stride=1 << 24)
+    refused(lib.ee_score_tokens(ctypes.byref(score_args(**size)), P, 1 << 60, None), "too many rows")
+    refused(lib.ee_distill(ctypes.byref(distill_args(d_logits_stride=1 << 24, **size)), P, 1 << 60, None), "too many rows")
