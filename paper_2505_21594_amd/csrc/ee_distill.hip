@@ -4,12 +4,13 @@
 //              dL/dz_i = (q_i - p_i) / T for those it names, q_i (1 - pi / rho) / T for the others;
 //   rest = 0:  p divided by its sum;  L = sum_j p_j (log p_j - log q_j),  dL/dz_i = (q_i - p_i) / T.
 //
-// Bound by the logits' bytes, read once, and the gradient's, written once (one MI355X: 4096 rows of 32000, bf16, 118 us, 4.45 TB/s): a workgroup holds its row in registers (RowPart) from the sums to the gradient.
-// Rows that are too few to fill the chip, or too long for a workgroup, are taken in parts by two launches, of which the second reads the logits again.
-// The tokens that the list names are marked in LDS, one bit each, a thread's bits in one word, and left out of the sums: rho is a sum of its own, not
-// a difference.  In powers of two, c = log2(e) / T rounded to fp32 (another temperature by 2^-24 of it, put right in 64 bits where the loss has an exponent itself): with r and S' = sum 2^(z c - r) the others' largest exponent
-// and sum, R the row's largest and A = 2^(r - R) / S their share's scale, rho = A S' and q_i (1 - pi / rho) = 2^(z_i c - r) (A - pi / S').
-// Everything that a row has once is in 64 bits: the loss is a small difference of large terms.
+// Bound by the logits' bytes, read once, and the gradient's, written once (one MI355X: 4096 rows of 32000, bf16, 118 us, 4.45 TB/s): a workgroup holds its row in
+// registers (RowPart) from the sums to the gradient. Rows that are too few to fill the chip, or too long for a workgroup, are taken in parts by two launches, of
+// which the second reads the logits again. The tokens that the list names are marked in LDS, one bit each, a thread's bits in one word, and left out of the sums:
+// rho is a sum of its own, not a difference.  In powers of two, c = log2(e) / T rounded to fp32 (another temperature by 2^-24 of it, the same one everywhere:
+// exponents put right beside sums that are not would take the digits of a small divergence): with r and S' = sum 2^(z c - r) the others' largest exponent and sum, R
+// the row's largest and A = 2^(r - R) / S their share's scale, rho = A S' and q_i (1 - pi / rho) = 2^(z_i c - r) (A - pi / S'). Everything that a row has once is in
+// 64 bits: the loss is a small difference of large terms.
 #include "ee_vocab.hpp"
 
 namespace ee {
@@ -30,7 +31,6 @@ struct DistillDev {
     long long stride, grad_stride;
     int type, grad_type, V, top, rest, parts, length;
     float c;                           // log2(e) / T
-    double fix;                        // ... by the c that it is rounded to
 };
 
 // The teacher's list of a row: a lane of a wave for each entry.
@@ -117,7 +117,7 @@ __device__ __forceinline__ RowTerms row_terms(const DistillDev &a, const Entry &
         others = A;
         if (pi != 0.0 && t.distinct < a.V) {
             others = s_rest > 0.0 ? A - pi / s_rest : 0.0;
-            tail = s_rest > 0.0 ? pi * (log2(pi) - (down * a.fix + log2(s_rest) - log_S)) * LN2 : (double)INFINITY;
+            tail = s_rest > 0.0 ? pi * (log2(pi) - (down + log2(s_rest) - log_S)) * LN2 : (double)INFINITY;
             if (s_rest != s_rest || pi != pi) others = tail = (double)NAN;
         }
     } else {
@@ -125,7 +125,7 @@ __device__ __forceinline__ RowTerms row_terms(const DistillDev &a, const Entry &
         shift = share > 0.0 ? log(share) : 0.0;
         others = share == 0.0 ? 0.0 : A;
     }
-    const double term = in && p != 0.0 && scale != 0.0 ? p * scale * (e.lp - shift - (z * a.fix - log_S) * LN2) : 0.0;
+    const double term = in && p != 0.0 && scale != 0.0 ? p * scale * (e.lp - shift - (z - log_S) * LN2) : 0.0;
     r.loss = wave_sum_d(term) + tail;
     double g = share == 0.0 && !a.rest ? 0.0 : q1 / S - t.both * scale;
     if (!valid) r.loss = others = g = (double)NAN;
@@ -402,7 +402,6 @@ extern "C" int ee_distill(const ee_distill_args *p, void *workspace, size_t work
     a.parts = pl.split.parts;
     a.length = pl.split.length;
     a.c = (float)(1.4426950408889634 / (double)p->temperature);
-    a.fix = 1.4426950408889634 / (double)p->temperature / (double)a.c;
     DeviceScope scope(p->device);
     HIP_TRY(scope.status);
     const hipStream_t s = static_cast<hipStream_t>(stream);

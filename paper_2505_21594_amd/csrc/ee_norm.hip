@@ -3,10 +3,10 @@
 //   x^ = (x - mu) r,  mu = mean x (0 without center),  r = 1 / sqrt(mean (x - mu)^2 + eps),   y = x^ g + b;
 //   u = dy g,   dx = r (u - mean u [center] - x^ mean(u x^)),   dg = sum over rows of dy x^,   db = sum over rows of dy.
 //
-// Bound by the rows' bytes (one MI355X, bf16: 8192 rows of 4096 forward 28.2 us, 4.8 TB/s, backward with all sums 48.7, 4.1 TB/s): a wave, or a workgroup, holds a row in registers, so that mean, squares about the mean (no difference of large sums) and
-// result read memory once.  Backward, mean(u x^) is taken with u (x - mu), which needs no r: its sum travels with the squares'.  The
-// gradients of gains and biases stay in registers while a workgroup goes over its rows; the workgroups' sums are added up in order by a second launch.
-// Statistics and sums are fp32.
+// Bound by the rows' bytes (one MI355X, bf16: 8192 rows of 4096 forward 28.2 us, 4.8 TB/s, backward with all sums 48.7, 4.1 TB/s): a wave, or a workgroup, holds a
+// row in registers, so that mean, squares about the mean (no difference of large sums) and result read memory once.  Backward, mean(u x^) is taken with u (x - mu),
+// which needs no r: its sum travels with the squares'.  The gradients of gains and biases stay in registers while a workgroup goes over its rows; the workgroups'
+// sums are added up in order by a second launch. Statistics and sums are fp32.
 #include "ee_vocab.hpp"
 
 namespace ee {

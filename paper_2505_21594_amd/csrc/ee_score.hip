@@ -2,13 +2,14 @@
 //
 //   log p_i = z_i / T - L,  L = log sum exp(z / T);   H = L - sum p z / T;   the `top` largest logits, of equal ones the lower token first.
 //
-// Bound by the logits' bytes (one MI355X: 2041 rows of 32000, bf16, 26.8 us without lists, 4.9 TB/s; with lists of 20 38.5).  A workgroup holds a row, or a part of it, in registers (RowPart): the sums and the search for the largest read memory
-// once.  Sums: every thread takes exponentials relative to its own maximum, so that nothing waits for the row's; they meet in 64 bits.  All of it in powers of two:
-// with c = log2(e) / T rounded to fp32 (another temperature by 2^-24 of it, which a sum does not feel; a far token's own exponent does and is put right in 64 bits) an exponential is 2^(z c - r), one multiply-add and one instruction, r a number
-// of fp32 itself, so that nothing is lost where the sums are put together.
-// The largest: a wave's bound for n is the n-th largest among the maxima of its 256 groups of chunks, which n of its elements reach.  The least of w waves' bounds
-// for top / w is one that `top` elements reach; the chunks with an element above it go to LDS, then their elements above it (a few more than `top`), and of those one
-// wave keeps exactly `top`.  Rows with so many equal elements, or one wave's so far below the others', that this overflows take as many rounds as tokens are wanted.
+// Bound by the logits' bytes (one MI355X: 2041 rows of 32000, bf16, 26.8 us without lists, 4.9 TB/s; with lists of 20 38.5).  A workgroup holds a row, or a part of
+// it, in registers (RowPart): the sums and the search for the largest read memory once.  Sums: every thread takes exponentials relative to its own maximum, so that
+// nothing waits for the row's; they meet in 64 bits.  All of it in powers of two: with c = log2(e) / T rounded to fp32 (another temperature by 2^-24 of it; log-
+// probabilities are put right to the first order in 64 bits, exponent and sum) an exponential is 2^(z c - r), one multiply-add and one instruction, r a number of
+// fp32 itself, so that nothing is lost where the sums are put together. The largest: a wave's bound for n is the n-th largest among the maxima of its 256 groups of
+// chunks, which n of its elements reach.  The least of w waves' bounds for top / w is one that `top` elements reach; the chunks with an element above it go to LDS,
+// then their elements above it (a few more than `top`), and of those one wave keeps exactly `top`.  Rows with so many equal elements, or one wave's so far below the
+// others', that this overflows take as many rounds as tokens are wanted.
 #include "ee_vocab.hpp"
 
 namespace ee {
@@ -126,15 +127,15 @@ __device__ __forceinline__ void write_row(const ScoreDev &a, int row, int lane, 
 {
     constexpr double LN2 = 0.6931471805599453;
     const bool valid = S > 0.0 && S < INFINITY;               // (NaN, +infinity or nothing but -infinity: no softmax)
-    const double c = (double)a.c, log_S = valid ? log2(S) : (double)NAN;
+    const double c = (double)a.c, mean = D / S, log_S = valid ? log2(S) : (double)NAN, log_q = log_S + mean * (a.fix - 1.0);   // (d log2 sum 2^(f y) / df = sum q y)
     if (lane == 0) {
         if (a.logprob) {
             const int t = as_global(a.tokens)[row];
             float lp = valid ? -INFINITY : NAN;
-            if (valid && t >= 0 && t < a.V) lp = (float)((((double)logit_at(a.type, row_at(a.logits, a.type, (size_t)row * a.stride), t) * c - (double)r) * a.fix - log_S) * LN2);
+            if (valid && t >= 0 && t < a.V) lp = (float)((((double)logit_at(a.type, row_at(a.logits, a.type, (size_t)row * a.stride), t) * c - (double)r) * a.fix - log_q) * LN2);
             as_global_mut(a.logprob)[row] = lp;
         }
-        if (a.entropy) as_global_mut(a.entropy)[row] = (float)fmax((log_S - D / S) * LN2, valid ? 0.0 : (double)NAN);
+        if (a.entropy) as_global_mut(a.entropy)[row] = (float)fmax((log_S - mean) * LN2, valid ? 0.0 : (double)NAN);
     }
     if (a.top == 0) return;
     if (!valid) n = 0;
@@ -148,7 +149,7 @@ __device__ __forceinline__ void write_row(const ScoreDev &a, int row, int lane, 
     if (lane < a.top) {
         const size_t at = (size_t)row * a.top + (lane < n ? rank : lane);
         as_global_mut(a.top_ids)[at] = mine.token;
-        as_global_mut(a.top_logprobs)[at] = lane < n ? (float)((((double)of_key(mine.key) * c - (double)r) * a.fix - log_S) * LN2) : valid ? -INFINITY : NAN;
+        as_global_mut(a.top_logprobs)[at] = lane < n ? (float)((((double)of_key(mine.key) * c - (double)r) * a.fix - log_q) * LN2) : valid ? -INFINITY : NAN;
     }
 }
 

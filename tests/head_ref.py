@@ -81,7 +81,7 @@ def distill(z, ids, logprobs, T, rest, weight=None, half=U, subnormal=0.0):
                     if np.isfinite(at).any():
                         log_rho = (at.max() - m) / T + np.log(np.exp((at - at.max()) / T).sum()) - np.log(e.sum())
                     loss[r] += pi * (np.log(pi) - log_rho)
-                    others = pi * np.exp(log_q - log_rho) if np.isfinite(log_rho) else others
+                    others = pi * np.exp(np.where(named, -np.inf, log_q - log_rho)) if np.isfinite(log_rho) else others
                 g[~named] = (q - others)[~named]
                 parts = np.where(named, q + p, q + others)
             else:
@@ -90,7 +90,23 @@ def distill(z, ids, logprobs, T, rest, weight=None, half=U, subnormal=0.0):
                 g = q - p / share if share > 0 else np.zeros(V)
                 parts = q + p / share if share > 0 else np.zeros(V)
         a = np.where(np.isfinite(x), np.abs(x - m) / T * 1.4427, 0.0)
-        loss_tol[r] = 2 * SUM * max(share, 1.0) + U * abs(loss[r]) if np.isfinite(loss[r]) else 0
+        # log2(e) / T in fp32 is off by U of it: the loss of a temperature that is, by U times d loss / d log T = sum p y - sum q y (the unnamed tokens' share pi spread as q is)
+        y = np.where(q > 0, (x - m) / T, 0.0)
+        at_p = 0.0
+        if entries and np.isfinite(loss[r]):
+            at_p = sum(np.exp(l) * (x[i] - m) / T for i, l in entries if np.isfinite(x[i])) / (1.0 if rest else max(share, 1e-300))
+            if rest and pi > 0 and not named.all():
+                weight_of = np.exp((at - at.max()) / T)
+                at_p += pi * (weight_of * np.where(weight_of > 0, (x - m) / T, 0.0)).sum() / weight_of.sum()
+        # An unnamed token's exponential is off by a factor 1 + e_i, |e_i| <= (2 + 2.1 |a| + 138) U: a its exponent from the largest unnamed one, the thread's sum in the rest.  It
+        # is in S, of which the loss has P log S (P: all of p), and in rho, of which it has - pi log rho: sum q_i (P - pi / rho) e_i, and squares.  All else is in 64 bits.
+        P, moved = (share + max(1 - share, 0.0) if rest else 1.0), 0.0
+        if entries and not named.all() and np.isfinite(x[~named]).any():
+            u = x[~named]
+            a_u = np.where(np.isfinite(u), (u.max() - u) / T * 1.4427, 0.0)
+            w_u = np.where(np.isfinite(u), np.exp((u - u.max()) / T), 0.0)
+            moved = (np.abs(P * q[~named] - (P - share if rest else 0.0) * w_u / w_u.sum()) * (140 + 2.1 * a_u)).sum() * U
+        loss_tol[r] = moved + P * SUM ** 2 + U * abs(loss[r]) + U * abs(at_p - P * (q * y).sum()) if np.isfinite(loss[r]) else 0
         grad[r] = g * w / T
         # a factor of the row that is off as two sums are, and the element's own exponential
         grad_tol[r] = np.abs(w / T) * parts * (2 * SUM + (6 + 2.1 * a) * U) + half * np.abs(grad[r]) + subnormal + 1e-37

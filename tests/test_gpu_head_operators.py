@@ -242,6 +242,21 @@ def test_log_probabilities_of_far_tokens(T):
     check_distill(far, "fp32", np.full((rows, 1), 4, np.int32), np.full((rows, 1), np.log(0.5), np.float32), T, True, "fp32")
 
 
+@pytest.mark.parametrize("T", [2.5, 0.7, 2.0])
+@pytest.mark.parametrize("rows,V", [(64, 1024), (5, 32000), (300, 9000), (3, 140001)])
+def test_small_divergences_keep_their_digits(rows, V, T):
+    """A teacher that is nearly the student: what the sums are off by cancels, and the loss is off by 2^-24 of it and of what the teacher differs by."""
+    rng = np.random.default_rng(rows + V)
+    z = logits(rng, rows, V, "fp32")
+    other = z + 1e-3 * rng.standard_normal(z.shape)
+    t = float(np.float32(T))
+    ids = np.argsort(-z, 1)[:, :32].astype(np.int32)
+    lse = other.max(1, keepdims=True) / t + np.log(np.exp((other - other.max(1, keepdims=True)) / t).sum(1, keepdims=True))
+    lp = (np.take_along_axis(other, ids, 1) / t - lse).astype(np.float32)
+    check_distill(z, "fp32", ids, lp, T, True, "fp32", want_grad=False)
+    check_distill(z, "fp32", ids, lp, T, False, "fp32")
+
+
 @pytest.mark.parametrize("rows,V,kind", [(2, 140001, "bf16"), (2, 70001, "fp32"), (260, 140001, "bf16")])
 def test_distill_in_place_in_parts(rows, V, kind):
     """Rows too long for a workgroup: the second launch reads logits where the first parts of the same row hold gradients already."""
