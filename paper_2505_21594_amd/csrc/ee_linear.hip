@@ -590,7 +590,7 @@ extern "C" int ee_linear(const ee_linear_args *p, void *workspace, size_t worksp
     if (rc != EE_OK) return rc;
     if (p->n_rows == 0) return EE_OK;
     if (!p->x || !p->weight || !p->y) return fail(EE_EINVAL, "%s: null x, weight or y", call);
-    if (p->y == p->x || p->y == p->weight || p->pre == p->x || p->pre == p->y) return fail(EE_EINVAL, "%s: y and pre must be arrays of their own", call);
+    if (p->y == p->x || p->y == p->weight || (p->pre && (p->pre == p->x || p->pre == p->weight || p->pre == p->y || p->pre == p->residual))) return fail(EE_EINVAL, "%s: y and pre must be arrays of their own", call);
     if (p->residual == p->y && (p->residual_dtype != p->out_dtype || (p->n_rows > 1 && p->residual_stride != p->y_stride)))
         return fail(EE_EINVAL, "%s: y may be residual only with the same type and stride", call);
     if (!aligned(p->bias, 4)) return fail(EE_EINVAL, "%s: fp32 arrays must be 4-byte aligned", call);

@@ -91,7 +91,7 @@ LINEAR = [(dict(device=-1), "device"), (dict(dtype=ee.FP32), "bf16 or fp16"), (d
 
 
 @pytest.mark.parametrize("kw,word", LINEAR + [(dict(out_dtype=4), "type"), (dict(residual_dtype=4), "type"), (dict(x=0), "null"), (dict(weight=0), "null"), (dict(y=0), "null"), (dict(y_stride=34), "alignment"),
-                                              (dict(residual_stride=28), "smaller"), (dict(y=P), "their own"), (dict(pre=Q), "their own"), (dict(residual=Q, residual_stride=36), "residual"), (dict(bias=P + 2), "4-byte")])
+                                              (dict(residual_stride=28), "smaller"), (dict(y=P), "their own"), (dict(pre=Q), "their own"), (dict(pre=3 * P), "their own"), (dict(pre=4 * P), "their own"), (dict(residual=Q, residual_stride=36), "residual"), (dict(bias=P + 2), "4-byte")])
 def test_linear_is_checked(kw, word):
     refused(ee.load_library().ee_linear(ctypes.byref(linear_args(**kw)), P, 1 << 30, None), word)
 
