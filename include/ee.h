@@ -513,8 +513,8 @@ int ee_accept_drafts(const ee_accept_args *args, void *workspace, size_t workspa
      top_ids, top_logprobs [n_rows][top]  the `top` (0 .. EE_MAX_TOP) largest logits, largest first, of equal ones the lower token, and their log p.
    Tokens whose logit is -infinity (masked ones) have no part in a row; where fewer than `top` are left the list ends with -1 and -infinity.  A row
    without a softmax (NaN, +infinity or nothing but -infinity among its logits) gets NaN, and -1 for its tokens.
-   logits [n_rows][vocab] of type `dtype` at any alignment of the type, sums in fp32 for each thread and 64 bits from there; results fp32, int32.  n_rows up to 2^20, vocab
-   up to 2^24 (EE_EINVAL where rows times parts of rows pass 2^22).  A row whose largest |logit| / temperature is above 2^126 may get NaN.
+   logits [n_rows][vocab] of type `dtype` at any alignment of the type, sums in fp32 for each thread and 64 bits from there; results fp32, int32; a finite logit
+   counts however large it is (rows masked with the type's lowest value, all of one too).  n_rows up to 2^20, vocab up to 2^24 (EE_EINVAL where rows times parts of rows pass 2^22).
    workspace: ee_score_workspace bytes (may be 0), 256-byte aligned; contents do not matter. */
 typedef struct {
     int32_t device, dtype, n_rows, vocab, top;

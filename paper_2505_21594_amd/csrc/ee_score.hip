@@ -20,8 +20,8 @@ constexpr int SC_CAND = 1024;          // candidates
 
 struct ScorePart {
     double sum, dot;                   // sum 2^(z c - r),  sum (z c - r) 2^(z c - r)
-    float r;
-    int count;                         // candidates that it has
+    double r;
+    int count, unused;                 // candidates that it has
 };
 // A token in the order of the results: the larger key first, of equal ones the lower token.
 struct Cand {
@@ -123,7 +123,7 @@ __device__ __forceinline__ int wave_best_of(const Cand *cands, int n, int k, int
 }
 
 // What one wave writes for a row: its n (at most 64) best in order, and the row's numbers.
-__device__ __forceinline__ void write_row(const ScoreDev &a, int row, int lane, double S, double D, float r, const Cand *list, int n)
+__device__ __forceinline__ void write_row(const ScoreDev &a, int row, int lane, double S, double D, double r, const Cand *list, int n)
 {
     constexpr double LN2 = 0.6931471805599453;
     const bool valid = S > 0.0 && S < INFINITY;               // (NaN, +infinity or nothing but -infinity: no softmax)
@@ -132,7 +132,7 @@ __device__ __forceinline__ void write_row(const ScoreDev &a, int row, int lane, 
         if (a.logprob) {
             const int t = as_global(a.tokens)[row];
             float lp = valid ? -INFINITY : NAN;
-            if (valid && t >= 0 && t < a.V) lp = (float)((((double)logit_at(a.type, row_at(a.logits, a.type, (size_t)row * a.stride), t) * c - (double)r) * a.fix - log_q) * LN2);
+            if (valid && t >= 0 && t < a.V) lp = (float)((((double)logit_at(a.type, row_at(a.logits, a.type, (size_t)row * a.stride), t) * c - r) * a.fix - log_q) * LN2);
             as_global_mut(a.logprob)[row] = lp;
         }
         if (a.entropy) as_global_mut(a.entropy)[row] = (float)fmax((log_S - mean) * LN2, valid ? 0.0 : (double)NAN);
@@ -149,11 +149,11 @@ __device__ __forceinline__ void write_row(const ScoreDev &a, int row, int lane, 
     if (lane < a.top) {
         const size_t at = (size_t)row * a.top + (lane < n ? rank : lane);
         as_global_mut(a.top_ids)[at] = mine.token;
-        as_global_mut(a.top_logprobs)[at] = lane < n ? (float)((((double)of_key(mine.key) * c - (double)r) * a.fix - log_q) * LN2) : valid ? -INFINITY : NAN;
+        as_global_mut(a.top_logprobs)[at] = lane < n ? (float)((((double)of_key(mine.key) * c - r) * a.fix - log_q) * LN2) : valid ? -INFINITY : NAN;
     }
 }
 
-// The waves' sums from their threads' (relative to the r of each, -infinity where it has no finite logit), relative to the part's r, which comes back.
+// The waves' sums from their threads' (relative to the r of each; nothing where that is below -BELOW), relative to the part's r, which comes back.
 template <int WAVES>
 __device__ __forceinline__ float wave_sums(float r, float s, float d, int lane, int wave, float *wr, double *ws, double *wd)
 {
@@ -163,7 +163,7 @@ __device__ __forceinline__ float wave_sums(float r, float s, float d, int lane, 
     float all = wr[0];
 #pragma unroll
     for (int w = 1; w < WAVES; ++w) all = fmaxf(all, wr[w]);
-    const float down = r == -INFINITY ? 0.f : r - all;        // (a thread without a finite maximum has sums of 0, or of NaN)
+    const float down = r < -BELOW ? 0.f : r - all;            // (such a thread has sums of 0, or of NaN)
     const float scale = __builtin_amdgcn_exp2f(down);
     const double S1 = (double)(s * scale), D1 = (double)(d * scale) + (s != 0.f ? (double)down * S1 : 0.0);
     const double S2 = wave_sum_d(S1), D2 = wave_sum_d(D1);
@@ -202,8 +202,7 @@ __global__ void __launch_bounds__(NT, NT == 512 ? 6 : 4) ee_score_kernel(ScoreDe
         for (int i = 1; i < N; ++i) cm[c] = larger(cm[c], x[i]);
         m = larger(m, cm[c]);
     }
-    float r = m * a.c;
-    const float ref = m == -INFINITY ? 0.f : r;
+    const float r = m * a.c, ref = reference_of(r);
     float s = 0.f, d = 0.f;
     z.again(m);
 #pragma unroll
@@ -231,7 +230,7 @@ __global__ void __launch_bounds__(NT, NT == 512 ? 6 : 4) ee_score_kernel(ScoreDe
         const unsigned t = wave < holding ? wave_bound(u, (k + holding - 1) / holding, 32, 16) : ~0u;
         if (lane == 0) bound[wave] = t;
     }
-    r = wave_sums<WAVES>(r, s, d, lane, wave, wr, ws, wd);
+    const float part_r = wave_sums<WAVES>(r, s, d, lane, wave, wr, ws, wd);
     __syncthreads();
     int count = 0;
     if (k > 0) {
@@ -317,6 +316,49 @@ __global__ void __launch_bounds__(NT, NT == 512 ? 6 : 4) ee_score_kernel(ScoreDe
             __syncthreads();
         }
     }
+    double R = (double)part_r;
+    if (fabsf(part_r) > FAR) {
+        // (by reading the part again, as above: few rows do)
+        const void *part_at = row_at(a.logits, TYPE, (size_t)row * a.stride + first);
+        float most = -INFINITY;
+#pragma unroll 1
+        for (int at = 0; at < len; at += Part::ROOM / E) {
+            RowPart<TYPE, 1, NT> some;
+            some.load(row_at(part_at, TYPE, at), len - at, tid);
+            float x[N];
+            some.chunk(0, x);
+#pragma unroll
+            for (int i = 0; i < N; ++i) most = fmaxf(most, x[i]);
+        }
+        most = wave_max_f(most);
+        if (lane == 0) wr[wave] = most;                      // (everybody has read it: two barriers since)
+        __syncthreads();
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) most = fmaxf(most, wr[w]);
+        if (fabsf(most) != INFINITY) {                       // (otherwise the sums are 0 or NaN, as they have to be)
+            float s = 0.f, d = 0.f;
+#pragma unroll 1
+            for (int at = 0; at < len; at += Part::ROOM / E) {
+                RowPart<TYPE, 1, NT> some;
+                some.load(row_at(part_at, TYPE, at), len - at, tid);
+                float x[N];
+                some.chunk(0, x);
+#pragma unroll
+                for (int i = 0; i < N; ++i) {
+                    const float y = (x[i] - most) * a.c, e = __builtin_amdgcn_exp2f(y);
+                    s += e;
+                    d += fmaxf(y, -3e38f) * e;
+                }
+            }
+            const double S = wave_sum_d((double)s), D = wave_sum_d((double)d);
+            if (lane == 0) {
+                ws[wave] = S;
+                wd[wave] = D;
+            }
+            R = (double)most * (double)a.c;
+            __syncthreads();
+        }
+    }
     if (wave != 0) return;
     wave_lds_order();
     double S = ws[0], D = wd[0];
@@ -325,7 +367,7 @@ __global__ void __launch_bounds__(NT, NT == 512 ? 6 : 4) ee_score_kernel(ScoreDe
         D += wd[w];
     }
     if (a.parts == 1) {
-        write_row(a, row, lane, S, D, r, best, count);
+        write_row(a, row, lane, S, D, R, best, count);
         return;
     }
     const size_t at = (size_t)row * a.parts + part;
@@ -333,8 +375,9 @@ __global__ void __launch_bounds__(NT, NT == 512 ? 6 : 4) ee_score_kernel(ScoreDe
         ScorePart p;
         p.sum = S;
         p.dot = D;
-        p.r = r;
+        p.r = R;
         p.count = count;
+        p.unused = 0;
         a.part[at] = p;
     }
     if (lane < count) a.cand[at * a.top + lane] = best[lane];
@@ -392,13 +435,13 @@ __global__ void __launch_bounds__(SC_THREADS) ee_score_join_kernel(ScoreDev a)
         n = wave_best(u, token, a.top, idle_bits(a.type), best);
         wave_lds_order();
     }
-    float r = -INFINITY;
-    for (int p = lane; p < a.parts; p += 64) r = fmaxf(r, parts[p].r);
-    r = wave_max_f(r);
+    double r = -INFINITY;
+    for (int p = lane; p < a.parts; p += 64) r = fmax(r, parts[p].r);
+    r = wave_max_d(r);
     double S = 0.0, D = 0.0;
     for (int p = lane; p < a.parts; p += 64) {
         const ScorePart x = parts[p];
-        const double down = x.r == -INFINITY ? 0.0 : (double)x.r - (double)r, e = exp2(down);
+        const double down = x.r == -INFINITY ? 0.0 : x.r - r, e = exp2(down);
         S += x.sum * e;
         if (x.sum != 0.0) D += (x.dot + down * x.sum) * e;
     }

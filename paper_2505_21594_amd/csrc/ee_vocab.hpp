@@ -171,6 +171,17 @@ struct RowPart {
 // The larger one; NaN where one is (what fmaxf does for NaN costs an instruction more for every value that comes from memory).
 __device__ __forceinline__ float larger(float a, float b) { return __builtin_elementwise_maximum(a, b); }
 
+// Exponents z c (c = log2(e) / T) of fp32.  Up to BELOW a thread takes its exponentials relative to its own largest, r = z c rounded: what the rounding leaves is 2^6 at most, which
+// an exponential holds.  A thread whose largest is below -BELOW (masked tokens: z of the type's lowest value, z c past fp32) takes them relative to 0, and has nothing.  That is
+// wrong only where the whole part's largest is that low, or above FAR: there the sums are taken again, relative to the largest logit itself, by 2^((z - m) c).
+constexpr float BELOW = 0x1p30f, FAR = 0x1p29f;
+__device__ __forceinline__ float reference_of(float r) { return r < -BELOW ? 0.f : r; }      // (NaN stays)
+__device__ __forceinline__ double wave_max_d(double x)
+{
+    for (int o = 32; o > 0; o >>= 1) x = fmax(x, __shfl_xor(x, o, 64));
+    return x;
+}
+
 // One element of a row.
 __device__ __forceinline__ float logit_at(int type, const void *row, size_t i)
 {
