@@ -17,7 +17,7 @@ namespace ee {
 
 struct DistillPart {
     double sum;                        // sum 2^(z c - r) over the tokens that the list does not name
-    float r, unused;                   // the largest z c of them
+    double r;                          // the largest z c of them: rounded to fp32, or as it is where that is beyond FAR
 };
 
 struct DistillDev {
@@ -98,16 +98,15 @@ struct RowTerms {
     float others;                      // gradient of a token that the list does not name: others * 2^(z c - r)
     float mine;                        // gradient of the lane's token
 };
-__device__ __forceinline__ RowTerms row_terms(const DistillDev &a, const Entry &e, const ListTerms &t, float r_rest, double s_rest, float d_loss)
+__device__ __forceinline__ RowTerms row_terms(const DistillDev &a, const Entry &e, const ListTerms &t, double r_rest, double s_rest, float d_loss)
 {
     constexpr double LN2 = 0.6931471805599453;
     RowTerms r;
     const bool in = e.id >= 0;
     const double c = (double)a.c, p = t.p, share = t.share;
-    const float largest = fmaxf(r_rest, wave_max_f(in ? e.z * a.c : -INFINITY));
-    const double R = largest == -INFINITY ? 0.0 : (double)largest;
+    const double largest = fmax(r_rest, (double)wave_max_f(in ? e.z : -INFINITY) * c), R = largest == -INFINITY ? 0.0 : largest;
     const double z = (double)e.z * c - R, q1 = in ? exp2(z) : 0.0;
-    const double down = r_rest == -INFINITY ? 0.0 : (double)r_rest - R, scale_rest = r_rest == -INFINITY ? 0.0 : exp2(down);
+    const double down = r_rest == -INFINITY ? 0.0 : r_rest - R, scale_rest = r_rest == -INFINITY ? 0.0 : exp2(down);
     const double S = wave_sum_d(t.first ? q1 : 0.0) + (s_rest != 0.0 ? s_rest * scale_rest : 0.0);
     const bool valid = S > 0.0 && S < INFINITY;
     const double log_S = log2(S), A = scale_rest / S;
@@ -136,16 +135,16 @@ __device__ __forceinline__ RowTerms row_terms(const DistillDev &a, const Entry &
 }
 
 // The others' largest exponent and sum from the parts of a row; one wave calls it.
-__device__ __forceinline__ double join_parts(const DistillDev &a, int row, int lane, float &r)
+__device__ __forceinline__ double join_parts(const DistillDev &a, int row, int lane, double &r)
 {
     const DistillPart *parts = a.part + (size_t)row * a.parts;
     r = -INFINITY;
-    for (int p = lane; p < a.parts; p += 64) r = fmaxf(r, parts[p].r);
-    r = wave_max_f(r);
+    for (int p = lane; p < a.parts; p += 64) r = fmax(r, parts[p].r);
+    r = wave_max_d(r);
     double S = 0.0;
     for (int p = lane; p < a.parts; p += 64) {
         const DistillPart x = parts[p];
-        if (x.sum != 0.0) S += x.sum * (x.r == -INFINITY ? 1.0 : exp2((double)x.r - (double)r));
+        if (x.sum != 0.0) S += x.sum * (x.r == -INFINITY ? 1.0 : exp2(x.r - r));
     }
     return wave_sum_d(S);
 }
@@ -160,7 +159,8 @@ __global__ void __launch_bounds__(NT, NT == 512 ? 6 : 4) ee_distill_kernel(Disti
     __shared__ uint32_t named[MODE == GRAD ? 1 : NT * E / 4];       // a byte for each chunk, a bit for each of its elements
     __shared__ float wr[WAVES];
     __shared__ double ws[WAVES];
-    __shared__ float others_s, r_s;
+    __shared__ float others_s, ref_s;
+    __shared__ int far_s;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int row = a.parts == 1 ? blockIdx.x : blockIdx.x / a.parts, part = a.parts == 1 ? 0 : blockIdx.x - row * a.parts;
     const int first = part * a.length, len = min(a.length, a.V - first);
@@ -176,7 +176,7 @@ __global__ void __launch_bounds__(NT, NT == 512 ? 6 : 4) ee_distill_kernel(Disti
     }
     const int at = e.id - first;
     const bool here = e.id >= 0 && at >= 0 && at < len;
-    float r_rest = 0.f;
+    double r_rest = 0.0;
     if constexpr (MODE != GRAD) {
 #pragma unroll
         for (int i = 0; i < E / 4; ++i) named[i * NT + tid] = 0;
@@ -198,7 +198,7 @@ __global__ void __launch_bounds__(NT, NT == 512 ? 6 : 4) ee_distill_kernel(Disti
 #pragma unroll
             for (int i = 0; i < N; ++i) m = larger(m, x[i]);
         }
-        const float r = m * a.c, ref = m == -INFINITY ? 0.f : r;
+        const float r = m * a.c, ref = reference_of(r);
         float s = 0.f;
         z.again(m);
 #pragma unroll
@@ -211,19 +211,56 @@ __global__ void __launch_bounds__(NT, NT == 512 ? 6 : 4) ee_distill_kernel(Disti
         const float wave_r = wave_max_f(r);
         if (lane == 0) wr[wave] = wave_r;
         __syncthreads();
-        r_rest = wr[0];
+        float part_r = wr[0];
 #pragma unroll
-        for (int w = 1; w < WAVES; ++w) r_rest = fmaxf(r_rest, wr[w]);
-        const double S1 = wave_sum_d((double)(s * __builtin_amdgcn_exp2f(m == -INFINITY ? 0.f : r - r_rest)));
+        for (int w = 1; w < WAVES; ++w) part_r = fmaxf(part_r, wr[w]);
+        const double S1 = wave_sum_d((double)(s * __builtin_amdgcn_exp2f(r < -BELOW ? 0.f : r - part_r)));
         if (lane == 0) ws[wave] = S1;
         __syncthreads();
+        r_rest = (double)part_r;
+        if (fabsf(part_r) > FAR) {
+            // (by reading the part again: few rows do, and registers that live through this cost every row of a call)
+            const auto chunk_of = [&](int c, float (&x)[N]) __attribute__((always_inline)) {
+                RowPart<TYPE, 1, NT> some;
+                const int at = c * NT * N;
+                some.load(row_at(logits, TYPE, first + at), len - at, tid);
+                some.drop(0, named[tid * (E / 4) + c / 4] >> (c % 4 * 8) & 255u);
+                some.chunk(0, x);
+            };
+            float most = -INFINITY;
+#pragma unroll 1
+            for (int c = 0; c * NT * N < len; ++c) {
+                float x[N];
+                chunk_of(c, x);
+#pragma unroll
+                for (int i = 0; i < N; ++i) most = fmaxf(most, x[i]);
+            }
+            most = wave_max_f(most);
+            if (lane == 0) wr[wave] = most;
+            __syncthreads();
+#pragma unroll
+            for (int w = 0; w < WAVES; ++w) most = fmaxf(most, wr[w]);
+            if (fabsf(most) != INFINITY) {                   // (otherwise the sums are 0 or NaN, as they have to be)
+                float s = 0.f;
+#pragma unroll 1
+                for (int c = 0; c * NT * N < len; ++c) {
+                    float x[N];
+                    chunk_of(c, x);
+#pragma unroll
+                    for (int i = 0; i < N; ++i) s += __builtin_amdgcn_exp2f((x[i] - most) * a.c);
+                }
+                const double S2 = wave_sum_d((double)s);
+                if (lane == 0) ws[wave] = S2;
+                r_rest = (double)most * (double)a.c;
+                __syncthreads();
+            }
+        }
         if constexpr (MODE == STATS) {
             if (tid == 0) {
                 DistillPart p;
                 p.sum = ws[0];
                 for (int w = 1; w < WAVES; ++w) p.sum += ws[w];
                 p.r = r_rest;
-                p.unused = 0.f;
                 a.part[(size_t)row * a.parts + part] = p;
             }
             return;
@@ -244,8 +281,10 @@ __global__ void __launch_bounds__(NT, NT == 512 ? 6 : 4) ee_distill_kernel(Disti
         }
         const RowTerms r = row_terms(a, e, list, r_rest, S, weight);
         if (lane == 0) {
+            const bool far = fabs(r_rest) > (double)FAR && fabs(r_rest) < (double)INFINITY;
             others_s = r.others;
-            r_s = r_rest;
+            far_s = far;
+            ref_s = far ? (float)(r_rest / (double)a.c) : r_rest == -INFINITY ? 0.f : (float)r_rest;     // (far: the logit itself, whose product r is, in 48 bits)
             if (a.loss && part == 0) as_global_mut(a.loss)[row] = (float)r.loss;
         }
         mine = nothing ? 0.f : r.mine;
@@ -253,12 +292,15 @@ __global__ void __launch_bounds__(NT, NT == 512 ? 6 : 4) ee_distill_kernel(Disti
     }
     if (!a.d_logits) return;
     __syncthreads();
-    const float others = others_s, ref = r_s == -INFINITY ? 0.f : r_s;
+    const float others = others_s, ref = ref_s;
+    const bool far = __builtin_amdgcn_readfirstlane(far_s);
     const size_t out = (size_t)row * a.grad_stride + first;
     auto gradient = [&](const u32x4_t &raw, float (&x)[N]) __attribute__((always_inline)) {
         Part::values(raw, x);
 #pragma unroll
-        for (int i = 0; i < N; ++i) x[i] = __builtin_amdgcn_exp2f(fmaf(x[i], a.c, -ref)) * others;
+        for (int i = 0; i < N; ++i) x[i] = far ? (x[i] - ref) * a.c : fmaf(x[i], a.c, -ref);
+#pragma unroll
+        for (int i = 0; i < N; ++i) x[i] = __builtin_amdgcn_exp2f(x[i]) * others;
         if (nothing)
 #pragma unroll
             for (int i = 0; i < N; ++i) x[i] = 0.f;
@@ -292,7 +334,7 @@ __global__ void __launch_bounds__(256) ee_distill_loss_kernel(DistillDev a, int 
     if (row >= n_rows) return;
     Entry e = entry_of(a, row, lane);
     if (e.id >= 0) e.z = as_global(a.z)[(size_t)row * a.top + lane];
-    float r_rest;
+    double r_rest;
     const double S = join_parts(a, row, lane, r_rest);
     const RowTerms r = row_terms(a, e, list_terms(a, e), r_rest, S, 1.f);
     if (lane == 0) as_global_mut(a.loss)[row] = (float)r.loss;
