@@ -60,13 +60,13 @@ __device__ __forceinline__ double readlane_d(double x, int l)
     return join_d((unsigned)__builtin_amdgcn_readlane((int)(unsigned)b, l), (unsigned)__builtin_amdgcn_readlane((int)(unsigned)(b >> 32), l));
 }
 
-// What the list alone says; one wave calls it (while its row is on the way).
+// What the list alone says; one wave calls it (while its row is on the way).  The log-probability of a token that is named twice becomes that of both.
 struct ListTerms {
-    double p, both, share;             // the lane's probability, that of all entries that name its token, all entries' sum
+    double p, both, share;             // the lane's share of the loss (its probability; its token's where it is the first of several that name it, and 0 of the others), its token's, all entries'
     int distinct;                      // tokens that are named
     bool first;                        // the lane's token is named here for the first time
 };
-__device__ __forceinline__ ListTerms list_terms(const DistillDev &a, const Entry &e)
+__device__ __forceinline__ ListTerms list_terms(const DistillDev &a, Entry &e)
 {
     ListTerms t;
     const int lane = threadIdx.x & 63;
@@ -80,15 +80,19 @@ __device__ __forceinline__ ListTerms list_terms(const DistillDev &a, const Entry
         twice = twice || (same && i != lane);
     }
     t.both = t.p;
+    t.share = wave_sum_d(t.p);
     if (__ballot(twice && e.id >= 0)) {
         t.both = 0.0;
         for (int i = 0; i < a.top; ++i) {
             const double other = readlane_d(t.p, i);
             if (__builtin_amdgcn_readlane(e.id, i) == e.id) t.both += other;
         }
+        if (twice && e.id >= 0) {
+            e.lp = log(t.both);
+            t.p = t.first ? t.both : 0.0;
+        }
     }
     t.distinct = __popcll(__ballot(t.first));
-    t.share = wave_sum_d(t.p);
     return t;
 }
 
@@ -336,7 +340,8 @@ __global__ void __launch_bounds__(256) ee_distill_loss_kernel(DistillDev a, int 
     if (e.id >= 0) e.z = as_global(a.z)[(size_t)row * a.top + lane];
     double r_rest;
     const double S = join_parts(a, row, lane, r_rest);
-    const RowTerms r = row_terms(a, e, list_terms(a, e), r_rest, S, 1.f);
+    const ListTerms list = list_terms(a, e);
+    const RowTerms r = row_terms(a, e, list, r_rest, S, 1.f);
     if (lane == 0) as_global_mut(a.loss)[row] = (float)r.loss;
 }
 

@@ -62,7 +62,11 @@ def distill(z, ids, logprobs, T, rest, weight=None, half=U, subnormal=0.0):
             q = e / e.sum()
             log_q = (x - m) / T - np.log(e.sum())
             p = np.zeros(V)
-            entries = [(int(i), float(l)) for i, l in zip(ids[r], logprobs[r].astype(np.float64)) if 0 <= i < V and l != -np.inf]
+            merged = {}                                          # (a token that is named twice has the sum of both probabilities)
+            for i, l in zip(ids[r], logprobs[r].astype(np.float64)):
+                if 0 <= i < V and l != -np.inf:
+                    merged[int(i)] = np.logaddexp(merged.get(int(i), -np.inf), l)
+            entries = list(merged.items())
             for i, l in entries:
                 p[i] += np.exp(l)
             named = np.zeros(V, bool)
