@@ -60,7 +60,8 @@ __device__ __forceinline__ double readlane_d(double x, int l)
     return join_d((unsigned)__builtin_amdgcn_readlane((int)(unsigned)b, l), (unsigned)__builtin_amdgcn_readlane((int)(unsigned)(b >> 32), l));
 }
 
-// What the list alone says; one wave calls it (while its row is on the way).  The log-probability of a token that is named twice becomes that of both.
+// What the list alone says; one wave calls it (while its row is on the way).  The log-probability of a token that is named twice becomes that of both; with rest = 0 they become relative
+// to the largest, so that a list whose probabilities are all below the numbers of 64 bits has a sum.
 struct ListTerms {
     double p, both, share;             // the lane's share of the loss (its probability; its token's where it is the first of several that name it, and 0 of the others), its token's, all entries'
     int distinct;                      // tokens that are named
@@ -70,6 +71,10 @@ __device__ __forceinline__ ListTerms list_terms(const DistillDev &a, Entry &e)
 {
     ListTerms t;
     const int lane = threadIdx.x & 63;
+    if (!a.rest) {
+        const float most = wave_max_f(e.id >= 0 ? (float)e.lp : -INFINITY);
+        if (most != -INFINITY) e.lp -= (double)most;
+    }
     t.p = e.id >= 0 ? exp(e.lp) : 0.0;
     // a token that is named twice has both probabilities (few lists do that: the sums only where one does)
     t.first = e.id >= 0;

@@ -3,7 +3,7 @@ import numpy as np
 import pytest
 
 from tests import head_ref as ref
-from tests.test_gpu_head_operators import close, logits, run_distill
+from tests.test_gpu_head_operators import check_distill, close, logits, run_distill
 
 pytestmark = pytest.mark.gpu
 
@@ -51,3 +51,33 @@ def test_a_student_equal_to_a_teacher_of_split_tokens_has_no_loss():
         close(loss, (want, tol), "loss")
         if rest:
             assert (np.abs(want) < 1e-6).all() and (np.abs(loss) < 2e-6).all()
+
+
+@pytest.mark.parametrize("rows,V", SIZES)
+def test_lists_below_every_number_are_divided_by_their_sum(rows, V):
+    """rest = 0: log-probabilities from -700 to -3e4, whose exponentials are 0 in 64 bits, and above 0: only their differences count."""
+    rng = np.random.default_rng(rows + 2 * V)
+    z = logits(rng, rows, V, "fp32")
+    ids = np.argsort(-z, 1)[:, :6].astype(np.int32)
+    near = np.log(rng.uniform(0.05, 0.3, (rows, 6)))
+    lp = (near + rng.choice([-700.0, -746.0, -1000.0, -3e4, 900.0], (rows, 1))).astype(np.float32)
+    lp[::4, 3] = -np.inf
+    shifted = lp.astype(np.float64) - np.where(np.isfinite(lp), lp.astype(np.float64), -np.inf).max(1, keepdims=True)
+    want = ref.distill(z, ids, shifted, 1.0, False)
+    for kw in (dict(), dict(want_grad=False)):
+        loss, grad = run_distill(z, "fp32", ids, lp, 1.0, False, "fp32", **kw)
+        close(loss, want[0], "loss")
+        if grad is not None:
+            close(grad, want[1], "gradient")
+
+
+def test_a_label_with_any_log_probability_is_cross_entropy():
+    rng = np.random.default_rng(2)
+    z = logits(rng, 6, 900, "fp32")
+    label = rng.integers(0, 900, (6, 1)).astype(np.int32)
+    lp = np.array([0, -3, -740, -800, -1e5, -1e30], np.float32)[:, None]
+    loss, grad = run_distill(z, "fp32", label, lp, 1.0, False, "fp32")
+    want = ref.distill(z, label, np.zeros((6, 1)), 1.0, False)
+    close(loss, want[0], "loss")
+    close(grad, want[1], "gradient")
+    check_distill(z, "fp32", label, np.zeros((6, 1), np.float32), 1.0, False, "fp32")

@@ -1,0 +1,70 @@
+"""ee_linear and ee_linear_grad where values are small: fp16 gradients in two terms, the far side of GELU."""
+import math
+
+import numpy as np
+import pytest
+
+import paper_2505_21594_amd as ee
+from tests import head_ref as ref
+from tests.test_gpu_head_operators import Rows, Space, close, empty, matrix, up8
+
+pytestmark = pytest.mark.gpu
+
+U = ref.U
+
+
+@pytest.mark.parametrize("size", [1.0, 1e-2, 1e-3, 1e-4, 1e-5])
+@pytest.mark.parametrize("rows,n_in,n_out", [(5, 72, 40), (70, 130, 96), (300, 264, 520)])
+def test_small_gradients_of_fp16_layers_keep_their_digits(rows, n_in, n_out, size):
+    """dz in two terms, of which the second is a multiple of 2^-11 of its own: 2^-22 of dz, or 2^-36 (half the smallest fp16 times 2^-11) where that is more."""
+    rng = np.random.default_rng(rows)
+    x, w = matrix(rng, rows, n_in, "fp16"), matrix(rng, n_out, n_in, "fp16", 0.2)
+    dy, pre = matrix(rng, rows, n_out, "fp16", size), matrix(rng, rows, n_out, "fp16", 1.5)
+    for act in (ee.ACT_SILU, ee.ACT_GELU):
+        dx, dw = empty(rows, n_in, "fp32", up8(n_in)), empty(n_out, n_in, "fp32", up8(n_in))
+        ws = Space(ee.ee_linear_grad_workspace(x.view, w.view, act=act))
+        ee.ee_linear_grad(x.view, w.view, dy.view, pre=pre.view, act=act, dx=dx.view, d_weight=dw.view, workspace=ws.view)
+        ws.check()
+        want = ref.linear_grad(x.values(), w.values(), dy.values(), pre.values(), act, U, U, 2.0 ** -22, 2.0 ** -22)
+        small = 2.0 ** -36
+        close(dx.result(), (want[0][0], want[0][1] + small * np.abs(w.values()).sum(0)), f"dx, activation {act}")
+        close(dw.result(), (want[1][0], want[1][1] + small * np.abs(x.values()).sum(0)), f"d_weight, activation {act}")
+
+
+def test_large_gradients_of_fp16_layers_in_two_terms():
+    """Up to the largest fp16 both terms are numbers of the type."""
+    rng = np.random.default_rng(3)
+    x, w, pre = Rows(np.eye(16), "fp16"), Rows(np.eye(16), "fp16"), Rows(np.full((16, 16), 20.0), "fp16")
+    dyv = rng.uniform(3e4, 65504, (16, 16)) * rng.choice([-1, 1], (16, 16))
+    dy, dx = Rows(dyv, "fp16"), empty(16, 16, "fp32")
+    ws = Space(ee.ee_linear_grad_workspace(x.view, w.view, act=ee.ACT_SILU))
+    ee.ee_linear_grad(x.view, w.view, dy.view, pre=pre.view, act=ee.ACT_SILU, dx=dx.view, workspace=ws.view)
+    want = ref.linear_grad(x.values(), w.values(), dy.values(), pre.values(), 1, U, U, 2.0 ** -22, 2.0 ** -22)
+    close(dx.result(), want[0], "dx")
+
+
+def tail():
+    z = -np.concatenate([np.linspace(0.25, 12, 95), [3, 4, 5, 6, 8, 10, 11, 12, 2.5]])
+    z = Rows(z.reshape(13, 8), "bf16")
+    v = z.values()
+    Phi = np.vectorize(lambda t: 0.5 * math.erfc(-t * 0.5 ** 0.5))(v)
+    return z, v, Phi, np.exp(-v * v / 2) / math.sqrt(2 * math.pi)
+
+
+def test_gelu_of_far_negative_arguments_keeps_its_digits():
+    """z Phi(z), Phi as erfc.  erfc(a) is off by 16 U of it and by what a is (1.5 U of it: constant and product), of which the logarithm's derivative makes at most a^2 2 + 2 = z^2 + 2 times."""
+    x, z, Phi, _ = tail()
+    w, y = Rows(np.eye(8), "bf16"), empty(13, 8, "fp32")
+    ee.ee_linear(x.view, w.view, y.view, act=ee.ACT_GELU, pre=empty(13, 8, "bf16").view, workspace=Space(ee.ee_linear_workspace(x.view, w.view)).view)
+    close(y.result(), (z * Phi, np.abs(z * Phi) * (18 + 2 * (z * z + 2)) * U), "y")
+
+
+def test_slope_of_gelu_at_far_negative_arguments_keeps_its_digits():
+    """Phi(z) + z phi(z): each part off by its own (erfc as above; the exponential by 4 U and its argument's z^2 / 2 times 2 U), dz by 2^-24 in three terms."""
+    pre, z, Phi, phi = tail()
+    w, dy, dx = Rows(np.eye(8), "bf16"), Rows(np.ones((13, 8)), "bf16"), empty(13, 8, "fp32")
+    x = Rows(np.zeros((13, 8)), "bf16")
+    ws = Space(ee.ee_linear_grad_workspace(x.view, w.view, act=ee.ACT_GELU))
+    ee.ee_linear_grad(x.view, w.view, dy.view, pre=pre.view, act=ee.ACT_GELU, dx=dx.view, workspace=ws.view)
+    tol = (Phi * (18 + 2 * (z * z + 2)) + np.abs(z) * phi * (8 + z * z) + 4 * np.abs(Phi + z * phi)) * U
+    close(dx.result(), (Phi + z * phi, tol), "dx")
