@@ -593,8 +593,8 @@ int ee_norm_grad(const ee_norm_grad_args *args, void *workspace, size_t workspac
    needs where there is an activation, or NULL.  fp32 sums, one rounding of each result.  An exit's adapters are two such calls (the down matrices stacked, EE_ACT_SILU; the up
    matrices side by side, residual h).
    ee_linear_grad: dz = dy act'(pre);  dx = dz weight,  d_weight = dz^T x,  d_bias = sum over the rows of dz (fp32; written, not added to), each NULL where it is not wanted.  (The residual's
-   gradient is dy.)  dy and pre are of type dtype; dz is rounded to dtype where the result is of 16 bits, and is two (fp16) or three (bf16) terms of it where that is fp32 (past the
-   largest fp16 it is infinite).
+   gradient is dy.)  dy and pre are of type dtype; dz is rounded to dtype where the result is of 16 bits, and is two (fp16: off by 2^-22 of it, or by 2^-36 where that is more) or three
+   (bf16: 2^-24 of it) terms where that is fp32 (past the largest fp16 it is infinite).
    Every row starts at a multiple of 16 bytes.  Any sizes up to EE_LINEAR_MAX, odd ones too (EE_EINVAL where two of them make 2^23 tiles of 64 x 64).
    workspace: bytes by the _workspace calls (may be 0), 256-byte aligned; contents do not matter. */
 #define EE_ACT_NONE 0

@@ -13,7 +13,7 @@ typedef __attribute__((ext_vector_type(8))) _Float16 f16x8_t;
 // C[i][j] = sum_c A(i, c) B(j, c): an operand lies in memory with the sum's index contiguous ([i][c]) or with the result's ([c][i]).
 struct GemmDev {
     const uint16_t *A, *B;
-    long long lda, ldb, plane;         // plane: from one term of A to the next
+    long long lda, ldb, plane;         // plane: from one term of A to the next, the larger one (the sum of both is A; of fp16 the smaller one times 2^-11)
     int terms, I, J, K;
     const float *bias;                 // [J]
     const void *residual;
