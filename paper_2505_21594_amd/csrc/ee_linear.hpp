@@ -36,12 +36,15 @@ __device__ __forceinline__ f32x4_t mfma16(const u32x4_t &a, const u32x4_t &b, co
 }
 
 // fp32 activations and their derivatives: SiLU z / (1 + e^-z), GELU z Phi(z).  The exponential as 2^(z log2 e) and the reciprocal are the hardware's (1 ulp, and the
-// argument's rounding, |z| 2^-24 of e^-z): a few units in 2^-24 of z.
+// argument's rounding, |z| 2^-24 of e^-z): a few units in 2^-24 of z, of GELU's value too, its far side's relative to itself.
 __device__ __forceinline__ float logistic(float z) { return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(z * -1.44269504f)); }
+// Phi(z) as half of erfc(-z / sqrt 2): 1 + erf(z / sqrt 2) has next to nothing left of it below z = -4 (a twentieth off at -5, nothing at -6); it costs
+// 2 % (2041 x 4096 x 11008 with GELU, bf16, 210 -> 215 us).
+__device__ __forceinline__ float normal(float z) { return 0.5f * erfcf(z * -0.70710678f); }
 __device__ __forceinline__ float act_of(int act, float z)
 {
     if (act == EE_ACT_SILU) return z * logistic(z);
-    if (act == EE_ACT_GELU) return 0.5f * z * (1.f + erff(z * 0.70710678f));
+    if (act == EE_ACT_GELU) return z * normal(z);
     return z;
 }
 __device__ __forceinline__ float act_slope(int act, float z)
@@ -51,7 +54,7 @@ __device__ __forceinline__ float act_slope(int act, float z)
         const float s = logistic(z);
         return s * (1.f + z * (1.f - s));
     }
-    if (act == EE_ACT_GELU) return 0.5f * (1.f + erff(z * 0.70710678f)) + z * expf(-0.5f * z * z) * 0.39894228f;
+    if (act == EE_ACT_GELU) return normal(z) + z * expf(-0.5f * z * z) * 0.39894228f;
     return 1.f;
 }
 

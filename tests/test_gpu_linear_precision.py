@@ -1,4 +1,6 @@
 """ee_linear and ee_linear_grad where values are small."""
+import math
+
 import numpy as np
 import pytest
 
@@ -39,3 +41,30 @@ def test_large_gradients_of_fp16_layers_in_two_terms():
     ee.ee_linear_grad(x.view, w.view, dy.view, pre=pre.view, act=ee.ACT_SILU, dx=dx.view, workspace=ws.view)
     want = ref.linear_grad(x.values(), w.values(), dy.values(), pre.values(), 1, U, U, 2.0 ** -22, 2.0 ** -22)
     close(dx.result(), want[0], "dx")
+
+
+def tail():
+    z = -np.concatenate([np.linspace(0.25, 12, 95), [3, 4, 5, 6, 8, 10, 11, 12, 2.5]])
+    z = Rows(z.reshape(13, 8), "bf16")
+    v = z.values()
+    Phi = np.vectorize(lambda t: 0.5 * math.erfc(-t * 0.5 ** 0.5))(v)
+    return z, v, Phi, np.exp(-v * v / 2) / math.sqrt(2 * math.pi)
+
+
+def test_gelu_of_far_negative_arguments_keeps_its_digits():
+    """z Phi(z), Phi as erfc.  erfc(a) is off by 16 U of it and by what a is (1.5 U of it: constant and product), of which the logarithm's derivative makes at most a^2 2 + 2 = z^2 + 2 times."""
+    x, z, Phi, _ = tail()
+    w, y = Rows(np.eye(8), "bf16"), empty(13, 8, "fp32")
+    ee.ee_linear(x.view, w.view, y.view, act=ee.ACT_GELU, pre=empty(13, 8, "bf16").view, workspace=Space(ee.ee_linear_workspace(x.view, w.view)).view)
+    close(y.result(), (z * Phi, np.abs(z * Phi) * (18 + 2 * (z * z + 2)) * U), "y")
+
+
+def test_slope_of_gelu_at_far_negative_arguments_keeps_its_digits():
+    """Phi(z) + z phi(z): each part off by its own (erfc as above; the exponential by 4 U and its argument's z^2 / 2 times 2 U), dz by 2^-24 in three terms."""
+    pre, z, Phi, phi = tail()
+    w, dy, dx = Rows(np.eye(8), "bf16"), Rows(np.ones((13, 8)), "bf16"), empty(13, 8, "fp32")
+    x = Rows(np.zeros((13, 8)), "bf16")
+    ws = Space(ee.ee_linear_grad_workspace(x.view, w.view, act=ee.ACT_GELU))
+    ee.ee_linear_grad(x.view, w.view, dy.view, pre=pre.view, act=ee.ACT_GELU, dx=dx.view, workspace=ws.view)
+    tol = (Phi * (18 + 2 * (z * z + 2)) + np.abs(z) * phi * (8 + z * z) + 4 * np.abs(Phi + z * phi)) * U
+    close(dx.result(), (Phi + z * phi, tol), "dx")
