@@ -393,6 +393,10 @@ int ee_debug_mfma_layout(int device);
    divisors (host array, each >= 1, n <= 65536); *mismatches must come back 0. */
 int ee_debug_div_small(int device, const int32_t *divisors, int n, long long *mismatches);
 
+/* Host arithmetic, for tests: how a product of ee_linear (product 0) or ee_linear_grad (1: dx, 2: d_weight) of these sizes is taken: plan = rows and columns of a tile of results, parts of
+   the sum, length of a part. */
+int ee_debug_linear_plan(int32_t n_rows, int32_t n_in, int32_t n_out, int32_t product, int32_t plan[4]);
+
 /* ------------------------------------------------------------------ operators on device memory
    Steps of a decoder layer's attention and of a round's verification, for callers that run layers of their own around a
    paged cache.  They take DEVICE pointers (of GPU `device`, which need not be the current one) and enqueue kernels on

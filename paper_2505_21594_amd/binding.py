@@ -41,7 +41,7 @@ EXPORTS = [
     "ee_session_create", "ee_session_free", "ee_session_fork", "ee_prefill", "ee_prefill_embeds", "ee_verify",
     "ee_verify_batch", "ee_verify_static", "ee_verify_sampled", "ee_wait_exit", "ee_query_exit", "ee_wait_final", "ee_query_final",
     "ee_pass_time_ms", "ee_kv_truncate", "ee_set_pending", "ee_kv_len", "ee_pending",
-    "ee_verify_sampled_batch", "ee_debug_logits", "ee_debug_mfma_layout", "ee_debug_div_small", "ee_tune_k_split", "ee_device_synchronize", "ee_session_option",
+    "ee_verify_sampled_batch", "ee_debug_logits", "ee_debug_mfma_layout", "ee_debug_div_small", "ee_debug_linear_plan", "ee_tune_k_split", "ee_device_synchronize", "ee_session_option",
     "ee_launch_times", "ee_debug_copy", "ee_exit_pop", "ee_exit_order", "ee_latency_model",
     "ee_kv_append", "ee_attend", "ee_attend_workspace", "ee_accept_drafts", "ee_accept_workspace",
     "ee_score_tokens", "ee_score_workspace", "ee_distill", "ee_distill_workspace", "ee_norm", "ee_norm_grad", "ee_norm_grad_workspace",
@@ -194,6 +194,7 @@ def load_library():
     lib.ee_debug_mfma_layout.argtypes = [ci]
     lib.ee_tune_k_split.argtypes = [ctypes.c_uint, ci]
     lib.ee_debug_div_small.argtypes = [ci, ctypes.POINTER(ctypes.c_int32), ci, ctypes.POINTER(ctypes.c_longlong)]
+    lib.ee_debug_linear_plan.argtypes = [ctypes.c_int32] * 4 + [ctypes.POINTER(ctypes.c_int32)]
     lib.ee_device_synchronize.argtypes = [ci]
     lib.ee_session_option.argtypes = [vp, ci, ci]
     lib.ee_exit_pop.argtypes = [vp, ci, P(ci), P(ctypes.c_float)]
@@ -278,6 +279,13 @@ def ee_debug_div_small(divisors, device: int = 0) -> int:
     bad = ctypes.c_longlong(-1)
     _check(load_library().ee_debug_div_small(device, d.ctypes.data_as(ctypes.POINTER(ctypes.c_int32)), int(d.size), ctypes.byref(bad)))
     return int(bad.value)
+
+
+def ee_debug_linear_plan(n_rows: int, n_in: int, n_out: int, product: int = 0) -> tuple:
+    """(rows and columns of a tile, parts of the sum, length of a part) of a product of ee_linear (0), or of ee_linear_grad (1: dx, 2: d_weight)."""
+    plan = (ctypes.c_int32 * 4)()
+    _check(load_library().ee_debug_linear_plan(n_rows, n_in, n_out, product, plan))
+    return tuple(plan)
 
 
 @dataclass

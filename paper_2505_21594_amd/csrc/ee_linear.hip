@@ -581,6 +581,23 @@ static int check_linear_grad(const char *call, const ee_linear_grad_args *p)
 
 using namespace ee;
 
+extern "C" int ee_debug_linear_plan(int32_t n_rows, int32_t n_in, int32_t n_out, int32_t product, int32_t plan[4])
+{
+    static const char *const call = "ee_debug_linear_plan";
+    if (!plan) return fail(EE_EINVAL, "%s: null argument", call);
+    if (product < 0 || product > 2) return fail(EE_EINVAL, "%s: product %d not in [0,2]", call, product);
+    int rc = check_sizes(call, 0, EE_BF16, EE_ACT_NONE, n_rows, n_in, n_out);
+    if (rc != EE_OK) return rc;
+    const bool a_along = product != 2, b_along = product == 0;
+    const int I = product == 2 ? n_out : n_rows;
+    const GemmPlan16 pl = product == 0 ? plan_gemm16(I, n_out, n_in, true, true) : plan_gemm16(I, n_in, product == 1 ? n_out : n_rows, a_along, b_along);
+    plan[0] = pl.form == THIN ? (I > 16 ? 32 : 16) : pl.form == LARGE ? (a_along ? 192 : 256) : pl.form == MEDIUM ? 128 : 64;
+    plan[1] = pl.form == THIN ? 16 * pl.tn : pl.form == SMALL ? 64 : 128;
+    plan[2] = pl.splits;
+    plan[3] = pl.per;
+    return EE_OK;
+}
+
 extern "C" int ee_linear_workspace(const ee_linear_args *p, size_t *bytes)
 {
     static const char *const call = "ee_linear_workspace";
