@@ -167,9 +167,9 @@ __global__ void __launch_bounds__(NT, NT == 512 ? 6 : 4) ee_distill_kernel(Disti
     constexpr int N = Part::N, WAVES = NT / 64;
     __shared__ uint32_t named[MODE == GRAD ? 1 : NT * E / 4];       // a byte for each chunk, a bit for each of its elements
     __shared__ float wr[WAVES];
-    __shared__ double ws[WAVES];
-    __shared__ float others_s, ref_s;
-    __shared__ int far_s;
+    __shared__ double ws[WAVES], kept[MODE == WHOLE ? 4 : 1][64];
+    __shared__ float kept_z[64];
+    __shared__ float others_s, ref_s, taken_s;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int row = a.parts == 1 ? blockIdx.x : blockIdx.x / a.parts, part = a.parts == 1 ? 0 : blockIdx.x - row * a.parts;
     const int first = part * a.length, len = min(a.length, a.V - first);
@@ -186,6 +186,7 @@ __global__ void __launch_bounds__(NT, NT == 512 ? 6 : 4) ee_distill_kernel(Disti
     const int at = e.id - first;
     const bool here = e.id >= 0 && at >= 0 && at < len;
     double r_rest = 0.0;
+    float ref = 0.f;                                         // of the row's exponents, where the gradient is taken
     if constexpr (MODE != GRAD) {
 #pragma unroll
         for (int i = 0; i < E / 4; ++i) named[i * NT + tid] = 0;
@@ -194,76 +195,62 @@ __global__ void __launch_bounds__(NT, NT == 512 ? 6 : 4) ee_distill_kernel(Disti
             const int q = at / N, byte = (q % NT) * E + q / NT;
             atomicOr(&named[byte / 4], 1u << (byte % 4 * 8 + at % N));
         }
-        if (MODE == WHOLE && wave == 0) list = list_terms(a, e);
-        __syncthreads();
-        // (the named ones become -infinity, which no sum notices)
-        float m = -INFINITY;
-#pragma unroll
-        for (int c = 0; c < E; ++c) {
-            const uint32_t marks = named[tid * (E / 4) + c / 4] >> (c % 4 * 8) & 255u;
-            if (marks) z.drop(c, marks);
-            float x[N];
-            z.chunk(c, x);
-#pragma unroll
-            for (int i = 0; i < N; ++i) m = larger(m, x[i]);
+        if (MODE == WHOLE && wave == 0) {
+            // (in LDS between the walks over the row: in registers these cost every wave spills)
+            list = list_terms(a, e);
+            kept[0][lane] = e.lp;
+            kept[1][lane] = list.p;
+            kept[2][lane] = list.both;
+            kept[3][lane] = list.share;
+            kept_z[lane] = e.z;
         }
-        const float r = m * a.c, ref = reference_of(r);
-        float s = 0.f;
-        z.again(m);
-#pragma unroll
-        for (int c = 0; c < E; ++c) {
-            float x[N];
-            z.chunk(c, x);
-#pragma unroll
-            for (int i = 0; i < N; ++i) s += __builtin_amdgcn_exp2f(fmaf(x[i], a.c, -ref));
-        }
-        const float wave_r = wave_max_f(r);
-        if (lane == 0) wr[wave] = wave_r;
         __syncthreads();
-        float part_r = wr[0];
+        // (Twice only where the largest logit is beyond FAR: the second time all of them are less by it.)
+        float part_r, taken = 0.f;
+        for (int pass = 0;; ++pass) {
+            // (the named ones become -infinity, which no sum notices)
+            float m = -INFINITY;
 #pragma unroll
-        for (int w = 1; w < WAVES; ++w) part_r = fmaxf(part_r, wr[w]);
-        const double S1 = wave_sum_d((double)(s * __builtin_amdgcn_exp2f(r < -BELOW ? 0.f : r - part_r)));
-        if (lane == 0) ws[wave] = S1;
-        __syncthreads();
-        r_rest = (double)part_r;
-        if (fabsf(part_r) > FAR) {
-            // (by reading the part again: few rows do, and registers that live through this cost every row of a call)
-            const auto chunk_of = [&](int c, float (&x)[N]) __attribute__((always_inline)) {
-                RowPart<TYPE, 1, NT> some;
-                const int at = c * NT * N;
-                some.load(row_at(logits, TYPE, first + at), len - at, tid);
-                some.drop(0, named[tid * (E / 4) + c / 4] >> (c % 4 * 8) & 255u);
-                some.chunk(0, x);
-            };
-            float most = -INFINITY;
-#pragma unroll 1
-            for (int c = 0; c * NT * N < len; ++c) {
+            for (int c = 0; c < E; ++c) {
+                const uint32_t marks = named[tid * (E / 4) + c / 4] >> (c % 4 * 8) & 255u;
+                if (marks) z.drop(c, marks);
                 float x[N];
-                chunk_of(c, x);
+                z.chunk(c, x);
 #pragma unroll
-                for (int i = 0; i < N; ++i) most = fmaxf(most, x[i]);
+                for (int i = 0; i < N; ++i) m = larger(m, x[i]);
             }
-            most = wave_max_f(most);
+            const float r = m * a.c, ref = reference_of(r);
+            float s = 0.f;
+            z.again(m);
+#pragma unroll
+            for (int c = 0; c < E; ++c) {
+                float x[N];
+                z.chunk(c, x);
+#pragma unroll
+                for (int i = 0; i < N; ++i) s += __builtin_amdgcn_exp2f(fmaf(x[i], a.c, -ref));
+            }
+            const float wave_r = wave_max_f(r);
+            if (lane == 0) wr[wave] = wave_r;
+            __syncthreads();
+            part_r = wr[0];
+#pragma unroll
+            for (int w = 1; w < WAVES; ++w) part_r = fmaxf(part_r, wr[w]);
+            const double S1 = wave_sum_d((double)(s * __builtin_amdgcn_exp2f(r < -BELOW ? 0.f : r - part_r)));
+            if (lane == 0) ws[wave] = S1;
+            __syncthreads();
+            if (pass || !(fabsf(part_r) > FAR)) break;
+            float most = wave_max_f(m);
             if (lane == 0) wr[wave] = most;
             __syncthreads();
 #pragma unroll
             for (int w = 0; w < WAVES; ++w) most = fmaxf(most, wr[w]);
-            if (fabsf(most) != INFINITY) {                   // (otherwise the sums are 0 or NaN, as they have to be)
-                float s = 0.f;
-#pragma unroll 1
-                for (int c = 0; c * NT * N < len; ++c) {
-                    float x[N];
-                    chunk_of(c, x);
-#pragma unroll
-                    for (int i = 0; i < N; ++i) s += __builtin_amdgcn_exp2f((x[i] - most) * a.c);
-                }
-                const double S2 = wave_sum_d((double)s);
-                if (lane == 0) ws[wave] = S2;
-                r_rest = (double)most * (double)a.c;
-                __syncthreads();
-            }
+            if (fabsf(most) == INFINITY) break;              // (the sums are 0 or NaN, as they have to be)
+            __syncthreads();
+            taken = most;
+            z.less(taken);
         }
+        r_rest = (double)part_r + (double)taken * (double)a.c;
+        ref = part_r == -INFINITY ? 0.f : part_r;
         if constexpr (MODE == STATS) {
             if (tid == 0) {
                 DistillPart p;
@@ -287,13 +274,20 @@ __global__ void __launch_bounds__(NT, NT == 512 ? 6 : 4) ee_distill_kernel(Disti
         } else {
             S = ws[0];
             for (int w = 1; w < WAVES; ++w) S += ws[w];
+            e.lp = kept[0][lane];
+            list.p = kept[1][lane];
+            list.both = kept[2][lane];
+            list.share = kept[3][lane];
+            e.z = kept_z[lane];
         }
         const RowTerms r = row_terms(a, e, list, r_rest, S, weight);
         if (lane == 0) {
-            const bool far = fabs(r_rest) > (double)FAR && fabs(r_rest) < (double)INFINITY;
             others_s = r.others;
-            far_s = far;
-            ref_s = far ? (float)(r_rest / (double)a.c) : r_rest == -INFINITY ? 0.f : (float)r_rest;     // (far: the logit itself, whose product r is, in 48 bits)
+            if constexpr (MODE == GRAD) {
+                const bool far = fabs(r_rest) > (double)FAR && fabs(r_rest) < (double)INFINITY;
+                taken_s = far ? (float)(r_rest / (double)a.c) : 0.f;                     // (the logit whose product r is, all 48 bits of it)
+                ref_s = far || r_rest == -INFINITY ? 0.f : (float)r_rest;
+            }
             if (a.loss && part == 0) as_global_mut(a.loss)[row] = (float)r.loss;
         }
         mine = nothing ? 0.f : r.mine;
@@ -301,15 +295,17 @@ __global__ void __launch_bounds__(NT, NT == 512 ? 6 : 4) ee_distill_kernel(Disti
     }
     if (!a.d_logits) return;
     __syncthreads();
-    const float others = others_s, ref = ref_s;
-    const bool far = __builtin_amdgcn_readfirstlane(far_s);
+    const float others = others_s;
+    if constexpr (MODE == GRAD) {
+        const float taken = __int_as_float(__builtin_amdgcn_readfirstlane(__float_as_int(taken_s)));
+        ref = ref_s;
+        if (taken != 0.f) z.less(taken);
+    }
     const size_t out = (size_t)row * a.grad_stride + first;
     auto gradient = [&](const u32x4_t &raw, float (&x)[N]) __attribute__((always_inline)) {
         Part::values(raw, x);
 #pragma unroll
-        for (int i = 0; i < N; ++i) x[i] = far ? (x[i] - ref) * a.c : fmaf(x[i], a.c, -ref);
-#pragma unroll
-        for (int i = 0; i < N; ++i) x[i] = __builtin_amdgcn_exp2f(x[i]) * others;
+        for (int i = 0; i < N; ++i) x[i] = __builtin_amdgcn_exp2f(fmaf(x[i], a.c, -ref)) * others;
         if (nothing)
 #pragma unroll
             for (int i = 0; i < N; ++i) x[i] = 0.f;
@@ -325,8 +321,12 @@ __global__ void __launch_bounds__(NT, NT == 512 ? 6 : 4) ee_distill_kernel(Disti
     }
     const int last = len / N;                                // the chunk that the part's end is in
     if (len % N != 0 && tid == last % NT) {
+        u32x4_t end = z.raw[0];
+#pragma unroll
+        for (int c = 1; c < E; ++c)
+            if (c == last / NT) end = z.raw[c];
         float x[N];
-        gradient(z.end, x);
+        gradient(end, x);
 #pragma unroll
         for (int i = 0; i < N; ++i)
             if (last * N + i < len) store_one(a.grad_type, a.d_logits, out + last * N + i, x[i]);

@@ -79,7 +79,6 @@ struct RowPart {
     static constexpr int N = TYPE == EE_FP32 ? 4 : 8;      // elements of a chunk
     static constexpr int ROOM = E * NT * N;                // of a part at most
     u32x4_t raw[E];
-    u32x4_t end;                                           // the chunk that the part's end is in, of the thread that has it
 
     static __device__ __forceinline__ int offset(int c, int tid) { return (c * NT + tid) * N; }
     // the part of `n` elements at `p` (the same in every lane), which is aligned to the element type
@@ -100,7 +99,6 @@ struct RowPart {
         }
         // the chunk that the part's end is in
         const int last = n / N;
-        end = (u32x4_t){NOTHING, NOTHING, NOTHING, NOTHING};
         if (n % N != 0 && tid == last % NT) {
             uint32_t w[4] = {NOTHING, NOTHING, NOTHING, NOTHING};
             const EE_GLOBAL char *const q = base + (size_t)last * 16;
@@ -112,10 +110,9 @@ struct RowPart {
                     else
                         w[i / 2] = i % 2 ? (w[i / 2] & 0xFFFFu) | (uint32_t) * (const EE_GLOBAL uint16_t *)(q + i * 2) << 16 : (w[i / 2] & 0xFFFF0000u) | *(const EE_GLOBAL uint16_t *)(q + i * 2);
                 }
-            end = (u32x4_t){w[0], w[1], w[2], w[3]};
 #pragma unroll
             for (int c = 0; c < E; ++c)
-                if (c == last / NT) raw[c] = end;
+                if (c == last / NT) raw[c] = (u32x4_t){w[0], w[1], w[2], w[3]};
         }
     }
     static __device__ __forceinline__ void values(const u32x4_t &r, float (&x)[N])
@@ -153,6 +150,20 @@ struct RowPart {
             raw[c][i] = w;
         }
     }
+    // Every element becomes less by m, an element of the type itself: exactly where the two are within a factor of two of each other (their difference is a multiple of the smaller
+    // one's last place), and elsewhere rounded to the type.
+    __device__ __forceinline__ void less(float m)
+    {
+        again(m);
+#pragma unroll
+        for (int c = 0; c < E; ++c) {
+            float x[N];
+            chunk(c, x);
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                raw[c][i] = TYPE == EE_FP32 ? __float_as_uint(x[i] - m) : TYPE == EE_BF16 ? pack_bf16(x[N / 4 * i] - m, x[N / 4 * i + N / 4 - 1] - m) : pack_fp16(x[N / 4 * i] - m, x[N / 4 * i + N / 4 - 1] - m);
+        }
+    }
     // Between two walks over the part, the first of which gave `done` and `too`: the compiler takes the elements as others than before, and does not keep them all as floats
     // in the meantime (twice the registers).
     __device__ __forceinline__ void again(float done, float too = 0.f)
@@ -173,13 +184,25 @@ __device__ __forceinline__ float larger(float a, float b) { return __builtin_ele
 
 // Exponents z c (c = log2(e) / T) of fp32.  Up to BELOW a thread takes its exponentials relative to its own largest, r = z c rounded: what the rounding leaves is 2^6 at most, which
 // an exponential holds.  A thread whose largest is below -BELOW (masked tokens: z of the type's lowest value, z c past fp32) takes them relative to 0, and has nothing.  That is
-// wrong only where the whole part's largest is that low, or above FAR: there the sums are taken again, relative to the largest logit itself, by 2^((z - m) c).
+// wrong only where the whole part's largest is that low, or above FAR: there the sums are taken again, relative to the largest logit m itself, by 2^((z - m) c) (what z - m is
+// rounded by, where it is, is nothing beside exponents of that size).
 constexpr float BELOW = 0x1p30f, FAR = 0x1p29f;
 __device__ __forceinline__ float reference_of(float r) { return r < -BELOW ? 0.f : r; }      // (NaN stays)
 __device__ __forceinline__ double wave_max_d(double x)
 {
-    for (int o = 32; o > 0; o >>= 1) x = fmax(x, __shfl_xor(x, o, 64));
-    return x;
+    x = fmax(x, dpp_d<DPP_XOR1>(x));
+    x = fmax(x, dpp_d<DPP_XOR2>(x));
+    x = fmax(x, dpp_d<DPP_HALF_MIRROR>(x));
+    x = fmax(x, dpp_d<DPP_MIRROR>(x));
+    unsigned la, lb, ha, hb;
+    unsigned long long b = (unsigned long long)__double_as_longlong(x);
+    pair16((unsigned)b, la, lb);
+    pair16((unsigned)(b >> 32), ha, hb);
+    x = fmax(join_d(la, ha), join_d(lb, hb));
+    b = (unsigned long long)__double_as_longlong(x);
+    pair32((unsigned)b, la, lb);
+    pair32((unsigned)(b >> 32), ha, hb);
+    return fmax(join_d(la, ha), join_d(lb, hb));
 }
 
 // One element of a row.
