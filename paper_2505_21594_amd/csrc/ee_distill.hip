@@ -42,14 +42,12 @@ struct Entry {
 __device__ __forceinline__ Entry entry_of(const DistillDev &a, int row, int lane)
 {
     Entry e = {-1, 0.f, 0.0};
-    if (lane < a.top) {
-        const size_t at = (size_t)row * a.top + lane;
-        const int id = as_global(a.ids)[at];
-        const float lp = as_global(a.logprobs)[at];
-        if (id >= 0 && id < a.V && lp != -INFINITY) {
-            e.id = id;
-            e.lp = (double)lp;
-        }
+    const size_t at = (size_t)row * a.top + min(lane, a.top - 1);      // (no branch before the loads: they go out together with others)
+    const int id = as_global(a.ids)[at];
+    const float lp = as_global(a.logprobs)[at];
+    if (lane < a.top && id >= 0 && id < a.V && lp != -INFINITY) {
+        e.id = id;
+        e.lp = (double)lp;
     }
     return e;
 }
@@ -77,22 +75,23 @@ __device__ __forceinline__ ListTerms list_terms(const DistillDev &a, Entry &e)
     }
     t.p = e.id >= 0 ? exp(e.lp) : 0.0;
     // a token that is named twice has both probabilities (few lists do that: the sums only where one does)
-    t.first = e.id >= 0;
-    bool twice = false;
-    for (int i = 0; i < a.top; ++i) {
-        const bool same = __builtin_amdgcn_readlane(e.id, i) == e.id;
-        t.first = t.first && !(same && i < lane);
-        twice = twice || (same && i != lane);
-    }
+    unsigned long long again = 0;                            // lanes behind one that names the same token
+#pragma unroll 4
+    for (int i = 0; i < a.top; ++i) again |= __ballot(__builtin_amdgcn_readlane(e.id, i) == e.id) & ~0ull << i << 1;
+    t.first = e.id >= 0 && !(again >> lane & 1);
     t.both = t.p;
     t.share = wave_sum_d(t.p);
-    if (__ballot(twice && e.id >= 0)) {
+    if (__builtin_expect(__ballot(e.id >= 0 && !t.first) != 0, 0)) {
+        int times = 0;
         t.both = 0.0;
         for (int i = 0; i < a.top; ++i) {
             const double other = readlane_d(t.p, i);
-            if (__builtin_amdgcn_readlane(e.id, i) == e.id) t.both += other;
+            if (__builtin_amdgcn_readlane(e.id, i) == e.id) {
+                t.both += other;
+                ++times;
+            }
         }
-        if (twice && e.id >= 0) {
+        if (e.id >= 0 && times > 1) {
             e.lp = log(t.both);
             t.p = t.first ? t.both : 0.0;
         }
@@ -143,17 +142,19 @@ __device__ __forceinline__ RowTerms row_terms(const DistillDev &a, const Entry &
     return r;
 }
 
-// The others' largest exponent and sum from the parts of a row; one wave calls it.
-__device__ __forceinline__ double join_parts(const DistillDev &a, int row, int lane, double &r)
+// The others' largest exponent and sum from the parts of a row, x: of lane l its part l (or any other past the last); one wave calls it.
+__device__ __forceinline__ DistillPart first_part(const DistillDev &a, int row, int lane) { return a.part[(size_t)row * a.parts + min(lane, a.parts - 1)]; }
+__device__ __forceinline__ double join_parts(const DistillDev &a, int row, int lane, DistillPart x, double &r)
 {
     const DistillPart *parts = a.part + (size_t)row * a.parts;
-    r = -INFINITY;
-    for (int p = lane; p < a.parts; p += 64) r = fmax(r, parts[p].r);
+    r = x.r;
+    for (int p = lane + 64; p < a.parts; p += 64) r = fmax(r, parts[p].r);
     r = wave_max_d(r);
     double S = 0.0;
-    for (int p = lane; p < a.parts; p += 64) {
-        const DistillPart x = parts[p];
+    for (int p = lane; p < a.parts;) {
         if (x.sum != 0.0) S += x.sum * (x.r == -INFINITY ? 1.0 : exp2(x.r - r));
+        p += 64;
+        if (p < a.parts) x = parts[p];
     }
     return wave_sum_d(S);
 }
@@ -270,7 +271,7 @@ __global__ void __launch_bounds__(NT, NT == 512 ? 6 : 4) ee_distill_kernel(Disti
         double S;
         if constexpr (MODE == GRAD) {
             list = list_terms(a, e);
-            S = join_parts(a, row, lane, r_rest);
+            S = join_parts(a, row, lane, first_part(a, row, lane), r_rest);
         } else {
             S = ws[0];
             for (int w = 1; w < WAVES; ++w) S += ws[w];
@@ -341,10 +342,12 @@ __global__ void __launch_bounds__(256) ee_distill_loss_kernel(DistillDev a, int 
 {
     const int lane = threadIdx.x & 63, row = blockIdx.x * 4 + (threadIdx.x >> 6);
     if (row >= n_rows) return;
+    const DistillPart part = first_part(a, row, lane);
+    const float z = as_global(a.z)[(size_t)row * a.top + min(lane, a.top - 1)];
     Entry e = entry_of(a, row, lane);
-    if (e.id >= 0) e.z = as_global(a.z)[(size_t)row * a.top + lane];
+    e.z = z;
     double r_rest;
-    const double S = join_parts(a, row, lane, r_rest);
+    const double S = join_parts(a, row, lane, part, r_rest);
     const ListTerms list = list_terms(a, e);
     const RowTerms r = row_terms(a, e, list, r_rest, S, 1.f);
     if (lane == 0) as_global_mut(a.loss)[row] = (float)r.loss;
