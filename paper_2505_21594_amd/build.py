@@ -52,10 +52,14 @@ def build(force: bool = True, verbose: bool = False) -> str:
     return LIB_PATH
 
 
+# Kernels that are faster with so many bytes of spills than without (both sides are measured where they are written).
+ACCEPTED_SCRATCH = {"ee_accept_draw_kernel": 12, "ee_attend_wide_kernel": 40, "ee_distill_kernel": 28, "ee_norm_grad_kernel": 164}
+
+
 def check_resources(compiler_output: str):
-    """Kernels of the pass must not use scratch memory (register spills or stack arrays):
+    """Kernels must not use scratch memory (register spills or stack arrays), beyond what is accepted above:
     measured on MI355X, a few hundred bytes of scratch per lane add tens of microseconds to
-    every launch of these 256-workgroup kernels.  Returns warning lines."""
+    every launch of the pass's 256-workgroup kernels.  Returns warning lines."""
     import re
     name, out = None, []
     for line in compiler_output.splitlines():
@@ -63,7 +67,7 @@ def check_resources(compiler_output: str):
         if m:
             name = m.group(1)
         m = re.search(r"ScratchSize \[bytes/lane\]: (\d+)", line)
-        if m and name and int(m.group(1)) > 0 and any(k in name for k in ("ee_gemm_kernel", "att_kernel", "misc_kernel", "sample_kernel", "pf_gemm_kernel", "append_kernel", "attend_kernel", "shared_att", "accept_", "score_", "gemm16_", "slope_")):
+        if m and name and int(m.group(1)) > max((n for k, n in ACCEPTED_SCRATCH.items() if k in name), default=0):
             out.append(f"WARNING: {name} uses {m.group(1)} bytes of scratch per lane (expect slow launches)")
     return out
 

@@ -161,6 +161,7 @@ __device__ __forceinline__ double join_parts(const DistillDev &a, int row, int l
 
 enum DistillMode { WHOLE = 0, STATS = 1, GRAD = 2 };
 
+// (512 threads: six waves a SIMD with 20 to 28 bytes of spill, of wave 0's arithmetic with doubles; five without any: 4096 rows of 32000 142 us for 119, 300 of 200003 95 for 89.)
 template <int TYPE, int E, int NT, int MODE>
 __global__ void __launch_bounds__(NT, NT == 512 ? 6 : 4) ee_distill_kernel(DistillDev a)
 {

@@ -331,7 +331,8 @@ static NormShape norm_shape(int dim)
     return {(pieces + threads - 1) / threads, threads, false};
 }
 // Backward, a chunk a lane, whose registers hold its part of the gains' and biases' gradients too; waves in fours, and few enough registers, so that a compute unit's SIMDs have room
-// for a second workgroup (8191 rows of 5120: ten waves of 92 registers 83 us, twelve of 80 67.5; 8192 of 4096 by eight 48.7; 2000 of 16384 85).
+// for a second workgroup (8191 rows of 5120: ten waves of 92 registers 83 us, twelve of 80 67.5, 12 bytes of them spilled; 8192 of 4096 by eight 48.7).  Two chunks a lane, with 52 bytes of
+// spill (fp32 164): 2000 rows of 16384 90 us, fp32 173; with the gains loaded again for every row (40 and 176 bytes) 91 and 183.
 static NormShape norm_grad_shape(int dim)
 {
     const int pieces = (dim + 7) / 8;
