@@ -399,15 +399,22 @@ __global__ void __launch_bounds__(SL_COLS *SL_SUBS) ee_slope_kernel(SlopeDev a)
 }
 
 typedef void (*gemm16_kernel_t)(GemmDev);
+template <int TYPE, typename TILE>
+static gemm16_kernel_t gemm16_kernel(bool a_along, bool b_along)
+{
+    // (a kernel that no plan takes is not built)
+    if constexpr (TILE::TI == 256) {
+        return ee_gemm16_kernel<TYPE, false, false, TILE>;
+    } else if constexpr (TILE::TI == 192) {
+        return b_along ? ee_gemm16_kernel<TYPE, true, true, TILE> : ee_gemm16_kernel<TYPE, true, false, TILE>;
+    } else {
+        return a_along ? (b_along ? ee_gemm16_kernel<TYPE, true, true, TILE> : ee_gemm16_kernel<TYPE, true, false, TILE>) : ee_gemm16_kernel<TYPE, false, false, TILE>;
+    }
+}
 template <typename TILE>
 static gemm16_kernel_t gemm16_kernel(bool bf16, bool a_along, bool b_along)
 {
-    if constexpr (TILE::TI == 256)
-        return bf16 ? ee_gemm16_kernel<EE_BF16, false, false, TILE> : ee_gemm16_kernel<EE_FP16, false, false, TILE>;
-    if constexpr (TILE::TI == 192)
-        return bf16 ? (b_along ? ee_gemm16_kernel<EE_BF16, true, true, TILE> : ee_gemm16_kernel<EE_BF16, true, false, TILE>) : (b_along ? ee_gemm16_kernel<EE_FP16, true, true, TILE> : ee_gemm16_kernel<EE_FP16, true, false, TILE>);
-    if (bf16) return a_along ? (b_along ? ee_gemm16_kernel<EE_BF16, true, true, TILE> : ee_gemm16_kernel<EE_BF16, true, false, TILE>) : ee_gemm16_kernel<EE_BF16, false, false, TILE>;
-    return a_along ? (b_along ? ee_gemm16_kernel<EE_FP16, true, true, TILE> : ee_gemm16_kernel<EE_FP16, true, false, TILE>) : ee_gemm16_kernel<EE_FP16, false, false, TILE>;
+    return bf16 ? gemm16_kernel<EE_BF16, TILE>(a_along, b_along) : gemm16_kernel<EE_FP16, TILE>(a_along, b_along);
 }
 
 template <int TYPE, int MT>
