@@ -8,8 +8,9 @@
 // probabilities are put right to the first order in 64 bits, exponent and sum) an exponential is 2^(z c - r), one multiply-add and one instruction, r a number of
 // fp32 itself, so that nothing is lost where the sums are put together. The largest: a wave's bound for n is the n-th largest among the maxima of its 256 groups of
 // chunks, which n of its elements reach.  The least of w waves' bounds for top / w is one that `top` elements reach; the chunks with an element above it go to LDS,
-// then their elements above it (a few more than `top`), and of those one wave keeps exactly `top`.  Rows with so many equal elements, or one wave's so far below the
-// others', that this overflows take as many rounds as tokens are wanted.
+// then their elements above it (a few more than `top`), and of those one wave keeps exactly `top`.  (Only waves all of whose lanes have a chunk give a bound: one with a chunk or two
+// would let everything through, 2041 rows of 1040 tokens with lists of 64 in 150 us for 20.)  Where this overflows, the row takes as many rounds as tokens are wanted: rows of so many equal
+// elements, or of so many that share the 16 bits of the bound's key (fp32 beside a large offset), or one wave's so far below the others' (2041 rows of 32000 all alike, lists of 20: 463 us).
 #include "ee_vocab.hpp"
 
 namespace ee {
@@ -217,7 +218,7 @@ __global__ void __launch_bounds__(NT, NT == 512 ? 6 : 4) ee_score_kernel(ScoreDe
         }
     }
     z.again(s, d);
-    const int k = min(a.top, len), holding = min((len + 64 * N - 1) / (64 * N), WAVES);      // (waves that have elements at all)
+    const int k = min(a.top, len), holding = max(min(len / (64 * N), WAVES), 1);             // (waves all of whose lanes have a chunk: as many groups as a list is long)
     if (k > 0) {
         unsigned u[4];
 #pragma unroll
