@@ -544,7 +544,7 @@ int ee_score_tokens(const ee_score_args *args, void *workspace, size_t workspace
    twice has the sum of both probabilities.
    loss fp32 [n_rows], or NULL;  d_logits [n_rows][vocab] of type grad_dtype, or NULL: d_loss[row] (fp32 [n_rows]; NULL: 1) times the gradient; rows whose
    d_loss is 0 get zeros, whatever their logits are.  d_logits may be logits (same type and stride).  A row without a softmax has loss and gradient NaN.  A student that
-   gives a named token, or all the others where pi > 0, no probability (-infinity) has an infinite loss; its gradient is finite (0 where q is).  Sums in fp32 for
+   gives a named token, or all the others where pi > 0, no probability (-infinity) has an infinite loss; its gradient is finite (0 for others of no probability).  Sums in fp32 for
    each thread and 64 bits from there, everything that a row has once in 64 bits.  n_rows up to 2^20, vocab up to 2^24 (EE_EINVAL where rows times parts of rows pass 2^22).
    A finite logit counts however large it is (rows masked with the type's lowest value too).  1 / temperature is held to 24 bits: results are those of a temperature that is off by 2^-24 of it at most.
    workspace: ee_distill_workspace bytes (may be 0), 256-byte aligned; contents do not matter. */

@@ -439,6 +439,7 @@ extern "C" int ee_distill(const ee_distill_args *p, void *workspace, size_t work
     if (pl.bytes > workspace_bytes || (pl.bytes && (!workspace || !aligned(workspace, 256))))
         return fail(EE_EINVAL, "%s: the workspace has %zu bytes of %zu, or is not 256-byte aligned", call, workspace_bytes, pl.bytes);
     if ((long long)p->n_rows * pl.split.parts >= 1 << 22) return fail(EE_EINVAL, "%s: too many rows of so many tokens", call);
+    if (p->loss && p->loss == p->d_loss) return fail(EE_EINVAL, "%s: loss and d_loss must be arrays of their own", call);    // (a row's parts read d_loss when the first one writes the loss)
     DistillDev a;
     a.logits = p->logits;
     a.ids = p->ids;
