@@ -504,8 +504,9 @@ int ee_accept_workspace(const ee_accept_args *args, size_t *bytes);
 int ee_accept_drafts(const ee_accept_args *args, void *workspace, size_t workspace_bytes, void *stream);
 
 /* ------------------------------------------------------------------ operators around the LM head
-   What teaches an exit head (its adapters, norm and head matrix, or a draft model's) what the target says, and what reports the target's answer: linear layers and
-   norms with their gradients, scores of tokens, distillation.  As the operators above: DEVICE pointers, a caller's stream, nothing allocated, copied or
+   What teaches an exit head (its adapters, norm and head matrix, or a draft model's) what the target says, and what reports a row of logits: linear layers and
+   norms with their gradients, scores of tokens, distillation, for callers with a layer loop and memory of their own (a session's hidden states stay in the library, and its logits leave it by
+   ee_debug_logits alone).  As the operators above: DEVICE pointers, a caller's stream, nothing allocated, copied or
    waited for, host checks before anything is enqueued.  A row stride counts elements (of a single row it says nothing); every result is written whole and depends on
    nothing but its inputs (sums are taken in one order).  Outputs are arrays of their own unless said otherwise: one that overlaps an input in part gives
    nothing meaningful. */

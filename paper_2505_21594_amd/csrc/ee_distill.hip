@@ -4,7 +4,7 @@
 //              dL/dz_i = (q_i - p_i) / T for those it names, q_i (1 - pi / rho) / T for the others;
 //   rest = 0:  p divided by its sum;  L = sum_j p_j (log p_j - log q_j),  dL/dz_i = (q_i - p_i) / T.
 //
-// Bound by the logits' bytes, read once, and the gradient's, written once (one MI355X: 4096 rows of 32000, bf16, 118 us, 4.45 TB/s): a workgroup holds its row in
+// Bound by the logits' bytes, read once, and the gradient's, written once (one MI355X: 4096 rows of 32000, bf16, 111 us, 4.7 TB/s): a workgroup holds its row in
 // registers (RowPart) from the sums to the gradient. Rows that are too few to fill the chip, or too long for a workgroup, are taken in parts by two launches, of
 // which the second reads the logits again. The tokens that the list names are marked in LDS, one bit each, a thread's bits in one word, and left out of the sums:
 // rho is a sum of its own, not a difference.  In powers of two, c = log2(e) / T rounded to fp32 (another temperature by 2^-24 of it, the same one everywhere:
@@ -161,7 +161,7 @@ __device__ __forceinline__ double join_parts(const DistillDev &a, int row, int l
 
 enum DistillMode { WHOLE = 0, STATS = 1, GRAD = 2 };
 
-// (512 threads: six waves a SIMD with 20 to 28 bytes of spill, of wave 0's arithmetic with doubles; five without any: 4096 rows of 32000 142 us for 119, 300 of 200003 95 for 89.)
+// (512 threads: six waves a SIMD with 20 to 28 bytes of spill, of wave 0's arithmetic with doubles; five without any: 4096 rows of 32000 130 us for 111, 300 of 200003 86.5 for 85.)
 template <int TYPE, int E, int NT, int MODE>
 __global__ void __launch_bounds__(NT, NT == 512 ? 6 : 4) ee_distill_kernel(DistillDev a)
 {
@@ -364,9 +364,9 @@ static DistillPlan plan_distill(const ee_distill_args &p, bool grad)
 {
     DistillPlan pl;
     const int n = p.dtype == EE_FP32 ? 4 : 8, room[4] = {256 * 4 * n, 512 * 8 * n, 1024 * 8 * n, 1024 * 16 * n};
-    // us, bf16 and fp16, one launch for all of a row / two, of which the second reads the logits again.  With a gradient: 600 rows of 100003 87 / 108, 1500 of 70000 138 / 145, so that a row
+    // us, one launch for all of a row / two, of which the second reads the logits again.  With a gradient: 600 rows of 100003 85 / 102, 1500 of 70000 139 / 137, fp32 600 of 50003 68 / 83 and 1500 of 60000 154 / 213, so that a row
     // that a workgroup can hold is one part, in the smallest workgroup that can where rows fill the chip and of 1024 threads where they do not (five rows of 32000, fp32, by sixteen
-    // chunks a thread 19.4, by eight 8.9).  The loss alone: 4096 rows of 32000 72 / 61, 600 of 100003 149 / 44, five of 32000 17.3 / 7.4: the first launch alone has half the registers.
+    // chunks a thread 10.6, by eight 8.7).  The loss alone: 4096 rows of 32000 68 / 62, 600 of 100003 61 / 44, 1500 of 70000 88 / 48, five of 32000 6.9 / 7.1: the first launch alone has half the registers.
     const bool many = p.n_rows >= 256;
     pl.whole = grad && p.vocab <= room[3];
     if (pl.whole) {

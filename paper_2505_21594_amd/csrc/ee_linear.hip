@@ -430,7 +430,7 @@ enum GemmForm { LARGE, MEDIUM, SMALL, THIN };
 // How a product is split: in tiles (or few rows at a time), and parts of the sum, by an estimate of its time in us: the tiles of the busiest compute unit at 4.7e-7 us for each
 // element of a tile and of the sum (times what a tile's shape costs, and what workgroups with few beside them on their compute unit do), a start and an end, and the
 // parts' way through memory.  Measured, us, the chosen way first, then the best of the others (L, M, S: the tile, parts behind it): 2041 x 4096 x 11008 forward L1 181,
-// M1 186; dx M1 176, L2 205; dW L1 184, M1 205; 4096 columns M1 69, L1 82; 384 columns S1 19.6, S2 18.4, M6 20.8; 128 rows of 4096 x 4096 S4 13.7, S2 15.2; 300 x 1000 x
+// M1 186; dx M1 176, L2 205; dW L1 184, M1 205; 4096 columns M1 69, L1 82; 384 columns S1 19.6, S2 18.4 (which the estimate misses), M6 20.8; 128 rows of 4096 x 4096 S4 13.7, S2 15.2; 300 x 1000 x
 // 1000 S1 8.0, M4 11.5; dW of 512 x 512 from 8000 rows S4 16.3, S6 15.8, M12 20.1.
 static double gemm_time(int form, bool a_along, double tiles, int area, int K, int splits, double results)
 {
