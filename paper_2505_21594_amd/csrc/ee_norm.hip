@@ -154,6 +154,14 @@ __device__ __forceinline__ void row_sums(float (&v)[COUNT], float (*swap)[3][16]
     }
 }
 
+// Sum / dim to the last place: elements that are all alike have themselves for a mean, and nothing left about it, where their sum is a number of fp32 (of 8 bits, up to 2^16 elements; of fp16's
+// 11 up to 2^13).  With 1 / dim alone 1000 elements of 30000 are 0.002 off, times r = 316.
+__device__ __forceinline__ float mean_of(float sum, const NormDev &a)
+{
+    const float m = sum * a.inv_dim;
+    return fmaf(fmaf(-m, (float)a.dim, sum), a.inv_dim, m);
+}
+
 // ONE: a wave holds a row, a workgroup of 256 threads four of them; otherwise the workgroup, of as many waves as it takes.
 template <int E, bool ONE>
 __global__ void __launch_bounds__(ONE ? 256 : 512) ee_norm_kernel(NormDev a)
@@ -174,7 +182,7 @@ __global__ void __launch_bounds__(ONE ? 256 : 512) ee_norm_kernel(NormDev a)
 #pragma unroll
             for (int i = 0; i < 8; ++i) v[0] += x[c][i];
         row_sums<ONE>(v, swap, turn);
-        mu = v[0] * a.inv_dim;
+        mu = mean_of(v[0], a);
     }
     float v[1] = {0.f};
 #pragma unroll
@@ -236,7 +244,7 @@ __global__ void __launch_bounds__(ONE ? 256 : 1024, !ONE && E == 1 && !WIDE ? (D
 #pragma unroll
                 for (int i = 0; i < 8; ++i) v[0] += x[c][i];
             row_sums<ONE>(v, swap, turn);
-            mu = v[0] * a.inv_dim;
+            mu = mean_of(v[0], a);
         }
         float v[3] = {0.f, 0.f, 0.f};
 #pragma unroll
