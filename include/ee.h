@@ -595,7 +595,7 @@ int ee_norm_grad(const ee_norm_grad_args *args, void *workspace, size_t workspac
 
 /* ee_linear: z = x weight^T + bias,  y = act(z) + residual.  x [n_rows][n_in] and weight [n_out][n_in] of type dtype (EE_BF16, EE_FP16), bias fp32 [n_out] or NULL,
    residual [n_rows][n_out] of residual_dtype or NULL (it may be y, with the same type and stride), y of out_dtype; pre (an array of its own): z rounded to dtype, what ee_linear_grad
-   needs where there is an activation, or NULL.  fp32 sums, one rounding of each result.  An exit's adapters are two such calls (the down matrices stacked, EE_ACT_SILU; the up
+   needs where there is an activation, or NULL.  fp32 sums (in which a subnormal fp16 is rounded as one of 2^-14), one rounding of each result.  An exit's adapters are two such calls (the down matrices stacked, EE_ACT_SILU; the up
    matrices side by side, residual h).
    ee_linear_grad: dz = dy act'(pre);  dx = dz weight,  d_weight = dz^T x,  d_bias = sum over the rows of dz (fp32; written, not added to), each NULL where it is not wanted.  (The residual's
    gradient is dy.)  dy and pre are of type dtype; dz is rounded to dtype where the result is of 16 bits, and is two (fp16: off by 2^-22 of it, or by 2^-36 where that is more) or three
